@@ -18,8 +18,14 @@ class GemError(RuntimeError):
         super().__init__(f"{where}: {status_string(status)} ({status})")
 
 
+class GemSeq(C.Structure):
+    """gem_seq_t: a [B][T][D] tensor given by its address and its batch and time strides."""
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64)]
+
+
 def _declare(L):
     p, i, sz = C.c_void_p, C.c_int, C.c_size_t
+    f, i64, seq = C.c_float, C.c_int64, C.POINTER(GemSeq)
     sig = {
         "gem_create": ([sz, i, C.c_float, C.c_float, C.c_float, p], i),
         "gem_destroy": ([p], None),
@@ -76,6 +82,12 @@ def _declare(L):
         "gem_synth_cnn_theta0": ([C.c_uint64, p, p, p], i),
         "gem_synth_dropout": ([C.c_uint64, C.c_uint64, i, i, i, C.c_float, p, p], i),
         "gem_synth_cnn_data": ([C.c_uint64, i, i, i, p, p, p], i),
+        "gem_glr_saved_count": ([i64, i64, i64], i64),
+        "gem_glr_forward": ([i, i, i64, i64, i64, seq, seq, p, p, p, seq, p, p, p], i),
+        "gem_glr_backward": ([i, i, i64, i64, i64, seq, seq, p, p, p, seq, p, seq, seq, p, p], i),
+        "gem_distill": ([i, i64, i64, p, i64, i, p, p, p, p, p, f, f, p, p, i64, p], i),
+        "gem_token_logp": ([i, i64, i64, p, i64, p, f, i, p, p, p, p, p, p], i),
+        "gem_token_logp_grad": ([i, i64, i64, p, i64, p, f, p, p, p, p, p, i64, p], i),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)

@@ -1,0 +1,55 @@
+// Shared by the language-model operators (internal): element types, checks of arguments.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "../../include/gem_lm.h"
+#include "pdl.h"
+
+namespace gem {
+namespace lm {
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+
+// Rounds to nearest even; fp16 overflows to infinity.
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+inline int dtype_size(int dtype) { return dtype == GEM_F32 ? 4 : 2; }
+inline bool dtype_ok(int dtype) { return dtype == GEM_F32 || dtype == GEM_BF16 || dtype == GEM_F16; }
+
+inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+// A required / an optional array of 4-byte values.
+inline bool array_ok(const void* p) { return p && aligned_to(p, 4); }
+inline bool optional_ok(const void* p) { return aligned_to(p, 4); }
+
+// Sizes and strides that 64-bit offsets hold with room to spare.
+constexpr int64_t kMaxExtent = int64_t(1) << 31;
+constexpr int64_t kMaxStride = int64_t(1) << 46;
+
+inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
+
+// Ends a call: a launch that failed is reported, and its error is not left for the caller's
+// next check.
+inline int launch_status(cudaError_t e) {
+  if (e == cudaSuccess) return GEM_OK;
+  cudaGetLastError();
+  return GEM_ECUDA;
+}
+
+}  // namespace lm
+}  // namespace gem
