@@ -2,6 +2,8 @@
 // u = (1 - a) x or x, and its backward pass.
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "lm_internal.h"
 
 namespace cg = cooperative_groups;
@@ -40,10 +42,15 @@ __device__ __forceinline__ int64_t steps_of(const GlrArgs& p, int64_t b) {
 // a = 1 / (1 + e) and b = e a.  f below -80 counts as -80 (a = 2e-35): e stays finite.  NaN stays.
 template <typename E>
 __device__ __forceinline__ void gate(float f, float& a, float& b) {
+  float e;
   asm("max.NaN.f32 %0, %0, 0fC2A00000;" : "+f"(f));
-  // 16-bit inputs carry 2^-9 themselves; the fast exponential's 2 + |f| units are far below that
-  const float e = sizeof(E) == 4 ? expf(-f) : __expf(-f);
-  a = __fdividef(1.0f, 1.0f + e);
+  if constexpr (sizeof(E) == 4) {
+    e = expf(-f);
+  } else {
+    // 16-bit inputs carry 2^-9 themselves; rounding f log2(e) costs |f| 2^-24 of e
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f * -1.44269504f));
+  }
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.0f + e));
   b = e * a;
 }
 
@@ -92,45 +99,52 @@ constexpr int64_t kStepT = 2;   // longest call of the kernel above (one chunk: 
 // an infinity would not).
 
 constexpr int kMaxWarps = 8;
+constexpr int kMaxCluster = 8;
 
 template <int V>
 struct Map {
   float A[V], H[V];
 };
 
+// Applies m to h, and composes m after the maps so far.  RESETS: a map may forget.
 template <int V>
-__device__ __forceinline__ void apply(float (&h)[V], const Map<V>& m) {
-#pragma unroll
-  for (int v = 0; v < V; ++v) h[v] = m.A[v] < 0.0f ? m.H[v] : fmaf(m.A[v], h[v], m.H[v]);
-}
-
-// m after the maps composed so far.
-template <int V>
-__device__ __forceinline__ void compose(Map<V>& sofar, const Map<V>& m) {
+__device__ __forceinline__ void apply(float (&h)[V], const Map<V>& m, bool resets) {
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    const bool forgets = m.A[v] < 0.0f;
-    sofar.H[v] = forgets ? m.H[v] : fmaf(m.A[v], sofar.H[v], m.H[v]);
-    sofar.A[v] = forgets || sofar.A[v] < 0.0f ? -1.0f : sofar.A[v] * m.A[v];
+    const float moved = fmaf(m.A[v], h[v], m.H[v]);
+    h[v] = resets && m.A[v] < 0.0f ? m.H[v] : moved;
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void compose(Map<V>& sofar, const Map<V>& m, bool resets) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const bool forgets = resets && m.A[v] < 0.0f;
+    const float moved = fmaf(m.A[v], sofar.H[v], m.H[v]);
+    sofar.H[v] = forgets ? m.H[v] : moved;
+    sofar.A[v] = forgets || (resets && sofar.A[v] < 0.0f) ? -1.0f : sofar.A[v] * m.A[v];
   }
 }
 
 // From every thread's map of a round: the state before the thread's chunk, and `state` moved on to
 // the state after the round.  maps: [2][kMaxWarps][32], blocks: [2][C][32] (C > 1) in shared memory.
 template <int V>
-__device__ __forceinline__ void scan_round(const Map<V>& own, int round, int warps, int rank, int C, Map<V>* maps,
+__device__ __forceinline__ void scan_round(const Map<V>& own, int round, int warps, int rank, int C, bool resets, Map<V>* maps,
                                            Map<V>* blocks, float (&state)[V], float (&before)[V]) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  Map<V>* buf = maps + (round & 1) * kMaxWarps * 32;
-  buf[warp * 32 + lane] = own;
+  Map<V>* buf = maps + (round & 1) * kMaxWarps * 32 + lane;
+  buf[warp * 32] = own;
   __syncthreads();
   if (C == 1) {
-    for (int w = 0; w < warps; ++w) {
+#pragma unroll
+    for (int w = 0; w < kMaxWarps; ++w) {
+      if (w >= warps) break;
       if (w == warp) {
 #pragma unroll
         for (int v = 0; v < V; ++v) before[v] = state[v];
       }
-      apply<V>(state, buf[w * 32 + lane]);
+      apply<V>(state, buf[w * 32], resets);
     }
     return;
   }
@@ -141,61 +155,155 @@ __device__ __forceinline__ void scan_round(const Map<V>& own, int round, int war
     all.H[v] = 0.0f;
   }
   mine = all;
-  for (int w = 0; w < warps; ++w) {
+#pragma unroll
+  for (int w = 0; w < kMaxWarps; ++w) {
+    if (w >= warps) break;
     if (w == warp) mine = all;
-    compose<V>(all, buf[w * 32 + lane]);
+    compose<V>(all, buf[w * 32], resets);
   }
   cg::cluster_group cluster = cg::this_cluster();
-  Map<V>* out = blocks + (round & 1) * C * 32;
-  for (int c = warp; c < C; c += warps) cluster.map_shared_rank(out, c)[rank * 32 + lane] = all;
+  Map<V>* out = blocks + (round & 1) * C * 32 + lane;
+  for (int c = warp; c < C; c += warps) cluster.map_shared_rank(out, c)[rank * 32] = all;
   cluster.sync();
   for (int c = 0; c < C; ++c) {
     if (c == rank) {
 #pragma unroll
       for (int v = 0; v < V; ++v) before[v] = state[v];
     }
-    apply<V>(state, out[c * 32 + lane]);
+    apply<V>(state, out[c * 32], resets);
   }
-  apply<V>(before, mine);
+  apply<V>(before, mine, resets);
 }
 
-// V elements of one word.
+// A word of channels as V floats, and back.
 template <typename E, int V>
 __device__ __forceinline__ void unpack(uint32_t w, float (&v)[V]) {
   if constexpr (sizeof(E) == 4) {
     v[0] = __uint_as_float(w);
+  } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+    v[0] = __uint_as_float(w << 16);
+    if constexpr (V == 2) v[1] = __uint_as_float(w & 0xffff0000u);
   } else {
-    const E* e = reinterpret_cast<const E*>(&w);
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = to_f32(e[k]);
+    const __half2 h = *reinterpret_cast<const __half2*>(&w);
+    v[0] = __low2float(h);
+    if constexpr (V == 2) v[1] = __high2float(h);
   }
 }
 
 template <typename E, int V>
-__device__ __forceinline__ void store(E* at, const float (&v)[V]) {
-  if constexpr (V == 2) {
-    E e[2] = {from_f32<E>(v[0]), from_f32<E>(v[1])};
-    *reinterpret_cast<uint32_t*>(at) = *reinterpret_cast<uint32_t*>(e);
+__device__ __forceinline__ uint32_t pack(const float (&v)[V]) {
+  if constexpr (sizeof(E) == 4) {
+    return __float_as_uint(v[0]);
+  } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+    const __nv_bfloat162 w = __floats2bfloat162_rn(v[0], V == 2 ? v[V - 1] : 0.0f);
+    return *reinterpret_cast<const uint32_t*>(&w);
   } else {
-    *at = from_f32<E>(v[0]);
+    const __half2 w = __floats2half2_rn(v[0], V == 2 ? v[V - 1] : 0.0f);
+    return *reinterpret_cast<const uint32_t*>(&w);
   }
 }
 
-// Copies one word of channels to a slot of the calling thread: asynchronously where it is 4 bytes
-// at a 4-byte boundary, else (one 16-bit channel) through a register.
-template <typename E, int V>
-__device__ __forceinline__ void fetch(uint32_t* slot, const E* from) {
-  if constexpr (sizeof(E) * V == 4) {
-    const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(slot));
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
-  } else {
-    *reinterpret_cast<E*>(slot) = *from;
-  }
-}
+// A warp's tile of one tensor: kChunk rows of 32 words in shared memory, row k the channels of
+// step k.  MODE: how the tensors' rows lie in memory.
+//   kVector  every row starts at a 16-byte boundary and D fills whole 16-byte pieces: lane l moves
+//            piece l % 8 of rows l / 8, l / 8 + 4, ...
+//   kWord    rows start at 4-byte boundaries: lane l moves word l of each row
+//   kHalf    16-bit rows start anywhere; a word holds one channel
+enum Mode { kVector, kWord, kHalf };
+constexpr int kTile = kChunk * 32;
+
 __device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void fetch_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Where a thread works: sequence b, its own channel word d.., and the channels it moves.
+struct Place {
+  int64_t b, d, move_d;
+  int rank, warp, warps, lane;
+  bool on, moves;
+};
+
+template <typename E, int V, Mode MODE>
+__device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
+  Place w;
+  const int64_t slabs = (p.D + 32 * V - 1) / (32 * V);
+  const int64_t id = blockIdx.x / C;
+  w.rank = blockIdx.x % C;
+  w.lane = threadIdx.x % 32;
+  w.warp = threadIdx.x / 32;
+  w.warps = blockDim.x / 32;
+  w.b = id / slabs;
+  const int64_t first = id % slabs * 32 * V;
+  w.d = first + w.lane * V;
+  w.on = w.d < p.D;
+  w.move_d = MODE == kVector ? first + w.lane % 8 * (16 / int(sizeof(E))) : w.d;
+  w.moves = w.move_d < p.D;
+  return w;
+}
+
+// Starts the copy of rows 0..m of a tile; from: the row of step 0 at the lane's channels (move_d).
+template <typename E, Mode MODE>
+__device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_t stride, int m, int lane) {
+  if constexpr (MODE == kVector) {
+    const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile)) + lane * 16;
+    from += lane / 8 * stride;
+#pragma unroll
+    for (int i = 0; i < kChunk / 4; ++i) {
+      if (lane / 8 + 4 * i < m)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + i * 512), "l"(from) : "memory");
+      from += 4 * stride;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
+      if (k < m) {
+        if constexpr (MODE == kWord) {
+          const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile + k * 32 + lane));
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
+        } else {
+          *reinterpret_cast<E*>(tile + k * 32 + lane) = *from;
+        }
+      }
+      from += stride;
+    }
+  }
+}
+
+// Stores rows 0..m of a tile that the warp has written (all lanes call; the tile is free after).
+template <typename E, Mode MODE>
+__device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t stride, int m, int lane, bool moves) {
+  __syncwarp();
+  if constexpr (MODE == kVector) {
+    const uint4* t = reinterpret_cast<const uint4*>(tile) + lane;
+    to += lane / 8 * stride;
+#pragma unroll
+    for (int i = 0; i < kChunk / 4; ++i) {
+      if (moves && lane / 8 + 4 * i < m) *reinterpret_cast<uint4*>(to) = t[i * 32];
+      to += 4 * stride;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
+      if (moves && k < m) {
+        if constexpr (MODE == kWord)
+          *reinterpret_cast<uint32_t*>(to) = tile[k * 32 + lane];
+        else
+          *to = *reinterpret_cast<const E*>(tile + k * 32 + lane);
+      }
+      to += stride;
+    }
+  }
+  __syncwarp();
+}
+
+// Zeros to rows t, t + step, ... below T (steps past a sequence's end).
+template <typename E, int V>
+__device__ __forceinline__ void store_zeros(E* to, int64_t stride, int64_t t, int64_t step, int64_t T) {
+  for (; t < T; t += step)
+#pragma unroll
+    for (int v = 0; v < V; ++v) to[t * stride + v] = from_f32<E>(0.0f);
 }
 
 // Bit k: a reset at step t0 + k (k < m).  All lanes of the warp call.
@@ -206,135 +314,130 @@ __device__ __forceinline__ uint32_t reset_bits(const GlrArgs& p, int64_t b, int6
   return __ballot_sync(~0u, r);
 }
 
-// Where a thread works: sequence b, channels d.., the rank of its block in the cluster.
-struct Place {
-  int64_t b, d;
-  int rank, warp, warps;
-  bool on;
-};
+// The steps of a chunk: all kChunk of them without a reset (PLAIN), or the first m with resets
+// where `fresh` has a bit.
+template <typename E, int V, bool LERP, bool PLAIN>
+__device__ __forceinline__ void forward_map(const uint32_t* x, const uint32_t* f, int m, uint32_t fresh,
+                                            float (&a)[kChunk][V], float (&u)[kChunk][V], Map<V>& own) {
+#pragma unroll
+  for (int k = 0; k < kChunk; ++k) {
+    float xv[V], fv[V];
+    unpack<E, V>(x[k * 32], xv);
+    unpack<E, V>(f[k * 32], fv);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      float g;
+      gate<E>(fv[v], a[k][v], g);
+      u[k][v] = LERP ? g * xv[v] : xv[v];
+      if (!PLAIN && k >= m) {
+        a[k][v] = 1.0f;
+        u[k][v] = 0.0f;
+      }
+      const float moved = fmaf(a[k][v], own.H[v], u[k][v]);
+      own.H[v] = !PLAIN && (fresh >> k & 1) ? u[k][v] : moved;
+      own.A[v] *= a[k][v];
+    }
+  }
+}
 
-template <int V>
-__device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
-  Place w;
-  const int64_t words = (p.D + 32 * V - 1) / (32 * V);
-  const int64_t id = blockIdx.x / C;
-  w.rank = blockIdx.x % C;
-  w.b = id / words;
-  w.d = (id % words * 32 + threadIdx.x % 32) * V;
-  w.on = w.d < p.D;
-  w.warp = threadIdx.x / 32;
-  w.warps = blockDim.x / 32;
-  return w;
+template <typename E, int V, bool PLAIN>
+__device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, const float (&a)[kChunk][V],
+                                              const float (&u)[kChunk][V], float (&h)[V]) {
+#pragma unroll
+  for (int k = 0; k < kChunk; ++k) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float moved = fmaf(a[k][v], h[v], u[k][v]);
+      h[v] = !PLAIN && (fresh >> k & 1) ? u[k][v] : moved;
+    }
+    out[k * 32] = pack<E, V>(h);
+  }
 }
 
 constexpr int kForwardStages = 3;
 
-template <typename E, int V, bool LERP>
+template <typename E, int V, Mode MODE, bool LERP>
 __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const GlrArgs p, int C) {
-  extern __shared__ __align__(16) uint32_t slots[];   // [stage][x, f][kChunk][threads], then the blocks' maps
+  extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
-  Map<V>* blocks = reinterpret_cast<Map<V>*>(slots + kForwardStages * 2 * kChunk * blockDim.x);
   pdl_entry();
-  const Place w = place_of<V>(p, C);
+  const Place w = place_of<E, V, MODE>(p, C);
+  constexpr int kStage = 2 * kTile;
+  uint32_t* const ring = tiles + w.warp * kForwardStages * kStage;
+  Map<V>* const blocks = reinterpret_cast<Map<V>*>(tiles + w.warps * kForwardStages * kStage);
   const int64_t n = steps_of(p, w.b);
-  const int threads = blockDim.x;
   const int64_t chunks = (n + kChunk - 1) / kChunk, all_chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t per_round = int64_t(w.warps) * C;
   const int rounds = int((chunks + per_round - 1) / per_round);
   const int64_t first = int64_t(w.rank) * w.warps + w.warp;   // chunk of round 0
-  const E* x = at<const E>(p.x, w.b, 0, w.d);
-  const E* f = at<const E>(p.f, w.b, 0, w.d);
-  E* h_out = at<E>(p.h, w.b, 0, w.d);
+  const bool resets = p.reset != nullptr;
+  const E* x = at<const E>(p.x, w.b, 0, w.move_d);
+  const E* f = at<const E>(p.f, w.b, 0, w.move_d);
+  E* h_out = at<E>(p.h, w.b, 0, w.move_d);
   const int64_t state_at = w.b * p.D + w.d;
   float state[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) state[v] = p.h0 && w.on ? p.h0[state_at + v] : 0.0f;
 
-  auto slot = [&](int stage, int what, int k) { return slots + ((stage * 2 + what) * kChunk + k) * threads + threadIdx.x; };
-  auto issue = [&](int round) {
+  auto issue = [&](int round, int stage) {
     const int64_t c = first + round * per_round;
-    if (round < rounds && c < chunks && w.on) {
+    if (round < rounds && c < chunks && w.moves) {
       const int64_t t0 = c * kChunk;
       const int m = int(n - t0 < kChunk ? n - t0 : kChunk);
-      const int stage = round % kForwardStages;
-      const E* xs = x + t0 * p.x.stride_t;
-      const E* fs = f + t0 * p.f.stride_t;
-#pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        if (k < m) {
-          fetch<E, V>(slot(stage, 0, k), xs);
-          fetch<E, V>(slot(stage, 1, k), fs);
-        }
-        xs += p.x.stride_t;
-        fs += p.f.stride_t;
-      }
+      fetch_tile<E, MODE>(ring + stage * kStage, x + t0 * p.x.stride_t, p.x.stride_t, m, w.lane);
+      fetch_tile<E, MODE>(ring + stage * kStage + kTile, f + t0 * p.f.stride_t, p.f.stride_t, m, w.lane);
     }
     fetch_commit();
   };
 #pragma unroll
-  for (int r = 0; r < kForwardStages - 1; ++r) issue(r);
+  for (int r = 0; r < kForwardStages - 1; ++r) issue(r, r);
 
+  int stage = 0;
   for (int round = 0; round < rounds; ++round) {
-    issue(round + kForwardStages - 1);
+    issue(round + kForwardStages - 1, stage == 0 ? kForwardStages - 1 : stage - 1);
     const int64_t c = first + round * per_round, t0 = c * kChunk;
     const bool busy = c < chunks;
     const int m = busy ? int(n - t0 < kChunk ? n - t0 : kChunk) : 0;
     const uint32_t fresh = reset_bits(p, w.b, t0, m);
     const bool plain = m == kChunk && fresh == 0;
     fetch_wait<kForwardStages - 1>();
-    const int stage = round % kForwardStages;
-    float a[kChunk][V], u[kChunk][V];
+    __syncwarp();
+    uint32_t* const tile = ring + stage * kStage;
+    stage = stage == kForwardStages - 1 ? 0 : stage + 1;
+    float a[kChunk][V], u[kChunk][V], h[V];
     Map<V> own;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       own.A[v] = 1.0f;
       own.H[v] = 0.0f;
     }
+    if (plain) {
+      forward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u, own);
+    } else {
+      forward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u, own);
+      if (fresh) {
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      float xv[V], fv[V];
-      unpack<E, V>(*slot(stage, 0, k), xv);
-      unpack<E, V>(*slot(stage, 1, k), fv);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        float g;
-        gate<E>(fv[v], a[k][v], g);
-        u[k][v] = LERP ? g * xv[v] : xv[v];
-        if (!plain && k >= m) {
-          a[k][v] = 1.0f;
-          u[k][v] = 0.0f;
-        }
-        own.H[v] = !plain && (fresh >> k & 1) ? u[k][v] : fmaf(a[k][v], own.H[v], u[k][v]);
-        own.A[v] *= a[k][v];
+        for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
       }
     }
-    if (fresh) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
-    }
-    float h[V];
-    scan_round<V>(own, round, w.warps, w.rank, C, maps, blocks, state, h);
-    if (!busy || !w.on) continue;
-    if (p.saved_out) {
+    scan_round<V>(own, round, w.warps, w.rank, C, resets, maps, blocks, state, h);
+    if (!busy) continue;
+    if (p.saved_out && w.on) {
       float* s = p.saved_out + (w.b * all_chunks + c) * p.D + w.d;
 #pragma unroll
       for (int v = 0; v < V; ++v) s[v] = h[v];
     }
-    E* out = h_out + t0 * p.h.stride_t;
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = !plain && (fresh >> k & 1) ? u[k][v] : fmaf(a[k][v], h[v], u[k][v]);
-      if (plain || k < m) store<E, V>(out, h);
-      out += p.h.stride_t;
-    }
+    if (plain)
+      forward_apply<E, V, true>(tile + w.lane, fresh, a, u, h);
+    else
+      forward_apply<E, V, false>(tile + w.lane, fresh, a, u, h);
+    store_tile<E, MODE>(tile, h_out + t0 * p.h.stride_t, p.h.stride_t, m, w.lane, w.moves);
   }
   // all have read h0 before it is replaced (rounds have barriers of their own)
   if (rounds == 0) C == 1 ? __syncthreads() : cg::this_cluster().sync();
   if (!w.on) return;
   // past the sequence's end: zeros, and the state as it stays
-  float zero[V] = {};
-  for (int64_t t = n + first; t < p.T; t += per_round) store<E, V>(h_out + t * p.h.stride_t, zero);
+  store_zeros<E, V>(at<E>(p.h, w.b, 0, w.d), p.h.stride_t, n + first, per_round, p.T);
   if (p.saved_out)
     for (int64_t c = chunks + first; c < all_chunks; c += per_round)
 #pragma unroll
@@ -347,169 +450,195 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
 
 // Backward: the same scan from the end.  A step's map is g -> a (dh + g), g being what the step
 // after it hands back.  The states before the chunk's steps are computed again from the saved one.
+// q: what the gate's gradient multiplies, h_{t-1} - x_t or h_{t-1}.
+template <typename E, int V, bool LERP, bool PLAIN>
+__device__ __forceinline__ void backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
+                                             float (&h)[V], float (&a)[kChunk][V], float (&b)[kChunk][V],
+                                             float (&q)[kChunk][V], Map<V>& own) {
+#pragma unroll
+  for (int k = 0; k < kChunk; ++k) {
+    float xv[V], fv[V];
+    unpack<E, V>(x[k * 32], xv);
+    unpack<E, V>(f[k * 32], fv);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      gate<E>(fv[v], a[k][v], b[k][v]);
+      const float u = LERP ? b[k][v] * xv[v] : xv[v];
+      const bool r = !PLAIN && (fresh >> k & 1);
+      q[k][v] = (r ? 0.0f : h[v]) - (LERP ? xv[v] : 0.0f);
+      const float moved = fmaf(a[k][v], h[v], u);
+      h[v] = r ? u : moved;
+    }
+  }
+#pragma unroll
+  for (int k = kChunk - 1; k >= 0; --k) {
+    float dv[V];
+    unpack<E, V>(dh[k * 32], dv);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (PLAIN || k < m) {
+        own.H[v] = !PLAIN && (fresh >> k & 1) ? 0.0f : a[k][v] * (dv[v] + own.H[v]);
+        own.A[v] *= a[k][v];
+      }
+    }
+  }
+}
+
+template <typename E, int V, bool LERP, bool PLAIN>
+__device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const uint32_t* dh, int m, uint32_t fresh,
+                                               const float (&a)[kChunk][V], const float (&b)[kChunk][V],
+                                               const float (&q)[kChunk][V], float (&g)[V]) {
+#pragma unroll
+  for (int k = kChunk - 1; k >= 0; --k) {
+    if (!PLAIN && k >= m) continue;
+    float dv[V], dxv[V], dfv[V];
+    unpack<E, V>(dh[k * 32], dv);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      g[v] += dv[v];
+      dxv[v] = LERP ? b[k][v] * g[v] : g[v];
+      g[v] = a[k][v] * g[v];
+      dfv[v] = g[v] * (q[k][v] * b[k][v]);
+      if (!PLAIN && (fresh >> k & 1)) g[v] = 0.0f;
+    }
+    dx[k * 32] = pack<E, V>(dxv);
+    df[k * 32] = pack<E, V>(dfv);
+  }
+}
+
 constexpr int kBackwardStages = 2;
 
-template <typename E, int V, bool LERP>
+template <typename E, int V, Mode MODE, bool LERP>
 __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const GlrArgs p, int C) {
-  constexpr int kWords = 3 * kChunk + V;
-  extern __shared__ __align__(16) uint32_t slots[];   // [stage][x, f, dh: kChunk each, saved: V][threads], then the blocks' maps
+  extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f, dh][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
-  Map<V>* blocks = reinterpret_cast<Map<V>*>(slots + kBackwardStages * kWords * blockDim.x);
   pdl_entry();
-  const Place w = place_of<V>(p, C);
+  const Place w = place_of<E, V, MODE>(p, C);
+  constexpr int kStage = 3 * kTile;
+  uint32_t* const ring = tiles + w.warp * kBackwardStages * kStage;
+  Map<V>* const blocks = reinterpret_cast<Map<V>*>(tiles + w.warps * kBackwardStages * kStage);
   const int64_t n = steps_of(p, w.b);
-  const int threads = blockDim.x;
   const int64_t chunks = (n + kChunk - 1) / kChunk, all_chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t per_round = int64_t(w.warps) * C;
   const int rounds = int((chunks + per_round - 1) / per_round);
   const int64_t first = int64_t(w.rank) * w.warps + w.warp;   // chunks are counted from the end
-  const E* x = at<const E>(p.x, w.b, 0, w.d);
-  const E* f = at<const E>(p.f, w.b, 0, w.d);
-  const E* dh = at<const E>(p.dh, w.b, 0, w.d);
-  E* dx_out = at<E>(p.dx, w.b, 0, w.d);
-  E* df_out = at<E>(p.df, w.b, 0, w.d);
+  const bool resets = p.reset != nullptr;
+  const E* x = at<const E>(p.x, w.b, 0, w.move_d);
+  const E* f = at<const E>(p.f, w.b, 0, w.move_d);
+  const E* dh = at<const E>(p.dh, w.b, 0, w.move_d);
+  E* dx_out = at<E>(p.dx, w.b, 0, w.move_d);
+  E* df_out = at<E>(p.df, w.b, 0, w.move_d);
   const int64_t state_at = w.b * p.D + w.d;
-  float state[V];
+  float state[V], saved[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) state[v] = p.dh_last && w.on ? p.dh_last[state_at + v] : 0.0f;
+  for (int v = 0; v < V; ++v) {
+    state[v] = p.dh_last && w.on ? p.dh_last[state_at + v] : 0.0f;
+    saved[v] = 0.0f;
+  }
 
-  auto slot = [&](int stage, int word) { return slots + (stage * kWords + word) * threads + threadIdx.x; };
-  auto issue = [&](int round) {
+  auto issue = [&](int round, int stage) {
     const int64_t l = first + round * per_round;
-    if (round < rounds && l < chunks && w.on) {
-      const int64_t c = chunks - 1 - l, t0 = c * kChunk;
+    if (round < rounds && l < chunks && w.moves) {
+      const int64_t t0 = (chunks - 1 - l) * kChunk;
       const int m = int(n - t0 < kChunk ? n - t0 : kChunk);
-      const int stage = round % kBackwardStages;
-      const E* xs = x + t0 * p.x.stride_t;
-      const E* fs = f + t0 * p.f.stride_t;
-      const E* ds = dh + t0 * p.dh.stride_t;
-#pragma unroll
-      for (int k = 0; k < kChunk; ++k) {
-        if (k < m) {
-          fetch<E, V>(slot(stage, k), xs);
-          fetch<E, V>(slot(stage, kChunk + k), fs);
-          fetch<E, V>(slot(stage, 2 * kChunk + k), ds);
-        }
-        xs += p.x.stride_t;
-        fs += p.f.stride_t;
-        ds += p.dh.stride_t;
-      }
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        fetch<float, 1>(slot(stage, 3 * kChunk + v), p.saved_in + (w.b * all_chunks + c) * p.D + w.d + v);
+      uint32_t* tile = ring + stage * kStage;
+      fetch_tile<E, MODE>(tile, x + t0 * p.x.stride_t, p.x.stride_t, m, w.lane);
+      fetch_tile<E, MODE>(tile + kTile, f + t0 * p.f.stride_t, p.f.stride_t, m, w.lane);
+      fetch_tile<E, MODE>(tile + 2 * kTile, dh + t0 * p.dh.stride_t, p.dh.stride_t, m, w.lane);
     }
     fetch_commit();
   };
+  // the saved state of a round, read one round ahead
+  auto load_saved = [&](int round) {
+    const int64_t l = first + round * per_round;
+    if (l < chunks && w.on) {
+      const float* s = p.saved_in + (w.b * all_chunks + chunks - 1 - l) * p.D + w.d;
 #pragma unroll
-  for (int r = 0; r < kBackwardStages - 1; ++r) issue(r);
+      for (int v = 0; v < V; ++v) saved[v] = s[v];
+    }
+  };
+#pragma unroll
+  for (int r = 0; r < kBackwardStages - 1; ++r) issue(r, r);
+  load_saved(0);
 
+  int stage = 0;
   for (int round = 0; round < rounds; ++round) {
-    issue(round + kBackwardStages - 1);
-    const int64_t l = first + round * per_round, c = chunks - 1 - l, t0 = c * kChunk;
+    issue(round + kBackwardStages - 1, stage == 0 ? kBackwardStages - 1 : stage - 1);
+    const int64_t l = first + round * per_round, t0 = (chunks - 1 - l) * kChunk;
     const bool busy = l < chunks;
     const int m = busy ? int(n - t0 < kChunk ? n - t0 : kChunk) : 0;
     const uint32_t fresh = reset_bits(p, w.b, t0, m);
     const bool plain = m == kChunk && fresh == 0;
     fetch_wait<kBackwardStages - 1>();
-    const int stage = round % kBackwardStages;
-    // a, b = 1 - a, and what the gate's gradient multiplies: h_{t-1} - x_t, or h_{t-1}
+    __syncwarp();
+    uint32_t* const tile = ring + stage * kStage;
+    const uint32_t* const dhs = tile + 2 * kTile + w.lane;
+    stage = stage == kBackwardStages - 1 ? 0 : stage + 1;
     float a[kChunk][V], b[kChunk][V], q[kChunk][V], h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = __uint_as_float(*slot(stage, 3 * kChunk + v));
-#pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      float xv[V], fv[V];
-      unpack<E, V>(*slot(stage, k), xv);
-      unpack<E, V>(*slot(stage, kChunk + k), fv);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        gate<E>(fv[v], a[k][v], b[k][v]);
-        const float u = LERP ? b[k][v] * xv[v] : xv[v];
-        const bool r = !plain && (fresh >> k & 1);
-        q[k][v] = (r ? 0.0f : h[v]) - (LERP ? xv[v] : 0.0f);
-        h[v] = r ? u : fmaf(a[k][v], h[v], u);
-      }
-    }
     Map<V> own;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
+      h[v] = saved[v];
       own.A[v] = 1.0f;
       own.H[v] = 0.0f;
     }
+    load_saved(round + 1);
+    if (plain) {
+      backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q, own);
+    } else {
+      backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q, own);
+      if (fresh) {
 #pragma unroll
-    for (int k = kChunk - 1; k >= 0; --k) {
-      float dv[V];
-      unpack<E, V>(*slot(stage, 2 * kChunk + k), dv);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (plain || k < m) {
-          own.H[v] = !plain && (fresh >> k & 1) ? 0.0f : a[k][v] * (dv[v] + own.H[v]);
-          own.A[v] *= a[k][v];
-        }
+        for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
       }
-    }
-    if (fresh) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
     }
     float g[V];
-    scan_round<V>(own, round, w.warps, w.rank, C, maps, blocks, state, g);
-    if (!busy || !w.on) continue;
-    E* dxs = dx_out + t0 * p.dx.stride_t;
-    E* dfs = df_out + t0 * p.df.stride_t;
-#pragma unroll
-    for (int k = kChunk - 1; k >= 0; --k) {
-      if (!plain && k >= m) continue;
-      float dv[V], dx[V], df[V];
-      unpack<E, V>(*slot(stage, 2 * kChunk + k), dv);
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        g[v] += dv[v];
-        dx[v] = LERP ? b[k][v] * g[v] : g[v];
-        df[v] = g[v] * q[k][v] * (a[k][v] * b[k][v]);
-        g[v] = !plain && (fresh >> k & 1) ? 0.0f : a[k][v] * g[v];
-      }
-      store<E, V>(dxs + k * p.dx.stride_t, dx);
-      store<E, V>(dfs + k * p.df.stride_t, df);
-    }
+    scan_round<V>(own, round, w.warps, w.rank, C, resets, maps, blocks, state, g);
+    if (!busy) continue;
+    if (plain)
+      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, a, b, q, g);
+    else
+      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, a, b, q, g);
+    store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves);
+    store_tile<E, MODE>(tile + kTile, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves);
   }
   if (rounds == 0) C == 1 ? __syncthreads() : cg::this_cluster().sync();
   if (!w.on) return;
-  float zero[V] = {};
-  for (int64_t t = n + first; t < p.T; t += per_round) {
-    store<E, V>(dx_out + t * p.dx.stride_t, zero);
-    store<E, V>(df_out + t * p.df.stride_t, zero);
-  }
+  store_zeros<E, V>(at<E>(p.dx, w.b, 0, w.d), p.dx.stride_t, n + first, per_round, p.T);
+  store_zeros<E, V>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T);
   if (p.dh0 && first == 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v) p.dh0[state_at + v] = state[v];
   }
 }
 
-// How the work is cut: warps of a block and blocks of a cluster are taken only as far as there are
-// chunks for them, and a cluster is as small as gives the GPU about 16 warps per SM (each with
-// copies of 8 KB and more in flight).
+// How the work is cut.  About 16 warps fit an SM (128 registers a thread).  Few slabs of channels:
+// clusters share a slab's time until the blocks fill the GPU twice over; many: blocks of fewer
+// warps, so that all slabs are resident.  Neither goes past the chunks there are.
 struct Cut {
   int warps, cluster;
   int64_t blocks;
 };
 
 Cut cut(const GlrArgs& p, int V) {
+  constexpr int kSms = 152;
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
-  const int64_t words = (p.D + 32 * V - 1) / (32 * V);
+  const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
+  auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
   Cut c;
-  c.warps = int(chunks < 1 ? 1 : chunks < kMaxWarps ? chunks : kMaxWarps);
-  c.cluster = 1;
-  while (c.cluster < 8 && words * p.B * c.cluster * c.warps < 152 * 16 && int64_t(c.cluster) * c.warps < chunks) c.cluster *= 2;
-  c.blocks = words * p.B * c.cluster;
+  c.cluster = int(clip(2 * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
+  const int64_t per_sm = (slabs * c.cluster + kSms - 1) / kSms;
+  c.warps = int(clip(2 * kMaxWarps / per_sm, 1, clip(chunks, 1, kMaxWarps)));
+  c.blocks = slabs * c.cluster;
   return c;
 }
 
-template <typename E, int V, bool LERP>
-cudaError_t launch_tiles(const GlrArgs& p, bool backward, cudaStream_t stream) {
+template <typename E, int V, Mode MODE>
+cudaError_t launch_tiles(const GlrArgs& p, bool lerp, bool backward, cudaStream_t stream) {
   const Cut c = cut(p, V);
-  auto* kernel = backward ? glr_backward_kernel<E, V, LERP> : glr_forward_kernel<E, V, LERP>;
-  const size_t smem = size_t(c.warps) * 32 * 4 * (backward ? kBackwardStages * (3 * kChunk + V) : kForwardStages * 2 * kChunk) +
+  auto* kernel = backward ? (lerp ? glr_backward_kernel<E, V, MODE, true> : glr_backward_kernel<E, V, MODE, false>)
+                          : (lerp ? glr_forward_kernel<E, V, MODE, true> : glr_forward_kernel<E, V, MODE, false>);
+  const size_t smem = size_t(c.warps) * kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2) +
                       (c.cluster > 1 ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
   if (e != cudaSuccess) return e;
@@ -523,16 +652,19 @@ cudaError_t launch(const GlrArgs& p, int form, bool backward, cudaStream_t strea
     const int64_t blocks = (p.B * p.D + 127) / 128;
     return launch_pdl(lerp ? glr_step_kernel<E, true> : glr_step_kernel<E, false>, dim3(unsigned(blocks)), dim3(128), 0, stream, p);
   }
-  if constexpr (sizeof(E) == 4) {
-    return lerp ? launch_tiles<E, 1, true>(p, backward, stream) : launch_tiles<E, 1, false>(p, backward, stream);
-  } else {
-    // pairs of channels where every row of every tensor starts at a 4-byte boundary
-    bool pairs = p.D % 2 == 0;
-    for (const gem_seq_t* s : {&p.x, &p.f, backward ? &p.dh : &p.h, backward ? &p.dx : &p.h, backward ? &p.df : &p.h})
-      pairs = pairs && aligned_to(s->data, 4) && (p.B == 1 || s->stride_b % 2 == 0) && (p.T == 1 || s->stride_t % 2 == 0);
-    if (pairs) return lerp ? launch_tiles<E, 2, true>(p, backward, stream) : launch_tiles<E, 2, false>(p, backward, stream);
-    return lerp ? launch_tiles<E, 1, true>(p, backward, stream) : launch_tiles<E, 1, false>(p, backward, stream);
+  // the largest power of two up to 16 bytes on which every row of every tensor starts and D ends
+  uint64_t bits = 16 | uint64_t(p.D) * sizeof(E);
+  for (const gem_seq_t* s : {&p.x, &p.f, backward ? &p.dh : &p.h, backward ? &p.dx : &p.h, backward ? &p.df : &p.h}) {
+    bits |= reinterpret_cast<uintptr_t>(s->data);
+    if (p.B > 1) bits |= uint64_t(s->stride_b) * sizeof(E);
+    if (p.T > 1) bits |= uint64_t(s->stride_t) * sizeof(E);
   }
+  constexpr int kWordV = 4 / sizeof(E);
+  if (bits % 16 == 0) return launch_tiles<E, kWordV, kVector>(p, lerp, backward, stream);
+  if constexpr (sizeof(E) == 2) {
+    if (bits % 4 != 0) return launch_tiles<E, 1, kHalf>(p, lerp, backward, stream);
+  }
+  return launch_tiles<E, kWordV, kWord>(p, lerp, backward, stream);
 }
 
 cudaError_t launch_glr(int dtype, const GlrArgs& p, int form, bool backward, cudaStream_t stream) {
