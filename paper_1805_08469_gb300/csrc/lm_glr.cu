@@ -38,19 +38,84 @@ __device__ __forceinline__ int64_t steps_of(const GlrArgs& p, int64_t b) {
   return n < 0 ? 0 : n > p.T ? p.T : n;
 }
 
+// V channels; for V = 2 sums and products are one packed instruction on the pair.
+template <int V>
+struct Vec {
+  float v[V];
+};
+
+__device__ __forceinline__ uint64_t bits(const Vec<2>& a) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
+  return r;
+}
+__device__ __forceinline__ Vec<2> pair(uint64_t r) {
+  Vec<2> a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
+  return a;
+}
+
+template <int V>
+__device__ __forceinline__ Vec<V> splat(float x) {
+  Vec<V> r;
+#pragma unroll
+  for (int k = 0; k < V; ++k) r.v[k] = x;
+  return r;
+}
+
+template <int V>
+__device__ __forceinline__ Vec<V> fma(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return pair(r);
+  } else {
+    return {fmaf(a.v[0], b.v[0], c.v[0])};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator*(const Vec<V>& a, const Vec<V>& b) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+  } else {
+    return {a.v[0] * b.v[0]};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator+(const Vec<V>& a, const Vec<V>& b) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+  } else {
+    return {a.v[0] + b.v[0]};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator-(const Vec<V>& a, const Vec<V>& b) {
+  return fma<V>(b, splat<V>(-1.0f), a);
+}
+
 // a = sigmoid(f) and b = 1 - a = sigmoid(-f), each to its own relative precision: with e = exp(-f),
 // a = 1 / (1 + e) and b = e a.  f below -80 counts as -80 (a = 2e-35): e stays finite.  NaN stays.
-template <typename E>
-__device__ __forceinline__ void gate(float f, float& a, float& b) {
-  float e;
-  asm("max.NaN.f32 %0, %0, 0fC2A00000;" : "+f"(f));
+template <typename E, int V>
+__device__ __forceinline__ void gate(Vec<V> f, Vec<V>& a, Vec<V>& b) {
+  Vec<V> e;
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("max.NaN.f32 %0, %0, 0fC2A00000;" : "+f"(f.v[k]));
   if constexpr (sizeof(E) == 4) {
-    e = expf(-f);
+    e.v[0] = expf(-f.v[0]);
   } else {
     // 16-bit inputs carry 2^-9 themselves; rounding f log2(e) costs |f| 2^-24 of e
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(f * -1.44269504f));
+    f = f * splat<V>(-1.44269504f);
+#pragma unroll
+    for (int k = 0; k < V; ++k) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.v[k]) : "f"(f.v[k]));
   }
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(1.0f + e));
+  const Vec<V> s = e + splat<V>(1.0f);
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.v[k]) : "f"(s.v[k]));
   b = e * a;
 }
 
@@ -68,11 +133,11 @@ __global__ void glr_step_kernel(const GlrArgs p) {
   for (int64_t t = 0; t < p.T; ++t) {
     float shown = 0.0f;
     if (t < n) {
-      float a, c;
-      gate<E>(to_f32(*at<const E>(p.f, b, t, d)), a, c);
+      Vec<1> a, c;
+      gate<E, 1>({to_f32(*at<const E>(p.f, b, t, d))}, a, c);
       const float x = to_f32(*at<const E>(p.x, b, t, d));
-      const float u = LERP ? c * x : x;
-      h = p.reset && p.reset[b * p.T + t] ? u : fmaf(a, h, u);
+      const float u = LERP ? c.v[0] * x : x;
+      h = p.reset && p.reset[b * p.T + t] ? u : fmaf(a.v[0], h, u);
       shown = h;
     }
     *at<E>(p.h, b, t, d) = from_f32<E>(shown);
@@ -103,102 +168,93 @@ constexpr int kMaxCluster = 8;
 
 template <int V>
 struct Map {
-  float A[V], H[V];
+  Vec<V> A, H;
 };
 
-// Applies m to h, and composes m after the maps so far.  RESETS: a map may forget.
-template <int V>
-__device__ __forceinline__ void apply(float (&h)[V], const Map<V>& m, bool resets) {
+// h after the map m, and m after the maps composed so far.  RESETS: a map may forget.
+template <int V, bool RESETS>
+__device__ __forceinline__ Vec<V> apply(const Vec<V>& h, const Map<V>& m) {
+  Vec<V> r = fma<V>(m.A, h, m.H);
+  if constexpr (RESETS) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const float moved = fmaf(m.A[v], h[v], m.H[v]);
-    h[v] = resets && m.A[v] < 0.0f ? m.H[v] : moved;
+    for (int k = 0; k < V; ++k) r.v[k] = m.A.v[k] < 0.0f ? m.H.v[k] : r.v[k];
   }
+  return r;
 }
 
-template <int V>
-__device__ __forceinline__ void compose(Map<V>& sofar, const Map<V>& m, bool resets) {
+template <int V, bool RESETS>
+__device__ __forceinline__ Map<V> compose(const Map<V>& sofar, const Map<V>& m) {
+  Map<V> r = {sofar.A * m.A, apply<V, RESETS>(sofar.H, m)};
+  if constexpr (RESETS) {
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    const bool forgets = resets && m.A[v] < 0.0f;
-    const float moved = fmaf(m.A[v], sofar.H[v], m.H[v]);
-    sofar.H[v] = forgets ? m.H[v] : moved;
-    sofar.A[v] = forgets || (resets && sofar.A[v] < 0.0f) ? -1.0f : sofar.A[v] * m.A[v];
+    for (int k = 0; k < V; ++k) r.A.v[k] = m.A.v[k] < 0.0f || sofar.A.v[k] < 0.0f ? -1.0f : r.A.v[k];
   }
+  return r;
 }
 
 // From every thread's map of a round: the state before the thread's chunk, and `state` moved on to
 // the state after the round.  maps: [2][kMaxWarps][32], blocks: [2][C][32] (C > 1) in shared memory.
-template <int V>
-__device__ __forceinline__ void scan_round(const Map<V>& own, int round, int warps, int rank, int C, bool resets, Map<V>* maps,
-                                           Map<V>* blocks, float (&state)[V], float (&before)[V]) {
+template <int V, bool RESETS>
+__device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int warps, int rank, int C, Map<V>* maps, Map<V>* blocks,
+                                             Vec<V>& state) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   Map<V>* buf = maps + (round & 1) * kMaxWarps * 32 + lane;
+  Vec<V> before = state;
   buf[warp * 32] = own;
   __syncthreads();
   if (C == 1) {
 #pragma unroll
     for (int w = 0; w < kMaxWarps; ++w) {
       if (w >= warps) break;
-      if (w == warp) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) before[v] = state[v];
-      }
-      apply<V>(state, buf[w * 32], resets);
+      if (w == warp) before = state;
+      state = apply<V, RESETS>(state, buf[w * 32]);
     }
-    return;
+    return before;
   }
-  Map<V> all, mine;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    all.A[v] = 1.0f;
-    all.H[v] = 0.0f;
-  }
-  mine = all;
+  Map<V> all = {splat<V>(1.0f), splat<V>(0.0f)}, mine = all;
 #pragma unroll
   for (int w = 0; w < kMaxWarps; ++w) {
     if (w >= warps) break;
     if (w == warp) mine = all;
-    compose<V>(all, buf[w * 32], resets);
+    all = compose<V, RESETS>(all, buf[w * 32]);
   }
   cg::cluster_group cluster = cg::this_cluster();
   Map<V>* out = blocks + (round & 1) * C * 32 + lane;
   for (int c = warp; c < C; c += warps) cluster.map_shared_rank(out, c)[rank * 32] = all;
   cluster.sync();
   for (int c = 0; c < C; ++c) {
-    if (c == rank) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) before[v] = state[v];
-    }
-    apply<V>(state, out[c * 32], resets);
+    if (c == rank) before = state;
+    state = apply<V, RESETS>(state, out[c * 32]);
   }
-  apply<V>(before, mine, resets);
+  return apply<V, RESETS>(before, mine);
 }
 
 // A word of channels as V floats, and back.
 template <typename E, int V>
-__device__ __forceinline__ void unpack(uint32_t w, float (&v)[V]) {
+__device__ __forceinline__ Vec<V> unpack(uint32_t w) {
+  Vec<V> r;
   if constexpr (sizeof(E) == 4) {
-    v[0] = __uint_as_float(w);
+    r.v[0] = __uint_as_float(w);
   } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
-    v[0] = __uint_as_float(w << 16);
-    if constexpr (V == 2) v[1] = __uint_as_float(w & 0xffff0000u);
+    r.v[0] = __uint_as_float(w << 16);
+    if constexpr (V == 2) r.v[1] = __uint_as_float(w & 0xffff0000u);
   } else {
     const __half2 h = *reinterpret_cast<const __half2*>(&w);
-    v[0] = __low2float(h);
-    if constexpr (V == 2) v[1] = __high2float(h);
+    r.v[0] = __low2float(h);
+    if constexpr (V == 2) r.v[1] = __high2float(h);
   }
+  return r;
 }
 
 template <typename E, int V>
-__device__ __forceinline__ uint32_t pack(const float (&v)[V]) {
+__device__ __forceinline__ uint32_t pack(const Vec<V>& a) {
   if constexpr (sizeof(E) == 4) {
-    return __float_as_uint(v[0]);
+    return __float_as_uint(a.v[0]);
   } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
-    const __nv_bfloat162 w = __floats2bfloat162_rn(v[0], V == 2 ? v[V - 1] : 0.0f);
+    const __nv_bfloat162 w = __floats2bfloat162_rn(a.v[0], V == 2 ? a.v[V - 1] : 0.0f);
     return *reinterpret_cast<const uint32_t*>(&w);
   } else {
-    const __half2 w = __floats2half2_rn(v[0], V == 2 ? v[V - 1] : 0.0f);
+    const __half2 w = __floats2half2_rn(a.v[0], V == 2 ? a.v[V - 1] : 0.0f);
     return *reinterpret_cast<const uint32_t*>(&w);
   }
 }
@@ -317,39 +373,34 @@ __device__ __forceinline__ uint32_t reset_bits(const GlrArgs& p, int64_t b, int6
 // The steps of a chunk: all kChunk of them without a reset (PLAIN), or the first m with resets
 // where `fresh` has a bit.
 template <typename E, int V, bool LERP, bool PLAIN>
-__device__ __forceinline__ void forward_map(const uint32_t* x, const uint32_t* f, int m, uint32_t fresh,
-                                            float (&a)[kChunk][V], float (&u)[kChunk][V], Map<V>& own) {
+__device__ __forceinline__ Map<V> forward_map(const uint32_t* x, const uint32_t* f, int m, uint32_t fresh, Vec<V> (&a)[kChunk],
+                                              Vec<V> (&u)[kChunk]) {
+  Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
-    float xv[V], fv[V];
-    unpack<E, V>(x[k * 32], xv);
-    unpack<E, V>(f[k * 32], fv);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      float g;
-      gate<E>(fv[v], a[k][v], g);
-      u[k][v] = LERP ? g * xv[v] : xv[v];
-      if (!PLAIN && k >= m) {
-        a[k][v] = 1.0f;
-        u[k][v] = 0.0f;
-      }
-      const float moved = fmaf(a[k][v], own.H[v], u[k][v]);
-      own.H[v] = !PLAIN && (fresh >> k & 1) ? u[k][v] : moved;
-      own.A[v] *= a[k][v];
+    Vec<V> b;
+    u[k] = unpack<E, V>(x[k * 32]);
+    gate<E, V>(unpack<E, V>(f[k * 32]), a[k], b);
+    if constexpr (LERP) u[k] = b * u[k];
+    if (!PLAIN && k >= m) {
+      a[k] = splat<V>(1.0f);
+      u[k] = splat<V>(0.0f);
     }
+    const Vec<V> moved = fma<V>(a[k], own.H, u[k]);
+    own.H = !PLAIN && (fresh >> k & 1) ? u[k] : moved;
+    own.A = own.A * a[k];
   }
+  if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
+  return own;
 }
 
 template <typename E, int V, bool PLAIN>
-__device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, const float (&a)[kChunk][V],
-                                              const float (&u)[kChunk][V], float (&h)[V]) {
+__device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, const Vec<V> (&a)[kChunk], const Vec<V> (&u)[kChunk],
+                                              Vec<V> h) {
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float moved = fmaf(a[k][v], h[v], u[k][v]);
-      h[v] = !PLAIN && (fresh >> k & 1) ? u[k][v] : moved;
-    }
+    const Vec<V> moved = fma<V>(a[k], h, u[k]);
+    h = !PLAIN && (fresh >> k & 1) ? u[k] : moved;
     out[k * 32] = pack<E, V>(h);
   }
 }
@@ -375,9 +426,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
   const E* f = at<const E>(p.f, w.b, 0, w.move_d);
   E* h_out = at<E>(p.h, w.b, 0, w.move_d);
   const int64_t state_at = w.b * p.D + w.d;
-  float state[V];
+  Vec<V> state;
 #pragma unroll
-  for (int v = 0; v < V; ++v) state[v] = p.h0 && w.on ? p.h0[state_at + v] : 0.0f;
+  for (int v = 0; v < V; ++v) state.v[v] = p.h0 && w.on ? p.h0[state_at + v] : 0.0f;
 
   auto issue = [&](int round, int stage) {
     const int64_t c = first + round * per_round;
@@ -404,28 +455,16 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
     __syncwarp();
     uint32_t* const tile = ring + stage * kStage;
     stage = stage == kForwardStages - 1 ? 0 : stage + 1;
-    float a[kChunk][V], u[kChunk][V], h[V];
-    Map<V> own;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      own.A[v] = 1.0f;
-      own.H[v] = 0.0f;
-    }
-    if (plain) {
-      forward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u, own);
-    } else {
-      forward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u, own);
-      if (fresh) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
-      }
-    }
-    scan_round<V>(own, round, w.warps, w.rank, C, resets, maps, blocks, state, h);
+    Vec<V> a[kChunk], u[kChunk];
+    const Map<V> own = plain ? forward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u)
+                             : forward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u);
+    const Vec<V> h = resets ? scan_round<V, true>(own, round, w.warps, w.rank, C, maps, blocks, state)
+                            : scan_round<V, false>(own, round, w.warps, w.rank, C, maps, blocks, state);
     if (!busy) continue;
     if (p.saved_out && w.on) {
       float* s = p.saved_out + (w.b * all_chunks + c) * p.D + w.d;
 #pragma unroll
-      for (int v = 0; v < V; ++v) s[v] = h[v];
+      for (int v = 0; v < V; ++v) s[v] = h.v[v];
     }
     if (plain)
       forward_apply<E, V, true>(tile + w.lane, fresh, a, u, h);
@@ -441,10 +480,10 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
   if (p.saved_out)
     for (int64_t c = chunks + first; c < all_chunks; c += per_round)
 #pragma unroll
-      for (int v = 0; v < V; ++v) p.saved_out[(w.b * all_chunks + c) * p.D + w.d + v] = state[v];
+      for (int v = 0; v < V; ++v) p.saved_out[(w.b * all_chunks + c) * p.D + w.d + v] = state.v[v];
   if (p.h_last && first == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) p.h_last[state_at + v] = state[v];
+    for (int v = 0; v < V; ++v) p.h_last[state_at + v] = state.v[v];
   }
 }
 
@@ -452,57 +491,42 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
 // after it hands back.  The states before the chunk's steps are computed again from the saved one.
 // q: what the gate's gradient multiplies, h_{t-1} - x_t or h_{t-1}.
 template <typename E, int V, bool LERP, bool PLAIN>
-__device__ __forceinline__ void backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
-                                             float (&h)[V], float (&a)[kChunk][V], float (&b)[kChunk][V],
-                                             float (&q)[kChunk][V], Map<V>& own) {
+__device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
+                                               Vec<V> h, Vec<V> (&a)[kChunk], Vec<V> (&b)[kChunk], Vec<V> (&q)[kChunk]) {
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
-    float xv[V], fv[V];
-    unpack<E, V>(x[k * 32], xv);
-    unpack<E, V>(f[k * 32], fv);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      gate<E>(fv[v], a[k][v], b[k][v]);
-      const float u = LERP ? b[k][v] * xv[v] : xv[v];
-      const bool r = !PLAIN && (fresh >> k & 1);
-      q[k][v] = (r ? 0.0f : h[v]) - (LERP ? xv[v] : 0.0f);
-      const float moved = fmaf(a[k][v], h[v], u);
-      h[v] = r ? u : moved;
-    }
+    const Vec<V> xv = unpack<E, V>(x[k * 32]);
+    gate<E, V>(unpack<E, V>(f[k * 32]), a[k], b[k]);
+    const Vec<V> u = LERP ? b[k] * xv : xv;
+    const bool r = !PLAIN && (fresh >> k & 1);
+    if (r) h = splat<V>(0.0f);
+    q[k] = LERP ? h - xv : h;
+    h = r ? u : fma<V>(a[k], h, u);
   }
+  Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
-    float dv[V];
-    unpack<E, V>(dh[k * 32], dv);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (PLAIN || k < m) {
-        own.H[v] = !PLAIN && (fresh >> k & 1) ? 0.0f : a[k][v] * (dv[v] + own.H[v]);
-        own.A[v] *= a[k][v];
-      }
-    }
+    if (!PLAIN && k >= m) continue;
+    const Vec<V> moved = a[k] * (unpack<E, V>(dh[k * 32]) + own.H);
+    own.H = !PLAIN && (fresh >> k & 1) ? splat<V>(0.0f) : moved;
+    own.A = own.A * a[k];
   }
+  if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
+  return own;
 }
 
 template <typename E, int V, bool LERP, bool PLAIN>
 __device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const uint32_t* dh, int m, uint32_t fresh,
-                                               const float (&a)[kChunk][V], const float (&b)[kChunk][V],
-                                               const float (&q)[kChunk][V], float (&g)[V]) {
+                                               const Vec<V> (&a)[kChunk], const Vec<V> (&b)[kChunk], const Vec<V> (&q)[kChunk],
+                                               Vec<V> g) {
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
     if (!PLAIN && k >= m) continue;
-    float dv[V], dxv[V], dfv[V];
-    unpack<E, V>(dh[k * 32], dv);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      g[v] += dv[v];
-      dxv[v] = LERP ? b[k][v] * g[v] : g[v];
-      g[v] = a[k][v] * g[v];
-      dfv[v] = g[v] * (q[k][v] * b[k][v]);
-      if (!PLAIN && (fresh >> k & 1)) g[v] = 0.0f;
-    }
-    dx[k * 32] = pack<E, V>(dxv);
-    df[k * 32] = pack<E, V>(dfv);
+    g = g + unpack<E, V>(dh[k * 32]);
+    dx[k * 32] = pack<E, V>(LERP ? b[k] * g : g);
+    g = a[k] * g;
+    df[k * 32] = pack<E, V>(g * (q[k] * b[k]));
+    if (!PLAIN && (fresh >> k & 1)) g = splat<V>(0.0f);
   }
 }
 
@@ -529,12 +553,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
   E* dx_out = at<E>(p.dx, w.b, 0, w.move_d);
   E* df_out = at<E>(p.df, w.b, 0, w.move_d);
   const int64_t state_at = w.b * p.D + w.d;
-  float state[V], saved[V];
+  Vec<V> state, saved = splat<V>(0.0f);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    state[v] = p.dh_last && w.on ? p.dh_last[state_at + v] : 0.0f;
-    saved[v] = 0.0f;
-  }
+  for (int v = 0; v < V; ++v) state.v[v] = p.dh_last && w.on ? p.dh_last[state_at + v] : 0.0f;
 
   auto issue = [&](int round, int stage) {
     const int64_t l = first + round * per_round;
@@ -554,7 +575,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     if (l < chunks && w.on) {
       const float* s = p.saved_in + (w.b * all_chunks + chunks - 1 - l) * p.D + w.d;
 #pragma unroll
-      for (int v = 0; v < V; ++v) saved[v] = s[v];
+      for (int v = 0; v < V; ++v) saved.v[v] = s[v];
     }
   };
 #pragma unroll
@@ -574,26 +595,13 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     uint32_t* const tile = ring + stage * kStage;
     const uint32_t* const dhs = tile + 2 * kTile + w.lane;
     stage = stage == kBackwardStages - 1 ? 0 : stage + 1;
-    float a[kChunk][V], b[kChunk][V], q[kChunk][V], h[V];
-    Map<V> own;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      h[v] = saved[v];
-      own.A[v] = 1.0f;
-      own.H[v] = 0.0f;
-    }
+    Vec<V> a[kChunk], b[kChunk], q[kChunk];
+    const Vec<V> h = saved;
     load_saved(round + 1);
-    if (plain) {
-      backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q, own);
-    } else {
-      backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q, own);
-      if (fresh) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) own.A[v] = -1.0f;
-      }
-    }
-    float g[V];
-    scan_round<V>(own, round, w.warps, w.rank, C, resets, maps, blocks, state, g);
+    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q)
+                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q);
+    const Vec<V> g = resets ? scan_round<V, true>(own, round, w.warps, w.rank, C, maps, blocks, state)
+                            : scan_round<V, false>(own, round, w.warps, w.rank, C, maps, blocks, state);
     if (!busy) continue;
     if (plain)
       backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, a, b, q, g);
@@ -608,7 +616,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
   store_zeros<E, V>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T);
   if (p.dh0 && first == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) p.dh0[state_at + v] = state[v];
+    for (int v = 0; v < V; ++v) p.dh0[state_at + v] = state.v[v];
   }
 }
 
