@@ -488,28 +488,31 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
 }
 
 // Backward: the same scan from the end.  A step's map is g -> a (dh + g), g being what the step
-// after it hands back.  The states before the chunk's steps are computed again from the saved one.
-// q: what the gate's gradient multiplies, h_{t-1} - x_t or h_{t-1}.
+// after it hands back.  A chunk's map is sum_k (a_0 .. a_k) dh_k + (a_0 .. a_15) g, so it is
+// composed in the same pass over the steps that computes the states before them again, from the
+// saved one; nothing counts from the first reset on.  q: what the gate's gradient multiplies,
+// h_{t-1} - x_t or h_{t-1}.
 template <typename E, int V, bool LERP, bool PLAIN>
 __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
-                                               Vec<V> h, Vec<V> (&a)[kChunk], Vec<V> (&b)[kChunk], Vec<V> (&q)[kChunk]) {
+                                               Vec<V> h, Vec<V> (&q)[kChunk]) {
+  Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
+  bool counts = true;
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
+    if (!PLAIN && k >= m) continue;
+    Vec<V> a, b;
     const Vec<V> xv = unpack<E, V>(x[k * 32]);
-    gate<E, V>(unpack<E, V>(f[k * 32]), a[k], b[k]);
-    const Vec<V> u = LERP ? b[k] * xv : xv;
+    gate<E, V>(unpack<E, V>(f[k * 32]), a, b);
+    const Vec<V> u = LERP ? b * xv : xv;
     const bool r = !PLAIN && (fresh >> k & 1);
     if (r) h = splat<V>(0.0f);
     q[k] = LERP ? h - xv : h;
-    h = r ? u : fma<V>(a[k], h, u);
-  }
-  Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
-#pragma unroll
-  for (int k = kChunk - 1; k >= 0; --k) {
-    if (!PLAIN && k >= m) continue;
-    const Vec<V> moved = a[k] * (unpack<E, V>(dh[k * 32]) + own.H);
-    own.H = !PLAIN && (fresh >> k & 1) ? splat<V>(0.0f) : moved;
-    own.A = own.A * a[k];
+    h = r ? u : fma<V>(a, h, u);
+    if (r) counts = false;
+    if (counts) {
+      own.A = own.A * a;
+      own.H = fma<V>(own.A, unpack<E, V>(dh[k * 32]), own.H);
+    }
   }
   if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
   return own;
@@ -517,15 +520,17 @@ __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t
 
 template <typename E, int V, bool LERP, bool PLAIN>
 __device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const uint32_t* dh, int m, uint32_t fresh,
-                                               const Vec<V> (&a)[kChunk], const Vec<V> (&b)[kChunk], const Vec<V> (&q)[kChunk],
-                                               Vec<V> g) {
+                                               const Vec<V> (&q)[kChunk], Vec<V> g) {
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
     if (!PLAIN && k >= m) continue;
     g = g + unpack<E, V>(dh[k * 32]);
-    dx[k * 32] = pack<E, V>(LERP ? b[k] * g : g);
-    g = a[k] * g;
-    df[k * 32] = pack<E, V>(g * (q[k] * b[k]));
+    // the gate again from f (its slot is df's): kept, it would take 64 registers
+    Vec<V> a, b;
+    gate<E, V>(unpack<E, V>(df[k * 32]), a, b);
+    dx[k * 32] = pack<E, V>(LERP ? b * g : g);
+    g = a * g;
+    df[k * 32] = pack<E, V>(g * (q[k] * b));
     if (!PLAIN && (fresh >> k & 1)) g = splat<V>(0.0f);
   }
 }
@@ -595,18 +600,18 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     uint32_t* const tile = ring + stage * kStage;
     const uint32_t* const dhs = tile + 2 * kTile + w.lane;
     stage = stage == kBackwardStages - 1 ? 0 : stage + 1;
-    Vec<V> a[kChunk], b[kChunk], q[kChunk];
+    Vec<V> q[kChunk];
     const Vec<V> h = saved;
     load_saved(round + 1);
-    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q)
-                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, a, b, q);
+    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q)
+                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q);
     const Vec<V> g = resets ? scan_round<V, true>(own, round, w.warps, w.rank, C, maps, blocks, state)
                             : scan_round<V, false>(own, round, w.warps, w.rank, C, maps, blocks, state);
     if (!busy) continue;
     if (plain)
-      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, a, b, q, g);
+      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, g);
     else
-      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, a, b, q, g);
+      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, g);
     store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves);
     store_tile<E, MODE>(tile + kTile, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves);
   }
