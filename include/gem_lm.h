@@ -121,7 +121,7 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *     = ld: row_scale[n] dL/dlogits.
  * A student logit of -inf has p = 0: its gradient is that of the formula, and the loss is +inf
  * where the teacher gives it mass.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
- * temperature <= 1e20, 0 <= alpha <= 1, V >= 1, ld >= V (or 0: one row of logits for all), grad_ld >= V. */
+ * temperature <= 1e20, 0 <= alpha <= 1, 1 <= V <= 2^30, N <= 2^27, ld >= V (or 0: one row of logits for all), grad_ld >= V. */
 int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld, int K,
                 const int32_t* top_idx, const float* top_logits, const float* teacher_lse,
                 const int32_t* labels, const float* row_scale, float temperature, float alpha,

@@ -653,7 +653,7 @@ cudaError_t launch_tiles(const GlrArgs& p, bool lerp, bool backward, cudaStream_
                           : (lerp ? glr_forward_kernel<E, V, MODE, true> : glr_forward_kernel<E, V, MODE, false>);
   const size_t smem = size_t(c.warps) * kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2) +
                       (c.cluster > 1 ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  const cudaError_t e = allow_smem(kernel, smem);
   if (e != cudaSuccess) return e;
   return launch_cluster_pdl(kernel, unsigned(c.blocks), unsigned(c.warps * 32), unsigned(c.cluster), smem, stream, p, c.cluster);
 }

@@ -43,6 +43,13 @@ constexpr int64_t kMaxStride = int64_t(1) << 46;
 
 inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 
+// Lets a kernel be launched with this much dynamic shared memory (48 KB together with its static
+// shared memory, of which these kernels have up to 16 KB, need no permission).
+template <typename Kernel>
+cudaError_t allow_smem(Kernel* kernel, size_t bytes) {
+  return bytes <= 32 << 10 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+}
+
 // launch_pdl for a grid of clusters of `cluster` blocks.
 template <typename... KArgs, typename... Args>
 cudaError_t launch_cluster_pdl(void (*kernel)(KArgs...), unsigned blocks, unsigned threads, unsigned cluster, size_t smem,
