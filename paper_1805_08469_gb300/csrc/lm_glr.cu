@@ -38,66 +38,6 @@ __device__ __forceinline__ int64_t steps_of(const GlrArgs& p, int64_t b) {
   return n < 0 ? 0 : n > p.T ? p.T : n;
 }
 
-// V channels; for V = 2 sums and products are one packed instruction on the pair.
-template <int V>
-struct Vec {
-  float v[V];
-};
-
-__device__ __forceinline__ uint64_t bits(const Vec<2>& a) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
-  return r;
-}
-__device__ __forceinline__ Vec<2> pair(uint64_t r) {
-  Vec<2> a;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
-  return a;
-}
-
-template <int V>
-__device__ __forceinline__ Vec<V> splat(float x) {
-  Vec<V> r;
-#pragma unroll
-  for (int k = 0; k < V; ++k) r.v[k] = x;
-  return r;
-}
-
-template <int V>
-__device__ __forceinline__ Vec<V> fma(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
-  if constexpr (V == 2) {
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
-    return pair(r);
-  } else {
-    return {fmaf(a.v[0], b.v[0], c.v[0])};
-  }
-}
-template <int V>
-__device__ __forceinline__ Vec<V> operator*(const Vec<V>& a, const Vec<V>& b) {
-  if constexpr (V == 2) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-    return pair(r);
-  } else {
-    return {a.v[0] * b.v[0]};
-  }
-}
-template <int V>
-__device__ __forceinline__ Vec<V> operator+(const Vec<V>& a, const Vec<V>& b) {
-  if constexpr (V == 2) {
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-    return pair(r);
-  } else {
-    return {a.v[0] + b.v[0]};
-  }
-}
-template <int V>
-__device__ __forceinline__ Vec<V> operator-(const Vec<V>& a, const Vec<V>& b) {
-  return fma<V>(b, splat<V>(-1.0f), a);
-}
-
 // a = sigmoid(f) and b = 1 - a = sigmoid(-f), each to its own relative precision: with e = exp(-f),
 // a = 1 / (1 + e) and b = e a.  f below -80 counts as -80 (a = 2e-35): e stays finite.  NaN stays.
 template <typename E, int V>

@@ -28,6 +28,66 @@ __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { retu
 template <>
 __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
 
+// V floats; for V = 2 sums and products are one packed instruction on the pair.
+template <int V>
+struct Vec {
+  float v[V];
+};
+
+__device__ __forceinline__ uint64_t bits(const Vec<2>& a) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a.v[0]), "f"(a.v[1]));
+  return r;
+}
+__device__ __forceinline__ Vec<2> pair(uint64_t r) {
+  Vec<2> a;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a.v[0]), "=f"(a.v[1]) : "l"(r));
+  return a;
+}
+
+template <int V>
+__device__ __forceinline__ Vec<V> splat(float x) {
+  Vec<V> r;
+#pragma unroll
+  for (int k = 0; k < V; ++k) r.v[k] = x;
+  return r;
+}
+
+template <int V>
+__device__ __forceinline__ Vec<V> fma(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+    return pair(r);
+  } else {
+    return {fmaf(a.v[0], b.v[0], c.v[0])};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator*(const Vec<V>& a, const Vec<V>& b) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+  } else {
+    return {a.v[0] * b.v[0]};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator+(const Vec<V>& a, const Vec<V>& b) {
+  if constexpr (V == 2) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
+    return pair(r);
+  } else {
+    return {a.v[0] + b.v[0]};
+  }
+}
+template <int V>
+__device__ __forceinline__ Vec<V> operator-(const Vec<V>& a, const Vec<V>& b) {
+  return fma<V>(b, splat<V>(-1.0f), a);
+}
+
 inline int dtype_size(int dtype) { return dtype == GEM_F32 ? 4 : 2; }
 inline bool dtype_ok(int dtype) { return dtype == GEM_F32 || dtype == GEM_BF16 || dtype == GEM_F16; }
 

@@ -334,37 +334,39 @@ __device__ __forceinline__ void load_slice(const Slice<E>& s, uint4* data) {
 }
 __device__ __forceinline__ void load_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
-// The piece's elements as floats.
+// A piece's elements as pairs of floats, and back.
 template <typename E>
-__device__ __forceinline__ void unpack(const uint4& w, float (&v)[kPer<E>]) {
+constexpr int kPairs = kPer<E> / 2;
+
+template <typename E>
+__device__ __forceinline__ void unpack(const uint4& w, Vec<2> (&v)[kPairs<E>]) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kPairs<E>; ++k) {
     if constexpr (sizeof(E) == 4) {
-      v[k] = __uint_as_float(u[k]);
+      v[k] = {__uint_as_float(u[2 * k]), __uint_as_float(u[2 * k + 1])};
     } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
-      v[2 * k] = __uint_as_float(u[k] << 16);
-      v[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u);
+      v[k] = {__uint_as_float(u[k] << 16), __uint_as_float(u[k] & 0xffff0000u)};
     } else {
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[k]));
-      v[2 * k] = f.x;
-      v[2 * k + 1] = f.y;
+      v[k] = {f.x, f.y};
     }
   }
 }
 
 template <typename E>
-__device__ __forceinline__ uint4 pack(const float (&v)[kPer<E>]) {
+__device__ __forceinline__ uint4 pack(const Vec<2> (&v)[kPairs<E>]) {
   uint32_t u[4];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kPairs<E>; ++k) {
     if constexpr (sizeof(E) == 4) {
-      u[k] = __float_as_uint(v[k]);
+      u[2 * k] = __float_as_uint(v[k].v[0]);
+      u[2 * k + 1] = __float_as_uint(v[k].v[1]);
     } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
-      const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(v[k].v[0], v[k].v[1]);
       u[k] = *reinterpret_cast<const uint32_t*>(&h);
     } else {
-      const __half2 h = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+      const __half2 h = __floats2half2_rn(v[k].v[0], v[k].v[1]);
       u[k] = *reinterpret_cast<const uint32_t*>(&h);
     }
   }
@@ -389,56 +391,82 @@ __device__ __forceinline__ float piece_max(const uint4& w) {
 struct Stats {
   float m, s, e, s1;
 };
+__device__ __forceinline__ Stats no_stats() { return {-INFINITY, 0.0f, 0.0f, 0.0f}; }
 
-// Joins b to a (c = log2(e) / tau).
-__device__ __forceinline__ void join(Stats& a, const Stats& b, float c) {
-  const float m = fmaxf(a.m, b.m);
-  const float ref = m == -INFINITY ? 0.0f : m;
-  const float da = a.m - ref, db = b.m - ref;   // -inf where a side is empty: its sums then count 0
-  const float fa = exp2_fast(da * c), fb = exp2_fast(db * c);
-  // (far below the other side nothing is left of a side, and its e must not be infinite by then)
-  a.e = (a.e + fmaxf(da * c, -1000.0f) * a.s) * fa + (b.e + fmaxf(db * c, -1000.0f) * b.s) * fb;
-  a.s = a.s * fa + b.s * fb;
-  a.s1 = a.s1 * exp2_fast(da * kLog2e) + b.s1 * exp2_fast(db * kLog2e);
+// a relative to m >= a.m instead (c = log2(e) / tau); an empty set stays one.
+__device__ __forceinline__ void rebase(Stats& a, float m, float c) {
+  const float d = a.m - (m == -INFINITY ? 0.0f : m), f = exp2_fast(d * c);
+  // (far below m nothing is left of a set, and its e must not be infinite by then)
+  a.e = (a.e + fmaxf(d * c, -1000.0f) * a.s) * f;
+  a.s *= f;
+  a.s1 *= exp2_fast(d * kLog2e);
   a.m = m;
 }
 
+// Joins b to a.
+__device__ __forceinline__ void join(Stats& a, Stats b, float c) {
+  const float m = fmaxf(a.m, b.m);
+  rebase(a, m, c);
+  rebase(b, m, c);
+  a.s += b.s;
+  a.e += b.e;
+  a.s1 += b.s1;
+}
+
+// The warp's set from its lanes', in every lane with the same bits.
 __device__ __forceinline__ Stats warp_join(Stats a, float c) {
+  float m = a.m;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+  rebase(a, m, c);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    Stats b;
-    b.m = __shfl_xor_sync(~0u, a.m, o);
-    b.s = __shfl_xor_sync(~0u, a.s, o);
-    b.e = __shfl_xor_sync(~0u, a.e, o);
-    b.s1 = __shfl_xor_sync(~0u, a.s1, o);
-    // both lanes of a pair join in the same order, so that all lanes get the same bits
-    if (threadIdx.x & o) {
-      const Stats t = a;
-      a = b;
-      b = t;
-    }
-    join(a, b, c);
+    a.s += __shfl_xor_sync(~0u, a.s, o);
+    a.e += __shfl_xor_sync(~0u, a.e, o);
+    a.s1 += __shfl_xor_sync(~0u, a.s1, o);
   }
   return a;
+}
+
+// A thread's sums over its pieces, relative to a.m.
+template <typename E, bool ENTROPY, bool HARD, bool CLAMP>
+__device__ __forceinline__ void thread_sums(const uint4* data, int pieces, float c, Stats& a) {
+  const Vec<2> ref = splat<2>(a.m == -INFINITY ? -0.0f : -a.m), scale = splat<2>(c);
+  Vec<2> s = splat<2>(0.0f), e = s, s1 = s;
+#pragma unroll 2
+  for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
+    Vec<2> v[kPairs<E>];
+    unpack<E>(data[i], v);
+#pragma unroll
+    for (int k = 0; k < kPairs<E>; ++k) {
+      const Vec<2> d = v[k] + ref;
+      Vec<2> x = d * scale;
+      const Vec<2> p = {exp2_fast(x.v[0]), exp2_fast(x.v[1])};
+      s = s + p;
+      if constexpr (ENTROPY) {
+        if constexpr (CLAMP) x = {fmaxf(x.v[0], -1000.0f), fmaxf(x.v[1], -1000.0f)};
+        e = fma<2>(p, x, e);
+      }
+      if constexpr (HARD) {
+        const Vec<2> y = d * splat<2>(kLog2e);
+        s1 = s1 + Vec<2>{exp2_fast(y.v[0]), exp2_fast(y.v[1])};
+      }
+    }
+  }
+  a.s = s.v[0] + s.v[1];
+  a.e = e.v[0] + e.v[1];
+  a.s1 = s1.v[0] + s1.v[1];
 }
 
 // A thread's statistics over its pieces.
 template <typename E, bool ENTROPY, bool HARD>
 __device__ __forceinline__ Stats thread_stats(const uint4* data, int pieces, float c) {
-  Stats a = {-INFINITY, 0.0f, 0.0f, 0.0f};
+  Stats a = no_stats();
+#pragma unroll 4
   for (int i = threadIdx.x; i < pieces; i += blockDim.x) a.m = fmaxf(a.m, piece_max<E>(data[i]));
-  const float ref = a.m == -INFINITY ? 0.0f : a.m;
-  for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
-    float v[kPer<E>];
-    unpack<E>(data[i], v);
-#pragma unroll
-    for (int k = 0; k < kPer<E>; ++k) {
-      const float d = v[k] - ref, x = d * c, p = exp2_fast(x);
-      a.s += p;
-      if constexpr (ENTROPY) a.e += p * fmaxf(x, -1000.0f);
-      if constexpr (HARD) a.s1 += exp2_fast(d * kLog2e);
-    }
-  }
+  thread_sums<E, ENTROPY, HARD, false>(data, pieces, c, a);
+  // 0 times -inf, from logits of -inf or far below the others: again with their x bounded
+  if (ENTROPY && isnan(a.e)) thread_sums<E, ENTROPY, HARD, true>(data, pieces, c, a);
   return a;
 }
 
@@ -471,23 +499,23 @@ __device__ __forceinline__ void publish_stats(const Stats& mine, Stats* all, int
 }
 __device__ __forceinline__ Stats collect_stats(const Stats* all, int C, float c) {
   const int lane = threadIdx.x % 32, n = C * int(blockDim.x / 32);
-  Stats a = {-INFINITY, 0.0f, 0.0f, 0.0f};
-  if (lane < n) a = all[lane];
-  if (lane + 32 < n) join(a, all[lane + 32], c);
+  Stats a = lane < n ? all[lane] : no_stats();
+  if (n > 32) join(a, lane + 32 < n ? all[lane + 32] : no_stats(), c);
   return warp_join(a, c);
 }
 
-// Writes f(j, z) of every element j of the slice to out[j]: whole pieces where the output has the
+// Writes f of every pair of elements of the slice to out: whole pieces where the output has the
 // logits' alignment, else element by element.
 template <typename E, typename F>
 __device__ __forceinline__ void write_slice(const Slice<E>& s, const uint4* data, E* out, F f) {
   const bool same = int(reinterpret_cast<uintptr_t>(out) % 16 / sizeof(E)) == s.shift;
+#pragma unroll 2
   for (int i = threadIdx.x; i < s.pieces; i += blockDim.x) {
     const int j = s.index(i);
-    float v[kPer<E>];
+    Vec<2> v[kPairs<E>];
     unpack<E>(data[i], v);
 #pragma unroll
-    for (int k = 0; k < kPer<E>; ++k) v[k] = f(v[k]);
+    for (int k = 0; k < kPairs<E>; ++k) v[k] = f(v[k]);
     const uint4 w = pack<E>(v);
     if (same && j >= 0 && j + kPer<E> <= s.V) {
       *reinterpret_cast<uint4*>(out + j) = w;
@@ -500,13 +528,147 @@ __device__ __forceinline__ void write_slice(const Slice<E>& s, const uint4* data
   }
 }
 
+// The teacher's side of a row, taken by a block's first warp (lane l holds entries l, l + 32, ...)
+// while the others go ahead with the student's row.
+constexpr int kTableBits = 9;
+struct Teacher {
+  int at[GEM_TOP_MAX];      // index of an entry; -1: absent, or another entry has it
+  float q[GEM_TOP_MAX];     // mass there, that of all entries with the index
+  float z[GEM_TOP_MAX];     // the student's logit there
+  int table[1 << kTableBits];
+  float mass;               // sum of q
+  Stats top;                // the student's entries
+  int label_is_entry;
+};
+
+constexpr int kPerLane = GEM_TOP_MAX / 32;
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+  return v;
+}
+
+// Fills t; q and logq: the lane's own entries (0 and anything where absent).
+template <typename E>
+__device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, const E* z, int label, float c, Teacher& t,
+                                             float (&q)[kPerLane], float (&logq)[kPerLane], float (&zk)[kPerLane]) {
+  const int lane = threadIdx.x % 32;
+  const float inv_tau = 1.0f / p.tau;
+  int j[kPerLane];
+  float most = -INFINITY;
+#pragma unroll
+  for (int e = 0; e < kPerLane; ++e) {
+    const int k = e * 32 + lane;
+    j[e] = -1;
+    logq[e] = -INFINITY;
+    if (k < p.K) {
+      const int a = p.top_idx[n * p.K + k];
+      if (a >= 0 && a < p.V) {
+        logq[e] = p.top_logits[n * p.K + k] * inv_tau;
+        if (logq[e] != -INFINITY) j[e] = a;
+      }
+    }
+    zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
+    most = fmaxf(most, logq[e]);
+  }
+  for (int i = lane; i < 1 << kTableBits; i += 32) t.table[i] = -1;
+  float lse;
+  if (p.teacher_lse) {
+    lse = p.teacher_lse[n];
+  } else {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (e * 32 < p.K && j[e] >= 0) sum += expf(logq[e] - most);
+    lse = most + logf(warp_sum(sum));
+  }
+  __syncwarp();
+  float mass = 0.0f;
+  bool again = false, label_here = false;
+  Stats top = no_stats();
+#pragma unroll
+  for (int e = 0; e < kPerLane; ++e) {
+    q[e] = 0.0f;
+    if (e * 32 >= p.K) continue;
+    const int k = e * 32 + lane;
+    if (j[e] >= 0) {
+      logq[e] -= lse;
+      q[e] = expf(logq[e]);
+      mass += q[e];
+      label_here |= j[e] == label;
+      // a table of the indices seen: who finds an index there is not its first entry
+      unsigned h = unsigned(j[e]) * 2654435761u >> (32 - kTableBits);
+      for (;;) {   // (at most half of the table is ever taken)
+        const int other = atomicCAS(&t.table[h], -1, j[e]);
+        if (other == -1) break;
+        if (other == j[e]) {
+          again = true;
+          break;
+        }
+        h = (h + 1) & ((1 << kTableBits) - 1);
+      }
+    }
+    if (k < p.K) {
+      t.at[k] = j[e];
+      t.q[k] = q[e];
+      t.z[k] = zk[e];
+    }
+  }
+  mass = warp_sum(mass);
+  label_here = __any_sync(~0u, label_here);
+  if (__any_sync(~0u, again)) {
+    // entries with the same index add up in the first of them; the others leave
+    float sum[kPerLane];
+    bool first[kPerLane];
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e) {
+      const int k = e * 32 + lane;
+      sum[e] = 0.0f;
+      first[e] = true;
+      if (j[e] < 0) continue;
+      for (int i = 0; i < p.K; ++i)
+        if (t.at[i] == j[e]) {
+          sum[e] += t.q[i];
+          if (i < k) first[e] = false;
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (j[e] >= 0) {
+        if (first[e])
+          t.q[e * 32 + lane] = sum[e];
+        else
+          t.at[e * 32 + lane] = j[e] = -1;
+      }
+  }
+  if (p.teacher_lse) {
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (e * 32 < p.K) {
+        Stats one = no_stats();
+        if (j[e] >= 0 && !(zk[e] == -INFINITY)) one = {zk[e], 1.0f, 0.0f, 1.0f};
+        if (isnan(zk[e])) one = {-INFINITY, zk[e], 0.0f, zk[e]};
+        join(top, one, c);
+      }
+    top = warp_join(top, c);
+  }
+  if (lane == 0) {
+    t.mass = mass;
+    t.top = top;
+    t.label_is_entry = label_here;
+  }
+}
+
 template <typename E, bool HARD>
 __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillArgs p, int C) {
   extern __shared__ uint4 data[];
-  __shared__ float buf[kRowWarps];
   __shared__ Stats all[kRowCluster * kRowWarps];
-  __shared__ int at[GEM_TOP_MAX];
-  __shared__ float qs[GEM_TOP_MAX];
+  __shared__ Teacher teacher;
   pdl_entry();
   const int64_t n = blockIdx.x / C;
   const int rank = blockIdx.x % C, tid = threadIdx.x;
@@ -515,66 +677,32 @@ __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillAr
   const Slice<E> s = slice_of(z, p.V, rank, C);
   const float w = p.row_scale ? p.row_scale[n] : 1.0f;
   if (w == 0.0f) {
-    for (int i = tid; i < s.pieces; i += blockDim.x) data[i] = make_uint4(0, 0, 0, 0);
-    if (grad) write_slice<E>(s, data, grad, [](float) { return 0.0f; });
+    if (grad) write_slice<E>(s, data, grad, [](Vec<2>) { return splat<2>(0.0f); });
     if (rank == 0 && tid == 0) p.loss[n] = 0.0f;
     return;
   }
   row_start(C);
   load_slice(s, data);
   const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
-
-  // the teacher, while the row is on its way: thread k holds entry k
-  int j = -1;
-  float t = -INFINITY;
-  if (tid < p.K) {
-    j = p.top_idx[n * p.K + tid];
-    if (j >= 0 && j < p.V) t = p.top_logits[n * p.K + tid] * inv_tau;
-    if (t == -INFINITY) j = -1;
-    at[tid] = j;
-  }
-  const bool there = j >= 0;
-  const float zk = there ? to_f32(z[j]) : -INFINITY;
   int label = -1;
   float zl = 0.0f;
   if constexpr (HARD) {
     label = p.labels[n];
     if (label >= 0 && label < p.V) zl = to_f32(z[label]);
   }
-  float lse;
-  if (p.teacher_lse) {
-    lse = p.teacher_lse[n];
-  } else {
-    const float mt = block_reduce(t, buf, Max());
-    const float st = block_reduce(there ? expf(t - mt) : 0.0f, buf, Sum());
-    lse = mt + logf(st);
-  }
-  const float logq = t - lse;
-  const float q = there ? expf(logq) : 0.0f;
-  if (tid < p.K) qs[tid] = q;
-  const float mass = block_reduce(q, buf, Sum());   // (its barriers also publish at and qs)
-  // entries with the same index: the first of them stands for all in the gradient
-  bool first = there, label_is_entry = false;
-  float q_here = 0.0f;
-  for (int k = 0; k < p.K; ++k) {
-    const int a = at[k];
-    if (a == j) {
-      q_here += qs[k];
-      if (k < tid) first = false;
-    }
-    if (HARD && a == label) label_is_entry = true;
-  }
-  // in_slice: where this block holds an element
+  float q[kPerLane], logq[kPerLane], zk[kPerLane];
+  if (tid < 32) read_teacher<E>(p, n, z, label, c, teacher, q, logq, zk);
+  // where this block holds an element, or -1
   auto place = [&](int e) {
     const int k = e + s.shift - s.piece0 * kPer<E>;
-    return k >= 0 && k < s.pieces * kPer<E> ? k : -1;
+    return e >= 0 && k >= 0 && k < s.pieces * kPer<E> ? k : -1;
   };
   const bool tail = p.teacher_lse != nullptr;
   load_wait();
   if (tail) {
     // the mass outside the entries is summed by itself (1 - sum p_k would cancel): they leave the row
     __syncthreads();
-    const int k = first ? place(j) : -1;
+    const int k = tid < p.K ? place(teacher.at[tid]) : -1;   // (blocks have K threads or more)
     if (k >= 0) reinterpret_cast<E*>(data)[k] = from_f32<E>(-INFINITY);
     __syncthreads();
   }
@@ -582,17 +710,9 @@ __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillAr
   row_started(C);
   publish_stats(mine, all, rank, C, c);
   row_sync(C);
-  Stats r = collect_stats(all, C, c);
-  Stats rest = r;
-  if (tail) {
-    Stats top = {first ? zk : -INFINITY, first && zk > -INFINITY ? 1.0f : 0.0f, 0.0f, first && zk > -INFINITY ? 1.0f : 0.0f};
-    if (first && isnan(zk)) top.s = top.s1 = zk;
-    __syncthreads();
-    top = warp_join(top, c);
-    if (tid % 32 == 0) all[tid / 32] = top;
-    __syncthreads();
-    join(r, collect_stats(all, 1, c), c);
-  }
+  const Stats rest = collect_stats(all, C, c);
+  Stats r = rest;
+  if (tail) join(r, teacher.top, c);
   const float ref = r.m == -INFINITY ? 0.0f : r.m;
   const float inv_s = r.s == 0.0f ? 0.0f : 1.0f / r.s;
   const float log_s = r.s == 0.0f ? 0.0f : logf(r.s);
@@ -600,6 +720,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillAr
   // outside are taken relative to the largest logit there, low: p_j = exp((z_j - low) / tau) to_low.
   const float low = tail && rest.s > 0.0f ? rest.m : ref;
   const float to_low = exp2_fast((low - ref) * c) * inv_s;
+  const float mass = teacher.mass;
   float factor = mass, rest_share = 0.0f, kl_rest = 0.0f;
   if (tail && rest.s > 0.0f) {
     const float qr = fmaxf(1.0f - mass, 0.0f);
@@ -614,8 +735,12 @@ __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillAr
     hard = label >= 0;
     inv_s1 = label >= p.V ? NAN : hard && r.s1 != 0.0f ? 1.0f / r.s1 : 0.0f;
   }
-  if (rank == 0) {
-    float kl = block_reduce(q > 0.0f ? q * (logq - ((zk - ref) * inv_tau - log_s)) : 0.0f, buf, Sum());
+  if (rank == 0 && tid < 32) {
+    float kl = 0.0f;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (e * 32 < p.K && !(q[e] == 0.0f)) kl += q[e] * (logq[e] - ((zk[e] - ref) * inv_tau - log_s));
+    kl = warp_sum(kl);
     if (tid == 0) {
       float loss = soft * p.tau * (kl + kl_rest);
       if (hard) loss -= p.alpha * (label < p.V ? (zl - ref) - (r.s1 == 0.0f ? 0.0f : logf(r.s1)) : NAN);
@@ -625,22 +750,29 @@ __global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillAr
   if (!grad) return;
   const float k_soft = w * soft, k_hard = w * p.alpha * inv_s1 * exp2_fast((low - ref) * kLog2e);
   const float k_out = k_soft * (to_low * factor - rest_share);
-  auto outside = [&](float v) {
-    const float d = v - low;
-    float g = k_out * exp2_grad<E>(d * c);
-    if constexpr (HARD) g += k_hard * exp2_grad<E>(d * kLog2e);
+  const Vec<2> neg_low = splat<2>(-low);
+  auto outside = [&](Vec<2> v) {
+    const Vec<2> d = v + neg_low, x = d * splat<2>(c);
+    Vec<2> g = splat<2>(k_out) * Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])};
+    if constexpr (HARD) {
+      const Vec<2> y = d * splat<2>(kLog2e);
+      g = fma<2>(splat<2>(k_hard), Vec<2>{exp2_grad<E>(y.v[0]), exp2_grad<E>(y.v[1])}, g);
+    }
     return g;
   };
   write_slice<E>(s, data, grad, outside);
   // the entries' and the label's own values, over what was just written
   __syncthreads();
-  if (first && place(j) >= 0) {
-    float g = k_soft * (exp2_grad<E>((zk - ref) * c) * inv_s * factor - q_here);
-    if (HARD && hard) g += w * p.alpha * (inv_s1 * exp2_grad<E>((zk - ref) * kLog2e) - (j == label ? 1.0f : 0.0f));
+  for (int k = tid; k < p.K; k += blockDim.x) {
+    const int j = teacher.at[k];
+    if (place(j) < 0) continue;
+    const float d = teacher.z[k] - ref;
+    float g = k_soft * (exp2_grad<E>(d * c) * inv_s * factor - teacher.q[k]);
+    if (HARD && hard) g += w * p.alpha * (inv_s1 * exp2_grad<E>(d * kLog2e) - (j == label ? 1.0f : 0.0f));
     grad[j] = from_f32<E>(g);
   }
-  if (HARD && tid == 0 && hard && label < p.V && !label_is_entry && place(label) >= 0)
-    grad[label] = from_f32<E>(outside(zl) - w * p.alpha);
+  if (HARD && tid == 0 && hard && label < p.V && !teacher.label_is_entry && place(label) >= 0)
+    grad[label] = from_f32<E>(outside(splat<2>(zl)).v[0] - w * p.alpha);
 }
 
 // Top K of a row on chip.  The blocks' threads are cut into G groups of neighbours; the K-th largest
@@ -660,11 +792,39 @@ struct TopShared {
   float bound;
 };
 
-template <typename E>
-__device__ __forceinline__ float key_value(unsigned long long key) {
-  const unsigned u = unsigned(key >> 32);
-  return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+// A value that at least K of the G (at least K) values reach, and hardly more do: bisection over the
+// floats in their order, ended when at most K / 4 too many remain.  One warp calls.
+__device__ __forceinline__ float group_bound(const float* values, int G, int K) {
+  const int lane = threadIdx.x % 32;
+  auto order = [](float v) {
+    const int u = __float_as_int(v);
+    return u ^ (u >> 31 & 0x7fffffff);
+  };
+  int lo = INT32_MAX, hi = INT32_MIN;
+  for (int i = lane; i < G; i += 32) {
+    const int v = order(values[i]);
+    lo = min(lo, v);
+    hi = max(hi, v);
+  }
+  lo = __reduce_min_sync(~0u, lo);
+  hi = __reduce_max_sync(~0u, hi);
+  // K values reach lo; fewer than K reach hi + 1
+  int reach = G;
+  while (lo < hi && reach > K + K / 4) {
+    const int mid = int((int64_t(lo) + hi + 1) >> 1);
+    int n = 0;
+    for (int i = lane; i < G; i += 32) n += order(values[i]) >= mid;
+    n = __reduce_add_sync(~0u, n);
+    if (n >= K) {
+      lo = mid;
+      reach = n;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  return __int_as_float(lo ^ (lo >> 31 & 0x7fffffff));
 }
+
 __device__ __forceinline__ int key_index(unsigned long long key) { return int(~unsigned(key)); }
 
 // Calls f(key) for every element of the thread's pieces.
@@ -673,11 +833,11 @@ __device__ __forceinline__ void each_key(const Slice<E>& s, const uint4* data, F
   for (int i = threadIdx.x; i < s.pieces; i += blockDim.x) {
     const uint4 w = data[i];
     const int j = s.index(i);
-    float v[kPer<E>];
+    Vec<2> v[kPairs<E>];
     unpack<E>(w, v);
 #pragma unroll
     for (int k = 0; k < kPer<E>; ++k)
-      if (j + k >= 0 && j + k < s.V) f(order_key(v[k], j + k));
+      if (j + k >= 0 && j + k < s.V) f(order_key(v[k / 2].v[k % 2], j + k));
   }
 }
 
@@ -730,30 +890,30 @@ __global__ void __launch_bounds__(kRowThreads, 3) token_logp_kernel(const LogpAr
   };
   bool listed = !isnan(r.s);
   if (listed) {
-    // the K-th largest group maximum: every thread ranks some of them
-    for (int i = tid; i < groups; i += T) {
-      const float v = top.group_max[i];
-      int above = 0;
-      for (int k = 0; k < groups; ++k) {
-        const float o = top.group_max[k];
-        above += o > v || (o == v && k < i);
-      }
-      if (above == p.K - 1) top.bound = v;
+    if (tid < 32) {
+      const float bound = group_bound(top.group_max, groups, p.K);
+      if (tid == 0) top.bound = bound;
     }
     __syncthreads();
     const float bound = top.bound;
-    for (int i = tid; i < s.pieces; i += T) {
-      const uint4 w = data[i];
-      if (piece_max<E>(w) < bound) continue;
-      const int j = s.index(i);
-      float v[kPer<E>];
-      unpack<E>(w, v);
+    // a thread whose maximum reaches the bound: its pieces are searched by the warp together
+    for (unsigned hit = __ballot_sync(~0u, mine.m >= bound); hit; hit &= hit - 1) {
+      const int owner = tid - lane + __ffs(hit) - 1;
+      for (int i = owner + lane * T; i < s.pieces; i += 32 * T) {
+        const uint4 w = data[i];
+        if (piece_max<E>(w) < bound) continue;
+        const int j = s.index(i);
+        Vec<2> v[kPairs<E>];
+        unpack<E>(w, v);
 #pragma unroll
-      for (int k = 0; k < kPer<E>; ++k)
-        if (v[k] >= bound && j + k >= 0 && j + k < s.V) {
-          const int at = atomicAdd(&top.count, 1);   // (the order in the list does not matter)
-          if (at < kList) top.list[at] = order_key(v[k], j + k);
+        for (int k = 0; k < kPer<E>; ++k) {
+          const float x = v[k / 2].v[k % 2];
+          if (x >= bound && j + k >= 0 && j + k < s.V) {
+            const int at = atomicAdd(&top.count, 1);   // (the order in the list does not matter)
+            if (at < kList) top.list[at] = order_key(x, j + k);
+          }
         }
+      }
     }
     __syncthreads();
     if (C > 1 && tid < C) cg::this_cluster().map_shared_rank(&top, tid)->counts[rank] = top.count;
@@ -851,15 +1011,18 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
   for (int i = 0; i < kGradPieces; ++i) {
     const int j = s.index(first + i * kRowThreads);
     if (j >= s.V) break;
-    float v[kPer<E>];
+    Vec<2> v[kPairs<E>];
     unpack<E>(w[i], v);
 #pragma unroll
-    for (int k = 0; k < kPer<E>; ++k) {
-      const float lp = v[k] * inv_tau - off;
-      const float e = none * exp2_grad<E>(lp * kLog2e);
-      float g = -e * (dl + dh * (fmaxf(lp, -1000.0f) + H));
-      if (j + k == y) g += dl;
-      v[k] = g * inv_tau;
+    for (int k = 0; k < kPairs<E>; ++k) {
+      const Vec<2> lp = fma<2>(v[k], splat<2>(inv_tau), splat<2>(-off)), x = lp * splat<2>(kLog2e);
+      const Vec<2> e = Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])} * splat<2>(-none);
+      const Vec<2> bounded = {fmaxf(lp.v[0], -1000.0f), fmaxf(lp.v[1], -1000.0f)};
+      Vec<2> g = e * fma<2>(splat<2>(dh), bounded, splat<2>(fmaf(dh, H, dl)));
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+        if (j + 2 * k + m == y) g.v[m] += dl;
+      v[k] = g * splat<2>(inv_tau);
     }
     const uint4 o = pack<E>(v);
     if (same && j >= 0 && j + kPer<E> <= s.V) {
@@ -882,7 +1045,7 @@ struct RowCut {
 };
 
 RowCut row_cut(int dtype, int64_t N, int64_t V, int K) {
-  constexpr int64_t kSlice = 64 << 10, kLeast = 8 << 10, kMost = 200 << 10;
+  constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 200 << 10;
   const int64_t bytes = V * dtype_size(dtype) + 32;   // with the pieces at both ends
   RowCut c = {1, kRowThreads, 0};
   while (c.cluster < kRowCluster && bytes > kSlice * c.cluster) c.cluster *= 2;
