@@ -2,6 +2,7 @@
 // logits, log probabilities of tokens with entropy and top alternatives, and their gradients.
 #include <cooperative_groups.h>
 
+#include <mutex>
 #include <type_traits>
 
 #include "lm_internal.h"
@@ -257,18 +258,23 @@ __global__ void __launch_bounds__(kThreads) token_logp_stream_kernel(const LogpA
 
 // ---- rows on chip ----
 //
-// A row is read once into the shared memory of a cluster of C blocks, each holding a slice of it as
-// 16-byte pieces at the alignment they have in memory; all later passes read it there.  Elements of
-// the first and last piece that lie outside the row are -inf.  A thread copies pieces t, t + T, ...
-// of its block's slice and is the one that reads them, so the passes need no barrier between.
+// A row is read once into the shared memory of a cluster of C blocks; all later passes read it
+// there.  It is taken as its whole 16-byte pieces in memory, cut evenly over the blocks, and up to 14
+// edge elements before and after them.  A thread copies pieces t, t + T, ... of its block's slice and
+// is the one that reads them, so the passes over a slice need no barrier between.
+//
+// Clusters stay and take row after row.  The last pass over a row copies the next row's piece into
+// each slot as soon as it has read it, and one warp of the block beside the T others (its side warp)
+// does what is short and serial: the teacher's entries, the loss, the choice of alternatives, the
+// edge elements.  It works on the next or the previous row while the others stream, so that
+// neither memory nor the passes wait for it.  One cluster barrier per row keeps them in step.
 //
 // Maximum and sum in one go: every thread takes the maximum of its own pieces, then the sum
 // relative to that; warps and blocks join (m, s) pairs by m = max m_i, s = sum s_i exp((m_i - m) / tau),
-// in the order that the sizes fix.  The blocks' warps write their pairs to every block of the
-// cluster, which joins all of them after one cluster barrier.
+// in the order that the sizes fix.  The warps write their pairs to every block of the cluster.
 
-constexpr int kRowThreads = 256;
-constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 256;                 // most threads beside the side warp
+constexpr int kRowParts = kRowThreads / 32 + 1;  // most warps of a block
 constexpr int kRowCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -292,16 +298,19 @@ __device__ __forceinline__ float exp2_grad(float x) {
 template <typename E>
 constexpr int kPer = 16 / int(sizeof(E));   // elements of a piece
 
-// A block's slice of a row.
+// A row and the block's slice of its whole pieces.
 template <typename E>
 struct Slice {
   const E* row;
   int V;
-  int shift;    // elements between the 16-byte boundary below the row's start and the row
-  int piece0;   // first piece
-  int pieces;   // number of pieces
-  // index in the row of the slice's piece i's first element (may be negative, or past V)
-  __device__ int index(int i) const { return (piece0 + i) * kPer<E> - shift; }
+  int lead;     // elements before the first whole piece
+  int whole;    // whole pieces of the row
+  int first;    // first one of the slice
+  int pieces;   // number of the slice's
+  __device__ int index(int i) const { return lead + (first + i) * kPer<E>; }   // first element of the slice's piece i
+  __device__ const uint4* data() const { return reinterpret_cast<const uint4*>(row + index(0)); }
+  __device__ int edges() const { return V - whole * kPer<E>; }
+  __device__ int edge(int e) const { return e < lead ? e : e + whole * kPer<E>; }   // index of an edge element
 };
 
 template <typename E>
@@ -309,30 +318,37 @@ __device__ __forceinline__ Slice<E> slice_of(const E* row, int V, int rank, int 
   Slice<E> s;
   s.row = row;
   s.V = V;
-  s.shift = int(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(E));
-  const int all = (s.shift + V + kPer<E> - 1) / kPer<E>;
-  const int per = (all + C - 1) / C;
-  s.piece0 = min(rank * per, all);
-  s.pieces = min(per, all - s.piece0);
+  s.lead = min(int((16 - reinterpret_cast<uintptr_t>(row) % 16) % 16 / sizeof(E)), V);
+  s.whole = (V - s.lead) / kPer<E>;
+  const int per = (s.whole + C - 1) / C;
+  s.first = min(rank * per, s.whole);
+  s.pieces = min(per, s.whole - s.first);
   return s;
 }
 
-template <typename E>
-__device__ __forceinline__ void load_slice(const Slice<E>& s, uint4* data) {
-  for (int i = threadIdx.x; i < s.pieces; i += blockDim.x) {
-    const int j = s.index(i);
-    if (j >= 0 && j + kPer<E> <= s.V) {
-      const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(data + i));
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(s.row + j) : "memory");
-    } else {
-      E e[kPer<E>];
-      for (int k = 0; k < kPer<E>; ++k) e[k] = j + k >= 0 && j + k < s.V ? s.row[j + k] : from_f32<E>(-INFINITY);
-      data[i] = *reinterpret_cast<const uint4*>(e);
-    }
-  }
-  asm volatile("cp.async.commit_group;" ::: "memory");
+__device__ __forceinline__ void load_piece(uint4* slot, const uint4* from) {
+  const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slot));
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void load_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void load_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+
+// The cluster barrier, in two halves.  Relaxed: only that all blocks have started.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ void cluster_start() {
+  asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+// A barrier of `threads` threads of the block.
+__device__ __forceinline__ void part_sync(int id, int threads) {
+  asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// The variable of another block of the cluster (this block's own where rank is its own).
+template <typename X>
+__device__ __forceinline__ X* of_block(X* x, int rank) {
+  return cg::this_cluster().map_shared_rank(x, rank);
+}
 
 // A piece's elements as pairs of floats, and back.
 template <typename E>
@@ -428,15 +444,17 @@ __device__ __forceinline__ Stats warp_join(Stats a, float c) {
   return a;
 }
 
-// A thread's sums over its pieces, relative to a.m.
-template <typename E, bool ENTROPY, bool HARD, bool CLAMP>
-__device__ __forceinline__ void thread_sums(const uint4* data, int pieces, float c, Stats& a) {
+// A thread's sums over its pieces (t, t + T, ...), relative to a.m.  after(i) runs when piece i has
+// been read.
+template <typename E, bool ENTROPY, bool HARD, bool CLAMP, typename F>
+__device__ __forceinline__ void thread_sums(const uint4* data, int pieces, int T, float c, Stats& a, F after) {
   const Vec<2> ref = splat<2>(a.m == -INFINITY ? -0.0f : -a.m), scale = splat<2>(c);
   Vec<2> s = splat<2>(0.0f), e = s, s1 = s;
 #pragma unroll 2
-  for (int i = threadIdx.x; i < pieces; i += blockDim.x) {
+  for (int i = threadIdx.x; i < pieces; i += T) {
     Vec<2> v[kPairs<E>];
     unpack<E>(data[i], v);
+    after(i);
 #pragma unroll
     for (int k = 0; k < kPairs<E>; ++k) {
       const Vec<2> d = v[k] + ref;
@@ -458,88 +476,64 @@ __device__ __forceinline__ void thread_sums(const uint4* data, int pieces, float
   a.s1 = s1.v[0] + s1.v[1];
 }
 
-// A thread's statistics over its pieces.
-template <typename E, bool ENTROPY, bool HARD>
-__device__ __forceinline__ Stats thread_stats(const uint4* data, int pieces, float c) {
-  Stats a = no_stats();
+template <typename E>
+__device__ __forceinline__ float thread_max(const uint4* data, int pieces, int T) {
+  float m = -INFINITY;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < pieces; i += blockDim.x) a.m = fmaxf(a.m, piece_max<E>(data[i]));
-  thread_sums<E, ENTROPY, HARD, false>(data, pieces, c, a);
-  // 0 times -inf, from logits of -inf or far below the others: again with their x bounded
-  if (ENTROPY && isnan(a.e)) thread_sums<E, ENTROPY, HARD, true>(data, pieces, c, a);
-  return a;
+  for (int i = threadIdx.x; i < pieces; i += T) m = fmaxf(m, piece_max<E>(data[i]));
+  return m;
 }
 
-// Blocks of a cluster may write to one another once all have started: row_start early, and
-// row_started before the first write.
-__device__ __forceinline__ void row_start(int C) {
-  if (C > 1) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
-}
-__device__ __forceinline__ void row_started(int C) {
-  if (C > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
+// An edge element alone.
+__device__ __forceinline__ Stats one_element(float z) {
+  if (isnan(z)) return {-INFINITY, z, z, z};
+  return z == -INFINITY ? no_stats() : Stats{z, 1.0f, 0.0f, 1.0f};
 }
 
-// A cluster barrier (the block's alone where there is one block).
-__device__ __forceinline__ void row_sync(int C) {
-  if (C == 1)
-    __syncthreads();
-  else
-    cg::this_cluster().sync();
-}
-
-// The row's statistics, from every thread's.  all: [kRowCluster * kRowWarps] in every block.
-__device__ __forceinline__ void publish_stats(const Stats& mine, Stats* all, int rank, int C, float c) {
+// A warp's set to every block of the cluster (all: [C * parts]), and the row's set from them.
+__device__ __forceinline__ void publish_stats(const Stats& mine, Stats* all, int rank, int C, int parts, float c) {
   const Stats a = warp_join(mine, c);
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
-  if (C == 1) {
-    if (lane == 0) all[warp] = a;
-  } else if (lane < C) {
-    cg::this_cluster().map_shared_rank(all, lane)[rank * warps + warp] = a;
-  }
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (lane < C) of_block(all, lane)[rank * parts + warp] = a;
 }
-__device__ __forceinline__ Stats collect_stats(const Stats* all, int C, float c) {
-  const int lane = threadIdx.x % 32, n = C * int(blockDim.x / 32);
+__device__ __forceinline__ Stats collect_stats(const Stats* all, int C, int parts, float c) {
+  const int lane = threadIdx.x % 32, n = C * parts;
   Stats a = lane < n ? all[lane] : no_stats();
-  if (n > 32) join(a, lane + 32 < n ? all[lane + 32] : no_stats(), c);
+  for (int i = lane + 32; i < n; i += 32) join(a, all[i], c);
   return warp_join(a, c);
 }
 
-// Writes f of every pair of elements of the slice to out: whole pieces where the output has the
-// logits' alignment, else element by element.
-template <typename E, typename F>
-__device__ __forceinline__ void write_slice(const Slice<E>& s, const uint4* data, E* out, F f) {
-  const bool same = int(reinterpret_cast<uintptr_t>(out) % 16 / sizeof(E)) == s.shift;
-#pragma unroll 2
-  for (int i = threadIdx.x; i < s.pieces; i += blockDim.x) {
-    const int j = s.index(i);
-    Vec<2> v[kPairs<E>];
-    unpack<E>(data[i], v);
-#pragma unroll
-    for (int k = 0; k < kPairs<E>; ++k) v[k] = f(v[k]);
-    const uint4 w = pack<E>(v);
-    if (same && j >= 0 && j + kPer<E> <= s.V) {
-      *reinterpret_cast<uint4*>(out + j) = w;
-    } else {
-      const E* e = reinterpret_cast<const E*>(&w);
-#pragma unroll
-      for (int k = 0; k < kPer<E>; ++k)
-        if (j + k >= 0 && j + k < s.V) out[j + k] = e[k];
-    }
-  }
-}
-
-// The teacher's side of a row, taken by a block's first warp (lane l holds entries l, l + 32, ...)
-// while the others go ahead with the student's row.
-constexpr int kTableBits = 9;
+// The teacher's side of a row, taken by the side warp (lane l holds entries l, l + 32, ...).  Arrays of
+// K values in dynamic shared memory.
 struct Teacher {
-  int at[GEM_TOP_MAX];      // index of an entry; -1: absent, or another entry has it
-  float q[GEM_TOP_MAX];     // mass there, that of all entries with the index
-  float z[GEM_TOP_MAX];     // the student's logit there
-  int table[1 << kTableBits];
-  float mass;               // sum of q
-  Stats top;                // the student's entries
-  int label_is_entry;
+  int* at;        // index of an entry; -1: absent, or another entry has it
+  float* q;       // mass there, that of all entries with the index
+  float* z;       // the student's logit there
+  float* logq;    // the entry's own log mass, -inf where absent (of the current row only)
+  int* table;     // the indices, hashed (of the current row only)
+  int table_bits;
 };
+// What every row of a block needs of them: 7 K words and a table of at least 2 K.
+__host__ __device__ inline int table_bits(int K) {
+  int bits = 5;
+  while ((1 << bits) < 2 * K) ++bits;
+  return bits;
+}
+inline size_t teacher_bytes(int K) { return (size_t(7) * K + (size_t(1) << table_bits(K))) * 4; }
+__device__ __forceinline__ Teacher teacher_at(void* shared, int K, int b) {
+  int* w = static_cast<int*>(shared);
+  Teacher t;
+  t.at = w + (3 * b) * K;
+  t.q = reinterpret_cast<float*>(w + (3 * b + 1) * K);
+  t.z = reinterpret_cast<float*>(w + (3 * b + 2) * K);
+  t.logq = reinterpret_cast<float*>(w + 6 * K);
+  t.table = w + 7 * K;
+  t.table_bits = table_bits(K);
+  return t;
+}
+__device__ __forceinline__ unsigned table_slot(const Teacher& t, int j) {
+  return unsigned(j) * 2654435761u >> (32 - t.table_bits);
+}
 
 constexpr int kPerLane = GEM_TOP_MAX / 32;
 
@@ -549,13 +543,14 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Fills t; q and logq: the lane's own entries (0 and anything where absent).
+// Returns the sum of q; top: the student's statistics of the entries (where the rest is a class).
 template <typename E>
-__device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, const E* z, int label, float c, Teacher& t,
-                                             float (&q)[kPerLane], float (&logq)[kPerLane], float (&zk)[kPerLane]) {
+__device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, const E* z, int label, float c, const Teacher& t,
+                                              Stats& top, bool& label_here) {
   const int lane = threadIdx.x % 32;
   const float inv_tau = 1.0f / p.tau;
   int j[kPerLane];
+  float logq[kPerLane], zk[kPerLane];
   float most = -INFINITY;
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
@@ -572,7 +567,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, co
     zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
     most = fmaxf(most, logq[e]);
   }
-  for (int i = lane; i < 1 << kTableBits; i += 32) t.table[i] = -1;
+  for (int i = lane; i < 1 << t.table_bits; i += 32) t.table[i] = -1;
   float lse;
   if (p.teacher_lse) {
     lse = p.teacher_lse[n];
@@ -587,20 +582,21 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, co
   }
   __syncwarp();
   float mass = 0.0f;
-  bool again = false, label_here = false;
-  Stats top = no_stats();
+  bool again = false;
+  label_here = false;
+  top = no_stats();
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
-    q[e] = 0.0f;
     if (e * 32 >= p.K) continue;
     const int k = e * 32 + lane;
+    float q = 0.0f;
     if (j[e] >= 0) {
       logq[e] -= lse;
-      q[e] = expf(logq[e]);
-      mass += q[e];
+      q = expf(logq[e]);
+      mass += q;
       label_here |= j[e] == label;
       // a table of the indices seen: who finds an index there is not its first entry
-      unsigned h = unsigned(j[e]) * 2654435761u >> (32 - kTableBits);
+      unsigned h = table_slot(t, j[e]);
       for (;;) {   // (at most half of the table is ever taken)
         const int other = atomicCAS(&t.table[h], -1, j[e]);
         if (other == -1) break;
@@ -608,13 +604,14 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, co
           again = true;
           break;
         }
-        h = (h + 1) & ((1 << kTableBits) - 1);
+        h = (h + 1) & ((1 << t.table_bits) - 1);
       }
     }
     if (k < p.K) {
       t.at[k] = j[e];
-      t.q[k] = q[e];
+      t.q[k] = q;
       t.z[k] = zk[e];
+      t.logq[k] = logq[e];
     }
   }
   mass = warp_sum(mass);
@@ -657,140 +654,263 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& p, int64_t n, co
       }
     top = warp_join(top, c);
   }
-  if (lane == 0) {
-    t.mass = mass;
-    t.top = top;
-    t.label_is_entry = label_here;
+  __syncwarp();
+  return mass;
+}
+
+// Whether index j is one of the entries.
+__device__ __forceinline__ bool is_entry(const Teacher& t, int j) {
+  for (unsigned h = table_slot(t, j);; h = (h + 1) & ((1 << t.table_bits) - 1)) {   // (at least half of the table is empty)
+    const int other = t.table[h];
+    if (other == j || other == -1) return other == j;
   }
 }
 
-template <typename E, bool HARD>
-__global__ void __launch_bounds__(kRowThreads, 3) distill_kernel(const DistillArgs p, int C) {
-  extern __shared__ uint4 data[];
-  __shared__ Stats all[kRowCluster * kRowWarps];
-  __shared__ Teacher teacher;
-  pdl_entry();
-  const int64_t n = blockIdx.x / C;
-  const int rank = blockIdx.x % C, tid = threadIdx.x;
-  const E* z = static_cast<const E*>(p.logits) + n * p.ld;
-  E* grad = p.grad ? static_cast<E*>(p.grad) + n * p.grad_ld : nullptr;
-  const Slice<E> s = slice_of(z, p.V, rank, C);
-  const float w = p.row_scale ? p.row_scale[n] : 1.0f;
-  if (w == 0.0f) {
-    if (grad) write_slice<E>(s, data, grad, [](Vec<2>) { return splat<2>(0.0f); });
-    if (rank == 0 && tid == 0) p.loss[n] = 0.0f;
-    return;
-  }
-  row_start(C);
-  load_slice(s, data);
-  const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
-  int label = -1;
-  float zl = 0.0f;
-  if constexpr (HARD) {
-    label = p.labels[n];
-    if (label >= 0 && label < p.V) zl = to_f32(z[label]);
-  }
-  float q[kPerLane], logq[kPerLane], zk[kPerLane];
-  if (tid < 32) read_teacher<E>(p, n, z, label, c, teacher, q, logq, zk);
-  // where this block holds an element, or -1
-  auto place = [&](int e) {
-    const int k = e + s.shift - s.piece0 * kPer<E>;
-    return e >= 0 && k >= 0 && k < s.pieces * kPer<E> ? k : -1;
-  };
+// What the gradient of a row needs beside its elements.
+struct Coefficients {
+  float ref, log_s, inv_s;   // largest logit (0 where there is none), log and inverse of the sum
+  float factor;              // of p_j at the entries
+  float low, k_out, k_hard;  // outside: k_out exp((z - low) / tau) + k_hard exp(z - low)
+  float k_soft, k_one, inv_s1, kl_rest;
+};
+
+template <bool HARD>
+__device__ __forceinline__ Coefficients coefficients(const DistillArgs& p, const Stats& rest, const Stats& top, float mass,
+                                                     float w, int label, float c) {
   const bool tail = p.teacher_lse != nullptr;
-  load_wait();
-  if (tail) {
-    // the mass outside the entries is summed by itself (1 - sum p_k would cancel): they leave the row
-    __syncthreads();
-    const int k = tid < p.K ? place(teacher.at[tid]) : -1;   // (blocks have K threads or more)
-    if (k >= 0) reinterpret_cast<E*>(data)[k] = from_f32<E>(-INFINITY);
-    __syncthreads();
-  }
-  const Stats mine = thread_stats<E, false, HARD>(data, s.pieces, c);
-  row_started(C);
-  publish_stats(mine, all, rank, C, c);
-  row_sync(C);
-  const Stats rest = collect_stats(all, C, c);
   Stats r = rest;
-  if (tail) join(r, teacher.top, c);
-  const float ref = r.m == -INFINITY ? 0.0f : r.m;
-  const float inv_s = r.s == 0.0f ? 0.0f : 1.0f / r.s;
-  const float log_s = r.s == 0.0f ? 0.0f : logf(r.s);
+  if (tail) join(r, top, c);
+  Coefficients k;
+  k.ref = r.m == -INFINITY ? 0.0f : r.m;
+  k.inv_s = r.s == 0.0f ? 0.0f : 1.0f / r.s;
+  k.log_s = r.s == 0.0f ? 0.0f : logf(r.s);
   // With q_rest the factor of p_j outside the entries is mass + q_rest - q_rest / p_rest.  Exponentials
-  // outside are taken relative to the largest logit there, low: p_j = exp((z_j - low) / tau) to_low.
-  const float low = tail && rest.s > 0.0f ? rest.m : ref;
-  const float to_low = exp2_fast((low - ref) * c) * inv_s;
-  const float mass = teacher.mass;
-  float factor = mass, rest_share = 0.0f, kl_rest = 0.0f;
+  // outside are taken relative to the largest logit there, low.
+  k.low = tail && rest.s > 0.0f ? rest.m : k.ref;
+  k.factor = mass;
+  k.kl_rest = 0.0f;
+  float rest_share = 0.0f;
   if (tail && rest.s > 0.0f) {
     const float qr = fmaxf(1.0f - mass, 0.0f);
-    factor += qr;
+    k.factor += qr;
     rest_share = qr / rest.s;
-    if (qr > 0.0f) kl_rest = qr * (logf(qr) - (logf(rest.s) + (low - ref) * inv_tau - log_s));
+    if (qr > 0.0f) k.kl_rest = qr * (logf(qr) - (logf(rest.s) + (k.low - k.ref) * (1.0f / p.tau) - k.log_s));
   }
-  const float soft = (1.0f - p.alpha) * p.tau;
-  bool hard = false;
-  float inv_s1 = 0.0f;
+  k.k_soft = w * (1.0f - p.alpha) * p.tau;
+  k.k_one = w * p.alpha;
+  k.inv_s1 = !HARD ? 0.0f : label >= p.V ? NAN : label >= 0 && r.s1 != 0.0f ? 1.0f / r.s1 : 0.0f;
+  k.k_out = k.k_soft * (exp2_fast((k.low - k.ref) * c) * k.inv_s * k.factor - rest_share);
+  k.k_hard = !HARD ? 0.0f : k.k_one * k.inv_s1 * exp2_fast((k.low - k.ref) * kLog2e);
+  return k;
+}
+
+template <typename E, bool HARD>
+__device__ __forceinline__ Vec<2> outside_grad(Vec<2> v, const Coefficients& k, float c) {
+  const Vec<2> d = v + splat<2>(-k.low), x = d * splat<2>(c);
+  Vec<2> g = splat<2>(k.k_out) * Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])};
   if constexpr (HARD) {
-    hard = label >= 0;
-    inv_s1 = label >= p.V ? NAN : hard && r.s1 != 0.0f ? 1.0f / r.s1 : 0.0f;
+    const Vec<2> y = d * splat<2>(kLog2e);
+    g = fma<2>(splat<2>(k.k_hard), Vec<2>{exp2_grad<E>(y.v[0]), exp2_grad<E>(y.v[1])}, g);
   }
-  if (rank == 0 && tid < 32) {
-    float kl = 0.0f;
+  return g;
+}
+
+template <typename E, bool HARD>
+__global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const DistillArgs p, int64_t N, int C, int slots) {
+  extern __shared__ uint4 data[];
+  __shared__ Stats all[2][kRowCluster * kRowParts];
+  __shared__ Stats tops[2];
+  __shared__ float masses[2];
+  pdl_entry();
+  const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x - 32, parts = blockDim.x / 32, lane = tid % 32;
+  const int64_t step = gridDim.x / C;
+  void* const teachers = data + slots;
+  const float c = kLog2e * (1.0f / p.tau);
+  const bool tail = p.teacher_lse != nullptr;
+  const E* const logits = static_cast<const E*>(p.logits);
+  E* const grads = static_cast<E*>(p.grad);
+  auto scale = [&](int64_t n) { return n < N ? p.row_scale ? p.row_scale[n] : 1.0f : 0.0f; };
+  auto label_of = [&](int64_t n) { return HARD && n < N ? p.labels[n] : -1; };
+  int64_t n = blockIdx.x / C;
+  float w = scale(n);
+  int label = label_of(n);
+  cluster_start();
+
+  if (tid < T) {
+    Slice<E> s = slice_of(logits + n * p.ld, p.V, rank, C);
+    if (w != 0.0f)
+      for (int i = tid; i < s.pieces; i += T) load_piece(data + i, s.data() + i);
+    load_commit();
+    for (int b = 0; n < N; n += step, b ^= 1) {
+      // the next row, whose pieces follow this one's
+      const float next_w = scale(n + step);
+      const int next_label = label_of(n + step);
+      const Slice<E> next = slice_of(logits + (n + step) * p.ld, p.V, rank, C);
+      const int next_pieces = n + step < N && next_w != 0.0f ? next.pieces : 0;
+      load_wait();
+      if (tail) {
+        // the mass outside the entries is summed by itself (1 - sum p_k would cancel): they leave the row
+        part_sync(1, T + 32);
+        const int j = tid < p.K && w != 0.0f ? teacher_at(teachers, p.K, b).at[tid] : -1;   // (T >= K)
+        const int at = j - s.index(0);
+        if (j >= 0 && at >= 0 && at < s.pieces * kPer<E>) reinterpret_cast<E*>(data)[at] = from_f32<E>(-INFINITY);
+        part_sync(2, T);
+      }
+      Stats mine = no_stats();
+      if (w != 0.0f) {
+        mine.m = thread_max<E>(data, s.pieces, T);
+        thread_sums<E, false, HARD, false>(data, s.pieces, T, c, mine, [](int) {});
+      }
+      publish_stats(mine, all[b], rank, C, parts, c);
+      cluster_arrive();
+      cluster_wait();
+      const Coefficients k = coefficients<HARD>(p, collect_stats(all[b], C, parts, c), tops[b], masses[b], w, label, c);
+      E* const out = grads ? grads + n * p.grad_ld + s.index(0) : nullptr;
+      const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
+      const int most = max(s.pieces, next_pieces);
+#pragma unroll 2
+      for (int i = tid; i < most; i += T) {
+        if (grads && i < s.pieces) {
+          Vec<2> v[kPairs<E>];
+          if (w != 0.0f) unpack<E>(data[i], v);
 #pragma unroll
-    for (int e = 0; e < kPerLane; ++e)
-      if (e * 32 < p.K && !(q[e] == 0.0f)) kl += q[e] * (logq[e] - ((zk[e] - ref) * inv_tau - log_s));
-    kl = warp_sum(kl);
-    if (tid == 0) {
-      float loss = soft * p.tau * (kl + kl_rest);
-      if (hard) loss -= p.alpha * (label < p.V ? (zl - ref) - (r.s1 == 0.0f ? 0.0f : logf(r.s1)) : NAN);
-      p.loss[n] = loss;
+          for (int m = 0; m < kPairs<E>; ++m) v[m] = w != 0.0f ? outside_grad<E, HARD>(v[m], k, c) : splat<2>(0.0f);
+          const uint4 g = pack<E>(v);
+          if (aligned) {
+            *reinterpret_cast<uint4*>(out + int64_t(i) * kPer<E>) = g;
+          } else {
+            const E* e = reinterpret_cast<const E*>(&g);
+#pragma unroll
+            for (int m = 0; m < kPer<E>; ++m) out[int64_t(i) * kPer<E> + m] = e[m];
+          }
+        }
+        if (i < next_pieces) load_piece(data + i, next.data() + i);
+      }
+      load_commit();
+      s = next;
+      w = next_w;
+      label = next_label;
     }
+    cluster_arrive();
+    cluster_wait();
+    return;
   }
-  if (!grad) return;
-  const float k_soft = w * soft, k_hard = w * p.alpha * inv_s1 * exp2_fast((low - ref) * kLog2e);
-  const float k_out = k_soft * (to_low * factor - rest_share);
-  const Vec<2> neg_low = splat<2>(-low);
-  auto outside = [&](Vec<2> v) {
-    const Vec<2> d = v + neg_low, x = d * splat<2>(c);
-    Vec<2> g = splat<2>(k_out) * Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])};
-    if constexpr (HARD) {
-      const Vec<2> y = d * splat<2>(kLog2e);
-      g = fma<2>(splat<2>(k_hard), Vec<2>{exp2_grad<E>(y.v[0]), exp2_grad<E>(y.v[1])}, g);
+
+  // the side warp.  The first block's does the row's loss, edges and entries; the others' know the
+  // teacher only where the entries leave their slices.
+  Coefficients k = {};
+  E* out = nullptr;
+  float zl = 0.0f;
+  int last_label = -1;
+  bool label_is_entry = false;
+  bool pending = false;   // the entries' and the label's own values of the row before, over what was written there
+  auto finish = [&](const Teacher& t) {
+    for (int i = lane; i < p.K; i += 32) {
+      const int j = t.at[i];
+      if (j < 0) continue;
+      const float d = t.z[i] - k.ref;
+      float g = k.k_soft * (exp2_grad<E>(d * c) * k.inv_s * k.factor - t.q[i]);
+      if (HARD && last_label >= 0) g += k.k_one * (k.inv_s1 * exp2_grad<E>(d * kLog2e) - (j == last_label ? 1.0f : 0.0f));
+      out[j] = from_f32<E>(g);
     }
-    return g;
+    if (HARD && lane == 0 && last_label >= 0 && last_label < p.V && !label_is_entry)
+      out[last_label] = from_f32<E>(outside_grad<E, HARD>(splat<2>(zl), k, c).v[0] - k.k_one);
   };
-  write_slice<E>(s, data, grad, outside);
-  // the entries' and the label's own values, over what was just written
-  __syncthreads();
-  for (int k = tid; k < p.K; k += blockDim.x) {
-    const int j = teacher.at[k];
-    if (place(j) < 0) continue;
-    const float d = teacher.z[k] - ref;
-    float g = k_soft * (exp2_grad<E>(d * c) * inv_s * factor - teacher.q[k]);
-    if (HARD && hard) g += w * p.alpha * (inv_s1 * exp2_grad<E>(d * kLog2e) - (j == label ? 1.0f : 0.0f));
-    grad[j] = from_f32<E>(g);
+  int b = 0;
+  for (; n < N; n += step, b ^= 1) {
+    const E* z = logits + n * p.ld;
+    const Slice<E> s = slice_of(z, p.V, rank, C);
+    const Teacher t = teacher_at(teachers, p.K, b);
+    Stats top = no_stats();
+    bool label_here = false;
+    const bool live = w != 0.0f;
+    Stats edge = no_stats();
+    float ze = 0.0f, next_zl = 0.0f, mass = 0.0f;
+    const int je = lane < s.edges() ? s.edge(lane) : -1;
+    if (live) {
+      if (HARD && label >= 0 && label < p.V) next_zl = to_f32(z[label]);
+      if (rank == 0 && je >= 0) ze = to_f32(z[je]);
+      if (rank == 0 || tail) mass = read_teacher<E>(p, n, z, label, c, t, top, label_here);
+      if (rank == 0 && je >= 0 && !(tail && is_entry(t, je))) edge = one_element(ze);
+    }
+    if (tail) {
+      if (lane == 0) tops[b] = top;
+      part_sync(1, T + 32);
+    }
+    if (rank == 0 && lane < C) *of_block(&masses[b], lane) = mass;
+    publish_stats(edge, all[b], rank, C, parts, c);
+    cluster_arrive();
+    cluster_wait();
+    if (rank == 0) {
+      if (pending) finish(teacher_at(teachers, p.K, b ^ 1));
+      pending = live && grads;
+      out = grads + n * p.grad_ld;
+      last_label = label;
+      label_is_entry = label_here;
+      zl = next_zl;
+      float loss = 0.0f;
+      if (live) {
+        const Stats rest = collect_stats(all[b], C, parts, c);
+        k = coefficients<HARD>(p, rest, top, mass, w, label, c);
+        float kl = 0.0f;
+        for (int i = lane; i < p.K; i += 32) {
+          const float logq = t.logq[i], q = expf(logq);
+          if (q != 0.0f) kl += q * (logq - ((t.z[i] - k.ref) * (1.0f / p.tau) - k.log_s));
+        }
+        loss = (1.0f - p.alpha) * p.tau * p.tau * (warp_sum(kl) + k.kl_rest);
+        if (HARD && label >= 0)
+          loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);
+      }
+      if (lane == 0) p.loss[n] = loss;
+      if (grads && je >= 0) out[je] = from_f32<E>(live ? outside_grad<E, HARD>(splat<2>(ze), k, c).v[0] : 0.0f);
+      __syncwarp();
+    }
+    w = scale(n + step);
+    label = label_of(n + step);
   }
-  if (HARD && tid == 0 && hard && label < p.V && !teacher.label_is_entry && place(label) >= 0)
-    grad[label] = from_f32<E>(outside(splat<2>(zl)).v[0] - w * p.alpha);
+  cluster_arrive();
+  cluster_wait();
+  if (rank == 0 && pending) finish(teacher_at(teachers, p.K, b ^ 1));
 }
 
 // Top K of a row on chip.  The blocks' threads are cut into G groups of neighbours; the K-th largest
 // of the groups' maxima is a bound that K elements reach, and few others do (about G ln(G / (G - K))
-// for elements in no order).  Those that do are collected and ranked against one another.  Where
-// more reach it than the lists hold (ties, adverse orders), and in rows that are not finite, K
-// rounds each find the next element instead.
-constexpr int kMaxGroups = 1024;
-constexpr int kList = 512;
-
+// for elements in no order).  The side warps look for them in the pieces of the threads whose maximum
+// reaches it (read again, from L2) and send them to the first block, whose side warp ranks them
+// against one another.  Where more reach it than the list holds (ties, adverse orders), and in rows
+// that are not finite, that warp finds the K-th element exactly, by bisection over the row.
+//
+// Dynamic shared memory after the slots, twice each (rows take turns):
+//   list [entries]       first block: keys of the elements that reached the bound, a share for each block
+//   group_max [groups]   (the last group is the edge elements)
+//   thread_max [T]
+//   counts [C]           first block: elements of each block that reached the bound
+// and owners [T].
+__host__ __device__ inline int top_entries(int K) { return K < 32 ? 128 : 4 * K; }
+inline size_t top_bytes(int K, int groups, int T) {
+  return K == 0 ? 0 : size_t(2) * top_entries(K) * 8 + (size_t(2) * (groups + T + kRowCluster) + T) * 4;
+}
 struct TopShared {
-  float group_max[kMaxGroups];
-  unsigned long long list[kList];
-  unsigned long long best[kRowWarps];
-  unsigned long long round_best[2][kRowCluster];
-  int count, counts[kRowCluster];
-  float bound;
+  unsigned long long* lists;
+  float* floats;
+  int entries, groups, T;
+  __device__ TopShared(void* shared, int K, int groups, int T)
+      : lists(static_cast<unsigned long long*>(shared)), floats(reinterpret_cast<float*>(lists + 2 * top_entries(K))),
+        entries(top_entries(K)), groups(groups), T(T) {}
+  __device__ unsigned long long* list(int b) const { return lists + b * entries; }
+  __device__ float* group_max(int b) const { return floats + b * (groups + T); }
+  __device__ float* thread_max(int b) const { return group_max(b) + groups; }
+  __device__ int* counts(int b) const { return reinterpret_cast<int*>(group_max(2)) + b * kRowCluster; }
+  __device__ int* owners() const { return counts(2); }
 };
+
+// Order of the alternatives in 32 bits: larger logits above, NaN above all, -0 as 0.
+__device__ __forceinline__ unsigned value_order(float v) { return unsigned(order_key(v, 0) >> 32); }
+__device__ __forceinline__ float key_value(unsigned long long key) {
+  const unsigned u = unsigned(key >> 32);
+  return u == 0xFFFFFFF0u ? NAN : __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ int key_index(unsigned long long key) { return int(~unsigned(key)); }
 
 // A value that at least K of the G (at least K) values reach, and hardly more do: bisection over the
 // floats in their order, ended when at most K / 4 too many remain.  One warp calls.
@@ -825,151 +945,266 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
   return __int_as_float(lo ^ (lo >> 31 & 0x7fffffff));
 }
 
-__device__ __forceinline__ int key_index(unsigned long long key) { return int(~unsigned(key)); }
-
-// Calls f(key) for every element of the thread's pieces.
+// Takes a warp over a row in ascending index: f(orders, first, count) gets each lane's next `count`
+// elements from index `first` on, lanes side by side, and returns whether to go on (the same in all).
 template <typename E, typename F>
-__device__ __forceinline__ void each_key(const Slice<E>& s, const uint4* data, F f) {
-  for (int i = threadIdx.x; i < s.pieces; i += blockDim.x) {
-    const uint4 w = data[i];
-    const int j = s.index(i);
-    Vec<2> v[kPairs<E>];
-    unpack<E>(w, v);
+__device__ __forceinline__ void walk_row(const E* z, int V, F f) {
+  const int lane = threadIdx.x % 32;
+  const Slice<E> s = slice_of(z, V, 0, 1);
+  unsigned o[kPer<E>] = {};
+  if (lane < s.lead) o[0] = value_order(to_f32(z[lane]));
+  if (!f(o, lane, lane < s.lead ? 1 : 0)) return;
+  constexpr int kAhead = 4;
+  for (int i0 = 0; i0 < s.pieces; i0 += 32 * kAhead) {
+    uint4 w[kAhead];
 #pragma unroll
-    for (int k = 0; k < kPer<E>; ++k)
-      if (j + k >= 0 && j + k < s.V) f(order_key(v[k / 2].v[k % 2], j + k));
+    for (int u = 0; u < kAhead; ++u)
+      if (i0 + 32 * u + lane < s.pieces) w[u] = s.data()[i0 + 32 * u + lane];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + 32 * u + lane;
+      Vec<2> v[kPairs<E>] = {};
+      if (i < s.pieces) unpack<E>(w[u], v);
+#pragma unroll
+      for (int k = 0; k < kPer<E>; ++k) o[k] = value_order(v[k / 2].v[k % 2]);
+      if (!f(o, s.index(i), i < s.pieces ? kPer<E> : 0)) return;
+    }
   }
+  const int j = s.lead + s.whole * kPer<E> + lane;
+  if (j < V) o[0] = value_order(to_f32(z[j]));
+  f(o, j, j < V ? 1 : 0);
+}
+
+// The K largest elements of a row by (value, index), into list [entries] in no order.  At least K
+// elements have an order of lo or above, none one above hi.  One warp calls.
+template <typename E>
+__device__ __noinline__ void exact_top(const E* z, int V, int K, unsigned lo, unsigned hi, unsigned long long* list, int entries) {
+  const int lane = threadIdx.x % 32;
+  int have = 0;
+  auto collect = [&](bool ties, int most) {
+    walk_row<E>(z, V, [&](const unsigned (&o)[kPer<E>], int first, int count) {
+      int mine = 0;
+#pragma unroll
+      for (int k = 0; k < kPer<E>; ++k) mine += k < count && (ties ? o[k] == lo : o[k] > lo);
+      if (!__any_sync(~0u, mine)) return true;
+      int at = mine;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int other = __shfl_up_sync(~0u, at, d);
+        if (lane >= d) at += other;
+      }
+      const int all = __shfl_sync(~0u, at, 31);
+      at += have - mine;
+#pragma unroll
+      for (int k = 0; k < kPer<E>; ++k)
+        if (k < count && (ties ? o[k] == lo : o[k] > lo)) {
+          if (at < most) list[at] = static_cast<unsigned long long>(o[k]) << 32 | ~unsigned(first + k);
+          ++at;
+        }
+      have += all;
+      return have < most;
+    });
+  };
+  // most often few elements are above lo (what reaches it is ties); else the K-th order by bisection
+  collect(false, entries);
+  if (have >= K) {
+    while (lo < hi) {
+      const unsigned mid = lo + (hi - lo) / 2 + 1;
+      int n = 0;
+      walk_row<E>(z, V, [&](const unsigned (&o)[kPer<E>], int, int count) {
+#pragma unroll
+        for (int k = 0; k < kPer<E>; ++k) n += k < count && o[k] >= mid;
+        return true;
+      });
+      if (__reduce_add_sync(~0u, n) >= K)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    have = 0;
+    collect(false, entries);
+  }
+  collect(true, K);
+  __syncwarp();
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kRowThreads, 3) token_logp_kernel(const LogpArgs p, int C, int group_lanes) {
+__global__ void __launch_bounds__(kRowThreads + 32, 3) token_logp_kernel(const LogpArgs p, int64_t N, int C, int slots, int group_lanes) {
   extern __shared__ uint4 data[];
-  __shared__ Stats all[kRowCluster * kRowWarps];
-  __shared__ TopShared top;
+  __shared__ Stats all[2][kRowCluster * kRowParts];
   pdl_entry();
-  const int64_t n = blockIdx.x / C;
-  const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x, lane = tid % 32;
-  const E* z = static_cast<const E*>(p.logits) + n * p.ld;
-  const Slice<E> s = slice_of(z, p.V, rank, C);
-  row_start(C);
-  load_slice(s, data);
+  const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x - 32, parts = blockDim.x / 32, lane = tid % 32;
+  const int64_t step = gridDim.x / C;
   const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
-  int y = -1;
-  float zy = 0.0f;
-  if (rank == 0 && tid == 0 && p.logp) {
-    y = p.tokens[n];
-    if (y >= 0 && y < p.V) zy = to_f32(z[y]);
-  }
-  if (tid == 0) top.count = 0;
-  load_wait();
-  const Stats mine = thread_stats<E, true, false>(data, s.pieces, c);
-  row_started(C);
-  publish_stats(mine, all, rank, C, c);
-  const int per_block = T / group_lanes, groups = per_block * C;
-  if (p.K > 0) {
-    float g = mine.m;
-    for (int o = 1; o < group_lanes; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-    const int id = rank * per_block + tid / group_lanes;
-    for (int k = tid % group_lanes; k < C; k += group_lanes)
-      (C == 1 ? &top : cg::this_cluster().map_shared_rank(&top, k))->group_max[id] = g;
-  }
-  row_sync(C);
-  const Stats r = collect_stats(all, C, c);
-  const bool empty = r.m == -INFINITY && r.s == 0.0f;
-  const float ref = r.m == -INFINITY ? 0.0f : r.m;
-  const float log_s = empty ? 0.0f : logf(r.s);
-  if (rank == 0 && tid == 0) {
-    if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
-    if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
-    if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
-  }
-  if (p.K == 0) return;
-  auto write = [&](int k, unsigned long long key) {
-    p.top_idx[n * p.K + k] = key_index(key);
-    p.top_logp[n * p.K + k] = (to_f32(z[key_index(key)]) - ref) * inv_tau - log_s;
-  };
-  bool listed = !isnan(r.s);
-  if (listed) {
-    if (tid < 32) {
-      const float bound = group_bound(top.group_max, groups, p.K);
-      if (tid == 0) top.bound = bound;
-    }
-    __syncthreads();
-    const float bound = top.bound;
-    // a thread whose maximum reaches the bound: its pieces are searched by the warp together
-    for (unsigned hit = __ballot_sync(~0u, mine.m >= bound); hit; hit &= hit - 1) {
-      const int owner = tid - lane + __ffs(hit) - 1;
-      for (int i = owner + lane * T; i < s.pieces; i += 32 * T) {
-        const uint4 w = data[i];
-        if (piece_max<E>(w) < bound) continue;
-        const int j = s.index(i);
-        Vec<2> v[kPairs<E>];
-        unpack<E>(w, v);
-#pragma unroll
-        for (int k = 0; k < kPer<E>; ++k) {
-          const float x = v[k / 2].v[k % 2];
-          if (x >= bound && j + k >= 0 && j + k < s.V) {
-            const int at = atomicAdd(&top.count, 1);   // (the order in the list does not matter)
-            if (at < kList) top.list[at] = order_key(x, j + k);
-          }
-        }
+  const E* const logits = static_cast<const E*>(p.logits);
+  const int per_block = T / group_lanes, groups = per_block * C + 1;
+  const TopShared top(data + slots, p.K, groups, T);
+  int64_t n = blockIdx.x / C;
+  cluster_start();
+
+  if (tid < T) {
+    Slice<E> s = slice_of(logits + n * p.ld, p.V, rank, C);
+    for (int i = tid; i < s.pieces; i += T) load_piece(data + i, s.data() + i);
+    load_commit();
+    for (int b = 0, row = 0; n < N; n += step, b ^= 1, ++row) {
+      const Slice<E> next = slice_of(logits + (n + step) * p.ld, p.V, rank, C);
+      const int next_pieces = n + step < N ? next.pieces : 0;
+      load_wait();
+      Stats mine = no_stats();
+      mine.m = thread_max<E>(data, s.pieces, T);
+      const float m = mine.m;
+      thread_sums<E, true, false, false>(data, s.pieces, T, c, mine, [&](int i) {
+        if (i < next_pieces) load_piece(data + i, next.data() + i);
+      });
+      for (int i = s.pieces + (tid - s.pieces % T + T) % T; i < next_pieces; i += T) load_piece(data + i, next.data() + i);
+      load_commit();
+      // 0 times -inf, from logits of -inf or far below the others: again, with their x bounded
+      if (isnan(mine.e)) thread_sums<E, true, false, true>(s.data(), s.pieces, T, c, mine, [](int) {});
+      // the side warps have read what the row before last left in these buffers
+      if (row > 0) cluster_wait();
+      publish_stats(mine, all[b], rank, C, parts, c);
+      if (p.K > 0) {
+        top.thread_max(b)[tid] = m;
+        float g = m;
+        for (int o = 1; o < group_lanes; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+        for (int k = tid % group_lanes; k < C; k += group_lanes)
+          of_block(top.group_max(b), k)[rank * per_block + tid / group_lanes] = g;
       }
+      cluster_arrive();
+      s = next;
     }
-    __syncthreads();
-    if (C > 1 && tid < C) cg::this_cluster().map_shared_rank(&top, tid)->counts[rank] = top.count;
-    if (C == 1 && tid == 0) top.counts[0] = top.count;
-    row_sync(C);
+    cluster_wait();
+    cluster_arrive();
+    cluster_wait();
+    return;
+  }
+
+  // the side warp: the outputs of a row, and the ranking of the row before it
+  int64_t done = -1;      // the row whose alternatives are to be ranked
+  Stats done_stats = no_stats();
+  float done_bound = 0.0f;
+  auto ranked = [&](int b) {
+    const bool empty = done_stats.m == -INFINITY && done_stats.s == 0.0f;
+    const float ref = done_stats.m == -INFINITY ? 0.0f : done_stats.m, log_s = empty ? 0.0f : logf(done_stats.s);
+    unsigned long long* list = top.list(b);
+    const int share = top_entries(p.K) / C;
     int total = 0;
-    for (int k = 0; k < C; ++k) total += top.counts[k] > kList ? kList * kRowCluster + 1 : top.counts[k];
-    listed = total <= kList;
-    if (listed) {
-      // the first block takes the lists together: its own stays, the others' follow
-      if (rank == 0 && C > 1) {
-        int from = top.counts[0];
-        for (int b = 1; b < C; ++b) {
-          const unsigned long long* theirs = cg::this_cluster().map_shared_rank(&top, b)->list;
-          for (int k = tid; k < top.counts[b]; k += T) top.list[from + k] = theirs[k];
-          from += top.counts[b];
-        }
+    bool fits = !isnan(done_stats.s);
+    for (int k = 0; k < C; ++k) fits = fits && top.counts(b)[k] <= share;
+    if (fits) {
+      // the blocks' shares moved together
+      for (int k = 0; k < C; ++k) {
+        const int count = top.counts(b)[k];
+        if (k > 0)
+          for (int i0 = 0; i0 < count; i0 += 32) {
+            const unsigned long long key = i0 + lane < count ? list[k * share + i0 + lane] : 0;
+            __syncwarp();
+            if (i0 + lane < count) list[total + i0 + lane] = key;
+            __syncwarp();
+          }
+        total += count;
       }
-      row_sync(C);
-      if (rank == 0)
-        for (int i = tid; i < total; i += T) {
-          const unsigned long long key = top.list[i];
-          int above = 0;
-          for (int k = 0; k < total; ++k) above += top.list[k] > key;
-          if (above < p.K) write(above, key);
-        }
-      return;
-    }
-  }
-  unsigned long long last = ~0ull;
-  for (int k = 0; k < p.K; ++k) {
-    unsigned long long b = 0;
-    each_key<E>(s, data, [&](unsigned long long key) {
-      if (key < last && key > b) b = key;
-    });
-    for (int o = 16; o > 0; o >>= 1) {
-      const unsigned long long other = __shfl_xor_sync(~0u, b, o);
-      b = other > b ? other : b;
-    }
-    if (lane == 0) top.best[tid / 32] = b;
-    __syncthreads();
-    for (int i = 0; i < T / 32; ++i) b = top.best[i] > b ? top.best[i] : b;
-    if (C > 1) {
-      if (tid < C) cg::this_cluster().map_shared_rank(&top, tid)->round_best[k & 1][rank] = b;
-      row_sync(C);
-      for (int i = 0; i < C; ++i) b = top.round_best[k & 1][i] > b ? top.round_best[k & 1][i] : b;
     } else {
-      __syncthreads();
+      const bool finite = !isnan(done_stats.s);
+      exact_top<E>(logits + done * p.ld, p.V, p.K, finite ? value_order(done_bound) : 1u,
+                   finite ? value_order(done_stats.m) : value_order(NAN), list, top.entries);
+      total = p.K;
     }
-    last = b;
-    if (rank == 0 && tid == 0) write(k, b);
+    for (int i = lane; i < total; i += 32) {
+      const unsigned long long key = list[i];
+      int above = 0;
+#pragma unroll 8
+      for (int k = 0; k < total; ++k) above += list[k] > key;
+      if (above < p.K) {
+        p.top_idx[done * p.K + above] = key_index(key);
+        p.top_logp[done * p.K + above] = (key_value(key) - ref) * inv_tau - log_s;
+      }
+    }
+    __syncwarp();
+  };
+  int b = 0;
+  for (; n < N; n += step, b ^= 1) {
+    const E* z = logits + n * p.ld;
+    const Slice<E> s = slice_of(z, p.V, rank, C);
+    const int je = rank == 0 && lane < s.edges() ? s.edge(lane) : -1;
+    const float ze = je >= 0 ? to_f32(z[je]) : -INFINITY;
+    int y = -1;
+    float zy = 0.0f;
+    if (rank == 0 && p.logp) {
+      y = p.tokens[n];
+      if (y >= 0 && y < p.V) zy = to_f32(z[y]);
+    }
+    publish_stats(je >= 0 ? one_element(ze) : no_stats(), all[b], rank, C, parts, c);
+    if (p.K > 0 && rank == 0) {
+      float g = ze;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+      if (lane < C) of_block(top.group_max(b), lane)[groups - 1] = g;
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (rank == 0 && done >= 0) ranked(b ^ 1);
+    const Stats r = collect_stats(all[b], C, parts, c);
+    if (rank == 0 && lane == 0) {
+      const bool empty = r.m == -INFINITY && r.s == 0.0f;
+      const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
+      if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
+      if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
+      if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
+    }
+    if (p.K == 0) continue;
+    done = n;
+    done_stats = r;
+    if (isnan(r.s)) continue;   // (the same in all blocks)
+    const float bound = group_bound(top.group_max(b), groups, p.K);
+    done_bound = bound;
+    const int share = top_entries(p.K) / C;
+    unsigned long long* const to = of_block(top.list(b), 0) + rank * share;
+    int count = 0;
+    auto push = [&](bool want, float v, int j) {
+      const unsigned votes = __ballot_sync(~0u, want);
+      const int at = count + __popc(votes & ((1u << lane) - 1));
+      if (want && at < share) to[at] = order_key(v, j);
+      count += __popc(votes);
+    };
+    push(je >= 0 && ze >= bound, ze, je);
+    int owners = 0;
+    for (int t = lane; t < T; t += 32) {
+      const bool hit = top.thread_max(b)[t] >= bound;
+      const unsigned votes = __ballot_sync(~0u, hit);
+      if (hit) top.owners()[owners + __popc(votes & ((1u << lane) - 1))] = t;
+      owners += __popc(votes);
+    }
+    __syncwarp();
+    const int each = (s.pieces + T - 1) / T, items = owners * each;
+    for (int i0 = 0; i0 < items && count <= share; i0 += 64) {
+      uint4 w[2];
+      int piece[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int i = i0 + u * 32 + lane;
+        piece[u] = i < items ? top.owners()[i / each] + i % each * T : s.pieces;
+        if (piece[u] < s.pieces) w[u] = s.data()[piece[u]];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool reach = piece[u] < s.pieces && piece_max<E>(w[u]) >= bound;
+        if (!__any_sync(~0u, reach)) continue;
+        Vec<2> v[kPairs<E>];
+        unpack<E>(w[u], v);
+#pragma unroll
+        for (int k = 0; k < kPer<E>; ++k)
+          push(reach && v[k / 2].v[k % 2] >= bound, v[k / 2].v[k % 2], s.index(piece[u]) + k);
+      }
+    }
+    if (lane == 0) of_block(top.counts(b), 0)[rank] = count;
   }
-  row_sync(C);   // no block leaves while another may still write to it
+  cluster_arrive();
+  cluster_wait();
+  if (rank == 0 && done >= 0) ranked(b ^ 1);
 }
 
-// ---- gradient of log probability and entropy: one pass, block by block of a row's pieces ----
+// ---- gradient of log probability and entropy: one pass over a row's pieces, cut over blocks ----
 
 constexpr int kGradPieces = 4;   // of a thread
 
@@ -979,22 +1214,17 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
   const int64_t n = blockIdx.x / blocks_per_row;
   const int part = blockIdx.x % blocks_per_row;
   const E* z = static_cast<const E*>(p.logits) + n * p.ld;
-  E* grad = static_cast<E*>(p.grad) + n * p.grad_ld;
   const Slice<E> s = slice_of(z, p.V, 0, 1);
-  const bool same = int(reinterpret_cast<uintptr_t>(grad) % 16 / sizeof(E)) == s.shift;
+  E* const grad = static_cast<E*>(p.grad) + n * p.grad_ld;
+  E* const out = grad + s.index(0);
+  const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
   const int first = part * kGradPieces * kRowThreads + threadIdx.x;
   uint4 w[kGradPieces];
 #pragma unroll
-  for (int i = 0; i < kGradPieces; ++i) {
-    const int j = s.index(first + i * kRowThreads);
-    if (j >= 0 && j + kPer<E> <= s.V) {
-      w[i] = *reinterpret_cast<const uint4*>(z + j);
-    } else {
-      E e[kPer<E>];
-      for (int k = 0; k < kPer<E>; ++k) e[k] = j + k >= 0 && j + k < s.V ? z[j + k] : from_f32<E>(0.0f);
-      w[i] = *reinterpret_cast<const uint4*>(e);
-    }
-  }
+  for (int i = 0; i < kGradPieces; ++i)
+    if (first + i * kRowThreads < s.pieces) w[i] = s.data()[first + i * kRowThreads];
+  const int je = part == 0 && int(threadIdx.x) < s.edges() ? s.edge(threadIdx.x) : -1;
+  const float ze = je >= 0 ? to_f32(z[je]) : 0.0f;
   const float inv_tau = 1.0f / p.tau;
   const float lse = p.lse[n];
   int y = -1;
@@ -1007,87 +1237,133 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
   const float H = p.dentropy ? p.entropy[n] : 0.0f;
   const float none = lse == -INFINITY ? 0.0f : 1.0f;   // a row without mass: p = 0
   const float off = lse == -INFINITY ? 0.0f : lse;
+  auto value = [&](Vec<2> v, int j) {
+    const Vec<2> lp = fma<2>(v, splat<2>(inv_tau), splat<2>(-off)), x = lp * splat<2>(kLog2e);
+    const Vec<2> e = Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])} * splat<2>(-none);
+    const Vec<2> bounded = {fmaxf(lp.v[0], -1000.0f), fmaxf(lp.v[1], -1000.0f)};
+    Vec<2> g = e * fma<2>(splat<2>(dh), bounded, splat<2>(fmaf(dh, H, dl)));
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+      if (j + m == y) g.v[m] += dl;
+    return g * splat<2>(inv_tau);
+  };
 #pragma unroll
   for (int i = 0; i < kGradPieces; ++i) {
-    const int j = s.index(first + i * kRowThreads);
-    if (j >= s.V) break;
+    const int piece = first + i * kRowThreads;
+    if (piece >= s.pieces) break;
+    const int j = s.index(piece);
     Vec<2> v[kPairs<E>];
     unpack<E>(w[i], v);
 #pragma unroll
-    for (int k = 0; k < kPairs<E>; ++k) {
-      const Vec<2> lp = fma<2>(v[k], splat<2>(inv_tau), splat<2>(-off)), x = lp * splat<2>(kLog2e);
-      const Vec<2> e = Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])} * splat<2>(-none);
-      const Vec<2> bounded = {fmaxf(lp.v[0], -1000.0f), fmaxf(lp.v[1], -1000.0f)};
-      Vec<2> g = e * fma<2>(splat<2>(dh), bounded, splat<2>(fmaf(dh, H, dl)));
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-        if (j + 2 * k + m == y) g.v[m] += dl;
-      v[k] = g * splat<2>(inv_tau);
-    }
+    for (int k = 0; k < kPairs<E>; ++k) v[k] = value(v[k], j + 2 * k);
     const uint4 o = pack<E>(v);
-    if (same && j >= 0 && j + kPer<E> <= s.V) {
+    if (aligned) {
       *reinterpret_cast<uint4*>(grad + j) = o;
     } else {
       const E* e = reinterpret_cast<const E*>(&o);
 #pragma unroll
-      for (int k = 0; k < kPer<E>; ++k)
-        if (j + k >= 0 && j + k < s.V) grad[j + k] = e[k];
+      for (int k = 0; k < kPer<E>; ++k) grad[j + k] = e[k];
     }
   }
+  if (je >= 0) grad[je] = from_f32<E>(value(splat<2>(ze), je).v[0]);
 }
 
-// How a row is held: blocks of a cluster, threads of a block and bytes of shared memory.  Slices of
-// up to 64 KB let three blocks share an SM, so that one loads or stores while another computes; few
-// rows are cut further, down to 8 KB, to use more SMs.  cluster = 0: the row does not fit on chip.
+// How a row is held: blocks of a cluster, threads of a block (the side warp's too) and bytes of
+// shared memory.  Slices of up to 65 KB let three blocks share an SM, so that one waits while others
+// work; few rows are cut further, down to 8 KB, to use more SMs.  cluster = 0: the row does not fit
+// on chip.
 struct RowCut {
-  int cluster, threads;
+  int cluster, threads, slots;
   size_t smem;
 };
 
 RowCut row_cut(int dtype, int64_t N, int64_t V, int K) {
   constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 200 << 10;
-  const int64_t bytes = V * dtype_size(dtype) + 32;   // with the pieces at both ends
-  RowCut c = {1, kRowThreads, 0};
+  const int64_t bytes = V * dtype_size(dtype);
+  RowCut c = {1, kRowThreads, 0, 0};
   while (c.cluster < kRowCluster && bytes > kSlice * c.cluster) c.cluster *= 2;
   while (c.cluster < kRowCluster && N * c.cluster < 2 * 152 && bytes >= 2 * kLeast * c.cluster) c.cluster *= 2;
-  c.smem = size_t((bytes / 16 + c.cluster) / c.cluster + 1) * 16;
-  if (int64_t(c.smem) > kMost) return {0, 0, 0};
+  c.slots = int((bytes / 16 + c.cluster - 1) / c.cluster);
+  c.smem = size_t(c.slots) * 16;
+  if (int64_t(c.smem) > kMost) return {0, 0, 0, 0};
   if (c.smem <= 8192 && K <= 128) c.threads = 128;
+  c.threads += 32;
   return c;
 }
 
-template <typename Kernel, typename... Args>
-cudaError_t launch_rows(Kernel kernel, const RowCut& c, int64_t N, cudaStream_t stream, Args... args) {
-  const cudaError_t e = allow_smem(kernel, c.smem);
+// Clusters of a kernel that the GPU holds at once.
+template <typename Kernel>
+cudaError_t resident_clusters(Kernel* kernel, const RowCut& c, int* clusters) {
+  struct Known {
+    const void* kernel;
+    int device, cluster, threads, clusters;
+    size_t smem;
+  };
+  static std::mutex mutex;
+  static Known known[32];
+  static int count = 0;
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  return launch_cluster_pdl(kernel, unsigned(N * c.cluster), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
+  const void* key = reinterpret_cast<const void*>(kernel);
+  std::lock_guard<std::mutex> lock(mutex);
+  for (const Known& k : known)
+    if (k.kernel == key && k.device == device && k.cluster == c.cluster && k.threads == c.threads && k.smem == c.smem) {
+      *clusters = k.clusters;
+      return cudaSuccess;
+    }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(c.cluster));
+  cfg.blockDim = dim3(unsigned(c.threads));
+  cfg.dynamicSmemBytes = c.smem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(c.cluster);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(clusters, kernel, &cfg);
+  if (e != cudaSuccess) return e;
+  if (*clusters < 1) return cudaErrorInvalidConfiguration;
+  known[count++ % 32] = {key, device, c.cluster, c.threads, *clusters, c.smem};
+  return cudaSuccess;
+}
+
+template <typename... KArgs, typename... Args>
+cudaError_t launch_rows(void (*kernel)(KArgs...), const RowCut& c, int64_t N, cudaStream_t stream, Args... args) {
+  cudaError_t e = allow_smem(kernel, c.smem);
+  int clusters = 0;
+  if (e == cudaSuccess) e = resident_clusters(kernel, c, &clusters);
+  if (e != cudaSuccess) return e;
+  const int64_t grid = (N < clusters ? N : clusters) * c.cluster;
+  return launch_cluster_pdl(kernel, unsigned(grid), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
 }
 
 template <typename E>
 cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  const RowCut c = row_cut(dtype, N, p.V, p.K);
+  RowCut c = row_cut(dtype, N, p.V, p.K);
   if (c.cluster == 0) return launch_pdl(distill_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
-  return p.alpha > 0.0f ? launch_rows(distill_kernel<E, true>, c, N, stream, p, c.cluster)
-                        : launch_rows(distill_kernel<E, false>, c, N, stream, p, c.cluster);
+  c.smem += teacher_bytes(p.K);
+  return p.alpha > 0.0f ? launch_rows(distill_kernel<E, true>, c, N, stream, p, N, c.cluster, c.slots)
+                        : launch_rows(distill_kernel<E, false>, c, N, stream, p, N, c.cluster, c.slots);
 }
 
 template <typename E>
 cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  const RowCut c = row_cut(dtype, N, p.V, p.K);
+  RowCut c = row_cut(dtype, N, p.V, p.K);
   if (c.cluster == 0) return launch_pdl(token_logp_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
-  // the widest groups of which there are at least 2 K with elements
-  const int64_t pieces = (int64_t(p.V) * sizeof(E) / 16 + c.cluster) / c.cluster;
-  const int64_t busy = (pieces < c.threads ? pieces : c.threads) * c.cluster;
+  // the widest groups of which there are at least 2 K with elements (T C of one lane: at least K)
+  const int T = c.threads - 32, busy = (c.slots < T ? c.slots : T) * c.cluster;
   int lanes = 32;
-  while (lanes > 1 && (busy < int64_t(2) * p.K * lanes || c.threads * c.cluster > kMaxGroups * lanes * 8)) lanes /= 2;
-  while (c.threads * c.cluster > kMaxGroups * lanes) lanes *= 2;
-  return launch_rows(token_logp_kernel<E>, c, N, stream, p, c.cluster, lanes);
+  while (lanes > 1 && busy < 2 * p.K * lanes) lanes /= 2;
+  c.smem += top_bytes(p.K, T / lanes * c.cluster + 1, T);
+  return launch_rows(token_logp_kernel<E>, c, N, stream, p, N, c.cluster, c.slots, lanes);
 }
 
 template <typename E>
 cudaError_t launch_logp_grad(const LogpGradArgs& p, int64_t N, cudaStream_t stream) {
   const int64_t per_block = int64_t(kGradPieces) * kRowThreads * kPer<E>;
-  const int64_t blocks = (p.V + 16 + per_block - 1) / per_block;
+  const int64_t blocks = (p.V + per_block - 1) / per_block;
   return launch_pdl(token_logp_grad_kernel<E>, dim3(unsigned(N * blocks)), dim3(kRowThreads), 0, stream, p, int(blocks));
 }
 
