@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreads) token_logp_stream_kernel(const LogpA
 // is the one that reads them, so the passes over a slice need no barrier between.
 //
 // Clusters stay and take row after row.  The last pass over a row copies the next row's piece into
-// each slot as soon as it has read it, and one warp of the block beside the T others (its side warp)
+// each slot as soon as it has read it, and one or two warps of the block beside the T threads (side warps)
 // does what is short and serial: the teacher's entries, the loss, the choice of alternatives, the
 // edge elements.  It works on the next or the previous row while the others stream, so that
 // neither memory nor the passes wait for it.  One cluster barrier per row keeps them in step.
@@ -552,19 +552,19 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, c
   int j[kPerLane];
   float logq[kPerLane], zk[kPerLane];
   float most = -INFINITY;
+  // (all loads of a kind together: their latencies overlap)
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
     const int k = e * 32 + lane;
-    j[e] = -1;
-    logq[e] = -INFINITY;
-    if (k < p.K) {
-      const int a = p.top_idx[n * p.K + k];
-      if (a >= 0 && a < p.V) {
-        logq[e] = p.top_logits[n * p.K + k] * inv_tau;
-        if (logq[e] != -INFINITY) j[e] = a;
-      }
-    }
+    j[e] = k < p.K ? p.top_idx[n * p.K + k] : -1;
+    logq[e] = k < p.K ? p.top_logits[n * p.K + k] : -INFINITY;
+  }
+#pragma unroll
+  for (int e = 0; e < kPerLane; ++e) {
+    if (j[e] < 0 || j[e] >= p.V || logq[e] == -INFINITY) j[e] = -1;
     zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
+    logq[e] = j[e] >= 0 ? logq[e] * inv_tau : -INFINITY;
+    if (logq[e] == -INFINITY) j[e] = -1;
     most = fmaxf(most, logq[e]);
   }
   for (int i = lane; i < 1 << t.table_bits; i += 32) t.table[i] = -1;
@@ -913,7 +913,7 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 __device__ __forceinline__ int key_index(unsigned long long key) { return int(~unsigned(key)); }
 
 // A value that at least K of the G (at least K) values reach, and hardly more do: bisection over the
-// floats in their order, ended when at most K / 4 too many remain.  One warp calls.
+// floats in their order, ended when at most 8 or K / 4 too many remain.  One warp calls.
 __device__ __forceinline__ float group_bound(const float* values, int G, int K) {
   const int lane = threadIdx.x % 32;
   auto order = [](float v) {
@@ -930,7 +930,7 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
   hi = __reduce_max_sync(~0u, hi);
   // K values reach lo; fewer than K reach hi + 1
   int reach = G;
-  while (lo < hi && reach > K + K / 4) {
+  while (lo < hi && reach > K + (K < 32 ? 8 : K / 4)) {
     const int mid = int((int64_t(lo) + hi + 1) >> 1);
     int n = 0;
     for (int i = lane; i < G; i += 32) n += order(values[i]) >= mid;
@@ -1029,16 +1029,19 @@ __device__ __noinline__ void exact_top(const E* z, int V, int K, unsigned lo, un
 }
 
 template <typename E>
-__global__ void __launch_bounds__(kRowThreads + 32, 3) token_logp_kernel(const LogpArgs p, int64_t N, int C, int slots, int group_lanes) {
+__global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const LogpArgs p, int64_t N, int C, int slots, int group_lanes) {
   extern __shared__ uint4 data[];
   __shared__ Stats all[2][kRowCluster * kRowParts];
+  __shared__ float bounds[2];
   pdl_entry();
-  const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x - 32, parts = blockDim.x / 32, lane = tid % 32;
+  // T threads stream; then the search warp and the rank warp
+  const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x - 64, parts = T / 32 + 1, lane = tid % 32;
   const int64_t step = gridDim.x / C;
   const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
   const E* const logits = static_cast<const E*>(p.logits);
   const int per_block = T / group_lanes, groups = per_block * C + 1;
   const TopShared top(data + slots, p.K, groups, T);
+  const int share = top_entries(p.K) / C;
   int64_t n = blockIdx.x / C;
   cluster_start();
 
@@ -1079,18 +1082,92 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) token_logp_kernel(const L
     return;
   }
 
-  // the side warp: the outputs of a row, and the ranking of the row before it
-  int64_t done = -1;      // the row whose alternatives are to be ranked
-  Stats done_stats = no_stats();
-  float done_bound = 0.0f;
+  if (tid < T + 32) {
+    // the search warp: the edge elements' statistics, and the elements that reach a row's bound
+    for (int b = 0; n < N; n += step, b ^= 1) {
+      const E* z = logits + n * p.ld;
+      const Slice<E> s = slice_of(z, p.V, rank, C);
+      const int je = rank == 0 && lane < s.edges() ? s.edge(lane) : -1;
+      const float ze = je >= 0 ? to_f32(z[je]) : -INFINITY;
+      publish_stats(je >= 0 ? one_element(ze) : no_stats(), all[b], rank, C, parts, c);
+      if (p.K > 0 && rank == 0) {
+        float g = ze;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+        if (lane < C) of_block(top.group_max(b), lane)[groups - 1] = g;
+      }
+      cluster_arrive();
+      cluster_wait();
+      if (p.K == 0) continue;
+      const float bound = group_bound(top.group_max(b), groups, p.K);
+      if (rank == 0 && lane == 0) bounds[b] = bound;
+      unsigned long long* const to = of_block(top.list(b), 0) + rank * share;
+      const unsigned below = (1u << lane) - 1;
+      int count = 0, owners = 0;
+      {
+        const unsigned votes = __ballot_sync(~0u, je >= 0 && ze >= bound);
+        if (votes >> lane & 1) {
+          const int at = __popc(votes & below);
+          if (at < share) to[at] = order_key(ze, je);
+        }
+        count = __popc(votes);
+      }
+#pragma unroll 8
+      for (int t = lane; t < T; t += 32) {
+        const unsigned votes = __ballot_sync(~0u, top.thread_max(b)[t] >= bound);
+        if (votes >> lane & 1) top.owners()[owners + __popc(votes & below)] = t;
+        owners += __popc(votes);
+      }
+      __syncwarp();
+      const int each = (s.pieces + T - 1) / T, items = owners * each;
+      constexpr int kAhead = 4;
+      for (int i0 = 0; i0 < items && count <= share; i0 += 32 * kAhead) {
+        uint4 w[kAhead];
+        int piece[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          const int i = i0 + u * 32 + lane;
+          piece[u] = i < items ? top.owners()[i / each] + i % each * T : s.pieces;
+          if (piece[u] < s.pieces) w[u] = s.data()[piece[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+          // a bit for each of the piece's elements that reach the bound
+          unsigned reach = 0;
+          if (piece[u] < s.pieces && piece_max<E>(w[u]) >= bound) {
+            Vec<2> v[kPairs<E>];
+            unpack<E>(w[u], v);
+#pragma unroll
+            for (int k = 0; k < kPer<E>; ++k) reach |= unsigned(v[k / 2].v[k % 2] >= bound) << k;
+          }
+          // one element of each lane at a time: lanes rarely have one, hardly ever two
+          for (unsigned votes; (votes = __ballot_sync(~0u, reach != 0)) != 0; reach &= reach - 1) {
+            if (reach) {
+              const int k = __ffs(reach) - 1, at = count + __popc(votes & below);
+              const E x = reinterpret_cast<const E*>(s.data() + piece[u])[k];   // (in L1)
+              if (at < share) to[at] = order_key(to_f32(x), s.index(piece[u]) + k);
+            }
+            count += __popc(votes);
+          }
+        }
+      }
+      if (lane == 0) of_block(top.counts(b), 0)[rank] = count;
+    }
+    cluster_arrive();
+    cluster_wait();
+    return;
+  }
+
+  // the rank warp: a row's values, and the alternatives of the row before it
+  int64_t done = -1;
+  Stats r = no_stats();
   auto ranked = [&](int b) {
-    const bool empty = done_stats.m == -INFINITY && done_stats.s == 0.0f;
-    const float ref = done_stats.m == -INFINITY ? 0.0f : done_stats.m, log_s = empty ? 0.0f : logf(done_stats.s);
+    const bool empty = r.m == -INFINITY && r.s == 0.0f;
+    const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
     unsigned long long* list = top.list(b);
-    const int share = top_entries(p.K) / C;
-    int total = 0;
-    bool fits = !isnan(done_stats.s);
+    bool fits = !isnan(r.s);
     for (int k = 0; k < C; ++k) fits = fits && top.counts(b)[k] <= share;
+    int total = 0;
     if (fits) {
       // the blocks' shares moved together
       for (int k = 0; k < C; ++k) {
@@ -1105,9 +1182,9 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) token_logp_kernel(const L
         total += count;
       }
     } else {
-      const bool finite = !isnan(done_stats.s);
-      exact_top<E>(logits + done * p.ld, p.V, p.K, finite ? value_order(done_bound) : 1u,
-                   finite ? value_order(done_stats.m) : value_order(NAN), list, top.entries);
+      const bool finite = !isnan(r.s);
+      exact_top<E>(logits + done * p.ld, p.V, p.K, finite ? value_order(bounds[b]) : 1u,
+                   finite ? value_order(r.m) : value_order(NAN), list, top.entries);
       total = p.K;
     }
     for (int i = lane; i < total; i += 32) {
@@ -1124,84 +1201,29 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) token_logp_kernel(const L
   };
   int b = 0;
   for (; n < N; n += step, b ^= 1) {
-    const E* z = logits + n * p.ld;
-    const Slice<E> s = slice_of(z, p.V, rank, C);
-    const int je = rank == 0 && lane < s.edges() ? s.edge(lane) : -1;
-    const float ze = je >= 0 ? to_f32(z[je]) : -INFINITY;
     int y = -1;
     float zy = 0.0f;
     if (rank == 0 && p.logp) {
       y = p.tokens[n];
-      if (y >= 0 && y < p.V) zy = to_f32(z[y]);
-    }
-    publish_stats(je >= 0 ? one_element(ze) : no_stats(), all[b], rank, C, parts, c);
-    if (p.K > 0 && rank == 0) {
-      float g = ze;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
-      if (lane < C) of_block(top.group_max(b), lane)[groups - 1] = g;
+      if (y >= 0 && y < p.V) zy = to_f32(logits[n * p.ld + y]);
     }
     cluster_arrive();
     cluster_wait();
-    if (rank == 0 && done >= 0) ranked(b ^ 1);
-    const Stats r = collect_stats(all[b], C, parts, c);
-    if (rank == 0 && lane == 0) {
+    if (rank != 0) continue;
+    if (done >= 0) ranked(b ^ 1);
+    r = collect_stats(all[b], C, parts, c);
+    if (lane == 0) {
       const bool empty = r.m == -INFINITY && r.s == 0.0f;
       const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
       if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
       if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
       if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
     }
-    if (p.K == 0) continue;
-    done = n;
-    done_stats = r;
-    if (isnan(r.s)) continue;   // (the same in all blocks)
-    const float bound = group_bound(top.group_max(b), groups, p.K);
-    done_bound = bound;
-    const int share = top_entries(p.K) / C;
-    unsigned long long* const to = of_block(top.list(b), 0) + rank * share;
-    int count = 0;
-    auto push = [&](bool want, float v, int j) {
-      const unsigned votes = __ballot_sync(~0u, want);
-      const int at = count + __popc(votes & ((1u << lane) - 1));
-      if (want && at < share) to[at] = order_key(v, j);
-      count += __popc(votes);
-    };
-    push(je >= 0 && ze >= bound, ze, je);
-    int owners = 0;
-    for (int t = lane; t < T; t += 32) {
-      const bool hit = top.thread_max(b)[t] >= bound;
-      const unsigned votes = __ballot_sync(~0u, hit);
-      if (hit) top.owners()[owners + __popc(votes & ((1u << lane) - 1))] = t;
-      owners += __popc(votes);
-    }
-    __syncwarp();
-    const int each = (s.pieces + T - 1) / T, items = owners * each;
-    for (int i0 = 0; i0 < items && count <= share; i0 += 64) {
-      uint4 w[2];
-      int piece[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int i = i0 + u * 32 + lane;
-        piece[u] = i < items ? top.owners()[i / each] + i % each * T : s.pieces;
-        if (piece[u] < s.pieces) w[u] = s.data()[piece[u]];
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bool reach = piece[u] < s.pieces && piece_max<E>(w[u]) >= bound;
-        if (!__any_sync(~0u, reach)) continue;
-        Vec<2> v[kPairs<E>];
-        unpack<E>(w[u], v);
-#pragma unroll
-        for (int k = 0; k < kPer<E>; ++k)
-          push(reach && v[k / 2].v[k % 2] >= bound, v[k / 2].v[k % 2], s.index(piece[u]) + k);
-      }
-    }
-    if (lane == 0) of_block(top.counts(b), 0)[rank] = count;
+    if (p.K > 0) done = n;
   }
   cluster_arrive();
   cluster_wait();
-  if (rank == 0 && done >= 0) ranked(b ^ 1);
+  if (done >= 0) ranked(b ^ 1);
 }
 
 // ---- gradient of log probability and entropy: one pass over a row's pieces, cut over blocks ----
@@ -1268,7 +1290,7 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
   if (je >= 0) grad[je] = from_f32<E>(value(splat<2>(ze), je).v[0]);
 }
 
-// How a row is held: blocks of a cluster, threads of a block (the side warp's too) and bytes of
+// How a row is held: blocks of a cluster, threads of a block (the side warps' too) and bytes of
 // shared memory.  Slices of up to 65 KB let three blocks share an SM, so that one waits while others
 // work; few rows are cut further, down to 8 KB, to use more SMs.  cluster = 0: the row does not fit
 // on chip.
@@ -1277,7 +1299,7 @@ struct RowCut {
   size_t smem;
 };
 
-RowCut row_cut(int dtype, int64_t N, int64_t V, int K) {
+RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
   constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 200 << 10;
   const int64_t bytes = V * dtype_size(dtype);
   RowCut c = {1, kRowThreads, 0, 0};
@@ -1287,7 +1309,7 @@ RowCut row_cut(int dtype, int64_t N, int64_t V, int K) {
   c.smem = size_t(c.slots) * 16;
   if (int64_t(c.smem) > kMost) return {0, 0, 0, 0};
   if (c.smem <= 8192 && K <= 128) c.threads = 128;
-  c.threads += 32;
+  c.threads += 32 * side_warps;
   return c;
 }
 
@@ -1341,7 +1363,7 @@ cudaError_t launch_rows(void (*kernel)(KArgs...), const RowCut& c, int64_t N, cu
 
 template <typename E>
 cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  RowCut c = row_cut(dtype, N, p.V, p.K);
+  RowCut c = row_cut(dtype, N, p.V, p.K, 1);
   if (c.cluster == 0) return launch_pdl(distill_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   c.smem += teacher_bytes(p.K);
   return p.alpha > 0.0f ? launch_rows(distill_kernel<E, true>, c, N, stream, p, N, c.cluster, c.slots)
@@ -1350,10 +1372,10 @@ cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStrea
 
 template <typename E>
 cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  RowCut c = row_cut(dtype, N, p.V, p.K);
+  RowCut c = row_cut(dtype, N, p.V, p.K, 2);
   if (c.cluster == 0) return launch_pdl(token_logp_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   // the widest groups of which there are at least 2 K with elements (T C of one lane: at least K)
-  const int T = c.threads - 32, busy = (c.slots < T ? c.slots : T) * c.cluster;
+  const int T = c.threads - 64, busy = (c.slots < T ? c.slots : T) * c.cluster;
   int lanes = 32;
   while (lanes > 1 && busy < 2 * p.K * lanes) lanes /= 2;
   c.smem += top_bytes(p.K, T / lanes * c.cluster + 1, T);
