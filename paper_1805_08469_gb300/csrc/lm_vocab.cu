@@ -496,6 +496,12 @@ __device__ __forceinline__ void publish_stats(const Stats& mine, Stats* all, int
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (lane < C) of_block(all, lane)[rank * parts + warp] = a;
 }
+// A warp's edge elements to every block, which most rows have none of.
+__device__ __forceinline__ void publish_edges(const Stats& mine, bool any, Stats* all, int rank, int C, int parts, float c) {
+  const Stats a = any ? warp_join(mine, c) : no_stats();
+  const int lane = threadIdx.x % 32;
+  if (lane < C) of_block(all, lane)[rank * parts + parts - 1] = a;
+}
 __device__ __forceinline__ Stats collect_stats(const Stats* all, int C, int parts, float c) {
   const int lane = threadIdx.x % 32, n = C * parts;
   Stats a = lane < n ? all[lane] : no_stats();
@@ -506,33 +512,23 @@ __device__ __forceinline__ Stats collect_stats(const Stats* all, int C, int part
 // The teacher's side of a row, taken by the side warp (lane l holds entries l, l + 32, ...).  Arrays of
 // K values in dynamic shared memory.
 struct Teacher {
-  int* at;        // index of an entry; -1: absent, or another entry has it
-  float* q;       // mass there, that of all entries with the index
-  float* z;       // the student's logit there
-  float* logq;    // the entry's own log mass, -inf where absent (of the current row only)
-  int* table;     // the indices, hashed (of the current row only)
-  int table_bits;
+  int* at;          // index of an entry; -1: absent, or another entry has it
+  float* q;         // mass there, that of all entries with the index
+  float* z;         // the student's logit there
+  uint8_t* table;   // entries by hashes of their indices, [kTable]
 };
-// What every row of a block needs of them: 7 K words and a table of at least 2 K.
-__host__ __device__ inline int table_bits(int K) {
-  int bits = 5;
-  while ((1 << bits) < 2 * K) ++bits;
-  return bits;
-}
-inline size_t teacher_bytes(int K) { return (size_t(7) * K + (size_t(1) << table_bits(K))) * 4; }
+constexpr int kTableBits = 10, kTable = 1 << kTableBits;
+static_assert(GEM_TOP_MAX <= 256, "an entry's number is a byte");
+// What a block needs of them: 3 K words for each of two rows, and the table.
+inline size_t teacher_bytes(int K) { return size_t(6) * K * 4 + kTable; }
 __device__ __forceinline__ Teacher teacher_at(void* shared, int K, int b) {
   int* w = static_cast<int*>(shared);
   Teacher t;
   t.at = w + (3 * b) * K;
   t.q = reinterpret_cast<float*>(w + (3 * b + 1) * K);
   t.z = reinterpret_cast<float*>(w + (3 * b + 2) * K);
-  t.logq = reinterpret_cast<float*>(w + 6 * K);
-  t.table = w + 7 * K;
-  t.table_bits = table_bits(K);
+  t.table = reinterpret_cast<uint8_t*>(w + 6 * K);
   return t;
-}
-__device__ __forceinline__ unsigned table_slot(const Teacher& t, int j) {
-  return unsigned(j) * 2654435761u >> (32 - t.table_bits);
 }
 
 constexpr int kPerLane = GEM_TOP_MAX / 32;
@@ -543,15 +539,24 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Returns the sum of q; top: the student's statistics of the entries (where the rest is a class).
+// The entries' part of the loss: sum q (log q - log p) = cross + mass (log S + (m - base) / tau), with base
+// the entries' largest logit, so that the sum is done before m and S are known and no large terms cancel.
+struct Entries {
+  float mass, cross, base;
+  Stats top;               // the student's statistics of the entries (where the rest is a class)
+  bool label_here;         // the label is one of them
+  unsigned edges_here;     // bit e: edge element e is one of them (asked for where the rest is a class)
+};
+
 template <typename E>
-__device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, const E* z, int label, float c, const Teacher& t,
-                                              Stats& top, bool& label_here) {
+__device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n, const Slice<E>& s, int label, float c,
+                                                const Teacher& t) {
+  const E* z = s.row;
   const int lane = threadIdx.x % 32;
   const float inv_tau = 1.0f / p.tau;
   int j[kPerLane];
   float logq[kPerLane], zk[kPerLane];
-  float most = -INFINITY;
+  float most = -INFINITY, base = -INFINITY;
   // (all loads of a kind together: their latencies overlap)
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
@@ -566,8 +571,11 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, c
     logq[e] = j[e] >= 0 ? logq[e] * inv_tau : -INFINITY;
     if (logq[e] == -INFINITY) j[e] = -1;
     most = fmaxf(most, logq[e]);
+    base = fmaxf(base, zk[e]);
   }
-  for (int i = lane; i < 1 << t.table_bits; i += 32) t.table[i] = -1;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) base = fmaxf(base, __shfl_xor_sync(~0u, base, o));
+  if (base == -INFINITY) base = 0.0f;
   float lse;
   if (p.teacher_lse) {
     lse = p.teacher_lse[n];
@@ -580,11 +588,7 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, c
       if (e * 32 < p.K && j[e] >= 0) sum += expf(logq[e] - most);
     lse = most + logf(warp_sum(sum));
   }
-  __syncwarp();
-  float mass = 0.0f;
-  bool again = false;
-  label_here = false;
-  top = no_stats();
+  Entries r = {0.0f, 0.0f, base, no_stats(), false, 0u};
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
     if (e * 32 >= p.K) continue;
@@ -593,29 +597,50 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, c
     if (j[e] >= 0) {
       logq[e] -= lse;
       q = expf(logq[e]);
-      mass += q;
-      label_here |= j[e] == label;
-      // a table of the indices seen: who finds an index there is not its first entry
-      unsigned h = table_slot(t, j[e]);
-      for (;;) {   // (at most half of the table is ever taken)
-        const int other = atomicCAS(&t.table[h], -1, j[e]);
-        if (other == -1) break;
-        if (other == j[e]) {
-          again = true;
-          break;
-        }
-        h = (h + 1) & ((1 << t.table_bits) - 1);
-      }
+      r.mass += q;
+      if (q != 0.0f) r.cross += q * (logq[e] - (zk[e] - base) * inv_tau);
+      r.label_here |= j[e] == label;
     }
     if (k < p.K) {
       t.at[k] = j[e];
       t.q[k] = q;
       t.z[k] = zk[e];
-      t.logq[k] = logq[e];
     }
   }
-  mass = warp_sum(mass);
-  label_here = __any_sync(~0u, label_here);
+  r.mass = warp_sum(r.mass);
+  r.cross = warp_sum(r.cross);
+  r.label_here = __any_sync(~0u, r.label_here);
+  // Do two entries have the same index?  All write their number to their index's place in the table;
+  // who finds another index's number there tries again with another hash, together with those that have
+  // its index, if any (they met the same).
+  __syncwarp();
+  bool again = false;
+  unsigned open = 0;   // bit e: entry e is not settled
+#pragma unroll
+  for (int e = 0; e < kPerLane; ++e) open |= unsigned(j[e] >= 0) << e;
+  unsigned odd = 2654435761u;
+  for (int round = 0; __any_sync(~0u, open); ++round, odd = odd * 0x9E3779B1u) {
+    if (round == 8) {   // (not seen: then the slow way)
+      again = true;
+      break;
+    }
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (e * 32 < p.K && (open >> e & 1)) t.table[unsigned(j[e]) * odd >> (32 - kTableBits)] = uint8_t(e * 32 + lane);
+    __syncwarp();
+    unsigned settled = 0;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e)
+      if (e * 32 < p.K && (open >> e & 1)) {
+        const int there = t.table[unsigned(j[e]) * odd >> (32 - kTableBits)];
+        if (t.at[there] == j[e]) {
+          settled |= 1u << e;
+          again |= there != e * 32 + lane;
+        }
+      }
+    open &= ~settled;
+    __syncwarp();
+  }
   if (__any_sync(~0u, again)) {
     // entries with the same index add up in the first of them; the others leave
     float sum[kPerLane];
@@ -650,20 +675,18 @@ __device__ __forceinline__ float read_teacher(const DistillArgs& p, int64_t n, c
         Stats one = no_stats();
         if (j[e] >= 0 && !(zk[e] == -INFINITY)) one = {zk[e], 1.0f, 0.0f, 1.0f};
         if (isnan(zk[e])) one = {-INFINITY, zk[e], 0.0f, zk[e]};
-        join(top, one, c);
+        join(r.top, one, c);
       }
-    top = warp_join(top, c);
+    r.top = warp_join(r.top, c);
+    for (int i = 0; i < s.edges(); ++i) {
+      bool here = false;
+#pragma unroll
+      for (int e = 0; e < kPerLane; ++e) here |= j[e] == s.edge(i);
+      r.edges_here |= unsigned(__any_sync(~0u, here)) << i;
+    }
   }
   __syncwarp();
-  return mass;
-}
-
-// Whether index j is one of the entries.
-__device__ __forceinline__ bool is_entry(const Teacher& t, int j) {
-  for (unsigned h = table_slot(t, j);; h = (h + 1) & ((1 << t.table_bits) - 1)) {   // (at least half of the table is empty)
-    const int other = t.table[h];
-    if (other == j || other == -1) return other == j;
-  }
+  return r;
 }
 
 // What the gradient of a row needs beside its elements.
@@ -821,24 +844,23 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
     const E* z = logits + n * p.ld;
     const Slice<E> s = slice_of(z, p.V, rank, C);
     const Teacher t = teacher_at(teachers, p.K, b);
-    Stats top = no_stats();
-    bool label_here = false;
+    Entries entries = {0.0f, 0.0f, 0.0f, no_stats(), false, 0u};
     const bool live = w != 0.0f;
     Stats edge = no_stats();
-    float ze = 0.0f, next_zl = 0.0f, mass = 0.0f;
+    float ze = 0.0f, next_zl = 0.0f;
     const int je = lane < s.edges() ? s.edge(lane) : -1;
     if (live) {
       if (HARD && label >= 0 && label < p.V) next_zl = to_f32(z[label]);
       if (rank == 0 && je >= 0) ze = to_f32(z[je]);
-      if (rank == 0 || tail) mass = read_teacher<E>(p, n, z, label, c, t, top, label_here);
-      if (rank == 0 && je >= 0 && !(tail && is_entry(t, je))) edge = one_element(ze);
+      if (rank == 0 || tail) entries = read_teacher<E>(p, n, s, label, c, t);
+      if (rank == 0 && je >= 0 && !(entries.edges_here >> lane & 1)) edge = one_element(ze);
     }
     if (tail) {
-      if (lane == 0) tops[b] = top;
+      if (lane == 0) tops[b] = entries.top;
       part_sync(1, T + 32);
     }
-    if (rank == 0 && lane < C) *of_block(&masses[b], lane) = mass;
-    publish_stats(edge, all[b], rank, C, parts, c);
+    if (rank == 0 && lane < C) *of_block(&masses[b], lane) = entries.mass;
+    publish_edges(edge, s.edges() > 0, all[b], rank, C, parts, c);
     cluster_arrive();
     cluster_wait();
     if (rank == 0) {
@@ -846,18 +868,14 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
       pending = live && grads;
       out = grads + n * p.grad_ld;
       last_label = label;
-      label_is_entry = label_here;
+      label_is_entry = entries.label_here;
       zl = next_zl;
       float loss = 0.0f;
       if (live) {
         const Stats rest = collect_stats(all[b], C, parts, c);
-        k = coefficients<HARD>(p, rest, top, mass, w, label, c);
-        float kl = 0.0f;
-        for (int i = lane; i < p.K; i += 32) {
-          const float logq = t.logq[i], q = expf(logq);
-          if (q != 0.0f) kl += q * (logq - ((t.z[i] - k.ref) * (1.0f / p.tau) - k.log_s));
-        }
-        loss = (1.0f - p.alpha) * p.tau * p.tau * (warp_sum(kl) + k.kl_rest);
+        k = coefficients<HARD>(p, rest, entries.top, entries.mass, w, label, c);
+        const float kl = entries.mass == 0.0f ? 0.0f : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
+        loss = (1.0f - p.alpha) * p.tau * p.tau * (kl + k.kl_rest);
         if (HARD && label >= 0)
           loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);
       }
@@ -873,36 +891,43 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
   if (rank == 0 && pending) finish(teacher_at(teachers, p.K, b ^ 1));
 }
 
-// Top K of a row on chip.  The blocks' threads are cut into G groups of neighbours; the K-th largest
-// of the groups' maxima is a bound that K elements reach, and few others do (about G ln(G / (G - K))
-// for elements in no order).  The side warps look for them in the pieces of the threads whose maximum
-// reaches it (read again, from L2) and send them to the first block, whose side warp ranks them
-// against one another.  Where more reach it than the list holds (ties, adverse orders), and in rows
-// that are not finite, that warp finds the K-th element exactly, by bisection over the row.
+// Top K of a row on chip.  Threads record the largest element of their pieces, the piece it is in, and
+// the largest of their other pieces.  They are cut into G groups of neighbours; the K-th largest of the
+// groups' maxima is a bound that K elements reach, and few others do (about G ln(G / (G - K)) for
+// elements in no order).  A block's search warp looks for them: in the recorded piece of each thread
+// whose maximum reaches the bound (read again, from L2), and in all pieces of the few whose second
+// value does.  It sends them to one block of the cluster, whose rank warp sorts them.  Where more
+// reach the bound than the list holds (ties, adverse orders), and in rows that are not finite, that warp
+// finds the K-th element exactly, by bisection over the row.
 //
 // Dynamic shared memory after the slots, twice each (rows take turns):
-//   list [entries]       first block: keys of the elements that reached the bound, a share for each block
+//   list [entries]       the block that ranks the row: keys of the elements that reached the bound, a
+//                        share for each block
 //   group_max [groups]   (the last group is the edge elements)
-//   thread_max [T]
-//   counts [C]           first block: elements of each block that reached the bound
+//   counts [C]           the block that ranks the row: elements of each block that reached the bound
+//   best, second [T]     threads' recorded values, and
+//   where [T]            their pieces
 // and owners [T].
-__host__ __device__ inline int top_entries(int K) { return K < 32 ? 128 : 4 * K; }
-inline size_t top_bytes(int K, int groups, int T) {
-  return K == 0 ? 0 : size_t(2) * top_entries(K) * 8 + (size_t(2) * (groups + T + kRowCluster) + T) * 4;
+__host__ __device__ inline int top_entries(int K) { return K < 64 ? 256 : 4 * K; }
+template <typename E>
+size_t top_bytes(int K, int groups, int T) {
+  return K == 0 ? 0 : size_t(2) * (top_entries(K) * 8 + (groups + kRowCluster) * 4 + T * (2 * sizeof(E) + 1)) + T;
 }
+template <typename E>
 struct TopShared {
   unsigned long long* lists;
-  float* floats;
   int entries, groups, T;
   __device__ TopShared(void* shared, int K, int groups, int T)
-      : lists(static_cast<unsigned long long*>(shared)), floats(reinterpret_cast<float*>(lists + 2 * top_entries(K))),
-        entries(top_entries(K)), groups(groups), T(T) {}
+      : lists(static_cast<unsigned long long*>(shared)), entries(top_entries(K)), groups(groups), T(T) {}
   __device__ unsigned long long* list(int b) const { return lists + b * entries; }
-  __device__ float* group_max(int b) const { return floats + b * (groups + T); }
-  __device__ float* thread_max(int b) const { return group_max(b) + groups; }
+  __device__ float* group_max(int b) const { return reinterpret_cast<float*>(list(2)) + b * groups; }
   __device__ int* counts(int b) const { return reinterpret_cast<int*>(group_max(2)) + b * kRowCluster; }
-  __device__ int* owners() const { return counts(2); }
+  __device__ E* best(int b) const { return reinterpret_cast<E*>(counts(2)) + 2 * b * T; }
+  __device__ E* second(int b) const { return best(b) + T; }
+  __device__ uint8_t* where(int b) const { return reinterpret_cast<uint8_t*>(best(2)) + b * T; }
+  __device__ uint8_t* owners() const { return where(2); }
 };
+static_assert(kRowThreads <= 256, "a thread's number is a byte");
 
 // Order of the alternatives in 32 bits: larger logits above, NaN above all, -0 as 0.
 __device__ __forceinline__ unsigned value_order(float v) { return unsigned(order_key(v, 0) >> 32); }
@@ -920,12 +945,20 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
     const int u = __float_as_int(v);
     return u ^ (u >> 31 & 0x7fffffff);
   };
-  int lo = INT32_MAX, hi = INT32_MIN;
-  for (int i = lane; i < G; i += 32) {
-    const int v = order(values[i]);
+  constexpr int kKept = 4;   // values of a lane in registers; there are hardly ever more
+  int kept[kKept], lo = INT32_MAX, hi = INT32_MIN;
+#pragma unroll
+  for (int e = 0; e < kKept; ++e) kept[e] = lane + 32 * e < G ? order(values[lane + 32 * e]) : INT32_MIN;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int e = 0; e < kKept; ++e)
+      if (lane + 32 * e < G) f(kept[e]);
+    for (int i = lane + 32 * kKept; i < G; i += 32) f(order(values[i]));
+  };
+  each([&](int v) {
     lo = min(lo, v);
     hi = max(hi, v);
-  }
+  });
   lo = __reduce_min_sync(~0u, lo);
   hi = __reduce_max_sync(~0u, hi);
   // K values reach lo; fewer than K reach hi + 1
@@ -933,7 +966,7 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
   while (lo < hi && reach > K + (K < 32 ? 8 : K / 4)) {
     const int mid = int((int64_t(lo) + hi + 1) >> 1);
     int n = 0;
-    for (int i = lane; i < G; i += 32) n += order(values[i]) >= mid;
+    each([&](int v) { n += v >= mid; });
     n = __reduce_add_sync(~0u, n);
     if (n >= K) {
       lo = mid;
@@ -1028,21 +1061,68 @@ __device__ __noinline__ void exact_top(const E* z, int V, int K, unsigned lo, un
   __syncwarp();
 }
 
+// Sorts 32 N keys, N a lane, descending: key e of lane l is number 32 e + l.
+template <int N>
+__device__ __forceinline__ void warp_sort(unsigned long long (&v)[N]) {
+  const int lane = threadIdx.x % 32;
+#pragma unroll
+  for (int k = 2; k <= 32 * N; k <<= 1)
+#pragma unroll
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      if (j >= 32) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const int o = e ^ (j / 32);
+          if (o > e) {
+            const bool descending = (e * 32 & k) == 0 || k == 32 * N;
+            const unsigned long long hi = v[e] > v[o] ? v[e] : v[o], lo = v[e] > v[o] ? v[o] : v[e];
+            v[e] = descending ? hi : lo;
+            v[o] = descending ? lo : hi;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const unsigned long long other = __shfl_xor_sync(~0u, v[e], j);
+          const bool descending = ((e * 32 + lane) & k) == 0 || k == 32 * N, lower = (lane & j) == 0;
+          const bool larger = descending == lower;
+          v[e] = (v[e] > other) == larger ? v[e] : other;
+        }
+      }
+    }
+}
+
+// The list's `total` keys (at most 32 N), sorted: f(rank, key) for the first K.
+template <int N, typename F>
+__device__ __forceinline__ void sorted(const unsigned long long* list, int total, int K, F f) {
+  const int lane = threadIdx.x % 32;
+  unsigned long long v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = e * 32 + lane < total ? list[e * 32 + lane] : 0ull;
+  warp_sort<N>(v);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e * 32 + lane < K) f(e * 32 + lane, v[e]);
+}
+
 template <typename E>
 __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const LogpArgs p, int64_t N, int C, int slots, int group_lanes) {
   extern __shared__ uint4 data[];
   __shared__ Stats all[2][kRowCluster * kRowParts];
   __shared__ float bounds[2];
   pdl_entry();
-  // T threads stream; then the search warp and the rank warp
+  // T threads stream; then there are the search warp and the rank warp
   const int rank = blockIdx.x % C, tid = threadIdx.x, T = blockDim.x - 64, parts = T / 32 + 1, lane = tid % 32;
   const int64_t step = gridDim.x / C;
   const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
   const E* const logits = static_cast<const E*>(p.logits);
   const int per_block = T / group_lanes, groups = per_block * C + 1;
-  const TopShared top(data + slots, p.K, groups, T);
-  const int share = top_entries(p.K) / C;
+  const TopShared<E> top(data + slots, p.K, groups, T);
+  const int share = top.entries / C;
   int64_t n = blockIdx.x / C;
+  // rows' rankings go round the cluster's blocks
+  int turn = 0;
+  auto next_turn = [&] { turn = turn + 1 == C ? 0 : turn + 1; };
   cluster_start();
 
   if (tid < T) {
@@ -1054,7 +1134,19 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
       const int next_pieces = n + step < N ? next.pieces : 0;
       load_wait();
       Stats mine = no_stats();
-      mine.m = thread_max<E>(data, s.pieces, T);
+      float second = -INFINITY;
+      int where = 0;
+      if (p.K == 0) {
+        mine.m = thread_max<E>(data, s.pieces, T);
+      } else {
+#pragma unroll 4
+        for (int i = tid, round = 0; i < s.pieces; i += T, ++round) {
+          const float m = piece_max<E>(data[i]);
+          second = fmaxf(second, fminf(mine.m, m));
+          if (m > mine.m) where = round;
+          mine.m = fmaxf(mine.m, m);
+        }
+      }
       const float m = mine.m;
       thread_sums<E, true, false, false>(data, s.pieces, T, c, mine, [&](int i) {
         if (i < next_pieces) load_piece(data + i, next.data() + i);
@@ -1067,7 +1159,9 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
       if (row > 0) cluster_wait();
       publish_stats(mine, all[b], rank, C, parts, c);
       if (p.K > 0) {
-        top.thread_max(b)[tid] = m;
+        top.best(b)[tid] = from_f32<E>(m);
+        top.second(b)[tid] = from_f32<E>(second);
+        top.where(b)[tid] = uint8_t(where);
         float g = m;
         for (int o = 1; o < group_lanes; o <<= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
         for (int k = tid % group_lanes; k < C; k += group_lanes)
@@ -1083,82 +1177,85 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
   }
 
   if (tid < T + 32) {
-    // the search warp: the edge elements' statistics, and the elements that reach a row's bound
-    for (int b = 0; n < N; n += step, b ^= 1) {
+    // the search warp: the elements that reach a row's bound (and the edge elements' statistics)
+    const unsigned below = (1u << lane) - 1;
+    for (int b = 0; n < N; n += step, b ^= 1, next_turn()) {
       const E* z = logits + n * p.ld;
       const Slice<E> s = slice_of(z, p.V, rank, C);
       const int je = rank == 0 && lane < s.edges() ? s.edge(lane) : -1;
       const float ze = je >= 0 ? to_f32(z[je]) : -INFINITY;
-      publish_stats(je >= 0 ? one_element(ze) : no_stats(), all[b], rank, C, parts, c);
+      const bool any = rank == 0 && s.edges() > 0;
+      publish_edges(je >= 0 ? one_element(ze) : no_stats(), any, all[b], rank, C, parts, c);
       if (p.K > 0 && rank == 0) {
         float g = ze;
+        if (any) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+          for (int o = 16; o > 0; o >>= 1) g = fmaxf(g, __shfl_xor_sync(~0u, g, o));
+        }
         if (lane < C) of_block(top.group_max(b), lane)[groups - 1] = g;
       }
       cluster_arrive();
       cluster_wait();
       if (p.K == 0) continue;
       const float bound = group_bound(top.group_max(b), groups, p.K);
-      if (rank == 0 && lane == 0) bounds[b] = bound;
-      unsigned long long* const to = of_block(top.list(b), 0) + rank * share;
-      const unsigned below = (1u << lane) - 1;
-      int count = 0, owners = 0;
-      {
-        const unsigned votes = __ballot_sync(~0u, je >= 0 && ze >= bound);
-        if (votes >> lane & 1) {
-          const int at = __popc(votes & below);
-          if (at < share) to[at] = order_key(ze, je);
-        }
-        count = __popc(votes);
-      }
+      if (rank == turn && lane == 0) bounds[b] = bound;
+      unsigned long long* const to = of_block(top.list(b), turn) + rank * share;
+      int count = 0;
+      auto push = [&](bool want, float v, int j) {
+        const unsigned votes = __ballot_sync(~0u, want);
+        if (votes == 0) return;
+        const int at = count + __popc(votes & below);
+        if (want && at < share) to[at] = order_key(v, j);
+        count += __popc(votes);
+      };
+      auto push_piece = [&](const uint4& w, int piece) {
+        const bool in = piece < s.pieces;
+        Vec<2> v[kPairs<E>] = {};
+        if (in) unpack<E>(w, v);
+#pragma unroll
+        for (int k = 0; k < kPer<E>; ++k) push(in && v[k / 2].v[k % 2] >= bound, v[k / 2].v[k % 2], s.index(piece) + k);
+      };
+      if (any) push(je >= 0 && ze >= bound, ze, je);
+      // the threads that have an element: a lane each
+      int owners = 0, more = 0;
+      uint8_t* const list = top.owners();
 #pragma unroll 8
       for (int t = lane; t < T; t += 32) {
-        const unsigned votes = __ballot_sync(~0u, top.thread_max(b)[t] >= bound);
-        if (votes >> lane & 1) top.owners()[owners + __popc(votes & below)] = t;
+        const bool hit = to_f32(top.best(b)[t]) >= bound;
+        const unsigned votes = __ballot_sync(~0u, hit);
+        if (hit) list[owners + __popc(votes & below)] = uint8_t(t);
         owners += __popc(votes);
       }
       __syncwarp();
-      const int each = (s.pieces + T - 1) / T, items = owners * each;
-      constexpr int kAhead = 4;
-      for (int i0 = 0; i0 < items && count <= share; i0 += 32 * kAhead) {
-        uint4 w[kAhead];
-        int piece[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          const int i = i0 + u * 32 + lane;
-          piece[u] = i < items ? top.owners()[i / each] + i % each * T : s.pieces;
-          if (piece[u] < s.pieces) w[u] = s.data()[piece[u]];
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-          // a bit for each of the piece's elements that reach the bound
-          unsigned reach = 0;
-          if (piece[u] < s.pieces && piece_max<E>(w[u]) >= bound) {
-            Vec<2> v[kPairs<E>];
-            unpack<E>(w[u], v);
-#pragma unroll
-            for (int k = 0; k < kPer<E>; ++k) reach |= unsigned(v[k / 2].v[k % 2] >= bound) << k;
-          }
-          // one element of each lane at a time: lanes rarely have one, hardly ever two
-          for (unsigned votes; (votes = __ballot_sync(~0u, reach != 0)) != 0; reach &= reach - 1) {
-            if (reach) {
-              const int k = __ffs(reach) - 1, at = count + __popc(votes & below);
-              const E x = reinterpret_cast<const E*>(s.data() + piece[u])[k];   // (in L1)
-              if (at < share) to[at] = order_key(to_f32(x), s.index(piece[u]) + k);
-            }
-            count += __popc(votes);
-          }
-        }
+      for (int o0 = 0; o0 < owners && count <= share; o0 += 32) {
+        const int t = o0 + lane < owners ? list[o0 + lane] : -1;
+        // those with elements in several pieces are taken below instead, all their pieces
+        const bool several = t >= 0 && to_f32(top.second(b)[t]) >= bound;
+        const int piece = t >= 0 && !several ? t + top.where(b)[t] * T : s.pieces;
+        uint4 w = {};
+        if (piece < s.pieces) w = s.data()[piece];
+        const unsigned votes = __ballot_sync(~0u, several);
+        if (several) list[more + __popc(votes & below)] = uint8_t(t);   // (more <= o0: read already)
+        more += __popc(votes);
+        push_piece(w, piece);
       }
-      if (lane == 0) of_block(top.counts(b), 0)[rank] = count;
+      __syncwarp();
+      const int each = (s.pieces + T - 1) / T;
+      for (int o = 0; o < more && count <= share; ++o)
+        for (int r = 0; r < each; r += 32) {
+          const int piece = r + lane < each ? list[o] + (r + lane) * T : s.pieces;
+          uint4 w = {};
+          if (piece < s.pieces) w = s.data()[piece];
+          push_piece(w, piece);
+        }
+      if (lane == 0) of_block(top.counts(b), turn)[rank] = count;
     }
     cluster_arrive();
     cluster_wait();
     return;
   }
 
-  // the rank warp: a row's values, and the alternatives of the row before it
+  // the rank warp: a row's values (the first block's), and the alternatives of the row before it
   int64_t done = -1;
   Stats r = no_stats();
   auto ranked = [&](int b) {
@@ -1169,7 +1266,7 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
     for (int k = 0; k < C; ++k) fits = fits && top.counts(b)[k] <= share;
     int total = 0;
     if (fits) {
-      // the blocks' shares moved together
+      // the shares moved together
       for (int k = 0; k < C; ++k) {
         const int count = top.counts(b)[k];
         if (k > 0)
@@ -1177,7 +1274,6 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
             const unsigned long long key = i0 + lane < count ? list[k * share + i0 + lane] : 0;
             __syncwarp();
             if (i0 + lane < count) list[total + i0 + lane] = key;
-            __syncwarp();
           }
         total += count;
       }
@@ -1187,20 +1283,30 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
                    finite ? value_order(r.m) : value_order(NAN), list, top.entries);
       total = p.K;
     }
-    for (int i = lane; i < total; i += 32) {
-      const unsigned long long key = list[i];
-      int above = 0;
+    __syncwarp();
+    auto write = [&](int k, unsigned long long key) {
+      p.top_idx[done * p.K + k] = key_index(key);
+      p.top_logp[done * p.K + k] = (key_value(key) - ref) * inv_tau - log_s;
+    };
+    if (total <= 32) {
+      sorted<1>(list, total, p.K, write);
+    } else if (total <= 64) {
+      sorted<2>(list, total, p.K, write);
+    } else if (total <= 128) {
+      sorted<4>(list, total, p.K, write);
+    } else {
+      for (int i = lane; i < total; i += 32) {
+        const unsigned long long key = list[i];
+        int above = 0;
 #pragma unroll 8
-      for (int k = 0; k < total; ++k) above += list[k] > key;
-      if (above < p.K) {
-        p.top_idx[done * p.K + above] = key_index(key);
-        p.top_logp[done * p.K + above] = (key_value(key) - ref) * inv_tau - log_s;
+        for (int k = 0; k < total; ++k) above += list[k] > key;
+        if (above < p.K) write(above, key);
       }
     }
     __syncwarp();
   };
   int b = 0;
-  for (; n < N; n += step, b ^= 1) {
+  for (; n < N; n += step, b ^= 1, next_turn()) {
     int y = -1;
     float zy = 0.0f;
     if (rank == 0 && p.logp) {
@@ -1209,17 +1315,19 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
     }
     cluster_arrive();
     cluster_wait();
-    if (rank != 0) continue;
     if (done >= 0) ranked(b ^ 1);
+    done = -1;
+    const bool mine = p.K > 0 && rank == turn;
+    if (rank != 0 && !mine) continue;
     r = collect_stats(all[b], C, parts, c);
-    if (lane == 0) {
+    if (mine) done = n;
+    if (rank == 0 && lane == 0) {
       const bool empty = r.m == -INFINITY && r.s == 0.0f;
       const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
       if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
       if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
       if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
     }
-    if (p.K > 0) done = n;
   }
   cluster_arrive();
   cluster_wait();
@@ -1378,7 +1486,7 @@ cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t st
   const int T = c.threads - 64, busy = (c.slots < T ? c.slots : T) * c.cluster;
   int lanes = 32;
   while (lanes > 1 && busy < 2 * p.K * lanes) lanes /= 2;
-  c.smem += top_bytes(p.K, T / lanes * c.cluster + 1, T);
+  c.smem += top_bytes<E>(p.K, T / lanes * c.cluster + 1, T);
   return launch_rows(token_logp_kernel<E>, c, N, stream, p, N, c.cluster, c.slots, lanes);
 }
 
