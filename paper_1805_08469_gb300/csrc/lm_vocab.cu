@@ -1061,12 +1061,13 @@ __device__ __noinline__ void exact_top(const E* z, int V, int K, unsigned lo, un
   __syncwarp();
 }
 
-// Sorts 32 N keys, N a lane, descending: key e of lane l is number 32 e + l.
-template <int N>
+// Bitonic sort of 32 N keys, N a lane, descending: key e of lane l is number 32 e + l.  The merges into
+// runs of FROM * 2, ..., TO keys, of which those of 32 N are sorted.
+template <int N, int FROM, int TO>
 __device__ __forceinline__ void warp_sort(unsigned long long (&v)[N]) {
   const int lane = threadIdx.x % 32;
 #pragma unroll
-  for (int k = 2; k <= 32 * N; k <<= 1)
+  for (int k = 2 * FROM; k <= TO; k <<= 1)
 #pragma unroll
     for (int j = k >> 1; j > 0; j >>= 1) {
       if (j >= 32) {
@@ -1074,7 +1075,7 @@ __device__ __forceinline__ void warp_sort(unsigned long long (&v)[N]) {
         for (int e = 0; e < N; ++e) {
           const int o = e ^ (j / 32);
           if (o > e) {
-            const bool descending = (e * 32 & k) == 0 || k == 32 * N;
+            const bool descending = (e * 32 & k) == 0;
             const unsigned long long hi = v[e] > v[o] ? v[e] : v[o], lo = v[e] > v[o] ? v[o] : v[e];
             v[e] = descending ? hi : lo;
             v[o] = descending ? lo : hi;
@@ -1084,25 +1085,11 @@ __device__ __forceinline__ void warp_sort(unsigned long long (&v)[N]) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
           const unsigned long long other = __shfl_xor_sync(~0u, v[e], j);
-          const bool descending = ((e * 32 + lane) & k) == 0 || k == 32 * N, lower = (lane & j) == 0;
-          const bool larger = descending == lower;
-          v[e] = (v[e] > other) == larger ? v[e] : other;
+          const bool descending = ((e * 32 + lane) & k) == 0, lower = (lane & j) == 0;
+          v[e] = (v[e] > other) == (descending == lower) ? v[e] : other;
         }
       }
     }
-}
-
-// The list's `total` keys (at most 32 N), sorted: f(rank, key) for the first K.
-template <int N, typename F>
-__device__ __forceinline__ void sorted(const unsigned long long* list, int total, int K, F f) {
-  const int lane = threadIdx.x % 32;
-  unsigned long long v[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = e * 32 + lane < total ? list[e * 32 + lane] : 0ull;
-  warp_sort<N>(v);
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (e * 32 + lane < K) f(e * 32 + lane, v[e]);
 }
 
 template <typename E>
@@ -1212,8 +1199,17 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
         const bool in = piece < s.pieces;
         Vec<2> v[kPairs<E>] = {};
         if (in) unpack<E>(w, v);
+        unsigned reach = 0;   // bit k: element k does; hardly ever two
 #pragma unroll
-        for (int k = 0; k < kPer<E>; ++k) push(in && v[k / 2].v[k % 2] >= bound, v[k / 2].v[k % 2], s.index(piece) + k);
+        for (int k = 0; k < kPer<E>; ++k) reach |= unsigned(in && v[k / 2].v[k % 2] >= bound) << k;
+        while (__any_sync(~0u, reach)) {
+          const int k = __ffs(reach) - 1;
+          float x = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kPer<E>; ++i) x = i == k ? v[i / 2].v[i % 2] : x;
+          push(reach != 0, x, s.index(piece) + k);
+          reach &= reach - 1;
+        }
       };
       if (any) push(je >= 0 && ze >= bound, ze, je);
       // the threads that have an element: a lane each
@@ -1240,13 +1236,26 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
         push_piece(w, piece);
       }
       __syncwarp();
+      // lanes side by side take the pieces of one or more of them
       const int each = (s.pieces + T - 1) / T;
-      for (int o = 0; o < more && count <= share; ++o)
-        for (int r = 0; r < each; r += 32) {
-          const int piece = r + lane < each ? list[o] + (r + lane) * T : s.pieces;
-          uint4 w = {};
-          if (piece < s.pieces) w = s.data()[piece];
-          push_piece(w, piece);
+      int bits = 0;
+      while (bits < 5 && (1 << bits) < each) ++bits;
+      const int at_once = 32 >> bits, my_owner = lane >> bits, my_piece = lane & ((1 << bits) - 1);
+      constexpr int kAhead = 4;
+      for (int o0 = 0; o0 < more && count <= share; o0 += kAhead * at_once)
+        for (int r = 0; r < each; r += 1 << bits) {
+          uint4 w[kAhead];
+          int piece[kAhead];
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u) {
+            const int o = o0 + u * at_once + my_owner;
+            piece[u] = o < more && r + my_piece < each ? list[o] + (r + my_piece) * T : s.pieces;
+            w[u] = {};
+            if (piece[u] < s.pieces) w[u] = s.data()[piece[u]];
+          }
+#pragma unroll
+          for (int u = 0; u < kAhead; ++u)
+            if (__any_sync(~0u, piece[u] < s.pieces && piece_max<E>(w[u]) >= bound)) push_piece(w[u], piece[u]);
         }
       if (lane == 0) of_block(top.counts(b), turn)[rank] = count;
     }
@@ -1255,83 +1264,119 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
     return;
   }
 
-  // the rank warp: a row's values (the first block's), and the alternatives of the row before it
-  int64_t done = -1;
+  // the rank warp: a row's values (the first block's), and the alternatives of the rows that are this
+  // block's turn.  Other blocks have theirs before its next one, so with several blocks the sort goes
+  // on over the next rows' barriers, a part after each.
+  int64_t done = -1;   // the row being ranked
   Stats r = no_stats();
-  auto ranked = [&](int b) {
+  int part = 0;
+  constexpr int kKeys = 4;   // of a lane
+  unsigned long long keys[kKeys];
+  auto write = [&](int k, unsigned long long key) {
     const bool empty = r.m == -INFINITY && r.s == 0.0f;
     const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
-    unsigned long long* list = top.list(b);
-    bool fits = !isnan(r.s);
-    for (int k = 0; k < C; ++k) fits = fits && top.counts(b)[k] <= share;
-    int total = 0;
-    if (fits) {
-      // the shares moved together
+    p.top_idx[done * p.K + k] = key_index(key);
+    p.top_logp[done * p.K + k] = (key_value(key) - ref) * inv_tau - log_s;
+  };
+  // the first part takes the keys from list b
+  auto rank_part = [&](int b) {
+    if (part == 0) {
+      unsigned long long* list = top.list(b);
+      bool fits = !isnan(r.s);
+      int total = 0;
       for (int k = 0; k < C; ++k) {
         const int count = top.counts(b)[k];
-        if (k > 0)
-          for (int i0 = 0; i0 < count; i0 += 32) {
-            const unsigned long long key = i0 + lane < count ? list[k * share + i0 + lane] : 0;
-            __syncwarp();
-            if (i0 + lane < count) list[total + i0 + lane] = key;
-          }
+        fits = fits && count <= share;
         total += count;
       }
-    } else {
-      const bool finite = !isnan(r.s);
-      exact_top<E>(logits + done * p.ld, p.V, p.K, finite ? value_order(bounds[b]) : 1u,
-                   finite ? value_order(r.m) : value_order(NAN), list, top.entries);
-      total = p.K;
-    }
-    __syncwarp();
-    auto write = [&](int k, unsigned long long key) {
-      p.top_idx[done * p.K + k] = key_index(key);
-      p.top_logp[done * p.K + k] = (key_value(key) - ref) * inv_tau - log_s;
-    };
-    if (total <= 32) {
-      sorted<1>(list, total, p.K, write);
-    } else if (total <= 64) {
-      sorted<2>(list, total, p.K, write);
-    } else if (total <= 128) {
-      sorted<4>(list, total, p.K, write);
-    } else {
-      for (int i = lane; i < total; i += 32) {
-        const unsigned long long key = list[i];
-        int above = 0;
+      // key number i of all shares one after the other, 0 past the last
+      auto key = [&](int i) {
+        if (i >= total) return 0ull;
+        int k = 0;
+        for (int count; i >= (count = top.counts(b)[k]); ++k) i -= count;
+        return list[k * share + i];
+      };
+      if (fits && total <= 32) {
+        unsigned long long one[1] = {key(lane)};
+        warp_sort<1, 1, 32>(one);
+        if (lane < p.K) write(lane, one[0]);
+        done = -1;
+      } else if (fits && total <= 32 * kKeys) {
+#pragma unroll
+        for (int e = 0; e < kKeys; ++e) keys[e] = key(e * 32 + lane);
+        warp_sort<kKeys, 1, 32>(keys);
+        part = 1;
+      } else {
+        if (fits) {
+          // the shares moved together
+          int to = top.counts(b)[0];
+          for (int k = 1; k < C; ++k) {
+            const int count = top.counts(b)[k];
+            for (int i0 = 0; i0 < count; i0 += 32) {
+              const unsigned long long key = i0 + lane < count ? list[k * share + i0 + lane] : 0;
+              __syncwarp();
+              if (i0 + lane < count) list[to + i0 + lane] = key;
+            }
+            to += count;
+          }
+        } else {
+          const bool finite = !isnan(r.s);
+          exact_top<E>(logits + done * p.ld, p.V, p.K, finite ? value_order(bounds[b]) : 1u,
+                       finite ? value_order(r.m) : value_order(NAN), list, top.entries);
+          total = p.K;
+        }
+        __syncwarp();
+        for (int i = lane; i < total; i += 32) {
+          const unsigned long long key = list[i];
+          int above = 0;
 #pragma unroll 8
-        for (int k = 0; k < total; ++k) above += list[k] > key;
-        if (above < p.K) write(above, key);
+          for (int k = 0; k < total; ++k) above += list[k] > key;
+          if (above < p.K) write(above, key);
+        }
+        __syncwarp();
+        done = -1;
       }
+    } else if (part == 1) {
+      warp_sort<kKeys, 32, 64>(keys);
+      part = 2;
+    } else {
+      warp_sort<kKeys, 64, 128>(keys);
+#pragma unroll
+      for (int e = 0; e < kKeys; ++e)
+        if (e * 32 + lane < p.K) write(e * 32 + lane, keys[e]);
+      part = 0;
+      done = -1;
     }
-    __syncwarp();
   };
-  int b = 0;
-  for (; n < N; n += step, b ^= 1, next_turn()) {
+  for (int b = 0;; n += step, b ^= 1, next_turn()) {
+    const bool live = n < N, mine = live && p.K > 0 && rank == turn;
     int y = -1;
     float zy = 0.0f;
-    if (rank == 0 && p.logp) {
+    if (live && rank == 0 && p.logp) {
       y = p.tokens[n];
       if (y >= 0 && y < p.V) zy = to_f32(logits[n * p.ld + y]);
     }
     cluster_arrive();
     cluster_wait();
-    if (done >= 0) ranked(b ^ 1);
-    done = -1;
-    const bool mine = p.K > 0 && rank == turn;
+    while (done >= 0) {
+      rank_part(b ^ 1);
+      if (live && !mine) break;   // the next part after the next row
+    }
+    if (!live) return;
     if (rank != 0 && !mine) continue;
-    r = collect_stats(all[b], C, parts, c);
-    if (mine) done = n;
+    const Stats now = collect_stats(all[b], C, parts, c);
+    if (mine) {
+      done = n;
+      r = now;
+    }
     if (rank == 0 && lane == 0) {
-      const bool empty = r.m == -INFINITY && r.s == 0.0f;
-      const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
-      if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
+      const bool empty = now.m == -INFINITY && now.s == 0.0f;
+      const float ref = now.m == -INFINITY ? 0.0f : now.m, log_s = empty ? 0.0f : logf(now.s);
+      if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - now.e / now.s * (1.0f / kLog2e);
       if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
       if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
     }
   }
-  cluster_arrive();
-  cluster_wait();
-  if (done >= 0) ranked(b ^ 1);
 }
 
 // ---- gradient of log probability and entropy: one pass over a row's pieces, cut over blocks ----
