@@ -586,16 +586,22 @@ Cut cut(const GlrArgs& p, int V) {
   return c;
 }
 
-template <typename E, int V, Mode MODE>
-cudaError_t launch_tiles(const GlrArgs& p, bool lerp, bool backward, cudaStream_t stream) {
+template <typename E, int V, Mode MODE, bool LERP>
+cudaError_t launch_tiles(const GlrArgs& p, bool backward, cudaStream_t stream) {
   const Cut c = cut(p, V);
-  auto* kernel = backward ? (lerp ? glr_backward_kernel<E, V, MODE, true> : glr_backward_kernel<E, V, MODE, false>)
-                          : (lerp ? glr_forward_kernel<E, V, MODE, true> : glr_forward_kernel<E, V, MODE, false>);
   const size_t smem = size_t(c.warps) * kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2) +
                       (c.cluster > 1 ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
-  const cudaError_t e = allow_smem(kernel, smem);
+  constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP>;
+  constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP>;
+  const cudaError_t e = backward ? allow_shared<kBackward>(smem) : allow_shared<kForward>(smem);
   if (e != cudaSuccess) return e;
-  return launch_cluster_pdl(kernel, unsigned(c.blocks), unsigned(c.warps * 32), unsigned(c.cluster), smem, stream, p, c.cluster);
+  return launch_cluster_pdl(backward ? kBackward : kForward, unsigned(c.blocks), unsigned(c.warps * 32), unsigned(c.cluster), smem,
+                            stream, p, c.cluster);
+}
+
+template <typename E, int V, Mode MODE>
+cudaError_t launch_tiles(const GlrArgs& p, bool lerp, bool backward, cudaStream_t stream) {
+  return lerp ? launch_tiles<E, V, MODE, true>(p, backward, stream) : launch_tiles<E, V, MODE, false>(p, backward, stream);
 }
 
 template <typename E>

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -103,11 +104,23 @@ constexpr int64_t kMaxStride = int64_t(1) << 46;
 
 inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 
-// Lets a kernel be launched with this much dynamic shared memory (48 KB together with its static
-// shared memory, of which these kernels have up to 16 KB, need no permission).
-template <typename Kernel>
-cudaError_t allow_smem(Kernel* kernel, size_t bytes) {
-  return bytes <= 32 << 10 ? cudaSuccess : cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(bytes));
+// Most dynamic shared memory of a block of these kernels (their static shared memory is below 5 KB).
+constexpr size_t kMaxShared = 222 << 10;
+
+// Lets a kernel be launched with up to kMaxShared of dynamic shared memory.  Asked of the runtime once
+// for each kernel (KERNEL keeps one flag for each) and device.
+template <auto KERNEL>
+cudaError_t allow_shared(size_t bytes) {
+  if (bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
+  static std::atomic<uint64_t> allowed{0};
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (device & 63);
+  if (device < 64 && (allowed.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxShared));
+  if (e == cudaSuccess && device < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 // launch_pdl for a grid of clusters of `cluster` blocks.

@@ -1453,7 +1453,7 @@ struct RowCut {
 };
 
 RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
-  constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 200 << 10;
+  constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 192 << 10;
   const int64_t bytes = V * dtype_size(dtype);
   RowCut c = {1, kRowThreads, 0, 0};
   while (c.cluster < kRowCluster && bytes > kSlice * c.cluster) c.cluster *= 2;
@@ -1466,9 +1466,8 @@ RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
   return c;
 }
 
-// Clusters of a kernel that the GPU holds at once.
-template <typename Kernel>
-cudaError_t resident_clusters(Kernel* kernel, const RowCut& c, int* clusters) {
+// Clusters of a kernel that the GPU holds at once (asked of the runtime once for each shape).
+cudaError_t resident_clusters(const void* kernel, const RowCut& c, int* clusters) {
   struct Known {
     const void* kernel;
     int device, cluster, threads, clusters;
@@ -1480,10 +1479,9 @@ cudaError_t resident_clusters(Kernel* kernel, const RowCut& c, int* clusters) {
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
-  const void* key = reinterpret_cast<const void*>(kernel);
   std::lock_guard<std::mutex> lock(mutex);
   for (const Known& k : known)
-    if (k.kernel == key && k.device == device && k.cluster == c.cluster && k.threads == c.threads && k.smem == c.smem) {
+    if (k.kernel == kernel && k.device == device && k.cluster == c.cluster && k.threads == c.threads && k.smem == c.smem) {
       *clusters = k.clusters;
       return cudaSuccess;
     }
@@ -1500,18 +1498,18 @@ cudaError_t resident_clusters(Kernel* kernel, const RowCut& c, int* clusters) {
   e = cudaOccupancyMaxActiveClusters(clusters, kernel, &cfg);
   if (e != cudaSuccess) return e;
   if (*clusters < 1) return cudaErrorInvalidConfiguration;
-  known[count++ % 32] = {key, device, c.cluster, c.threads, *clusters, c.smem};
+  known[count++ % 32] = {kernel, device, c.cluster, c.threads, *clusters, c.smem};
   return cudaSuccess;
 }
 
-template <typename... KArgs, typename... Args>
-cudaError_t launch_rows(void (*kernel)(KArgs...), const RowCut& c, int64_t N, cudaStream_t stream, Args... args) {
-  cudaError_t e = allow_smem(kernel, c.smem);
+template <auto KERNEL, typename... Args>
+cudaError_t launch_rows(const RowCut& c, int64_t N, cudaStream_t stream, const Args&... args) {
+  cudaError_t e = allow_shared<KERNEL>(c.smem);
   int clusters = 0;
-  if (e == cudaSuccess) e = resident_clusters(kernel, c, &clusters);
+  if (e == cudaSuccess) e = resident_clusters(reinterpret_cast<const void*>(KERNEL), c, &clusters);
   if (e != cudaSuccess) return e;
   const int64_t grid = (N < clusters ? N : clusters) * c.cluster;
-  return launch_cluster_pdl(kernel, unsigned(grid), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
+  return launch_cluster_pdl(KERNEL, unsigned(grid), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
 }
 
 template <typename E>
@@ -1519,8 +1517,8 @@ cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStrea
   RowCut c = row_cut(dtype, N, p.V, p.K, 1);
   if (c.cluster == 0) return launch_pdl(distill_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   c.smem += teacher_bytes(p.K);
-  return p.alpha > 0.0f ? launch_rows(distill_kernel<E, true>, c, N, stream, p, N, c.cluster, c.slots)
-                        : launch_rows(distill_kernel<E, false>, c, N, stream, p, N, c.cluster, c.slots);
+  return p.alpha > 0.0f ? launch_rows<distill_kernel<E, true>>(c, N, stream, p, N, c.cluster, c.slots)
+                        : launch_rows<distill_kernel<E, false>>(c, N, stream, p, N, c.cluster, c.slots);
 }
 
 template <typename E>
@@ -1532,7 +1530,7 @@ cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t st
   int lanes = 32;
   while (lanes > 1 && busy < 2 * p.K * lanes) lanes /= 2;
   c.smem += top_bytes<E>(p.K, T / lanes * c.cluster + 1, T);
-  return launch_rows(token_logp_kernel<E>, c, N, stream, p, N, c.cluster, c.slots, lanes);
+  return launch_rows<token_logp_kernel<E>>(c, N, stream, p, N, c.cluster, c.slots, lanes);
 }
 
 template <typename E>

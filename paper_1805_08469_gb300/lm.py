@@ -17,11 +17,17 @@ GEM_GLR_CHUNK = 16
 GEM_TOP_MAX = 256
 
 _DTYPES = {torch.float32: GEM_F32, torch.bfloat16: GEM_BF16, torch.float16: GEM_F16}
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+
+# The current stream's address; where torch offers it without building a Stream object (3 us), that way.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream) -> int:
+def _stream(stream, device) -> int:
     if stream is None:
-        stream = torch.cuda.current_stream()
+        if _raw_stream is not None:
+            return _raw_stream(device.index)
+        stream = torch.cuda.current_stream(device)
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -32,13 +38,13 @@ def _dtype(t, what: str) -> int:
     return d
 
 
-def _dense(t, what: str, dtype, *shape) -> int:
+def _dense(t, what: str, dtype, shape) -> int:
     """Address of an optional contiguous CUDA tensor of this type and shape."""
     if t is None:
         return 0
     if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{what}: expected a contiguous {dtype} CUDA tensor")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{what}: expected the shape {shape}, got {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -55,14 +61,14 @@ def _seq(t, what: str, like):
     return GemSeq(t.data_ptr(), sb, st)
 
 
-def _rows(t, what: str) -> int:
-    """Row pitch of a [N, V] tensor with contiguous rows."""
+def _rows(t, what: str):
+    """N, V and the row pitch of a [N, V] tensor with contiguous rows."""
     if t.dim() != 2:
         raise ValueError(f"{what}: expected a [N, V] tensor")
-    ld, one = t.stride()
-    if one != 1 and t.shape[1] > 1:
+    (N, V), (ld, one) = t.shape, t.stride()
+    if one != 1 and V > 1:
         raise TypeError(f"{what}: the rows must be contiguous")
-    return ld if t.shape[0] > 1 else max(ld, t.shape[1])
+    return N, V, ld if N > 1 or ld > V else V
 
 
 def _grad_rows(grad, logits) -> int:
@@ -70,7 +76,7 @@ def _grad_rows(grad, logits) -> int:
         raise TypeError(f"grad: expected a {logits.dtype} CUDA tensor")
     if grad.shape != logits.shape:
         raise ValueError(f"grad: expected the shape {tuple(logits.shape)}, got {tuple(grad.shape)}")
-    return _rows(grad, "grad")
+    return _rows(grad, "grad")[2]
 
 
 def gem_glr_saved_count(B: int, T: int, D: int) -> int:
@@ -78,11 +84,11 @@ def gem_glr_saved_count(B: int, T: int, D: int) -> int:
 
 
 def _reset(t, B, T) -> int:
-    return _dense(t.view(torch.uint8) if t is not None and t.dtype is torch.bool else t, "reset", torch.uint8, B, T)
+    return _dense(t.view(torch.uint8) if t is not None and t.dtype is torch.bool else t, "reset", _U8, (B, T))
 
 
 def _saved(t, B, T, D):
-    return _dense(t, "saved", torch.float32, B, -(-T // GEM_GLR_CHUNK), D)
+    return _dense(t, "saved", _F32, (B, -(-T // GEM_GLR_CHUNK), D))
 
 
 def gem_glr_forward(x, f, h, *, form: int = GEM_GLR_LERP, h0=None, lengths=None, reset=None,
@@ -94,10 +100,10 @@ def gem_glr_forward(x, f, h, *, form: int = GEM_GLR_LERP, h0=None, lengths=None,
     B, T, D = x.shape
     check(lib().gem_glr_forward(
         _dtype(x, "x"), form, B, T, D, _seq(x, "x", x), _seq(f, "f", x),
-        _dense(h0, "h0", torch.float32, B, D), _dense(lengths, "lengths", torch.int32, B),
+        _dense(h0, "h0", _F32, (B, D)), _dense(lengths, "lengths", _I32, (B,)),
         _reset(reset, B, T), _seq(h, "h", x),
-        _dense(h_last, "h_last", torch.float32, B, D), _saved(saved, B, T, D),
-        _stream(stream)), "gem_glr_forward")
+        _dense(h_last, "h_last", _F32, (B, D)), _saved(saved, B, T, D),
+        _stream(stream, x.device)), "gem_glr_forward")
 
 
 def gem_glr_backward(x, f, saved, dh, dx, df, *, form: int = GEM_GLR_LERP, lengths=None,
@@ -109,10 +115,10 @@ def gem_glr_backward(x, f, saved, dh, dx, df, *, form: int = GEM_GLR_LERP, lengt
     B, T, D = x.shape
     check(lib().gem_glr_backward(
         _dtype(x, "x"), form, B, T, D, _seq(x, "x", x), _seq(f, "f", x),
-        _dense(lengths, "lengths", torch.int32, B), _reset(reset, B, T),
+        _dense(lengths, "lengths", _I32, (B,)), _reset(reset, B, T),
         _saved(saved, B, T, D), _seq(dh, "dh", x),
-        _dense(dh_last, "dh_last", torch.float32, B, D), _seq(dx, "dx", x), _seq(df, "df", x),
-        _dense(dh0, "dh0", torch.float32, B, D), _stream(stream)), "gem_glr_backward")
+        _dense(dh_last, "dh_last", _F32, (B, D)), _seq(dx, "dx", x), _seq(df, "df", x),
+        _dense(dh0, "dh0", _F32, (B, D)), _stream(stream, x.device)), "gem_glr_backward")
 
 
 def gem_distill(logits, top_idx, top_logits, loss, grad=None, *, teacher_lse=None, labels=None,
@@ -120,47 +126,44 @@ def gem_distill(logits, top_idx, top_logits, loss, grad=None, *, teacher_lse=Non
     """logits and grad [N, V] (rows contiguous; grad may be logits or None); top_idx [N, K]
     int32 and top_logits [N, K] float32; loss, teacher_lse, row_scale [N] float32; labels [N]
     int32."""
-    ld = _rows(logits, "logits")
-    N, V = logits.shape
+    N, V, ld = _rows(logits, "logits")
     K = top_idx.shape[1]
     check(lib().gem_distill(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld, K,
-        _dense(top_idx, "top_idx", torch.int32, N, K),
-        _dense(top_logits, "top_logits", torch.float32, N, K),
-        _dense(teacher_lse, "teacher_lse", torch.float32, N),
-        _dense(labels, "labels", torch.int32, N),
-        _dense(row_scale, "row_scale", torch.float32, N), temperature, alpha,
-        _dense(loss, "loss", torch.float32, N), 0 if grad is None else grad.data_ptr(),
-        V if grad is None else _grad_rows(grad, logits), _stream(stream)), "gem_distill")
+        _dense(top_idx, "top_idx", _I32, (N, K)),
+        _dense(top_logits, "top_logits", _F32, (N, K)),
+        _dense(teacher_lse, "teacher_lse", _F32, (N,)),
+        _dense(labels, "labels", _I32, (N,)),
+        _dense(row_scale, "row_scale", _F32, (N,)), temperature, alpha,
+        _dense(loss, "loss", _F32, (N,)), 0 if grad is None else grad.data_ptr(),
+        V if grad is None else _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_distill")
 
 
 def gem_token_logp(logits, tokens=None, logp=None, entropy=None, *, temperature: float = 1.0,
                    lse=None, top_idx=None, top_logp=None, stream=None) -> None:
     """logits [N, V] (rows contiguous); tokens [N] int32; logp, entropy, lse [N] float32;
     top_idx [N, K] int32 and top_logp [N, K] float32 (both or neither)."""
-    ld = _rows(logits, "logits")
-    N, V = logits.shape
+    N, V, ld = _rows(logits, "logits")
     if (top_idx is None) != (top_logp is None):
         raise ValueError("top_idx and top_logp come together")
     K = 0 if top_idx is None else top_idx.shape[1]
     check(lib().gem_token_logp(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld,
-        _dense(tokens, "tokens", torch.int32, N), temperature, K,
-        _dense(logp, "logp", torch.float32, N), _dense(entropy, "entropy", torch.float32, N),
-        _dense(lse, "lse", torch.float32, N), _dense(top_idx, "top_idx", torch.int32, N, K),
-        _dense(top_logp, "top_logp", torch.float32, N, K), _stream(stream)), "gem_token_logp")
+        _dense(tokens, "tokens", _I32, (N,)), temperature, K,
+        _dense(logp, "logp", _F32, (N,)), _dense(entropy, "entropy", _F32, (N,)),
+        _dense(lse, "lse", _F32, (N,)), _dense(top_idx, "top_idx", _I32, (N, K)),
+        _dense(top_logp, "top_logp", _F32, (N, K)), _stream(stream, logits.device)), "gem_token_logp")
 
 
 def gem_token_logp_grad(logits, tokens, lse, entropy, dlogp, dentropy, grad, *,
                         temperature: float = 1.0, stream=None) -> None:
     """grad [N, V] (may be logits) from dlogp, dentropy [N] float32 (either may be None) with
     lse and entropy [N] as gem_token_logp wrote them."""
-    ld = _rows(logits, "logits")
-    N, V = logits.shape
+    N, V, ld = _rows(logits, "logits")
     check(lib().gem_token_logp_grad(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld,
-        _dense(tokens, "tokens", torch.int32, N), temperature,
-        _dense(lse, "lse", torch.float32, N), _dense(entropy, "entropy", torch.float32, N),
-        _dense(dlogp, "dlogp", torch.float32, N),
-        _dense(dentropy, "dentropy", torch.float32, N), grad.data_ptr(),
-        _grad_rows(grad, logits), _stream(stream)), "gem_token_logp_grad")
+        _dense(tokens, "tokens", _I32, (N,)), temperature,
+        _dense(lse, "lse", _F32, (N,)), _dense(entropy, "entropy", _F32, (N,)),
+        _dense(dlogp, "dlogp", _F32, (N,)),
+        _dense(dentropy, "dentropy", _F32, (N,)), grad.data_ptr(),
+        _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_token_logp_grad")
