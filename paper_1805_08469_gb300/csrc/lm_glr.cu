@@ -132,17 +132,85 @@ __device__ __forceinline__ Map<V> compose(const Map<V>& sofar, const Map<V>& m) 
   return r;
 }
 
+// The exchange of the blocks' maps in a cluster: each block sends its map to every block with stores
+// that count their bytes on the receiver's mbarrier, so nothing else (a cluster barrier would wait for
+// all of a block's stores to memory) holds the round up.
+struct Exchange {
+  uint32_t full;   // shared address of two mbarriers, one for each parity of the round
+  bool gave_up;    // a wait passed its limit: the states are NaN from there on
+};
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ uint32_t in_block(uint32_t address, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
+  return r;
+}
+
+template <int V>
+__device__ __forceinline__ void send(uint32_t to, const Map<V>& m, uint32_t mbarrier) {
+  if constexpr (V == 2)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
+                 "r"(__float_as_uint(m.A.v[0])), "r"(__float_as_uint(m.A.v[1])), "r"(__float_as_uint(m.H.v[0])),
+                 "r"(__float_as_uint(m.H.v[1])), "r"(mbarrier)
+                 : "memory");
+  else
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to),
+                 "r"(__float_as_uint(m.A.v[0])), "r"(__float_as_uint(m.H.v[0])), "r"(mbarrier)
+                 : "memory");
+}
+
+// Waits until the phase of this parity is complete; false after two seconds (it never takes
+// microseconds unless a block of the cluster is gone).
+__device__ __forceinline__ bool wait_phase(uint32_t mbarrier, uint32_t parity) {
+  uint64_t start = 0;
+  for (unsigned i = 1;; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(mbarrier), "r"(parity)
+        : "memory");
+    if (done) return true;
+    if (i % 256 == 0) {
+      uint64_t now;
+      asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+      if (start == 0)
+        start = now;
+      else if (now - start > 2000000000ull)
+        return false;
+    }
+  }
+}
+
+// Sets the mbarriers up; all threads call.  No block sends before all have.
+template <bool CLUSTER>
+__device__ __forceinline__ Exchange start_exchange(uint64_t (&mbarriers)[2]) {
+  Exchange x = {shared_address(mbarriers), false};
+  if constexpr (CLUSTER) {
+    if (threadIdx.x == 0) {
+      for (int b = 0; b < 2; ++b) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(x.full + 8 * b) : "memory");
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cg::this_cluster().sync();
+  }
+  return x;
+}
+
 // From every thread's map of a round: the state before the thread's chunk, and `state` moved on to
 // the state after the round.  maps: [2][kMaxWarps][32], blocks: [2][C][32] (C > 1) in shared memory.
-template <int V, bool RESETS>
+template <int V, bool RESETS, bool CLUSTER>
 __device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int warps, int rank, int C, Map<V>* maps, Map<V>* blocks,
-                                             Vec<V>& state) {
+                                             Exchange& x, Vec<V>& state) {
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   Map<V>* buf = maps + (round & 1) * kMaxWarps * 32 + lane;
   Vec<V> before = state;
   buf[warp * 32] = own;
   __syncthreads();
-  if (C == 1) {
+  if constexpr (!CLUSTER) {
 #pragma unroll
     for (int w = 0; w < kMaxWarps; ++w) {
       if (w >= warps) break;
@@ -158,13 +226,21 @@ __device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int w
     if (w == warp) mine = all;
     all = compose<V, RESETS>(all, buf[w * 32]);
   }
-  cg::cluster_group cluster = cg::this_cluster();
-  Map<V>* out = blocks + (round & 1) * C * 32 + lane;
-  for (int c = warp; c < C; c += warps) cluster.map_shared_rank(out, c)[rank * 32] = all;
-  cluster.sync();
+  // (a buffer is sent to again two rounds on: by then all have read it, or their maps of the round
+  // between would not have come)
+  Map<V>* in = blocks + (round & 1) * C * 32 + lane;
+  const uint32_t full = x.full + 8 * (round & 1), slot = shared_address(in + rank * 32);
+  for (int c = warp; c < C; c += warps) send<V>(in_block(slot, c), all, in_block(full, c));
+  if (threadIdx.x == 0)
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full), "r"(uint32_t(C * 32 * sizeof(Map<V>)))
+                 : "memory");
+  if (!x.gave_up && !wait_phase(full, uint32_t(round >> 1) & 1u)) {
+    x.gave_up = true;
+    state = splat<V>(NAN);
+  }
   for (int c = 0; c < C; ++c) {
     if (c == rank) before = state;
-    state = apply<V, RESETS>(state, out[c * 32]);
+    state = apply<V, RESETS>(state, in[c * 32]);
   }
   return apply<V, RESETS>(before, mine);
 }
@@ -347,11 +423,14 @@ __device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, con
 
 constexpr int kForwardStages = 3;
 
-template <typename E, int V, Mode MODE, bool LERP>
-__global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const GlrArgs p, int C) {
+template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER>
+__global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const GlrArgs p, int blocks_of_cluster) {
+  const int C = CLUSTER ? blocks_of_cluster : 1;
   extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
+  __shared__ uint64_t mbarriers[2];
   pdl_entry();
+  Exchange exchange = start_exchange<CLUSTER>(mbarriers);
   const Place w = place_of<E, V, MODE>(p, C);
   constexpr int kStage = 2 * kTile;
   uint32_t* const ring = tiles + w.warp * kForwardStages * kStage;
@@ -398,8 +477,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
     Vec<V> a[kChunk], u[kChunk];
     const Map<V> own = plain ? forward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u)
                              : forward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u);
-    const Vec<V> h = resets ? scan_round<V, true>(own, round, w.warps, w.rank, C, maps, blocks, state)
-                            : scan_round<V, false>(own, round, w.warps, w.rank, C, maps, blocks, state);
+    const Vec<V> h = resets ? scan_round<V, true, CLUSTER>(own, round, w.warps, w.rank, C, maps, blocks, exchange, state)
+                            : scan_round<V, false, CLUSTER>(own, round, w.warps, w.rank, C, maps, blocks, exchange, state);
     if (!busy) continue;
     if (p.saved_out && w.on) {
       float* s = p.saved_out + (w.b * all_chunks + c) * p.D + w.d;
@@ -412,8 +491,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
       forward_apply<E, V, false>(tile + w.lane, fresh, a, u, h);
     store_tile<E, MODE>(tile, h_out + t0 * p.h.stride_t, p.h.stride_t, m, w.lane, w.moves);
   }
-  // all have read h0 before it is replaced (rounds have barriers of their own)
-  if (rounds == 0) C == 1 ? __syncthreads() : cg::this_cluster().sync();
+  // all have read h0 before it is replaced, and no block leaves before what the others sent it
+  CLUSTER ? cg::this_cluster().sync() : __syncthreads();
   if (!w.on) return;
   // past the sequence's end: zeros, and the state as it stays
   store_zeros<E, V>(at<E>(p.h, w.b, 0, w.d), p.h.stride_t, n + first, per_round, p.T);
@@ -431,10 +510,14 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
 // after it hands back.  A chunk's map is sum_k (a_0 .. a_k) dh_k + (a_0 .. a_15) g, so it is
 // composed in the same pass over the steps that computes the states before them again, from the
 // saved one; nothing counts from the first reset on.  q: what the gate's gradient multiplies,
-// h_{t-1} - x_t or h_{t-1}.
+// h_{t-1} - x_t or h_{t-1}.  The gates are kept in registers for one channel a thread; for two they would
+// take 64 (and spilled: 173 us instead of 116 at 8 x 4096 x 2048 bf16), and are computed again.
+template <int V>
+constexpr int kKeep = V == 1 ? kChunk : 1;
+
 template <typename E, int V, bool LERP, bool PLAIN>
 __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
-                                               Vec<V> h, Vec<V> (&q)[kChunk]) {
+                                               Vec<V> h, Vec<V> (&q)[kChunk], Vec<V> (&gates)[2][kKeep<V>]) {
   Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
   bool counts = true;
 #pragma unroll
@@ -448,6 +531,10 @@ __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t
     if (r) h = splat<V>(0.0f);
     q[k] = LERP ? h - xv : h;
     h = r ? u : fma<V>(a, h, u);
+    if constexpr (V == 1) {
+      gates[0][k] = a;
+      gates[1][k] = b;
+    }
     if (r) counts = false;
     if (counts) {
       own.A = own.A * a;
@@ -460,14 +547,18 @@ __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t
 
 template <typename E, int V, bool LERP, bool PLAIN>
 __device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const uint32_t* dh, int m, uint32_t fresh,
-                                               const Vec<V> (&q)[kChunk], Vec<V> g) {
+                                               const Vec<V> (&q)[kChunk], const Vec<V> (&gates)[2][kKeep<V>], Vec<V> g) {
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
     if (!PLAIN && k >= m) continue;
     g = g + unpack<E, V>(dh[k * 32]);
-    // the gate again from f (its slot is df's): kept, it would take 64 registers
     Vec<V> a, b;
-    gate<E, V>(unpack<E, V>(df[k * 32]), a, b);
+    if constexpr (V == 1) {
+      a = gates[0][k];
+      b = gates[1][k];
+    } else {
+      gate<E, V>(unpack<E, V>(df[k * 32]), a, b);   // again from f (its slot is df's)
+    }
     dx[k * 32] = pack<E, V>(LERP ? b * g : g);
     g = a * g;
     df[k * 32] = pack<E, V>(g * (q[k] * b));
@@ -477,11 +568,14 @@ __device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const
 
 constexpr int kBackwardStages = 2;
 
-template <typename E, int V, Mode MODE, bool LERP>
-__global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const GlrArgs p, int C) {
+template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER>
+__global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const GlrArgs p, int blocks_of_cluster) {
+  const int C = CLUSTER ? blocks_of_cluster : 1;
   extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f, dh][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
+  __shared__ uint64_t mbarriers[2];
   pdl_entry();
+  Exchange exchange = start_exchange<CLUSTER>(mbarriers);
   const Place w = place_of<E, V, MODE>(p, C);
   constexpr int kStage = 3 * kTile;
   uint32_t* const ring = tiles + w.warp * kBackwardStages * kStage;
@@ -540,22 +634,22 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     uint32_t* const tile = ring + stage * kStage;
     const uint32_t* const dhs = tile + 2 * kTile + w.lane;
     stage = stage == kBackwardStages - 1 ? 0 : stage + 1;
-    Vec<V> q[kChunk];
+    Vec<V> q[kChunk], gates[2][kKeep<V>];
     const Vec<V> h = saved;
     load_saved(round + 1);
-    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q)
-                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q);
-    const Vec<V> g = resets ? scan_round<V, true>(own, round, w.warps, w.rank, C, maps, blocks, state)
-                            : scan_round<V, false>(own, round, w.warps, w.rank, C, maps, blocks, state);
+    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q, gates)
+                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q, gates);
+    const Vec<V> g = resets ? scan_round<V, true, CLUSTER>(own, round, w.warps, w.rank, C, maps, blocks, exchange, state)
+                            : scan_round<V, false, CLUSTER>(own, round, w.warps, w.rank, C, maps, blocks, exchange, state);
     if (!busy) continue;
     if (plain)
-      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, g);
+      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, gates, g);
     else
-      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, g);
+      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, gates, g);
     store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves);
     store_tile<E, MODE>(tile + kTile, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves);
   }
-  if (rounds == 0) C == 1 ? __syncthreads() : cg::this_cluster().sync();
+  CLUSTER ? cg::this_cluster().sync() : __syncthreads();
   if (!w.on) return;
   store_zeros<E, V>(at<E>(p.dx, w.b, 0, w.d), p.dx.stride_t, n + first, per_round, p.T);
   store_zeros<E, V>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T);
@@ -586,22 +680,28 @@ Cut cut(const GlrArgs& p, int V) {
   return c;
 }
 
-template <typename E, int V, Mode MODE, bool LERP>
-cudaError_t launch_tiles(const GlrArgs& p, bool backward, cudaStream_t stream) {
-  const Cut c = cut(p, V);
+template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER>
+cudaError_t launch_cut(const GlrArgs& p, const Cut& c, bool backward, cudaStream_t stream) {
   const size_t smem = size_t(c.warps) * kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2) +
-                      (c.cluster > 1 ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
-  constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP>;
-  constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP>;
+                      (CLUSTER ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
+  constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, CLUSTER>;
+  constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, CLUSTER>;
   const cudaError_t e = backward ? allow_shared<kBackward>(smem) : allow_shared<kForward>(smem);
   if (e != cudaSuccess) return e;
   return launch_cluster_pdl(backward ? kBackward : kForward, unsigned(c.blocks), unsigned(c.warps * 32), unsigned(c.cluster), smem,
                             stream, p, c.cluster);
 }
 
+template <typename E, int V, Mode MODE, bool LERP>
+cudaError_t launch_form(const GlrArgs& p, bool backward, cudaStream_t stream) {
+  const Cut c = cut(p, V);
+  return c.cluster > 1 ? launch_cut<E, V, MODE, LERP, true>(p, c, backward, stream)
+                       : launch_cut<E, V, MODE, LERP, false>(p, c, backward, stream);
+}
+
 template <typename E, int V, Mode MODE>
 cudaError_t launch_tiles(const GlrArgs& p, bool lerp, bool backward, cudaStream_t stream) {
-  return lerp ? launch_tiles<E, V, MODE, true>(p, backward, stream) : launch_tiles<E, V, MODE, false>(p, backward, stream);
+  return lerp ? launch_form<E, V, MODE, true>(p, backward, stream) : launch_form<E, V, MODE, false>(p, backward, stream);
 }
 
 template <typename E>

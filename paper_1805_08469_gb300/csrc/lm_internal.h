@@ -104,13 +104,15 @@ constexpr int64_t kMaxStride = int64_t(1) << 46;
 
 inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 
-// Most dynamic shared memory of a block of these kernels (their static shared memory is below 5 KB).
-constexpr size_t kMaxShared = 222 << 10;
+// Most dynamic shared memory of a block of these kernels: 227 KB less their static shared memory (up to
+// 8.3 KB).
+constexpr size_t kMaxShared = 216 << 10;
 
 // Lets a kernel be launched with up to kMaxShared of dynamic shared memory.  Asked of the runtime once
 // for each kernel (KERNEL keeps one flag for each) and device.
 template <auto KERNEL>
 cudaError_t allow_shared(size_t bytes) {
+  if (bytes > kMaxShared) return cudaErrorInvalidValue;
   if (bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
   static std::atomic<uint64_t> allowed{0};
   int device = 0;

@@ -1453,7 +1453,7 @@ struct RowCut {
 };
 
 RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
-  constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 192 << 10;
+  constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 188 << 10;
   const int64_t bytes = V * dtype_size(dtype);
   RowCut c = {1, kRowThreads, 0, 0};
   while (c.cluster < kRowCluster && bytes > kSlice * c.cluster) c.cluster *= 2;
