@@ -104,7 +104,7 @@ constexpr int64_t kStepT = 2;   // longest call of the kernel above (one chunk: 
 // an infinity would not).
 
 constexpr int kMaxWarps = 8;
-constexpr int kMaxCluster = 8;
+constexpr int kMaxCluster = 16;   // (more than 8 blocks are for this GPU only)
 
 template <int V>
 struct Map {
@@ -660,43 +660,38 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
 }
 
 // How the work is cut.  About 16 warps fit an SM (128 registers a thread).  Few slabs of channels:
-// clusters share a slab's time until the blocks fill the GPU twice over; many: blocks of fewer
-// warps, so that all slabs are resident.  Neither goes past the chunks there are.
-struct Cut {
-  int warps, cluster;
-  int64_t blocks;
-};
-
-Cut cut(const GlrArgs& p, int V) {
+// clusters share a slab's time, as large ones as leave all slabs resident at once; many: blocks of
+// fewer warps, so that all slabs are resident.  Neither goes past the chunks there are.
+template <typename E, int V, Mode MODE, bool LERP>
+cudaError_t launch_form(const GlrArgs& p, bool backward, cudaStream_t stream) {
   constexpr int kSms = 152;
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
+  const int stage = kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2);   // bytes of a warp's tiles
   auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
-  Cut c;
-  c.cluster = int(clip(2 * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
-  const int64_t per_sm = (slabs * c.cluster + kSms - 1) / kSms;
-  c.warps = int(clip(2 * kMaxWarps / per_sm, 1, clip(chunks, 1, kMaxWarps)));
-  c.blocks = slabs * c.cluster;
-  return c;
-}
-
-template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER>
-cudaError_t launch_cut(const GlrArgs& p, const Cut& c, bool backward, cudaStream_t stream) {
-  const size_t smem = size_t(c.warps) * kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2) +
-                      (CLUSTER ? size_t(2) * c.cluster * 32 * sizeof(Map<V>) : 0);
-  constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, CLUSTER>;
-  constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, CLUSTER>;
-  const cudaError_t e = backward ? allow_shared<kBackward>(smem) : allow_shared<kForward>(smem);
+  int cluster = int(clip(2 * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
+  if (cluster > 1) {
+    constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, true>;
+    constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, true>;
+    cudaError_t e = backward ? allow_shared<kBackward, true>(kMaxShared) : allow_shared<kForward, true>(kMaxShared);
+    if (e != cudaSuccess) return e;
+    auto* kernel = backward ? kBackward : kForward;
+    for (; cluster > 1; --cluster) {
+      const size_t shared = size_t(kMaxWarps) * stage + size_t(2) * cluster * 32 * sizeof(Map<V>);
+      int fit = 0;
+      e = resident_clusters(reinterpret_cast<const void*>(kernel), cluster, kMaxWarps * 32, shared, &fit);
+      if (e != cudaSuccess) return e;
+      if (fit >= slabs)
+        return launch_cluster_pdl(kernel, unsigned(slabs * cluster), unsigned(kMaxWarps * 32), unsigned(cluster), shared, stream, p, cluster);
+    }
+  }
+  constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, false>;
+  constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, false>;
+  const int warps = int(clip(2 * kMaxWarps / ((slabs + kSms - 1) / kSms), 1, clip(chunks, 1, kMaxWarps)));
+  const size_t shared = size_t(warps) * stage;
+  const cudaError_t e = backward ? allow_shared<kBackward>(shared) : allow_shared<kForward>(shared);
   if (e != cudaSuccess) return e;
-  return launch_cluster_pdl(backward ? kBackward : kForward, unsigned(c.blocks), unsigned(c.warps * 32), unsigned(c.cluster), smem,
-                            stream, p, c.cluster);
-}
-
-template <typename E, int V, Mode MODE, bool LERP>
-cudaError_t launch_form(const GlrArgs& p, bool backward, cudaStream_t stream) {
-  const Cut c = cut(p, V);
-  return c.cluster > 1 ? launch_cut<E, V, MODE, LERP, true>(p, c, backward, stream)
-                       : launch_cut<E, V, MODE, LERP, false>(p, c, backward, stream);
+  return launch_cluster_pdl(backward ? kBackward : kForward, unsigned(slabs), unsigned(warps * 32), 1, shared, stream, p, 1);
 }
 
 template <typename E, int V, Mode MODE>

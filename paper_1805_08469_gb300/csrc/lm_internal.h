@@ -8,6 +8,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstdint>
+#include <mutex>
 
 #include "../../include/gem_lm.h"
 #include "pdl.h"
@@ -108,12 +109,12 @@ inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 // 8.3 KB).
 constexpr size_t kMaxShared = 216 << 10;
 
-// Lets a kernel be launched with up to kMaxShared of dynamic shared memory.  Asked of the runtime once
-// for each kernel (KERNEL keeps one flag for each) and device.
-template <auto KERNEL>
+// Lets a kernel be launched with up to kMaxShared of dynamic shared memory (LARGE: and in clusters of
+// more than 8 blocks).  Asked of the runtime once for each kernel and device.
+template <auto KERNEL, bool LARGE = false>
 cudaError_t allow_shared(size_t bytes) {
   if (bytes > kMaxShared) return cudaErrorInvalidValue;
-  if (bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
+  if (!LARGE && bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
   static std::atomic<uint64_t> allowed{0};
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
@@ -121,6 +122,7 @@ cudaError_t allow_shared(size_t bytes) {
   const uint64_t bit = uint64_t(1) << (device & 63);
   if (device < 64 && (allowed.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
   e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxShared));
+  if (LARGE && e == cudaSuccess) e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess && device < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
   return e;
 }
@@ -144,6 +146,41 @@ cudaError_t launch_cluster_pdl(void (*kernel)(KArgs...), unsigned blocks, unsign
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...);
+}
+
+// Clusters of a kernel that the GPU holds at once (asked of the runtime once for each shape).
+inline cudaError_t resident_clusters(const void* kernel, int cluster, int threads, size_t shared, int* clusters) {
+  struct Known {
+    const void* kernel;
+    int device, cluster, threads, clusters;
+    size_t shared;
+  };
+  static std::mutex mutex;
+  static Known known[64];
+  static int count = 0;
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mutex);
+  for (const Known& k : known)
+    if (k.kernel == kernel && k.device == device && k.cluster == cluster && k.threads == threads && k.shared == shared) {
+      *clusters = k.clusters;
+      return cudaSuccess;
+    }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(cluster));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = shared;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(cluster);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaOccupancyMaxActiveClusters(clusters, kernel, &cfg);
+  if (e != cudaSuccess) return e;
+  known[count++ % 64] = {kernel, device, cluster, threads, *clusters, shared};
+  return cudaSuccess;
 }
 
 // Ends a call: a launch that failed is reported, and its error is not left for the caller's

@@ -2,7 +2,6 @@
 // logits, log probabilities of tokens with entropy and top alternatives, and their gradients.
 #include <cooperative_groups.h>
 
-#include <mutex>
 #include <type_traits>
 
 #include "lm_internal.h"
@@ -1466,47 +1465,12 @@ RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
   return c;
 }
 
-// Clusters of a kernel that the GPU holds at once (asked of the runtime once for each shape).
-cudaError_t resident_clusters(const void* kernel, const RowCut& c, int* clusters) {
-  struct Known {
-    const void* kernel;
-    int device, cluster, threads, clusters;
-    size_t smem;
-  };
-  static std::mutex mutex;
-  static Known known[32];
-  static int count = 0;
-  int device = 0;
-  cudaError_t e = cudaGetDevice(&device);
-  if (e != cudaSuccess) return e;
-  std::lock_guard<std::mutex> lock(mutex);
-  for (const Known& k : known)
-    if (k.kernel == kernel && k.device == device && k.cluster == c.cluster && k.threads == c.threads && k.smem == c.smem) {
-      *clusters = k.clusters;
-      return cudaSuccess;
-    }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(c.cluster));
-  cfg.blockDim = dim3(unsigned(c.threads));
-  cfg.dynamicSmemBytes = c.smem;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = unsigned(c.cluster);
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaOccupancyMaxActiveClusters(clusters, kernel, &cfg);
-  if (e != cudaSuccess) return e;
-  if (*clusters < 1) return cudaErrorInvalidConfiguration;
-  known[count++ % 32] = {kernel, device, c.cluster, c.threads, *clusters, c.smem};
-  return cudaSuccess;
-}
-
 template <auto KERNEL, typename... Args>
 cudaError_t launch_rows(const RowCut& c, int64_t N, cudaStream_t stream, const Args&... args) {
   cudaError_t e = allow_shared<KERNEL>(c.smem);
   int clusters = 0;
-  if (e == cudaSuccess) e = resident_clusters(reinterpret_cast<const void*>(KERNEL), c, &clusters);
+  if (e == cudaSuccess) e = resident_clusters(reinterpret_cast<const void*>(KERNEL), c.cluster, c.threads, c.smem, &clusters);
+  if (e == cudaSuccess && clusters < 1) e = cudaErrorInvalidConfiguration;
   if (e != cudaSuccess) return e;
   const int64_t grid = (N < clusters ? N : clusters) * c.cluster;
   return launch_cluster_pdl(KERNEL, unsigned(grid), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
