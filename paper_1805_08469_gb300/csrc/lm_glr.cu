@@ -421,10 +421,16 @@ __device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, con
   }
 }
 
-constexpr int kForwardStages = 3;
+// Stages of a thread's copies and blocks of an SM.  16-bit rows at odd addresses are copied through
+// registers, so more threads hide their latency instead of more stages (4 x 3,001 x 777 bf16: 34 us
+// against 52); fp32 rows gain nothing from it (276 against 270 at 100,003 x 1024).
+template <Mode MODE>
+constexpr int kForwardStages = MODE == kHalf ? 2 : 3;
+template <Mode MODE>
+constexpr int kForwardBlocks = MODE == kHalf ? 3 : 2;
 
 template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER>
-__global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const GlrArgs p, int blocks_of_cluster) {
+__global__ void __launch_bounds__(kMaxWarps * 32, kForwardBlocks<MODE>) glr_forward_kernel(const GlrArgs p, int blocks_of_cluster) {
   const int C = CLUSTER ? blocks_of_cluster : 1;
   extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
@@ -433,8 +439,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
   Exchange exchange = start_exchange<CLUSTER>(mbarriers);
   const Place w = place_of<E, V, MODE>(p, C);
   constexpr int kStage = 2 * kTile;
-  uint32_t* const ring = tiles + w.warp * kForwardStages * kStage;
-  Map<V>* const blocks = reinterpret_cast<Map<V>*>(tiles + w.warps * kForwardStages * kStage);
+  uint32_t* const ring = tiles + w.warp * kForwardStages<MODE> * kStage;
+  Map<V>* const blocks = reinterpret_cast<Map<V>*>(tiles + w.warps * kForwardStages<MODE> * kStage);
   const int64_t n = steps_of(p, w.b);
   const int64_t chunks = (n + kChunk - 1) / kChunk, all_chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t per_round = int64_t(w.warps) * C;
@@ -460,20 +466,20 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
     fetch_commit();
   };
 #pragma unroll
-  for (int r = 0; r < kForwardStages - 1; ++r) issue(r, r);
+  for (int r = 0; r < kForwardStages<MODE> - 1; ++r) issue(r, r);
 
   int stage = 0;
   for (int round = 0; round < rounds; ++round) {
-    issue(round + kForwardStages - 1, stage == 0 ? kForwardStages - 1 : stage - 1);
+    issue(round + kForwardStages<MODE> - 1, stage == 0 ? kForwardStages<MODE> - 1 : stage - 1);
     const int64_t c = first + round * per_round, t0 = c * kChunk;
     const bool busy = c < chunks;
     const int m = busy ? int(n - t0 < kChunk ? n - t0 : kChunk) : 0;
     const uint32_t fresh = reset_bits(p, w.b, t0, m);
     const bool plain = m == kChunk && fresh == 0;
-    fetch_wait<kForwardStages - 1>();
+    fetch_wait<kForwardStages<MODE> - 1>();
     __syncwarp();
     uint32_t* const tile = ring + stage * kStage;
-    stage = stage == kForwardStages - 1 ? 0 : stage + 1;
+    stage = stage == kForwardStages<MODE> - 1 ? 0 : stage + 1;
     Vec<V> a[kChunk], u[kChunk];
     const Map<V> own = plain ? forward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u)
                              : forward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, m, fresh, a, u);
@@ -667,9 +673,10 @@ cudaError_t launch_form(const GlrArgs& p, bool backward, cudaStream_t stream) {
   constexpr int kSms = 152;
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
-  const int stage = kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages * 2);   // bytes of a warp's tiles
+  const int stage = kTile * 4 * (backward ? kBackwardStages * 3 : kForwardStages<MODE> * 2);   // bytes of a warp's tiles
   auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
-  int cluster = int(clip(2 * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
+  const int blocks_per_sm = backward ? 2 : kForwardBlocks<MODE>;
+  int cluster = int(clip(blocks_per_sm * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
   if (cluster > 1) {
     constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, true>;
     constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, true>;
@@ -687,7 +694,7 @@ cudaError_t launch_form(const GlrArgs& p, bool backward, cudaStream_t stream) {
   }
   constexpr auto kForward = glr_forward_kernel<E, V, MODE, LERP, false>;
   constexpr auto kBackward = glr_backward_kernel<E, V, MODE, LERP, false>;
-  const int warps = int(clip(2 * kMaxWarps / ((slabs + kSms - 1) / kSms), 1, clip(chunks, 1, kMaxWarps)));
+  const int warps = int(clip(blocks_per_sm * kMaxWarps / ((slabs + kSms - 1) / kSms), 1, clip(chunks, 1, kMaxWarps)));
   const size_t shared = size_t(warps) * stage;
   const cudaError_t e = backward ? allow_shared<kBackward>(shared) : allow_shared<kForward>(shared);
   if (e != cudaSuccess) return e;
