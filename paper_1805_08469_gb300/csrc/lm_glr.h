@@ -1,0 +1,443 @@
+// Gated linear recurrence (include/gem_lm.h): what its forward and backward kernels share (internal).
+#pragma once
+
+#include <cooperative_groups.h>
+
+#include <type_traits>
+
+#include "lm_internal.h"
+
+namespace gem {
+namespace lm {
+namespace glr {
+
+namespace cg = cooperative_groups;
+
+constexpr int kChunk = GEM_GLR_CHUNK;
+
+struct GlrArgs {
+  gem_seq_t x, f, h, dh, dx, df;
+  const float* h0;
+  const int32_t* lengths;
+  const uint8_t* reset;
+  const float* saved_in;
+  float* saved_out;
+  float* h_last;
+  const float* dh_last;
+  float* dh0;
+  int64_t B, T, D;
+};
+
+template <typename E>
+__device__ __forceinline__ E* at(const gem_seq_t& s, int64_t b, int64_t t, int64_t d) {
+  return static_cast<E*>(s.data) + b * s.stride_b + t * s.stride_t + d;
+}
+
+__device__ __forceinline__ int64_t steps_of(const GlrArgs& p, int64_t b) {
+  if (!p.lengths) return p.T;
+  const int64_t n = p.lengths[b];
+  return n < 0 ? 0 : n > p.T ? p.T : n;
+}
+
+// a = sigmoid(f) and b = 1 - a = sigmoid(-f), each to its own relative precision: with e = exp(-f),
+// a = 1 / (1 + e) and b = e a.  f below -80 counts as -80 (a = 2e-35): e stays finite.  NaN stays.
+template <typename E, int V>
+__device__ __forceinline__ void gate(Vec<V> f, Vec<V>& a, Vec<V>& b) {
+  Vec<V> e;
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("max.NaN.f32 %0, %0, 0fC2A00000;" : "+f"(f.v[k]));
+  if constexpr (sizeof(E) == 4) {
+    e.v[0] = expf(-f.v[0]);
+  } else {
+    // 16-bit inputs carry 2^-9 themselves; rounding f log2(e) costs |f| 2^-24 of e
+    f = f * splat<V>(-1.44269504f);
+#pragma unroll
+    for (int k = 0; k < V; ++k) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.v[k]) : "f"(f.v[k]));
+  }
+  const Vec<V> s = e + splat<V>(1.0f);
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a.v[k]) : "f"(s.v[k]));
+  b = e * a;
+}
+
+// ---- tiles: a scan over time in registers, warps, blocks and rounds ----
+//
+// A step is the map h -> a h + u; maps compose, (A2, H2) after (A1, H1) being (A2 A1, A2 H1 + H2).
+// A thread takes kChunk steps of one 4-byte word of channels (two 16-bit ones or one), composes
+// their map, and applies the steps once it knows the state before them.  A warp is 32 words side by
+// side, 128 bytes of a row; the block's warps are consecutive chunks of time, the blocks of a
+// cluster consecutive groups of those, and the cluster goes over the sequence in rounds with the
+// state carried from one to the next.  Per round: one barrier of the block, after which every
+// thread composes the earlier warps' maps from shared memory, and in a cluster one exchange of the
+// blocks' maps over distributed shared memory.  Every element is read and written once.
+//
+// The copies of a thread's next rounds are in flight while it works (cp.async into slots of its
+// own, which need no barrier), so memory does not wait for the scan.
+//
+// A map whose steps contain a reset has A = -1: it forgets the state whatever that holds (0 times
+// an infinity would not).
+
+constexpr int kMaxWarps = 8;
+constexpr int kMaxCluster = 16;   // (more than 8 blocks are for this GPU only)
+
+template <int V>
+struct Map {
+  Vec<V> A, H;
+};
+
+// h after the map m, and m after the maps composed so far.  RESETS: a map may forget.
+template <int V, bool RESETS>
+__device__ __forceinline__ Vec<V> apply(const Vec<V>& h, const Map<V>& m) {
+  Vec<V> r = fma<V>(m.A, h, m.H);
+  if constexpr (RESETS) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) r.v[k] = m.A.v[k] < 0.0f ? m.H.v[k] : r.v[k];
+  }
+  return r;
+}
+
+template <int V, bool RESETS>
+__device__ __forceinline__ Map<V> compose(const Map<V>& sofar, const Map<V>& m) {
+  Map<V> r = {sofar.A * m.A, apply<V, RESETS>(sofar.H, m)};
+  if constexpr (RESETS) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) r.A.v[k] = m.A.v[k] < 0.0f || sofar.A.v[k] < 0.0f ? -1.0f : r.A.v[k];
+  }
+  return r;
+}
+
+// The exchange of the blocks' maps in a cluster: each block sends its map to every block with stores
+// that count their bytes on the receiver's mbarrier, so nothing else (a cluster barrier would wait for
+// all of a block's stores to memory) holds the round up.
+struct Exchange {
+  uint32_t full;   // shared address of two mbarriers, one for each parity of the round
+  bool gave_up;    // a wait passed its limit: the states are NaN from there on
+};
+
+__device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ uint32_t in_block(uint32_t address, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(address), "r"(rank));
+  return r;
+}
+
+template <int V>
+__device__ __forceinline__ void send(uint32_t to, const Map<V>& m, uint32_t mbarrier) {
+  if constexpr (V == 2)
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
+                 "r"(__float_as_uint(m.A.v[0])), "r"(__float_as_uint(m.A.v[1])), "r"(__float_as_uint(m.H.v[0])),
+                 "r"(__float_as_uint(m.H.v[1])), "r"(mbarrier)
+                 : "memory");
+  else
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to),
+                 "r"(__float_as_uint(m.A.v[0])), "r"(__float_as_uint(m.H.v[0])), "r"(mbarrier)
+                 : "memory");
+}
+
+// Waits until the phase of this parity is complete; false after two seconds (it never takes
+// microseconds unless a block of the cluster is gone).
+__device__ __forceinline__ bool wait_phase(uint32_t mbarrier, uint32_t parity) {
+  uint64_t start = 0;
+  for (unsigned i = 1;; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(mbarrier), "r"(parity)
+        : "memory");
+    if (done) return true;
+    if (i % 256 == 0) {
+      uint64_t now;
+      asm volatile("mov.u64 %0, %globaltimer;" : "=l"(now));
+      if (start == 0)
+        start = now;
+      else if (now - start > 2000000000ull)
+        return false;
+    }
+  }
+}
+
+// Sets the mbarriers up; all threads call.  No block sends before all have.
+template <bool CLUSTER>
+__device__ __forceinline__ Exchange start_exchange(uint64_t (&mbarriers)[2]) {
+  Exchange x = {shared_address(mbarriers), false};
+  if constexpr (CLUSTER) {
+    if (threadIdx.x == 0) {
+      for (int b = 0; b < 2; ++b) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(x.full + 8 * b) : "memory");
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cg::this_cluster().sync();
+  }
+  return x;
+}
+
+// From every thread's map of a round: the state before the thread's chunk, and `state` moved on to
+// the state after the round.  maps: [2][kMaxWarps][32], blocks: [2][C][32] (C > 1) in shared memory.
+template <int V, bool RESETS, bool CLUSTER>
+__device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int warps, int rank, int C, Map<V>* maps, Map<V>* blocks,
+                                             Exchange& x, Vec<V>& state) {
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  Map<V>* buf = maps + (round & 1) * kMaxWarps * 32 + lane;
+  Vec<V> before = state;
+  buf[warp * 32] = own;
+  __syncthreads();
+  if constexpr (!CLUSTER) {
+#pragma unroll
+    for (int w = 0; w < kMaxWarps; ++w) {
+      if (w >= warps) break;
+      if (w == warp) before = state;
+      state = apply<V, RESETS>(state, buf[w * 32]);
+    }
+    return before;
+  }
+  Map<V> all = {splat<V>(1.0f), splat<V>(0.0f)}, mine = all;
+#pragma unroll
+  for (int w = 0; w < kMaxWarps; ++w) {
+    if (w >= warps) break;
+    if (w == warp) mine = all;
+    all = compose<V, RESETS>(all, buf[w * 32]);
+  }
+  // (a buffer is sent to again two rounds on: by then all have read it, or their maps of the round
+  // between would not have come)
+  Map<V>* in = blocks + (round & 1) * C * 32 + lane;
+  const uint32_t full = x.full + 8 * (round & 1), slot = shared_address(in + rank * 32);
+  for (int c = warp; c < C; c += warps) send<V>(in_block(slot, c), all, in_block(full, c));
+  if (threadIdx.x == 0)
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full), "r"(uint32_t(C * 32 * sizeof(Map<V>)))
+                 : "memory");
+  if (!x.gave_up && !wait_phase(full, uint32_t(round >> 1) & 1u)) {
+    x.gave_up = true;
+    state = splat<V>(NAN);
+  }
+  for (int c = 0; c < C; ++c) {
+    if (c == rank) before = state;
+    state = apply<V, RESETS>(state, in[c * 32]);
+  }
+  return apply<V, RESETS>(before, mine);
+}
+
+// A word of channels as V floats, and back.
+template <typename E, int V>
+__device__ __forceinline__ Vec<V> unpack(uint32_t w) {
+  Vec<V> r;
+  if constexpr (sizeof(E) == 4) {
+    r.v[0] = __uint_as_float(w);
+  } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+    r.v[0] = __uint_as_float(w << 16);
+    if constexpr (V == 2) r.v[1] = __uint_as_float(w & 0xffff0000u);
+  } else {
+    const __half2 h = *reinterpret_cast<const __half2*>(&w);
+    r.v[0] = __low2float(h);
+    if constexpr (V == 2) r.v[1] = __high2float(h);
+  }
+  return r;
+}
+
+template <typename E, int V>
+__device__ __forceinline__ uint32_t pack(const Vec<V>& a) {
+  if constexpr (sizeof(E) == 4) {
+    return __float_as_uint(a.v[0]);
+  } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+    const __nv_bfloat162 w = __floats2bfloat162_rn(a.v[0], V == 2 ? a.v[V - 1] : 0.0f);
+    return *reinterpret_cast<const uint32_t*>(&w);
+  } else {
+    const __half2 w = __floats2half2_rn(a.v[0], V == 2 ? a.v[V - 1] : 0.0f);
+    return *reinterpret_cast<const uint32_t*>(&w);
+  }
+}
+
+// A warp's tile of one tensor: kChunk rows of 32 words in shared memory, row k the channels of
+// step k.  MODE: how the tensors' rows lie in memory.
+//   kVector  every row starts at a 16-byte boundary and D fills whole 16-byte pieces: lane l moves
+//            piece l % 8 of rows l / 8, l / 8 + 4, ...
+//   kWord    rows start at 4-byte boundaries: lane l moves word l of each row
+//   kHalf    16-bit rows start anywhere; a word holds one channel
+enum Mode { kVector, kWord, kHalf };
+constexpr int kTile = kChunk * 32;
+
+__device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void fetch_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Where a thread works: sequence b, its own channel word d.., and the channels it moves.
+struct Place {
+  int64_t b, d, move_d;
+  int rank, warp, warps, lane;
+  bool on, moves;
+};
+
+template <typename E, int V, Mode MODE>
+__device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
+  Place w;
+  const int64_t slabs = (p.D + 32 * V - 1) / (32 * V);
+  const int64_t id = blockIdx.x / C;
+  w.rank = blockIdx.x % C;
+  w.lane = threadIdx.x % 32;
+  w.warp = threadIdx.x / 32;
+  w.warps = blockDim.x / 32;
+  w.b = id / slabs;
+  const int64_t first = id % slabs * 32 * V;
+  w.d = first + w.lane * V;
+  w.on = w.d < p.D;
+  w.move_d = MODE == kVector ? first + w.lane % 8 * (16 / int(sizeof(E))) : w.d;
+  w.moves = w.move_d < p.D;
+  return w;
+}
+
+// Multiples of a stride are computed anew in each round: 16 of them held in registers over the rounds
+// make the rest spill.
+__device__ __forceinline__ void keep_out_of_registers(int64_t& stride) { asm volatile("" : "+l"(stride)); }
+
+// Starts the copy of rows 0..m of a tile; from: the row of step 0 at the lane's channels (move_d).
+template <typename E, Mode MODE>
+__device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_t stride, int m, int lane) {
+  keep_out_of_registers(stride);
+  if constexpr (MODE == kVector) {
+    const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile)) + lane * 16;
+    from += lane / 8 * stride;
+#pragma unroll
+    for (int i = 0; i < kChunk / 4; ++i) {
+      if (lane / 8 + 4 * i < m)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + i * 512), "l"(from) : "memory");
+      from += 4 * stride;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
+      if (k < m) {
+        if constexpr (MODE == kWord) {
+          const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile + k * 32 + lane));
+          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
+        } else {
+          *reinterpret_cast<E*>(tile + k * 32 + lane) = *from;
+        }
+      }
+      from += stride;
+    }
+  }
+}
+
+// Stores rows 0..m of a tile that the warp has written (all lanes call; the tile is free after).
+template <typename E, Mode MODE>
+__device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t stride, int m, int lane, bool moves) {
+  keep_out_of_registers(stride);
+  __syncwarp();
+  if constexpr (MODE == kVector) {
+    const uint4* t = reinterpret_cast<const uint4*>(tile) + lane;
+    to += lane / 8 * stride;
+#pragma unroll
+    for (int i = 0; i < kChunk / 4; ++i) {
+      if (moves && lane / 8 + 4 * i < m) *reinterpret_cast<uint4*>(to) = t[i * 32];
+      to += 4 * stride;
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
+      if (moves && k < m) {
+        if constexpr (MODE == kWord)
+          *reinterpret_cast<uint32_t*>(to) = tile[k * 32 + lane];
+        else
+          *to = *reinterpret_cast<const E*>(tile + k * 32 + lane);
+      }
+      to += stride;
+    }
+  }
+  __syncwarp();
+}
+
+// Zeros to rows t, t + step, ... below T (steps past a sequence's end).
+template <typename E, int V>
+__device__ __forceinline__ void store_zeros(E* to, int64_t stride, int64_t t, int64_t step, int64_t T) {
+  for (; t < T; t += step)
+#pragma unroll
+    for (int v = 0; v < V; ++v) to[t * stride + v] = from_f32<E>(0.0f);
+}
+
+// Bit k: a reset at step k of a chunk (k < m), from the lanes' bytes.  The bytes are read a round ahead.
+template <bool RESETS>
+__device__ __forceinline__ uint8_t load_reset(const GlrArgs& p, int64_t b, int64_t t) {
+  return RESETS && t < p.T && threadIdx.x % 32 < kChunk ? p.reset[b * p.T + t] : 0;
+}
+template <bool RESETS>
+__device__ __forceinline__ uint32_t reset_bits(uint8_t lane_byte, int m) {
+  return RESETS ? __ballot_sync(~0u, int(threadIdx.x % 32) < m && lane_byte != 0) : 0;
+}
+
+// How the work is cut.  About 16 warps fit an SM (128 registers a thread).  Few slabs of channels:
+// clusters share a slab's time, as large ones as leave all slabs resident at once; many: blocks of
+// fewer warps, so that all slabs are resident.  Neither goes past the chunks there are.
+//
+// DIRECTION names the kernel, its tensors copied in, stages and blocks of an SM.
+template <typename DIRECTION, typename E, int V, Mode MODE, bool LERP, bool RESETS>
+cudaError_t launch_form(const GlrArgs& p, cudaStream_t stream) {
+  constexpr int kSms = 152, kBlocks = DIRECTION::template blocks<MODE>();
+  constexpr size_t kWarpBytes = size_t(kTile) * 4 * DIRECTION::kTensors * DIRECTION::template stages<MODE>();
+  const int64_t chunks = (p.T + kChunk - 1) / kChunk;
+  const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
+  auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
+  int cluster = int(clip(kBlocks * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
+  if (cluster > 1) {
+    constexpr auto kKernel = DIRECTION::template kernel<E, V, MODE, LERP, true, RESETS>();
+    cudaError_t e = allow_shared<kKernel, true>(kMaxShared);
+    if (e != cudaSuccess) return e;
+    for (; cluster > 1; --cluster) {
+      const size_t shared = kMaxWarps * kWarpBytes + size_t(2) * cluster * 32 * sizeof(Map<V>);
+      int fit = 0;
+      e = resident_clusters(reinterpret_cast<const void*>(kKernel), cluster, kMaxWarps * 32, shared, &fit);
+      if (e != cudaSuccess) return e;
+      if (fit >= slabs)
+        return launch_cluster_pdl(kKernel, unsigned(slabs * cluster), unsigned(kMaxWarps * 32), unsigned(cluster), shared, stream, p,
+                                  cluster);
+    }
+  }
+  constexpr auto kKernel = DIRECTION::template kernel<E, V, MODE, LERP, false, RESETS>();
+  const int warps = int(clip(kBlocks * kMaxWarps / ((slabs + kSms - 1) / kSms), 1, clip(chunks, 1, kMaxWarps)));
+  const size_t shared = warps * kWarpBytes;
+  const cudaError_t e = allow_shared<kKernel>(shared);
+  if (e != cudaSuccess) return e;
+  return launch_cluster_pdl(kKernel, unsigned(slabs), unsigned(warps * 32), 1, shared, stream, p, 1);
+}
+
+template <typename DIRECTION, typename E, int V, Mode MODE>
+cudaError_t launch_mode(const GlrArgs& p, int form, cudaStream_t stream) {
+  if (form == GEM_GLR_LERP)
+    return p.reset ? launch_form<DIRECTION, E, V, MODE, true, true>(p, stream) : launch_form<DIRECTION, E, V, MODE, true, false>(p, stream);
+  return p.reset ? launch_form<DIRECTION, E, V, MODE, false, true>(p, stream) : launch_form<DIRECTION, E, V, MODE, false, false>(p, stream);
+}
+
+// By the largest power of two, 16 bytes at most, on which every row of every tensor starts and D ends.
+template <typename DIRECTION, typename E>
+cudaError_t launch_tiles(const GlrArgs& p, int form, cudaStream_t stream) {
+  uint64_t bits = 16 | uint64_t(p.D) * sizeof(E);
+  for (const gem_seq_t* s : DIRECTION::tensors(p)) {
+    bits |= reinterpret_cast<uintptr_t>(s->data);
+    if (p.B > 1) bits |= uint64_t(s->stride_b) * sizeof(E);
+    if (p.T > 1) bits |= uint64_t(s->stride_t) * sizeof(E);
+  }
+  constexpr int kWordV = 4 / sizeof(E);
+  if (bits % 16 == 0) return launch_mode<DIRECTION, E, kWordV, kVector>(p, form, stream);
+  if constexpr (sizeof(E) == 2) {
+    if (bits % 4 != 0) return launch_mode<DIRECTION, E, 1, kHalf>(p, form, stream);
+  }
+  return launch_mode<DIRECTION, E, kWordV, kWord>(p, form, stream);
+}
+
+template <typename DIRECTION>
+cudaError_t launch_tiles(int dtype, const GlrArgs& p, int form, cudaStream_t stream) {
+  switch (dtype) {
+    case GEM_F32: return launch_tiles<DIRECTION, float>(p, form, stream);
+    case GEM_BF16: return launch_tiles<DIRECTION, __nv_bfloat16>(p, form, stream);
+    default: return launch_tiles<DIRECTION, __half>(p, form, stream);
+  }
+}
+
+cudaError_t launch_backward(int dtype, const GlrArgs& p, int form, cudaStream_t stream);
+
+}  // namespace glr
+}  // namespace lm
+}  // namespace gem
