@@ -249,14 +249,35 @@ __device__ __forceinline__ uint32_t pack(const Vec<V>& a) {
   }
 }
 
-// A warp's tile of one tensor: kChunk rows of 32 words in shared memory, row k the channels of
+// A warp's tile of one tensor: kChunk rows of 32 words of channels in shared memory, row k those of
 // step k.  MODE: how the tensors' rows lie in memory.
 //   kVector  every row starts at a 16-byte boundary and D fills whole 16-byte pieces: lane l moves
 //            piece l % 8 of rows l / 8, l / 8 + 4, ...
-//   kWord    rows start at 4-byte boundaries: lane l moves word l of each row
-//   kHalf    16-bit rows start anywhere; a word holds one channel
-enum Mode { kVector, kWord, kHalf };
-constexpr int kTile = kChunk * 32;
+//   kWord    rows start at 4-byte boundaries and D fills whole words: lane l moves word l of each row
+//   kOdd     16-bit rows that start at any element: lane l moves the aligned word l that covers the
+//            row's channels 2 l and 2 l + 1 or, where the row starts in the middle of a word, 2 l - 1 and
+//            2 l; a row has one word more
+enum Mode { kVector, kWord, kOdd };
+template <Mode MODE>
+constexpr int kPitch = MODE == kOdd ? 33 : 32;
+template <Mode MODE>
+constexpr int kTile = kChunk * kPitch<MODE>;
+
+// Bit k: row k of a tile starts in the middle of a word.
+template <typename E, Mode MODE>
+__device__ __forceinline__ uint32_t odd_rows(const E* row0, int64_t stride) {
+  if constexpr (MODE != kOdd) return 0;
+  const uint32_t first = uint32_t(reinterpret_cast<uintptr_t>(row0) >> 1 & 1);
+  return ((stride & 1) ? 0xAAAAu : 0u) ^ (first ? 0xFFFFu : 0u);
+}
+
+// The lane's word of channels of row k; tile points to the lane's word of row 0.
+template <Mode MODE>
+__device__ __forceinline__ uint32_t read_word(const uint32_t* tile, int k, uint32_t odd) {
+  const uint32_t w = tile[k * kPitch<MODE>];
+  if constexpr (MODE == kOdd) return (odd >> k & 1) ? __funnelshift_r(w, tile[k * kPitch<MODE> + 1], 16) : w;
+  return w;
+}
 
 __device__ __forceinline__ void fetch_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -268,6 +289,8 @@ __device__ __forceinline__ void fetch_wait() {
 struct Place {
   int64_t b, d, move_d;
   int rank, warp, warps, lane;
+  int own;      // channels of the thread's word that exist: 0..V
+  int slab;     // and of the warp's slab (kOdd)
   bool on, moves;
 };
 
@@ -283,8 +306,10 @@ __device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
   w.b = id / slabs;
   const int64_t first = id % slabs * 32 * V;
   w.d = first + w.lane * V;
-  w.on = w.d < p.D;
-  w.move_d = MODE == kVector ? first + w.lane % 8 * (16 / int(sizeof(E))) : w.d;
+  w.own = int(w.d + V <= p.D ? V : w.d < p.D ? p.D - w.d : 0);
+  w.slab = int(p.D - first < 32 * V ? p.D - first : 32 * V);
+  w.on = w.own > 0;
+  w.move_d = MODE == kVector ? first + w.lane % 8 * (16 / int(sizeof(E))) : MODE == kOdd ? first : w.d;
   w.moves = w.move_d < p.D;
   return w;
 }
@@ -293,9 +318,15 @@ __device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
 // make the rest spill.
 __device__ __forceinline__ void keep_out_of_registers(int64_t& stride) { asm volatile("" : "+l"(stride)); }
 
-// Starts the copy of rows 0..m of a tile; from: the row of step 0 at the lane's channels (move_d).
+__device__ __forceinline__ void copy_word(uint32_t* slot, const void* from, int bytes) {
+  const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(slot));
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(s), "l"(from), "r"(bytes) : "memory");
+}
+
+// Starts the copy of rows 0..m of a tile; from: the row of step 0 at the lane's channels (move_d); data:
+// the tensor's first element, slab: its channels (kOdd).
 template <typename E, Mode MODE>
-__device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_t stride, int m, int lane) {
+__device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_t stride, int m, int lane, const void* data, int slab) {
   keep_out_of_registers(stride);
   if constexpr (MODE == kVector) {
     const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile)) + lane * 16;
@@ -306,25 +337,35 @@ __device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s + i * 512), "l"(from) : "memory");
       from += 4 * stride;
     }
-  } else {
+  } else if constexpr (MODE == kWord) {
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) {
-      if (k < m) {
-        if constexpr (MODE == kWord) {
-          const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(tile + k * 32 + lane));
-          asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
-        } else {
-          *reinterpret_cast<E*>(tile + k * 32 + lane) = *from;
-        }
-      }
+      if (k < m) copy_word(tile + k * 32 + lane, from, 4);
       from += stride;
+    }
+  } else {
+#pragma unroll 4
+    for (int k = 0; k < kChunk; ++k, from += stride) {
+      if (k >= m) break;
+      const int odd = int(reinterpret_cast<uintptr_t>(from) >> 1 & 1);
+      uint32_t* const row = tile + k * kPitch<MODE>;
+      const int c = 2 * lane - odd;   // the word's first channel
+      if (c < 0 && from == data) {
+        // the word would start before the tensor: its second half alone
+        reinterpret_cast<E*>(row)[1] = *from;
+      } else if (c < slab) {
+        // (the half before the slab is read with it, that after the slab is not)
+        copy_word(row + lane, from + c, c + 1 < slab ? 4 : 2);
+      }
+      if (lane == 0 && odd && slab == 64) copy_word(row + 32, from + 63, 2);
     }
   }
 }
 
-// Stores rows 0..m of a tile that the warp has written (all lanes call; the tile is free after).
+// Stores rows 0..m of a tile that the warp has written, word by word of its own channels (all lanes
+// call; the tile is free after).
 template <typename E, Mode MODE>
-__device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t stride, int m, int lane, bool moves) {
+__device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t stride, int m, int lane, bool moves, int slab) {
   keep_out_of_registers(stride);
   __syncwarp();
   if constexpr (MODE == kVector) {
@@ -335,27 +376,36 @@ __device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t 
       if (moves && lane / 8 + 4 * i < m) *reinterpret_cast<uint4*>(to) = t[i * 32];
       to += 4 * stride;
     }
-  } else {
+  } else if constexpr (MODE == kWord) {
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) {
-      if (moves && k < m) {
-        if constexpr (MODE == kWord)
-          *reinterpret_cast<uint32_t*>(to) = tile[k * 32 + lane];
-        else
-          *to = *reinterpret_cast<const E*>(tile + k * 32 + lane);
-      }
+      if (moves && k < m) *reinterpret_cast<uint32_t*>(to) = tile[k * 32 + lane];
       to += stride;
+    }
+  } else {
+#pragma unroll 4
+    for (int k = 0; k < kChunk; ++k, to += stride) {
+      if (k >= m) break;
+      const uint32_t* const row = tile + k * kPitch<MODE> + lane;
+      const bool odd = reinterpret_cast<uintptr_t>(to) >> 1 & 1;
+      const uint32_t w = row[0];
+      const E* const halves = reinterpret_cast<const E*>(&w);
+      const int c = 2 * lane + odd;   // first channel of the lane's aligned word
+      if (c + 1 < slab)
+        *reinterpret_cast<uint32_t*>(to + c) = odd ? __funnelshift_r(w, row[1], 16) : w;
+      else if (c < slab)
+        to[c] = halves[odd];
+      if (odd && lane == 0) to[0] = halves[0];
     }
   }
   __syncwarp();
 }
 
-// Zeros to rows t, t + step, ... below T (steps past a sequence's end).
-template <typename E, int V>
-__device__ __forceinline__ void store_zeros(E* to, int64_t stride, int64_t t, int64_t step, int64_t T) {
+// Zeros to a thread's `own` channels of rows t, t + step, ... below T (steps past a sequence's end).
+template <typename E>
+__device__ __forceinline__ void store_zeros(E* to, int64_t stride, int64_t t, int64_t step, int64_t T, int own) {
   for (; t < T; t += step)
-#pragma unroll
-    for (int v = 0; v < V; ++v) to[t * stride + v] = from_f32<E>(0.0f);
+    for (int v = 0; v < own; ++v) to[t * stride + v] = from_f32<E>(0.0f);
 }
 
 // Bit k: a reset at step k of a chunk (k < m), from the lanes' bytes.  The bytes are read a round ahead.
@@ -376,7 +426,7 @@ __device__ __forceinline__ uint32_t reset_bits(uint8_t lane_byte, int m) {
 template <typename DIRECTION, typename E, int V, Mode MODE, bool LERP, bool RESETS>
 cudaError_t launch_form(const GlrArgs& p, cudaStream_t stream) {
   constexpr int kSms = 152, kBlocks = DIRECTION::template blocks<MODE>();
-  constexpr size_t kWarpBytes = size_t(kTile) * 4 * DIRECTION::kTensors * DIRECTION::template stages<MODE>();
+  constexpr size_t kWarpBytes = size_t(kTile<MODE>) * 4 * DIRECTION::kTensors * DIRECTION::template stages<MODE>();
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
   auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
@@ -422,21 +472,16 @@ cudaError_t launch_tiles(const GlrArgs& p, int form, cudaStream_t stream) {
   constexpr int kWordV = 4 / sizeof(E);
   if (bits % 16 == 0) return launch_mode<DIRECTION, E, kWordV, kVector>(p, form, stream);
   if constexpr (sizeof(E) == 2) {
-    if (bits % 4 != 0) return launch_mode<DIRECTION, E, 1, kHalf>(p, form, stream);
+    if (bits % 4 != 0) return launch_mode<DIRECTION, E, kWordV, kOdd>(p, form, stream);
   }
   return launch_mode<DIRECTION, E, kWordV, kWord>(p, form, stream);
 }
 
-template <typename DIRECTION>
-cudaError_t launch_tiles(int dtype, const GlrArgs& p, int form, cudaStream_t stream) {
-  switch (dtype) {
-    case GEM_F32: return launch_tiles<DIRECTION, float>(p, form, stream);
-    case GEM_BF16: return launch_tiles<DIRECTION, __nv_bfloat16>(p, form, stream);
-    default: return launch_tiles<DIRECTION, __half>(p, form, stream);
-  }
-}
-
-cudaError_t launch_backward(int dtype, const GlrArgs& p, int form, cudaStream_t stream);
+// The directions' launches for one element type each, compiled apart (lm_glr_f32.cu and so on).
+template <typename E>
+cudaError_t launch_forward(const GlrArgs& p, int form, cudaStream_t stream);
+template <typename E>
+cudaError_t launch_backward(const GlrArgs& p, int form, cudaStream_t stream);
 
 }  // namespace glr
 }  // namespace lm

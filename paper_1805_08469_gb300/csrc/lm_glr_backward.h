@@ -1,4 +1,6 @@
-// Gated linear recurrence (include/gem_lm.h): backward kernels.
+// Gated linear recurrence: backward kernels (internal; included once for each element type).
+#pragma once
+
 #include <array>
 
 #include "lm_glr.h"
@@ -6,7 +8,6 @@
 namespace gem {
 namespace lm {
 namespace glr {
-namespace {
 
 // Backward: the same scan from the end.  A step's map is g -> a (dh + g), g being what the step
 // after it hands back.  A chunk's map is sum_k (a_0 .. a_k) dh_k + (a_0 .. a_15) g, so it is
@@ -14,11 +15,16 @@ namespace {
 // saved one; nothing counts from the first reset on.  q: what the gate's gradient multiplies,
 // h_{t-1} - x_t or h_{t-1}.  The gates are kept in registers for one channel a thread; for two they would
 // take 64 (and spilled: 173 us instead of 116 at 8 x 4096 x 2048 bf16), and are computed again.
+struct Words {
+  const uint32_t *x, *f, *dh;   // the lane's words of the tiles
+  uint32_t odd_x, odd_f, odd_dh;
+};
+
 template <int V>
 constexpr int kKeep = V == 1 ? kChunk : 1;
 
-template <typename E, int V, bool LERP, bool PLAIN>
-__device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t* f, const uint32_t* dh, int m, uint32_t fresh,
+template <typename E, int V, Mode MODE, bool LERP, bool PLAIN>
+__device__ __forceinline__ Map<V> backward_map(const Words& in, int m, uint32_t fresh,
                                                Vec<V> h, Vec<V> (&q)[kChunk], Vec<V> (&gates)[2][kKeep<V>]) {
   Map<V> own = {splat<V>(1.0f), splat<V>(0.0f)};
   bool counts = true;
@@ -26,8 +32,8 @@ __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t
   for (int k = 0; k < kChunk; ++k) {
     if (!PLAIN && k >= m) continue;
     Vec<V> a, b;
-    const Vec<V> xv = unpack<E, V>(x[k * 32]);
-    gate<E, V>(unpack<E, V>(f[k * 32]), a, b);
+    const Vec<V> xv = unpack<E, V>(read_word<MODE>(in.x, k, in.odd_x));
+    gate<E, V>(unpack<E, V>(read_word<MODE>(in.f, k, in.odd_f)), a, b);
     const Vec<V> u = LERP ? b * xv : xv;
     const bool r = !PLAIN && (fresh >> k & 1);
     if (r) h = splat<V>(0.0f);
@@ -40,30 +46,31 @@ __device__ __forceinline__ Map<V> backward_map(const uint32_t* x, const uint32_t
     if (r) counts = false;
     if (counts) {
       own.A = own.A * a;
-      own.H = fma<V>(own.A, unpack<E, V>(dh[k * 32]), own.H);
+      own.H = fma<V>(own.A, unpack<E, V>(read_word<MODE>(in.dh, k, in.odd_dh)), own.H);
     }
   }
   if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
   return own;
 }
 
-template <typename E, int V, bool LERP, bool PLAIN>
-__device__ __forceinline__ void backward_apply(uint32_t* dx, uint32_t* df, const uint32_t* dh, int m, uint32_t fresh,
+template <typename E, int V, Mode MODE, bool LERP, bool PLAIN>
+__device__ __forceinline__ void backward_apply(const Words& in, uint32_t* dx, uint32_t* df, int m, uint32_t fresh,
                                                const Vec<V> (&q)[kChunk], const Vec<V> (&gates)[2][kKeep<V>], Vec<V> g) {
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
     if (!PLAIN && k >= m) continue;
-    g = g + unpack<E, V>(dh[k * 32]);
+    g = g + unpack<E, V>(read_word<MODE>(in.dh, k, in.odd_dh));
     Vec<V> a, b;
     if constexpr (V == 1) {
       a = gates[0][k];
       b = gates[1][k];
     } else {
-      gate<E, V>(unpack<E, V>(df[k * 32]), a, b);   // again from f (its slot is df's)
+      gate<E, V>(unpack<E, V>(read_word<MODE>(in.f, k, in.odd_f)), a, b);   // again from f (its slot is df's)
     }
-    dx[k * 32] = pack<E, V>(LERP ? b * g : g);
+    if constexpr (MODE == kOdd) __syncwarp();   // (a neighbour reads the word of f that df replaces)
+    dx[k * kPitch<MODE>] = pack<E, V>(LERP ? b * g : g);
     g = a * g;
-    df[k * 32] = pack<E, V>(g * (q[k] * b));
+    df[k * kPitch<MODE>] = pack<E, V>(g * (q[k] * b));
     if (!PLAIN && (fresh >> k & 1)) g = splat<V>(0.0f);
   }
 }
@@ -79,7 +86,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
   pdl_entry();
   Exchange exchange = start_exchange<CLUSTER>(mbarriers);
   const Place w = place_of<E, V, MODE>(p, C);
-  constexpr int kStage = 3 * kTile;
+  constexpr int kStage = 3 * kTile<MODE>;
   uint32_t* const ring = tiles + w.warp * kBackwardStages * kStage;
   Map<V>* const blocks = reinterpret_cast<Map<V>*>(tiles + w.warps * kBackwardStages * kStage);
   const int64_t n = steps_of(p, w.b);
@@ -95,7 +102,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
   const int64_t state_at = w.b * p.D + w.d;
   Vec<V> state, saved = splat<V>(0.0f);
 #pragma unroll
-  for (int v = 0; v < V; ++v) state.v[v] = p.dh_last && w.on ? p.dh_last[state_at + v] : 0.0f;
+  for (int v = 0; v < V; ++v) state.v[v] = p.dh_last && v < w.own ? p.dh_last[state_at + v] : 0.0f;
 
   auto issue = [&](int round, int stage) {
     const int64_t l = first + round * per_round;
@@ -103,9 +110,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
       const int64_t t0 = (chunks - 1 - l) * kChunk;
       const int m = int(n - t0 < kChunk ? n - t0 : kChunk);
       uint32_t* tile = ring + stage * kStage;
-      fetch_tile<E, MODE>(tile, x + t0 * p.x.stride_t, p.x.stride_t, m, w.lane);
-      fetch_tile<E, MODE>(tile + kTile, f + t0 * p.f.stride_t, p.f.stride_t, m, w.lane);
-      fetch_tile<E, MODE>(tile + 2 * kTile, dh + t0 * p.dh.stride_t, p.dh.stride_t, m, w.lane);
+      fetch_tile<E, MODE>(tile, x + t0 * p.x.stride_t, p.x.stride_t, m, w.lane, p.x.data, w.slab);
+      fetch_tile<E, MODE>(tile + kTile<MODE>, f + t0 * p.f.stride_t, p.f.stride_t, m, w.lane, p.f.data, w.slab);
+      fetch_tile<E, MODE>(tile + 2 * kTile<MODE>, dh + t0 * p.dh.stride_t, p.dh.stride_t, m, w.lane, p.dh.data, w.slab);
     }
     fetch_commit();
   };
@@ -115,7 +122,8 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     if (l < chunks && w.on) {
       const float* s = p.saved_in + (w.b * all_chunks + chunks - 1 - l) * p.D + w.d;
 #pragma unroll
-      for (int v = 0; v < V; ++v) saved.v[v] = s[v];
+      for (int v = 0; v < V; ++v)
+        if (v < w.own) saved.v[v] = s[v];
     }
   };
 #pragma unroll
@@ -135,29 +143,32 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
     fetch_wait<kBackwardStages - 1>();
     __syncwarp();
     uint32_t* const tile = ring + stage * kStage;
-    const uint32_t* const dhs = tile + 2 * kTile + w.lane;
+    const Words in = {tile + w.lane, tile + kTile<MODE> + w.lane, tile + 2 * kTile<MODE> + w.lane,
+                      odd_rows<E, MODE>(x + t0 * p.x.stride_t, p.x.stride_t), odd_rows<E, MODE>(f + t0 * p.f.stride_t, p.f.stride_t),
+                      odd_rows<E, MODE>(dh + t0 * p.dh.stride_t, p.dh.stride_t)};
     stage = stage == kBackwardStages - 1 ? 0 : stage + 1;
     Vec<V> q[kChunk], gates[2][kKeep<V>];
     const Vec<V> h = saved;
     load_saved(round + 1);
-    const Map<V> own = plain ? backward_map<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q, gates)
-                             : backward_map<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, h, q, gates);
+    const Map<V> own = plain ? backward_map<E, V, MODE, LERP, true>(in, m, fresh, h, q, gates)
+                             : backward_map<E, V, MODE, LERP, false>(in, m, fresh, h, q, gates);
     const Vec<V> g = scan_round<V, RESETS, CLUSTER>(own, round, w.warps, w.rank, C, maps, blocks, exchange, state);
     if (!busy) continue;
     if (plain)
-      backward_apply<E, V, LERP, true>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, gates, g);
+      backward_apply<E, V, MODE, LERP, true>(in, tile + w.lane, tile + kTile<MODE> + w.lane, m, fresh, q, gates, g);
     else
-      backward_apply<E, V, LERP, false>(tile + w.lane, tile + kTile + w.lane, dhs, m, fresh, q, gates, g);
-    store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves);
-    store_tile<E, MODE>(tile + kTile, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves);
+      backward_apply<E, V, MODE, LERP, false>(in, tile + w.lane, tile + kTile<MODE> + w.lane, m, fresh, q, gates, g);
+    store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves, w.slab);
+    store_tile<E, MODE>(tile + kTile<MODE>, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves, w.slab);
   }
   CLUSTER ? cg::this_cluster().sync() : __syncthreads();
   if (!w.on) return;
-  store_zeros<E, V>(at<E>(p.dx, w.b, 0, w.d), p.dx.stride_t, n + first, per_round, p.T);
-  store_zeros<E, V>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T);
+  store_zeros<E>(at<E>(p.dx, w.b, 0, w.d), p.dx.stride_t, n + first, per_round, p.T, w.own);
+  store_zeros<E>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T, w.own);
   if (p.dh0 && first == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) p.dh0[state_at + v] = state.v[v];
+    for (int v = 0; v < V; ++v)
+      if (v < w.own) p.dh0[state_at + v] = state.v[v];
   }
 }
 
@@ -172,10 +183,9 @@ struct Backward {
   static std::array<const gem_seq_t*, 5> tensors(const GlrArgs& p) { return {&p.x, &p.f, &p.dh, &p.dx, &p.df}; }
 };
 
-}  // namespace
-
-cudaError_t launch_backward(int dtype, const GlrArgs& p, int form, cudaStream_t stream) {
-  return launch_tiles<Backward>(dtype, p, form, stream);
+template <typename E>
+cudaError_t launch_backward(const GlrArgs& p, int form, cudaStream_t stream) {
+  return launch_tiles<Backward, E>(p, form, stream);
 }
 
 }  // namespace glr

@@ -191,5 +191,9 @@ inline int launch_status(cudaError_t e) {
   return GEM_ECUDA;
 }
 
+// Calls F<E>(...) for the element type `dtype`.
+#define BY_TYPE(F, ...) \
+  (dtype == GEM_F32 ? F<float>(__VA_ARGS__) : dtype == GEM_BF16 ? F<__nv_bfloat16>(__VA_ARGS__) : F<__half>(__VA_ARGS__))
+
 }  // namespace lm
 }  // namespace gem

@@ -1539,12 +1539,6 @@ bool temperature_ok(float tau) { return tau >= 1.0e-20f && tau <= 1.0e20f; }
 using namespace gem;
 using namespace gem::lm;
 
-// Calls LAUNCH<E>(...) for the element type.
-#define LAUNCH_BY_TYPE(LAUNCH, ...)                                  \
-  launch_status(dtype == GEM_F32    ? LAUNCH<float>(__VA_ARGS__)         \
-                : dtype == GEM_BF16 ? LAUNCH<__nv_bfloat16>(__VA_ARGS__) \
-                                    : LAUNCH<__half>(__VA_ARGS__))
-
 extern "C" {
 
 int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld, int K,
@@ -1560,7 +1554,7 @@ int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
   if (grad && (!grad_ok(dtype, V, grad, grad_ld) || (grad == logits && grad_ld != ld))) return GEM_EINVAL;
   const DistillArgs p = {logits, grad, ld, grad_ld, int(V), K, top_idx, top_logits, teacher_lse,
                          labels, row_scale, temperature, alpha, loss};
-  return LAUNCH_BY_TYPE(launch_distill, p, dtype, N, static_cast<cudaStream_t>(stream));
+  return launch_status(BY_TYPE(launch_distill, p, dtype, N, static_cast<cudaStream_t>(stream)));
 }
 
 int gem_token_logp(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
@@ -1573,7 +1567,7 @@ int gem_token_logp(int dtype, int64_t N, int64_t V, const void* logits, int64_t 
   if (!optional_ok(logp) || !optional_ok(entropy) || !optional_ok(lse)) return GEM_EINVAL;
   if (logp && !array_ok(tokens)) return GEM_EINVAL;
   const LogpArgs p = {logits, ld, int(V), K, tokens, temperature, logp, entropy, lse, top_idx, top_logp};
-  return LAUNCH_BY_TYPE(launch_logp, p, dtype, N, static_cast<cudaStream_t>(stream));
+  return launch_status(BY_TYPE(launch_logp, p, dtype, N, static_cast<cudaStream_t>(stream)));
 }
 
 int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
@@ -1586,7 +1580,7 @@ int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int
   if (!array_ok(lse) || !optional_ok(dlogp) || !optional_ok(dentropy)) return GEM_EINVAL;
   if ((dlogp && !array_ok(tokens)) || (dentropy && !array_ok(entropy))) return GEM_EINVAL;
   const LogpGradArgs p = {logits, grad, ld, grad_ld, int(V), tokens, temperature, lse, entropy, dlogp, dentropy};
-  return LAUNCH_BY_TYPE(launch_logp_grad, p, N, static_cast<cudaStream_t>(stream));
+  return launch_status(BY_TYPE(launch_logp_grad, p, N, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
