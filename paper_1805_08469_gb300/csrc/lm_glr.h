@@ -344,20 +344,29 @@ __device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_
       from += stride;
     }
   } else {
-#pragma unroll 4
-    for (int k = 0; k < kChunk; ++k, from += stride) {
-      if (k >= m) break;
-      const int odd = int(reinterpret_cast<uintptr_t>(from) >> 1 & 1);
+    const uint32_t odd = odd_rows<E, MODE>(from, stride);
+    if ((odd & 1) && from == data) {
+      // the first word would start before the tensor: its second half alone
+      if (lane == 0)
+        for (int k = 0; k < m; ++k)
+          if (from + k * stride == data) reinterpret_cast<E*>(tile + k * kPitch<MODE>)[1] = *from;
+    }
+    // bytes of the lane's word that lie in the slab or before it, in even and odd rows
+    const int c = 2 * lane, even_bytes = c + 1 < slab ? 4 : c < slab ? 2 : 0, odd_bytes = c < slab ? 4 : c - 1 < slab ? 2 : 0;
+    const bool one_more = lane == 0 && slab == 64;
+    const E* word = from + c;
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
       uint32_t* const row = tile + k * kPitch<MODE>;
-      const int c = 2 * lane - odd;   // the word's first channel
-      if (c < 0 && from == data) {
-        // the word would start before the tensor: its second half alone
-        reinterpret_cast<E*>(row)[1] = *from;
-      } else if (c < slab) {
-        // (the half before the slab is read with it, that after the slab is not)
-        copy_word(row + lane, from + c, c + 1 < slab ? 4 : 2);
+      if (k < m) {
+        if (odd >> k & 1) {
+          if (odd_bytes && (lane > 0 || word != data)) copy_word(row + lane, word - 1, odd_bytes);
+          if (one_more) copy_word(row + 32, word + 63, 2);
+        } else if (even_bytes) {
+          copy_word(row + lane, word, even_bytes);
+        }
       }
-      if (lane == 0 && odd && slab == 64) copy_word(row + 32, from + 63, 2);
+      word += stride;
     }
   }
 }
@@ -383,19 +392,29 @@ __device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t 
       to += stride;
     }
   } else {
-#pragma unroll 4
-    for (int k = 0; k < kChunk; ++k, to += stride) {
-      if (k >= m) break;
+    const uint32_t odd = odd_rows<E, MODE>(to, stride);
+    const int c = 2 * lane;
+    E* word = to + c;
+#pragma unroll
+    for (int k = 0; k < kChunk; ++k) {
       const uint32_t* const row = tile + k * kPitch<MODE> + lane;
-      const bool odd = reinterpret_cast<uintptr_t>(to) >> 1 & 1;
-      const uint32_t w = row[0];
-      const E* const halves = reinterpret_cast<const E*>(&w);
-      const int c = 2 * lane + odd;   // first channel of the lane's aligned word
-      if (c + 1 < slab)
-        *reinterpret_cast<uint32_t*>(to + c) = odd ? __funnelshift_r(w, row[1], 16) : w;
-      else if (c < slab)
-        to[c] = halves[odd];
-      if (odd && lane == 0) to[0] = halves[0];
+      if (k < m) {
+        const uint32_t w = row[0];
+        const E* const halves = reinterpret_cast<const E*>(&w);
+        if (odd >> k & 1) {
+          // the aligned word of channels c + 1 and c + 2
+          if (c + 2 < slab)
+            *reinterpret_cast<uint32_t*>(word + 1) = __funnelshift_r(w, row[1], 16);
+          else if (c + 1 < slab)
+            word[1] = halves[1];
+          if (lane == 0) word[0] = halves[0];
+        } else if (c + 1 < slab) {
+          *reinterpret_cast<uint32_t*>(word) = w;
+        } else if (c < slab) {
+          word[0] = halves[0];
+        }
+      }
+      word += stride;
     }
   }
   __syncwarp();
