@@ -459,11 +459,11 @@ __device__ __forceinline__ Vec<2> second_exponential(const Vec<2>& first, const 
 // A thread's sums over its pieces (t, t + T, ...), relative to a.m.  after(i) runs when piece i has
 // been read.
 template <typename E, bool ENTROPY, Hard HARD, bool CLAMP, typename F>
-__device__ __forceinline__ void thread_sums(const uint4* data, int pieces, int T, float c, Stats& a, F after) {
+__device__ __forceinline__ void thread_sums(const uint4* data, int pieces, int t, int T, float c, Stats& a, F after) {
   const Vec<2> ref = splat<2>(a.m == -INFINITY ? -0.0f : -a.m), scale = splat<2>(c);
   Vec<2> s = splat<2>(0.0f), e = s, s1 = s;
 #pragma unroll 2
-  for (int i = threadIdx.x; i < pieces; i += T) {
+  for (int i = t; i < pieces; i += T) {
     Vec<2> v[kPairs<E>];
     unpack<E>(data[i], v);
     after(i);
@@ -486,10 +486,10 @@ __device__ __forceinline__ void thread_sums(const uint4* data, int pieces, int T
 }
 
 template <typename E>
-__device__ __forceinline__ float thread_max(const uint4* data, int pieces, int T) {
+__device__ __forceinline__ float thread_max(const uint4* data, int pieces, int t, int T) {
   float m = -INFINITY;
 #pragma unroll 4
-  for (int i = threadIdx.x; i < pieces; i += T) m = fmaxf(m, piece_max<E>(data[i]));
+  for (int i = t; i < pieces; i += T) m = fmaxf(m, piece_max<E>(data[i]));
   return m;
 }
 
@@ -747,6 +747,51 @@ __device__ __forceinline__ Vec<2> outside_grad(Vec<2> v, const Coefficients& k, 
   return fma<2>(splat<2>(k.k_hard), Vec<2>{exp2_grad<E>(y.v[0]), exp2_grad<E>(y.v[1])}, splat<2>(k.k_out) * e);
 }
 
+// Writes the gradient of one piece (live: of a row whose scale is not 0) to out, at any alignment.
+template <typename E, Hard HARD>
+__device__ __forceinline__ void write_piece(const uint4& w, bool live, E* out, bool aligned, const Coefficients& k, float c) {
+  Vec<2> v[kPairs<E>];
+  if (live) unpack<E>(w, v);
+#pragma unroll
+  for (int m = 0; m < kPairs<E>; ++m) v[m] = live ? outside_grad<E, HARD>(v[m], k, c) : splat<2>(0.0f);
+  const uint4 g = pack<E>(v);
+  if (aligned) {
+    *reinterpret_cast<uint4*>(out) = g;
+  } else {
+    const E* e = reinterpret_cast<const E*>(&g);
+#pragma unroll
+    for (int m = 0; m < kPer<E>; ++m) out[m] = e[m];
+  }
+}
+
+// The entries' and the label's own values of a row (zl: the label's logit), over what was written there.
+// One warp calls.
+template <typename E, Hard HARD>
+__device__ __forceinline__ void write_entries(const DistillArgs& p, const Teacher& t, const Coefficients& k, float c, int label,
+                                              bool label_is_entry, float zl, E* out) {
+  const int lane = threadIdx.x % 32;
+  for (int i = lane; i < p.K; i += 32) {
+    const int j = t.at[i];
+    if (j < 0) continue;
+    const float d = t.z[i] - k.ref;
+    float g = k.k_soft * (exp2_grad<E>(d * c) * k.inv_s * k.factor - t.q[i]);
+    if (HARD && label >= 0) g += k.k_one * (k.inv_s1 * exp2_grad<E>(d * kLog2e) - (j == label ? 1.0f : 0.0f));
+    out[j] = from_f32<E>(g);
+  }
+  if (HARD && lane == 0 && label >= 0 && label < p.V && !label_is_entry)
+    out[label] = from_f32<E>(outside_grad<E, HARD>(splat<2>(zl), k, c).v[0] - k.k_one);
+}
+
+// A row's loss.
+template <Hard HARD>
+__device__ __forceinline__ float row_loss(const DistillArgs& p, const Coefficients& k, const Entries& entries, int label, float zl) {
+  const float kl = entries.mass == 0.0f ? 0.0f : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
+  float loss = (1.0f - p.alpha) * p.tau * p.tau * (kl + k.kl_rest);
+  if (HARD && label >= 0)
+    loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);
+  return loss;
+}
+
 template <typename E, Hard HARD>
 __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const DistillArgs p, int64_t N, int C, int slots) {
   extern __shared__ uint4 data[];
@@ -790,8 +835,8 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
       }
       Stats mine = no_stats();
       if (w != 0.0f) {
-        mine.m = thread_max<E>(data, s.pieces, T);
-        thread_sums<E, false, HARD, false>(data, s.pieces, T, c, mine, [](int) {});
+        mine.m = thread_max<E>(data, s.pieces, tid, T);
+        thread_sums<E, false, HARD, false>(data, s.pieces, tid, T, c, mine, [](int) {});
       }
       publish_stats(mine, all[b], rank, C, parts, c);
       cluster_arrive();
@@ -802,20 +847,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
       const int most = max(s.pieces, next_pieces);
 #pragma unroll 2
       for (int i = tid; i < most; i += T) {
-        if (grads && i < s.pieces) {
-          Vec<2> v[kPairs<E>];
-          if (w != 0.0f) unpack<E>(data[i], v);
-#pragma unroll
-          for (int m = 0; m < kPairs<E>; ++m) v[m] = w != 0.0f ? outside_grad<E, HARD>(v[m], k, c) : splat<2>(0.0f);
-          const uint4 g = pack<E>(v);
-          if (aligned) {
-            *reinterpret_cast<uint4*>(out + int64_t(i) * kPer<E>) = g;
-          } else {
-            const E* e = reinterpret_cast<const E*>(&g);
-#pragma unroll
-            for (int m = 0; m < kPer<E>; ++m) out[int64_t(i) * kPer<E> + m] = e[m];
-          }
-        }
+        if (grads && i < s.pieces) write_piece<E, HARD>(data[i], w != 0.0f, out + int64_t(i) * kPer<E>, aligned, k, c);
         if (i < next_pieces) load_piece(data + i, next.data() + i);
       }
       load_commit();
@@ -836,18 +868,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
   int last_label = -1;
   bool label_is_entry = false;
   bool pending = false;   // the entries' and the label's own values of the row before, over what was written there
-  auto finish = [&](const Teacher& t) {
-    for (int i = lane; i < p.K; i += 32) {
-      const int j = t.at[i];
-      if (j < 0) continue;
-      const float d = t.z[i] - k.ref;
-      float g = k.k_soft * (exp2_grad<E>(d * c) * k.inv_s * k.factor - t.q[i]);
-      if (HARD && last_label >= 0) g += k.k_one * (k.inv_s1 * exp2_grad<E>(d * kLog2e) - (j == last_label ? 1.0f : 0.0f));
-      out[j] = from_f32<E>(g);
-    }
-    if (HARD && lane == 0 && last_label >= 0 && last_label < p.V && !label_is_entry)
-      out[last_label] = from_f32<E>(outside_grad<E, HARD>(splat<2>(zl), k, c).v[0] - k.k_one);
-  };
+  auto finish = [&](const Teacher& t) { write_entries<E, HARD>(p, t, k, c, last_label, label_is_entry, zl, out); };
   int b = 0;
   for (; n < N; n += step, b ^= 1) {
     const E* z = logits + n * p.ld;
@@ -883,10 +904,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
       if (live) {
         const Stats rest = collect_stats(all[b], C, parts, c);
         k = coefficients<HARD>(p, rest, entries.top, entries.mass, w, label, c);
-        const float kl = entries.mass == 0.0f ? 0.0f : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
-        loss = (1.0f - p.alpha) * p.tau * p.tau * (kl + k.kl_rest);
-        if (HARD && label >= 0)
-          loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);
+        loss = row_loss<HARD>(p, k, entries, label, zl);
       }
       if (lane == 0) p.loss[n] = loss;
       if (grads && je >= 0) out[je] = from_f32<E>(live ? outside_grad<E, HARD>(splat<2>(ze), k, c).v[0] : 0.0f);
@@ -946,8 +964,12 @@ __device__ __forceinline__ float key_value(unsigned long long key) {
 }
 __device__ __forceinline__ int key_index(unsigned long long key) { return int(~unsigned(key)); }
 
+// Group maxima that may reach a bound: 8 or K / 4 more than the K it takes, but no more than two thirds of the
+// groups (the elements that do grow without limit towards all of them), and K at least.
+__device__ __forceinline__ int bound_reach(int G, int K) { return max(K, min(K + (K < 32 ? 8 : K / 4), 2 * G / 3)); }
+
 // A value that at least K of the G (at least K) values reach, and hardly more do: bisection over the
-// floats in their order, ended when at most 8 or K / 4 too many remain.  One warp calls.
+// floats in their order, ended when few too many remain.  One warp calls.
 __device__ __forceinline__ float group_bound(const float* values, int G, int K) {
   const int lane = threadIdx.x % 32;
   auto order = [](float v) {
@@ -972,7 +994,8 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
   hi = __reduce_max_sync(~0u, hi);
   // K values reach lo; fewer than K reach hi + 1
   int reach = G;
-  while (lo < hi && reach > K + (K < 32 ? 8 : K / 4)) {
+  const int enough = bound_reach(G, K);
+  while (lo < hi && reach > enough) {
     const int mid = int((int64_t(lo) + hi + 1) >> 1);
     int n = 0;
     each([&](int v) { n += v >= mid; });
@@ -1101,6 +1124,19 @@ __device__ __forceinline__ void warp_sort(unsigned long long (&v)[N]) {
     }
 }
 
+// The list's `total` keys (at most 32 N), sorted: f(rank, key) for the first K.
+template <int N, typename F>
+__device__ __forceinline__ void write_sorted(const unsigned long long* list, int total, int K, F f) {
+  const int lane = threadIdx.x % 32;
+  unsigned long long v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = e * 32 + lane < total ? list[e * 32 + lane] : 0ull;
+  warp_sort<N, 1, 32 * N>(v);
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (e * 32 + lane < K) f(e * 32 + lane, v[e]);
+}
+
 template <typename E>
 __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const LogpArgs p, int64_t N, int C, int slots, int group_lanes) {
   extern __shared__ uint4 data[];
@@ -1133,7 +1169,7 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
       float second = -INFINITY;
       int where = 0;
       if (p.K == 0) {
-        mine.m = thread_max<E>(data, s.pieces, T);
+        mine.m = thread_max<E>(data, s.pieces, tid, T);
       } else {
 #pragma unroll 4
         for (int i = tid, round = 0; i < s.pieces; i += T, ++round) {
@@ -1144,13 +1180,13 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
         }
       }
       const float m = mine.m;
-      thread_sums<E, true, kNoLabels, false>(data, s.pieces, T, c, mine, [&](int i) {
+      thread_sums<E, true, kNoLabels, false>(data, s.pieces, tid, T, c, mine, [&](int i) {
         if (i < next_pieces) load_piece(data + i, next.data() + i);
       });
       for (int i = s.pieces + (tid - s.pieces % T + T) % T; i < next_pieces; i += T) load_piece(data + i, next.data() + i);
       load_commit();
       // 0 times -inf, from logits of -inf or far below the others: again, with their x bounded
-      if (isnan(mine.e)) thread_sums<E, true, kNoLabels, true>(s.data(), s.pieces, T, c, mine, [](int) {});
+      if (isnan(mine.e)) thread_sums<E, true, kNoLabels, true>(s.data(), s.pieces, tid, T, c, mine, [](int) {});
       // the side warps have read what the row before last left in these buffers
       if (row > 0) cluster_wait();
       publish_stats(mine, all[b], rank, C, parts, c);
@@ -1388,6 +1424,206 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
   }
 }
 
+// ---- short rows: a warp for each, nothing shared between warps ----
+
+constexpr int kShortWarps = 4;          // rows of a block
+constexpr int kShortPieces = 512;       // most whole pieces of a row (8 KB)
+constexpr int kShortOwn = kShortPieces / 32;
+constexpr int kShortList = 256;
+static_assert(kShortList >= GEM_TOP_MAX, "the list holds K");
+
+// The warp's part of dynamic shared memory.
+template <typename X>
+__device__ __forceinline__ X* warp_part(uint4* shared, size_t bytes_of_warp) {
+  return reinterpret_cast<X*>(reinterpret_cast<char*>(shared) + threadIdx.x / 32 * bytes_of_warp);
+}
+
+// Copies the row's pieces to the slots and waits for them (the lane's own, and after the warp's barrier all).
+template <typename E>
+__device__ __forceinline__ void load_row(const Slice<E>& s, uint4* slots) {
+  for (int i = threadIdx.x % 32; i < s.pieces; i += 32) load_piece(slots + i, s.data() + i);
+  load_commit();
+}
+
+template <typename E, Hard HARD>
+__global__ void __launch_bounds__(kShortWarps * 32) distill_short_kernel(const DistillArgs p, int64_t N, unsigned warp_bytes, int slots) {
+  extern __shared__ uint4 shared[];
+  pdl_entry();
+  const int64_t n = int64_t(blockIdx.x) * kShortWarps + threadIdx.x / 32;
+  if (n >= N) return;
+  const int lane = threadIdx.x % 32;
+  uint4* const data = warp_part<uint4>(shared, warp_bytes);
+  const E* z = static_cast<const E*>(p.logits) + n * p.ld;
+  E* const grad = p.grad ? static_cast<E*>(p.grad) + n * p.grad_ld : nullptr;
+  const Slice<E> s = slice_of(z, p.V, 0, 1);
+  const float w = p.row_scale ? p.row_scale[n] : 1.0f;
+  const bool live = w != 0.0f, tail = p.teacher_lse != nullptr;
+  const float c = kLog2e * (1.0f / p.tau);
+  const int je = lane < s.edges() ? s.edge(lane) : -1;
+  Coefficients k = {};
+  Entries entries = {};
+  const Teacher t = teacher_at(data + slots, p.K, 0);
+  float ze = 0.0f, zl = 0.0f, loss = 0.0f;
+  int label = -1;
+  if (live) {
+    load_row(s, data);
+    if (je >= 0) ze = to_f32(z[je]);
+    if constexpr (HARD) {
+      label = p.labels[n];
+      if (label >= 0 && label < p.V) zl = to_f32(z[label]);
+    }
+    entries = read_teacher<E>(p, n, s, label, c, t);
+    load_wait();
+    __syncwarp();
+    if (tail) {
+      for (int i = lane; i < p.K; i += 32) {
+        const int at = t.at[i] - s.index(0);
+        if (t.at[i] >= 0 && at >= 0 && at < s.pieces * kPer<E>) reinterpret_cast<E*>(data)[at] = from_f32<E>(-INFINITY);
+      }
+      __syncwarp();
+    }
+    Stats mine = no_stats();
+    mine.m = thread_max<E>(data, s.pieces, lane, 32);
+    thread_sums<E, false, HARD, false>(data, s.pieces, lane, 32, c, mine, [](int) {});
+    if (je >= 0 && !(entries.edges_here >> lane & 1)) join(mine, one_element(ze), c);
+    k = coefficients<HARD>(p, warp_join(mine, c), entries.top, entries.mass, w, label, c);
+    loss = row_loss<HARD>(p, k, entries, label, zl);
+  }
+  if (lane == 0) p.loss[n] = loss;
+  if (!grad) return;
+  E* const out = grad + s.index(0);
+  const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
+  for (int i = lane; i < s.pieces; i += 32) write_piece<E, HARD>(data[i], live, out + i * kPer<E>, aligned, k, c);
+  if (je >= 0) grad[je] = from_f32<E>(live ? outside_grad<E, HARD>(splat<2>(ze), k, c).v[0] : 0.0f);
+  if (!live) return;
+  __syncwarp();
+  write_entries<E, HARD>(p, t, k, c, label, entries.label_here, zl, grad);
+}
+
+template <typename E>
+__global__ void __launch_bounds__(kShortWarps * 32) token_logp_short_kernel(const LogpArgs p, int64_t N, unsigned warp_bytes, int slots) {
+  extern __shared__ uint4 shared[];
+  pdl_entry();
+  const int64_t n = int64_t(blockIdx.x) * kShortWarps + threadIdx.x / 32;
+  if (n >= N) return;
+  const int lane = threadIdx.x % 32;
+  uint4* const data = warp_part<uint4>(shared, warp_bytes);
+  const E* z = static_cast<const E*>(p.logits) + n * p.ld;
+  const Slice<E> s = slice_of(z, p.V, 0, 1);
+  load_row(s, data);
+  const float inv_tau = 1.0f / p.tau, c = kLog2e * inv_tau;
+  const int je = lane < s.edges() ? s.edge(lane) : -1;
+  const float ze = je >= 0 ? to_f32(z[je]) : -INFINITY;
+  int y = -1;
+  float zy = 0.0f;
+  if (p.logp) {
+    y = p.tokens[n];
+    if (y >= 0 && y < p.V) zy = to_f32(z[y]);
+  }
+  load_wait();
+  Stats mine = no_stats();
+  mine.m = thread_max<E>(data, s.pieces, lane, 32);
+  thread_sums<E, true, kNoLabels, false>(data, s.pieces, lane, 32, c, mine, [](int) {});
+  if (isnan(mine.e)) thread_sums<E, true, kNoLabels, true>(data, s.pieces, lane, 32, c, mine, [](int) {});
+  if (je >= 0) join(mine, one_element(ze), c);
+  const Stats r = warp_join(mine, c);
+  const bool empty = r.m == -INFINITY && r.s == 0.0f;
+  const float ref = r.m == -INFINITY ? 0.0f : r.m, log_s = empty ? 0.0f : logf(r.s);
+  if (lane == 0) {
+    if (p.entropy) p.entropy[n] = empty ? 0.0f : log_s - r.e / r.s * (1.0f / kLog2e);
+    if (p.lse) p.lse[n] = empty ? -INFINITY : ref * inv_tau + log_s;
+    if (p.logp) p.logp[n] = y < 0 ? 0.0f : y >= p.V ? NAN : (zy - ref) * inv_tau - log_s;
+  }
+  if (p.K == 0) return;
+  unsigned long long* const list = reinterpret_cast<unsigned long long*>(data + slots);
+  // a bound as in the kernel above, with the lanes' pieces as groups where there are 2 K of them, else the
+  // elements themselves
+  auto order = [](float v) {
+    const int u = __float_as_int(v);
+    return u ^ (u >> 31 & 0x7fffffff);
+  };
+  float best[kShortOwn];
+  int lo = INT32_MAX, hi = INT32_MIN;
+#pragma unroll
+  for (int e = 0; e < kShortOwn; ++e) {
+    best[e] = lane + 32 * e < s.pieces ? piece_max<E>(data[lane + 32 * e]) : -INFINITY;
+    if (lane + 32 * e < s.pieces) lo = min(lo, order(best[e]));
+  }
+  hi = order(r.m);
+  const bool by_piece = s.pieces >= 2 * p.K;
+  lo = by_piece ? __reduce_min_sync(~0u, lo) : order(-INFINITY);
+  int reach = by_piece ? s.pieces : p.V;
+  const int enough = by_piece ? bound_reach(s.pieces, p.K) : max(p.K, min(p.K + 64, kShortList));
+  auto value = [](int o) { return __int_as_float(o ^ (o >> 31 & 0x7fffffff)); };
+  while (lo < hi && reach > enough) {
+    const int mid = int((int64_t(lo) + hi + 1) >> 1);
+    const float x = value(mid);
+    int count = 0;
+#pragma unroll
+    for (int e = 0; e < kShortOwn; ++e) {
+      if (32 * e >= s.pieces) break;
+      if (by_piece) {
+        count += best[e] >= x && lane + 32 * e < s.pieces;
+      } else if (best[e] >= x && lane + 32 * e < s.pieces) {
+        Vec<2> v[kPairs<E>];
+        unpack<E>(data[lane + 32 * e], v);
+#pragma unroll
+        for (int k = 0; k < kPer<E>; ++k) count += v[k / 2].v[k % 2] >= x;
+      }
+    }
+    if (!by_piece) count += je >= 0 && ze >= x;
+    count = __reduce_add_sync(~0u, count);
+    if (count >= p.K) {
+      lo = mid;
+      reach = count;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  const float bound = value(lo);
+  // the elements that reach it
+  auto each_hit = [&](auto f) {
+    if (je >= 0 && ze >= bound) f(ze, je);
+    for (int i = lane; i < s.pieces; i += 32) {
+      const uint4 w = data[i];
+      if (piece_max<E>(w) < bound) continue;
+      Vec<2> v[kPairs<E>];
+      unpack<E>(w, v);
+#pragma unroll
+      for (int k = 0; k < kPer<E>; ++k)
+        if (v[k / 2].v[k % 2] >= bound) f(v[k / 2].v[k % 2], s.index(i) + k);
+    }
+  };
+  int hits = 0;
+  each_hit([&](float, int) { ++hits; });
+  int at = hits;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int other = __shfl_up_sync(~0u, at, d);
+    if (lane >= d) at += other;
+  }
+  int total = __shfl_sync(~0u, at, 31);
+  at -= hits;
+  if (isnan(r.s) || total > kShortList) {
+    const bool finite = !isnan(r.s);
+    exact_top<E>(z, p.V, p.K, finite ? value_order(bound) : 1u, finite ? value_order(r.m) : value_order(NAN), list, kShortList);
+    total = p.K;
+  } else {
+    each_hit([&](float v, int j) { list[at++] = order_key(v, j); });
+  }
+  __syncwarp();
+  auto write = [&](int k, unsigned long long key) {
+    p.top_idx[n * p.K + k] = key_index(key);
+    p.top_logp[n * p.K + k] = (key_value(key) - ref) * inv_tau - log_s;
+  };
+  if (total <= 32)
+    write_sorted<1>(list, total, p.K, write);
+  else if (total <= 128)
+    write_sorted<4>(list, total, p.K, write);
+  else
+    write_sorted<8>(list, total, p.K, write);
+}
+
 // ---- gradient of log probability and entropy: one pass over a row's pieces, cut over blocks ----
 
 constexpr int kGradPieces = 4;   // of a thread
@@ -1461,7 +1697,7 @@ struct RowCut {
   size_t smem;
 };
 
-RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
+RowCut row_cut(int dtype, int64_t N, int64_t V, int side_warps) {
   constexpr int64_t kSlice = 65 << 10, kLeast = 8 << 10, kMost = 188 << 10;
   const int64_t bytes = V * dtype_size(dtype);
   RowCut c = {1, kRowThreads, 0, 0};
@@ -1470,7 +1706,6 @@ RowCut row_cut(int dtype, int64_t N, int64_t V, int K, int side_warps) {
   c.slots = int((bytes / 16 + c.cluster - 1) / c.cluster);
   c.smem = size_t(c.slots) * 16;
   if (int64_t(c.smem) > kMost) return {0, 0, 0, 0};
-  if (c.smem <= 8192 && K <= 128) c.threads = 128;
   c.threads += 32 * side_warps;
   return c;
 }
@@ -1486,20 +1721,41 @@ cudaError_t launch_rows(const RowCut& c, int64_t N, cudaStream_t stream, const A
   return launch_cluster_pdl(KERNEL, unsigned(grid), unsigned(c.threads), unsigned(c.cluster), c.smem, stream, args...);
 }
 
+// Rows of up to 8 KB take a warp each.
+template <auto KERNEL, typename Args>
+cudaError_t launch_short(const Args& p, int dtype, int64_t N, size_t more_bytes, cudaStream_t stream) {
+  const int slots = int(int64_t(p.V) * dtype_size(dtype) / 16);
+  const unsigned warp_bytes = unsigned((size_t(slots) * 16 + more_bytes + 15) / 16 * 16);
+  const size_t shared = size_t(warp_bytes) * kShortWarps;
+  const cudaError_t e = allow_shared<KERNEL>(shared);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(KERNEL, dim3(unsigned((N + kShortWarps - 1) / kShortWarps)), dim3(kShortWarps * 32), shared, stream, p, N,
+                    warp_bytes, slots);
+}
+bool row_is_short(int dtype, int64_t V) { return V * dtype_size(dtype) <= kShortPieces * 16; }
+
+template <typename E, Hard HARD>
+cudaError_t launch_distill_as(const DistillArgs& p, int dtype, int64_t N, const RowCut& c, cudaStream_t stream) {
+  if (row_is_short(dtype, p.V)) return launch_short<distill_short_kernel<E, HARD>>(p, dtype, N, teacher_bytes(p.K), stream);
+  return launch_rows<distill_kernel<E, HARD>>(c, N, stream, p, N, c.cluster, c.slots);
+}
+
 template <typename E>
 cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  RowCut c = row_cut(dtype, N, p.V, p.K, 1);
+  RowCut c = row_cut(dtype, N, p.V, 1);
   if (c.cluster == 0) return launch_pdl(distill_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   c.smem += teacher_bytes(p.K);
-  if (p.alpha == 0.0f) return launch_rows<distill_kernel<E, kNoLabels>>(c, N, stream, p, N, c.cluster, c.slots);
-  if (p.tau == 1.0f) return launch_rows<distill_kernel<E, kTau1>>(c, N, stream, p, N, c.cluster, c.slots);
-  if (p.tau == 2.0f) return launch_rows<distill_kernel<E, kTau2>>(c, N, stream, p, N, c.cluster, c.slots);
-  return launch_rows<distill_kernel<E, kOwnExponential>>(c, N, stream, p, N, c.cluster, c.slots);
+  if (p.alpha == 0.0f) return launch_distill_as<E, kNoLabels>(p, dtype, N, c, stream);
+  if (p.tau == 1.0f) return launch_distill_as<E, kTau1>(p, dtype, N, c, stream);
+  if (p.tau == 2.0f) return launch_distill_as<E, kTau2>(p, dtype, N, c, stream);
+  return launch_distill_as<E, kOwnExponential>(p, dtype, N, c, stream);
 }
 
 template <typename E>
 cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t stream) {
-  RowCut c = row_cut(dtype, N, p.V, p.K, 2);
+  if (row_is_short(dtype, p.V))
+    return launch_short<token_logp_short_kernel<E>>(p, dtype, N, p.K > 0 ? kShortList * sizeof(unsigned long long) : 0, stream);
+  RowCut c = row_cut(dtype, N, p.V, 2);
   if (c.cluster == 0) return launch_pdl(token_logp_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   // the widest groups of which there are at least 2 K with elements (T C of one lane: at least K)
   const int T = c.threads - 64, busy = (c.slots < T ? c.slots : T) * c.cluster;
