@@ -318,9 +318,14 @@ __device__ __forceinline__ Place place_of(const GlrArgs& p, int C) {
 // make the rest spill.
 __device__ __forceinline__ void keep_out_of_registers(int64_t& stride) { asm volatile("" : "+l"(stride)); }
 
-__device__ __forceinline__ void copy_word(uint32_t* slot, const void* from, int bytes) {
+// Copies a word, or its first BYTES bytes.
+template <int BYTES>
+__device__ __forceinline__ void copy_word(uint32_t* slot, const void* from) {
   const uint32_t s = static_cast<uint32_t>(__cvta_generic_to_shared(slot));
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(s), "l"(from), "r"(bytes) : "memory");
+  if constexpr (BYTES == 4)
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(s), "l"(from) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(s), "l"(from), "n"(BYTES) : "memory");
 }
 
 // Starts the copy of rows 0..m of a tile; from: the row of step 0 at the lane's channels (move_d); data:
@@ -340,7 +345,7 @@ __device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_
   } else if constexpr (MODE == kWord) {
 #pragma unroll
     for (int k = 0; k < kChunk; ++k) {
-      if (k < m) copy_word(tile + k * 32 + lane, from, 4);
+      if (k < m) copy_word<4>(tile + k * 32 + lane, from);
       from += stride;
     }
   } else {
@@ -351,22 +356,36 @@ __device__ __forceinline__ void fetch_tile(uint32_t* tile, const E* from, int64_
         for (int k = 0; k < m; ++k)
           if (from + k * stride == data) reinterpret_cast<E*>(tile + k * kPitch<MODE>)[1] = *from;
     }
-    // bytes of the lane's word that lie in the slab or before it, in even and odd rows
-    const int c = 2 * lane, even_bytes = c + 1 < slab ? 4 : c < slab ? 2 : 0, odd_bytes = c < slab ? 4 : c - 1 < slab ? 2 : 0;
-    const bool one_more = lane == 0 && slab == 64;
-    const E* word = from + c;
+    // every other row starts alike: in a word's middle or not
+    const int c = 2 * lane;
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      uint32_t* const row = tile + k * kPitch<MODE>;
-      if (k < m) {
-        if (odd >> k & 1) {
-          if (odd_bytes && (lane > 0 || word != data)) copy_word(row + lane, word - 1, odd_bytes);
-          if (one_more) copy_word(row + 32, word + 63, 2);
-        } else if (even_bytes) {
-          copy_word(row + lane, word, even_bytes);
+    for (int r = 0; r < 2; ++r) {
+      const E* word = from + r * stride + c;
+      if (odd >> r & 1) {
+        const bool full = c < slab, half = c == slab, one_more = lane == 0 && slab == 64;
+        const bool before = lane == 0 && from == data, all_before = before && stride == 0;   // (copied above)
+#pragma unroll
+        for (int k = r; k < kChunk; k += 2) {
+          uint32_t* const row = tile + k * kPitch<MODE>;
+          if (k < m) {
+            if (full && !(k == 0 ? before : all_before)) copy_word<4>(row + lane, word - 1);
+            if (half) copy_word<2>(row + lane, word - 1);
+            if (one_more) copy_word<2>(row + 32, word + 63);
+          }
+          word += 2 * stride;
+        }
+      } else {
+        const bool full = c + 1 < slab, half = c + 1 == slab;
+#pragma unroll
+        for (int k = r; k < kChunk; k += 2) {
+          uint32_t* const row = tile + k * kPitch<MODE>;
+          if (k < m) {
+            if (full) copy_word<4>(row + lane, word);
+            if (half) copy_word<2>(row + lane, word);
+          }
+          word += 2 * stride;
         }
       }
-      word += stride;
     }
   }
 }
@@ -394,27 +413,37 @@ __device__ __forceinline__ void store_tile(const uint32_t* tile, E* to, int64_t 
   } else {
     const uint32_t odd = odd_rows<E, MODE>(to, stride);
     const int c = 2 * lane;
-    E* word = to + c;
 #pragma unroll
-    for (int k = 0; k < kChunk; ++k) {
-      const uint32_t* const row = tile + k * kPitch<MODE> + lane;
-      if (k < m) {
-        const uint32_t w = row[0];
-        const E* const halves = reinterpret_cast<const E*>(&w);
-        if (odd >> k & 1) {
-          // the aligned word of channels c + 1 and c + 2
-          if (c + 2 < slab)
-            *reinterpret_cast<uint32_t*>(word + 1) = __funnelshift_r(w, row[1], 16);
-          else if (c + 1 < slab)
-            word[1] = halves[1];
-          if (lane == 0) word[0] = halves[0];
-        } else if (c + 1 < slab) {
-          *reinterpret_cast<uint32_t*>(word) = w;
-        } else if (c < slab) {
-          word[0] = halves[0];
+    for (int r = 0; r < 2; ++r) {
+      E* word = to + r * stride + c;
+      if (odd >> r & 1) {
+        // the aligned word of channels c + 1 and c + 2; the slab's first channel and an even last one alone
+        const bool full = c + 2 < slab, half = c + 2 == slab;
+#pragma unroll
+        for (int k = r; k < kChunk; k += 2) {
+          const uint32_t* const row = tile + k * kPitch<MODE> + lane;
+          if (k < m) {
+            const uint32_t w = row[0];
+            const E* const halves = reinterpret_cast<const E*>(&w);
+            if (full) *reinterpret_cast<uint32_t*>(word + 1) = __funnelshift_r(w, row[1], 16);
+            if (half) word[1] = halves[1];
+            if (lane == 0) word[0] = halves[0];
+          }
+          word += 2 * stride;
+        }
+      } else {
+        const bool full = c + 1 < slab, half = c + 1 == slab;
+#pragma unroll
+        for (int k = r; k < kChunk; k += 2) {
+          const uint32_t w = tile[k * kPitch<MODE> + lane];
+          const E* const halves = reinterpret_cast<const E*>(&w);
+          if (k < m) {
+            if (full) *reinterpret_cast<uint32_t*>(word) = w;
+            if (half) word[0] = halves[0];
+          }
+          word += 2 * stride;
         }
       }
-      word += stride;
     }
   }
   __syncwarp();
