@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
       if (!top) r += expf((to_f32(z[i]) - ref) * inv_tau);
     }
     r = block_reduce(r, buf, Sum());
-    const float qr = r > 0.0f ? fmaxf(1.0f - mass, 0.0f) : 0.0f;
+    const float qr = r == 0.0f ? 0.0f : fmaxf(1.0f - mass, 0.0f);
     if (qr > 0.0f) {
       kl += qr * (logf(qr) - logf(r * inv_s));
       inside += qr;
@@ -718,11 +718,13 @@ __device__ __forceinline__ Coefficients coefficients(const DistillArgs& p, const
   k.log_s = r.s == 0.0f ? 0.0f : logf(r.s);
   // With q_rest the factor of p_j outside the entries is mass + q_rest - q_rest / p_rest.  Exponentials
   // outside are taken relative to the largest logit there, low.
-  k.low = tail && rest.s > 0.0f ? rest.m : k.ref;
+  // (a NaN logit makes the rest's sum NaN, and with it all of the row)
+  const bool rest_left = tail && !(rest.s == 0.0f);
+  k.low = rest_left ? rest.m : k.ref;
   k.factor = mass;
   k.kl_rest = 0.0f;
   float rest_share = 0.0f;
-  if (tail && rest.s > 0.0f) {
+  if (rest_left) {
     const float qr = fmaxf(1.0f - mass, 0.0f);
     k.factor += qr;
     rest_share = qr / rest.s;
