@@ -24,6 +24,8 @@
  *     timing: sums are taken in an order that the sizes fix.
  *   - Strides and row pitches count elements.  Tensors need the alignment of their element
  *     type, no more (aligned rows are read with wider loads).
+ *   - No kernel waits on another.  Blocks of a cluster of gem_glr_* wait for one another's maps for at
+ *     most two seconds; a wait that ran out shows as NaN in the states from there on.
  *   - Outputs overlap neither inputs nor one another except where a call says so.  A size of
  *     zero is valid and leaves nothing to do.
  */
@@ -121,7 +123,8 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *     = ld: row_scale[n] dL/dlogits.
  * A student logit of -inf has p = 0: its gradient is that of the formula, and the loss is +inf
  * where the teacher gives it mass.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
- * temperature <= 1e20, 0 <= alpha <= 1, 1 <= V <= 2^30, N <= 2^27, ld >= V (or 0: one row of logits for all), grad_ld >= V. */
+ * temperature <= 1e20, 0 <= alpha <= 1, 1 <= V <= 2^30, N <= 2^27,
+ * ld >= V (or 0: one row of logits for all), grad_ld >= V. */
 int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld, int K,
                 const int32_t* top_idx, const float* top_logits, const float* teacher_lse,
                 const int32_t* labels, const float* row_scale, float temperature, float alpha,

@@ -9,7 +9,7 @@ namespace {
 bool sizes_ok(int dtype, int form, int64_t B, int64_t T, int64_t D) {
   if (!dtype_ok(dtype) || (form != GEM_GLR_LERP && form != GEM_GLR_ADD)) return false;
   if (!extent_ok(B) || !extent_ok(T) || !extent_ok(D)) return false;
-  return B == 0 || (D + 31) / 32 <= (int64_t(1) << 27) / B;   // a grid of clusters of up to 8 blocks
+  return B == 0 || (D + 31) / 32 <= (int64_t(1) << 27) / B;   // a block at least for 32 channels of a sequence
 }
 
 // An input: any strides (0: one step or sequence for all).

@@ -71,8 +71,16 @@ __device__ __forceinline__ void gate(Vec<V> f, Vec<V>& a, Vec<V>& b) {
 // thread composes the earlier warps' maps from shared memory, and in a cluster one exchange of the
 // blocks' maps over distributed shared memory.  Every element is read and written once.
 //
-// The copies of a thread's next rounds are in flight while it works (cp.async into slots of its
-// own, which need no barrier), so memory does not wait for the scan.
+// The copies of a warp's next rounds are in flight while it works (cp.async into tiles of its own,
+// which need no block barrier), so memory does not wait for the scan.
+//
+// Forward moves 3, backward 5 elements a step and channel and a 16th of a float of saved state each;
+// about 25 instructions an element of 16 bits are near what the SMs issue in that time.  Measured (bf16,
+// 8 x 4096 x 2048): 69 us and 115 us, 5.8 TB/s both; fp32, 1 x 100,003 x 1024: 267 and 379 us (4.6 and 5.4
+// TB/s), where a round's latency (2.7 us: scan in the block, exchange in a cluster of 8 or 9) shows.
+// Steps that made it so: 16-byte copies through the warp's tile instead of 4-byte ones (157 -> 75 us
+// forward), sums and products of two channels in one instruction, no spilled registers (backward
+// 173 -> 116).
 //
 // A map whose steps contain a reset has A = -1: it forgets the state whatever that holds (0 times
 // an infinity would not).
@@ -135,8 +143,7 @@ __device__ __forceinline__ void send(uint32_t to, const Map<V>& m, uint32_t mbar
                  : "memory");
 }
 
-// Waits until the phase of this parity is complete; false after two seconds (it never takes
-// microseconds unless a block of the cluster is gone).
+// Waits until the phase of this parity is complete; false after two seconds (a round takes microseconds).
 __device__ __forceinline__ bool wait_phase(uint32_t mbarrier, uint32_t parity) {
   uint64_t start = 0;
   for (unsigned i = 1;; ++i) {

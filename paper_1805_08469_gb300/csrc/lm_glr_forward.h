@@ -9,7 +9,7 @@ namespace gem {
 namespace lm {
 namespace glr {
 
-// ---- a few steps: one thread per channel, one step after the other ----
+// ---- a few steps: one thread per channel, one step after the other (1.5 us for 4 x 1 x 1024) ----
 
 template <typename E, bool LERP>
 __global__ void glr_step_kernel(const GlrArgs p) {
