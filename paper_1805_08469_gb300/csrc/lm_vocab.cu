@@ -758,14 +758,17 @@ __device__ __forceinline__ Vec<2> outside_grad(Vec<2> v, const Coefficients& k, 
   return fma<2>(splat<2>(k.k_hard), Vec<2>{exp2_grad<E>(y.v[0]), exp2_grad<E>(y.v[1])}, splat<2>(k.k_out) * e);
 }
 
-// Writes the gradient of one piece (live: of a row whose scale is not 0) to out, at any alignment.
-template <typename E, Hard HARD>
-__device__ __forceinline__ void write_piece(const uint4& w, bool live, E* out, bool aligned, const Coefficients& k, float c) {
-  Vec<2> v[kPairs<E>];
-  if (live) unpack<E>(w, v);
+// Writes the gradient of one piece (LIVE: of a row whose scale is not 0) to out, at any alignment.
+template <typename E, Hard HARD, bool LIVE>
+__device__ __forceinline__ void write_piece(const uint4& w, E* out, bool aligned, const Coefficients& k, float c) {
+  uint4 g = make_uint4(0, 0, 0, 0);
+  if constexpr (LIVE) {
+    Vec<2> v[kPairs<E>];
+    unpack<E>(w, v);
 #pragma unroll
-  for (int m = 0; m < kPairs<E>; ++m) v[m] = live ? outside_grad<E, HARD>(v[m], k, c) : splat<2>(0.0f);
-  const uint4 g = pack<E>(v);
+    for (int m = 0; m < kPairs<E>; ++m) v[m] = outside_grad<E, HARD>(v[m], k, c);
+    g = pack<E>(v);
+  }
   if (aligned) {
     *reinterpret_cast<uint4*>(out) = g;
   } else {
@@ -856,10 +859,19 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
       E* const out = grads ? grads + n * p.grad_ld + s.index(0) : nullptr;
       const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
       const int most = max(s.pieces, next_pieces);
+      auto write = [&](auto live) {
 #pragma unroll 2
-      for (int i = tid; i < most; i += T) {
-        if (grads && i < s.pieces) write_piece<E, HARD>(data[i], w != 0.0f, out + int64_t(i) * kPer<E>, aligned, k, c);
-        if (i < next_pieces) load_piece(data + i, next.data() + i);
+        for (int i = tid; i < most; i += T) {
+          if (i < s.pieces) write_piece<E, HARD, decltype(live)::value>(data[i], out + int64_t(i) * kPer<E>, aligned, k, c);
+          if (i < next_pieces) load_piece(data + i, next.data() + i);
+        }
+      };
+      if (!grads) {
+        for (int i = tid; i < next_pieces; i += T) load_piece(data + i, next.data() + i);
+      } else if (w != 0.0f) {
+        write(std::true_type());
+      } else {
+        write(std::false_type());
       }
       load_commit();
       s = next;
@@ -1504,7 +1516,12 @@ __global__ void __launch_bounds__(kShortWarps * 32) distill_short_kernel(const D
   if (!grad) return;
   E* const out = grad + s.index(0);
   const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
-  for (int i = lane; i < s.pieces; i += 32) write_piece<E, HARD>(data[i], live, out + i * kPer<E>, aligned, k, c);
+  for (int i = lane; i < s.pieces; i += 32) {
+    if (live)
+      write_piece<E, HARD, true>(data[i], out + i * kPer<E>, aligned, k, c);
+    else
+      write_piece<E, HARD, false>(data[i], out + i * kPer<E>, aligned, k, c);
+  }
   if (je >= 0) grad[je] = from_f32<E>(live ? outside_grad<E, HARD>(splat<2>(ze), k, c).v[0] : 0.0f);
   if (!live) return;
   __syncwarp();

@@ -39,9 +39,7 @@ def _dtype(t, what: str) -> int:
 
 
 def _dense(t, what: str, dtype, shape) -> int:
-    """Address of an optional contiguous CUDA tensor of this type and shape."""
-    if t is None:
-        return 0
+    """Address of a contiguous CUDA tensor of this type and shape."""
     if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise TypeError(f"{what}: expected a contiguous {dtype} CUDA tensor")
     if t.shape != shape:
@@ -84,7 +82,7 @@ def gem_glr_saved_count(B: int, T: int, D: int) -> int:
 
 
 def _reset(t, B, T) -> int:
-    return _dense(t.view(torch.uint8) if t is not None and t.dtype is torch.bool else t, "reset", _U8, (B, T))
+    return _dense(t.view(torch.uint8) if t.dtype is torch.bool else t, "reset", _U8, (B, T))
 
 
 def _saved(t, B, T, D):
@@ -100,9 +98,9 @@ def gem_glr_forward(x, f, h, *, form: int = GEM_GLR_LERP, h0=None, lengths=None,
     B, T, D = x.shape
     check(lib().gem_glr_forward(
         _dtype(x, "x"), form, B, T, D, _seq(x, "x", x), _seq(f, "f", x),
-        _dense(h0, "h0", _F32, (B, D)), _dense(lengths, "lengths", _I32, (B,)),
-        _reset(reset, B, T), _seq(h, "h", x),
-        _dense(h_last, "h_last", _F32, (B, D)), _saved(saved, B, T, D),
+        0 if h0 is None else _dense(h0, "h0", _F32, (B, D)), 0 if lengths is None else _dense(lengths, "lengths", _I32, (B,)),
+        0 if reset is None else _reset(reset, B, T), _seq(h, "h", x),
+        0 if h_last is None else _dense(h_last, "h_last", _F32, (B, D)), 0 if saved is None else _saved(saved, B, T, D),
         _stream(stream, x.device)), "gem_glr_forward")
 
 
@@ -115,10 +113,10 @@ def gem_glr_backward(x, f, saved, dh, dx, df, *, form: int = GEM_GLR_LERP, lengt
     B, T, D = x.shape
     check(lib().gem_glr_backward(
         _dtype(x, "x"), form, B, T, D, _seq(x, "x", x), _seq(f, "f", x),
-        _dense(lengths, "lengths", _I32, (B,)), _reset(reset, B, T),
+        0 if lengths is None else _dense(lengths, "lengths", _I32, (B,)), 0 if reset is None else _reset(reset, B, T),
         _saved(saved, B, T, D), _seq(dh, "dh", x),
-        _dense(dh_last, "dh_last", _F32, (B, D)), _seq(dx, "dx", x), _seq(df, "df", x),
-        _dense(dh0, "dh0", _F32, (B, D)), _stream(stream, x.device)), "gem_glr_backward")
+        0 if dh_last is None else _dense(dh_last, "dh_last", _F32, (B, D)), _seq(dx, "dx", x), _seq(df, "df", x),
+        0 if dh0 is None else _dense(dh0, "dh0", _F32, (B, D)), _stream(stream, x.device)), "gem_glr_backward")
 
 
 def gem_distill(logits, top_idx, top_logits, loss, grad=None, *, teacher_lse=None, labels=None,
@@ -130,11 +128,10 @@ def gem_distill(logits, top_idx, top_logits, loss, grad=None, *, teacher_lse=Non
     K = top_idx.shape[1]
     check(lib().gem_distill(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld, K,
-        _dense(top_idx, "top_idx", _I32, (N, K)),
-        _dense(top_logits, "top_logits", _F32, (N, K)),
-        _dense(teacher_lse, "teacher_lse", _F32, (N,)),
-        _dense(labels, "labels", _I32, (N,)),
-        _dense(row_scale, "row_scale", _F32, (N,)), temperature, alpha,
+        _dense(top_idx, "top_idx", _I32, (N, K)), _dense(top_logits, "top_logits", _F32, (N, K)),
+        0 if teacher_lse is None else _dense(teacher_lse, "teacher_lse", _F32, (N,)),
+        0 if labels is None else _dense(labels, "labels", _I32, (N,)),
+        0 if row_scale is None else _dense(row_scale, "row_scale", _F32, (N,)), temperature, alpha,
         _dense(loss, "loss", _F32, (N,)), 0 if grad is None else grad.data_ptr(),
         V if grad is None else _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_distill")
 
@@ -149,10 +146,10 @@ def gem_token_logp(logits, tokens=None, logp=None, entropy=None, *, temperature:
     K = 0 if top_idx is None else top_idx.shape[1]
     check(lib().gem_token_logp(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld,
-        _dense(tokens, "tokens", _I32, (N,)), temperature, K,
-        _dense(logp, "logp", _F32, (N,)), _dense(entropy, "entropy", _F32, (N,)),
-        _dense(lse, "lse", _F32, (N,)), _dense(top_idx, "top_idx", _I32, (N, K)),
-        _dense(top_logp, "top_logp", _F32, (N, K)), _stream(stream, logits.device)), "gem_token_logp")
+        0 if tokens is None else _dense(tokens, "tokens", _I32, (N,)), temperature, K,
+        0 if logp is None else _dense(logp, "logp", _F32, (N,)), 0 if entropy is None else _dense(entropy, "entropy", _F32, (N,)),
+        0 if lse is None else _dense(lse, "lse", _F32, (N,)), 0 if top_idx is None else _dense(top_idx, "top_idx", _I32, (N, K)),
+        0 if top_logp is None else _dense(top_logp, "top_logp", _F32, (N, K)), _stream(stream, logits.device)), "gem_token_logp")
 
 
 def gem_token_logp_grad(logits, tokens, lse, entropy, dlogp, dentropy, grad, *,
@@ -162,8 +159,8 @@ def gem_token_logp_grad(logits, tokens, lse, entropy, dlogp, dentropy, grad, *,
     N, V, ld = _rows(logits, "logits")
     check(lib().gem_token_logp_grad(
         _dtype(logits, "logits"), N, V, logits.data_ptr(), ld,
-        _dense(tokens, "tokens", _I32, (N,)), temperature,
-        _dense(lse, "lse", _F32, (N,)), _dense(entropy, "entropy", _F32, (N,)),
-        _dense(dlogp, "dlogp", _F32, (N,)),
-        _dense(dentropy, "dentropy", _F32, (N,)), grad.data_ptr(),
+        0 if tokens is None else _dense(tokens, "tokens", _I32, (N,)), temperature,
+        0 if lse is None else _dense(lse, "lse", _F32, (N,)), 0 if entropy is None else _dense(entropy, "entropy", _F32, (N,)),
+        0 if dlogp is None else _dense(dlogp, "dlogp", _F32, (N,)),
+        0 if dentropy is None else _dense(dentropy, "dentropy", _F32, (N,)), grad.data_ptr(),
         _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_token_logp_grad")
