@@ -341,12 +341,11 @@ __device__ __forceinline__ void load_piece(uint4* slot, const uint4* from) {
 __device__ __forceinline__ void load_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void load_wait() { asm volatile("cp.async.wait_group 0;" ::: "memory"); }
 
-// The cluster barrier, in two halves.  Relaxed: only that all blocks have started.
+// The cluster barrier, in two halves.  cluster_started: the first half of one that only tells that all
+// blocks have started, which they must have before another writes to them.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ void cluster_start() {
-  asm volatile("barrier.cluster.arrive.relaxed;\n\tbarrier.cluster.wait;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_started() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
 // A barrier of `threads` threads of the block.
 __device__ __forceinline__ void part_sync(int id, int threads) {
   asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
@@ -825,13 +824,14 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
   int64_t n = blockIdx.x / C;
   float w = scale(n);
   int label = label_of(n);
-  cluster_start();
+  cluster_started();
 
   if (tid < T) {
     Slice<E> s = slice_of(logits + n * p.ld, p.V, rank, C);
     if (w != 0.0f)
       for (int i = tid; i < s.pieces; i += T) load_piece(data + i, s.data() + i);
     load_commit();
+    cluster_wait();
     for (int b = 0; n < N; n += step, b ^= 1) {
       // the next row, whose pieces follow this one's
       const float next_w = scale(n + step);
@@ -892,6 +892,7 @@ __global__ void __launch_bounds__(kRowThreads + 32, 3) distill_kernel(const Dist
   bool label_is_entry = false;
   bool pending = false;   // the entries' and the label's own values of the row before, over what was written there
   auto finish = [&](const Teacher& t) { write_entries<E, HARD>(p, t, k, c, last_label, label_is_entry, zl, out); };
+  cluster_wait();
   int b = 0;
   for (; n < N; n += step, b ^= 1) {
     const E* z = logits + n * p.ld;
@@ -1178,12 +1179,13 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
   // rows' rankings go round the cluster's blocks
   int turn = 0;
   auto next_turn = [&] { turn = turn + 1 == C ? 0 : turn + 1; };
-  cluster_start();
+  cluster_started();
 
   if (tid < T) {
     Slice<E> s = slice_of(logits + n * p.ld, p.V, rank, C);
     for (int i = tid; i < s.pieces; i += T) load_piece(data + i, s.data() + i);
     load_commit();
+    cluster_wait();
     for (int b = 0, row = 0; n < N; n += step, b ^= 1, ++row) {
       const Slice<E> next = slice_of(logits + (n + step) * p.ld, p.V, rank, C);
       const int next_pieces = n + step < N ? next.pieces : 0;
@@ -1234,6 +1236,7 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
   if (tid < T + 32) {
     // the search warp: the elements that reach a row's bound (and the edge elements' statistics)
     const unsigned below = (1u << lane) - 1;
+    cluster_wait();
     for (int b = 0; n < N; n += step, b ^= 1, next_turn()) {
       const E* z = logits + n * p.ld;
       const Slice<E> s = slice_of(z, p.V, rank, C);
@@ -1416,6 +1419,7 @@ __global__ void __launch_bounds__(kRowThreads + 64, 3) token_logp_kernel(const L
       done = -1;
     }
   };
+  cluster_wait();
   for (int b = 0;; n += step, b ^= 1, next_turn()) {
     const bool live = n < N, mine = live && p.K > 0 && rank == turn;
     int y = -1;
