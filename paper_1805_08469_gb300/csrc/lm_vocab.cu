@@ -1725,8 +1725,9 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
 
 // How a row is held: blocks of a cluster, threads of a block (the side warps' too) and bytes of
 // shared memory.  Slices of up to 65 KB let three blocks share an SM, so that one waits while others
-// work; few rows are cut further, down to 8 KB, to use more SMs.  cluster = 0: the row does not fit
-// on chip.
+// work; few rows are cut further, down to 8 KB, as long as all their blocks are resident at two an SM (64
+// x 50,001 fp16: 4 blocks a row 8.8 us, 8 of which some wait 12.5).  cluster = 0: the row does not fit on
+// chip.
 struct RowCut {
   int cluster, threads, slots;
   size_t smem;
@@ -1737,7 +1738,7 @@ RowCut row_cut(int dtype, int64_t N, int64_t V, int side_warps) {
   const int64_t bytes = V * dtype_size(dtype);
   RowCut c = {1, kRowThreads, 0, 0};
   while (c.cluster < kRowCluster && bytes > kSlice * c.cluster) c.cluster *= 2;
-  while (c.cluster < kRowCluster && N * c.cluster < 2 * 152 && bytes >= 2 * kLeast * c.cluster) c.cluster *= 2;
+  while (c.cluster < kRowCluster && N * c.cluster * 2 <= 2 * 152 && bytes >= 2 * kLeast * c.cluster) c.cluster *= 2;
   c.slots = int((bytes / 16 + c.cluster - 1) / c.cluster);
   c.smem = size_t(c.slots) * 16;
   if (int64_t(c.smem) > kMost) return {0, 0, 0, 0};
