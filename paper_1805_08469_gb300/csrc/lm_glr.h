@@ -475,7 +475,9 @@ __device__ __forceinline__ uint32_t reset_bits(uint8_t lane_byte, int m) {
 
 // How the work is cut.  About 16 warps fit an SM (128 registers a thread).  Few slabs of channels:
 // clusters share a slab's time, as large ones as leave all slabs resident at once; many: blocks of
-// fewer warps, so that all slabs are resident.  Neither goes past the chunks there are.
+// fewer warps, so that all slabs are resident.  Neither goes past the chunks there are.  A slab for two
+// SMs in three or more: no clusters, whose rounds take longer (bf16, forward: 128 slabs of 4,096 steps
+// 45 us without and 52 in clusters of two; 96 slabs of 8,000 steps 84 and 70 in threes).
 //
 // DIRECTION names the kernel, its tensors copied in, stages and blocks of an SM.
 template <typename DIRECTION, typename E, int V, Mode MODE, bool LERP, bool RESETS>
@@ -485,7 +487,7 @@ cudaError_t launch_form(const GlrArgs& p, cudaStream_t stream) {
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
   auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };
-  int cluster = int(clip(kBlocks * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
+  int cluster = int(clip(3 * slabs > 2 * kSms ? 1 : kBlocks * kSms / slabs, 1, clip((chunks + kMaxWarps - 1) / kMaxWarps, 1, kMaxCluster)));
   if (cluster > 1) {
     constexpr auto kKernel = DIRECTION::template kernel<E, V, MODE, LERP, true, RESETS>();
     cudaError_t e = allow_shared<kKernel, true>(kMaxShared);
