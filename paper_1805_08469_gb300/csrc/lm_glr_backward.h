@@ -58,7 +58,10 @@ __device__ __forceinline__ void backward_apply(const Words& in, uint32_t* dx, ui
                                                const Vec<V> (&q)[kChunk], const Vec<V> (&gates)[2][kKeep<V>], Vec<V> g) {
 #pragma unroll
   for (int k = kChunk - 1; k >= 0; --k) {
-    if (!PLAIN && k >= m) continue;
+    if (!PLAIN && k >= m) {   // a row past the sequence's end
+      dx[k * kPitch<MODE>] = df[k * kPitch<MODE>] = 0u;
+      continue;
+    }
     g = g + unpack<E, V>(read_word<MODE>(in.dh, k, in.odd_dh));
     Vec<V> a, b;
     if constexpr (V == 1) {
@@ -158,13 +161,17 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
       backward_apply<E, V, MODE, LERP, true>(in, tile + w.lane, tile + kTile<MODE> + w.lane, m, fresh, q, gates, g);
     else
       backward_apply<E, V, MODE, LERP, false>(in, tile + w.lane, tile + kTile<MODE> + w.lane, m, fresh, q, gates, g);
-    store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, m, w.lane, w.moves, w.slab);
-    store_tile<E, MODE>(tile + kTile<MODE>, df_out + t0 * p.df.stride_t, p.df.stride_t, m, w.lane, w.moves, w.slab);
+    const int shown = int(p.T - t0 < kChunk ? p.T - t0 : kChunk);
+    store_tile<E, MODE>(tile, dx_out + t0 * p.dx.stride_t, p.dx.stride_t, shown, w.lane, w.moves, w.slab);
+    store_tile<E, MODE>(tile + kTile<MODE>, df_out + t0 * p.df.stride_t, p.df.stride_t, shown, w.lane, w.moves, w.slab);
   }
   CLUSTER ? cg::this_cluster().sync() : __syncthreads();
+  if (chunks < all_chunks) {
+    clear_tile<E, MODE>(ring);
+    store_zeros<E, MODE>(ring, dx_out, p.dx.stride_t, chunks + first, per_round, all_chunks, p.T, w.lane, w.moves, w.slab);
+    store_zeros<E, MODE>(ring, df_out, p.df.stride_t, chunks + first, per_round, all_chunks, p.T, w.lane, w.moves, w.slab);
+  }
   if (!w.on) return;
-  store_zeros<E>(at<E>(p.dx, w.b, 0, w.d), p.dx.stride_t, n + first, per_round, p.T, w.own);
-  store_zeros<E>(at<E>(p.df, w.b, 0, w.d), p.df.stride_t, n + first, per_round, p.T, w.own);
   if (p.dh0 && first == 0) {
 #pragma unroll
     for (int v = 0; v < V; ++v)

@@ -61,13 +61,13 @@ __device__ __forceinline__ Map<V> forward_map(const uint32_t* x, const uint32_t*
 }
 
 template <typename E, int V, Mode MODE, bool PLAIN>
-__device__ __forceinline__ void forward_apply(uint32_t* out, uint32_t fresh, const Vec<V> (&a)[kChunk], const Vec<V> (&u)[kChunk],
+__device__ __forceinline__ void forward_apply(uint32_t* out, int m, uint32_t fresh, const Vec<V> (&a)[kChunk], const Vec<V> (&u)[kChunk],
                                               Vec<V> h) {
 #pragma unroll
   for (int k = 0; k < kChunk; ++k) {
     const Vec<V> moved = fma<V>(a[k], h, u[k]);
     h = !PLAIN && (fresh >> k & 1) ? u[k] : moved;
-    out[k * kPitch<MODE>] = pack<E, V>(h);
+    out[k * kPitch<MODE>] = PLAIN || k < m ? pack<E, V>(h) : 0u;   // (a row past the sequence's end)
   }
 }
 
@@ -140,16 +140,19 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
         if (v < w.own) s[v] = h.v[v];
     }
     if (plain)
-      forward_apply<E, V, MODE, true>(tile + w.lane, fresh, a, u, h);
+      forward_apply<E, V, MODE, true>(tile + w.lane, m, fresh, a, u, h);
     else
-      forward_apply<E, V, MODE, false>(tile + w.lane, fresh, a, u, h);
-    store_tile<E, MODE>(tile, h_out + t0 * p.h.stride_t, p.h.stride_t, m, w.lane, w.moves, w.slab);
+      forward_apply<E, V, MODE, false>(tile + w.lane, m, fresh, a, u, h);
+    store_tile<E, MODE>(tile, h_out + t0 * p.h.stride_t, p.h.stride_t, int(p.T - t0 < kChunk ? p.T - t0 : kChunk), w.lane, w.moves, w.slab);
   }
   // all have read h0 before it is replaced, and no block leaves before what the others sent it
   CLUSTER ? cg::this_cluster().sync() : __syncthreads();
-  if (!w.on) return;
   // past the sequence's end: zeros, and the state as it stays
-  store_zeros<E>(at<E>(p.h, w.b, 0, w.d), p.h.stride_t, n + first, per_round, p.T, w.own);
+  if (chunks < all_chunks) {
+    clear_tile<E, MODE>(ring);
+    store_zeros<E, MODE>(ring, h_out, p.h.stride_t, chunks + first, per_round, all_chunks, p.T, w.lane, w.moves, w.slab);
+  }
+  if (!w.on) return;
   if (p.saved_out)
     for (int64_t c = chunks + first; c < all_chunks; c += per_round)
 #pragma unroll
