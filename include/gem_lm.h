@@ -150,7 +150,8 @@ int gem_token_logp(int dtype, int64_t N, int64_t V, const void* logits, int64_t 
  *   grad_j = (dlogp ([j = token] - p_j) - dentropy p_j (log p_j + entropy)) / temperature
  *
  * with dlogp [N] and dentropy [N] (either may be NULL: zeros), and lse [N] and, with dentropy,
- * entropy [N] as that call wrote them.  A row without a token has no first term; one with a
+ * entropy [N] as that call wrote them.  (In a row whose |lse| is 128 or more, where the rounding of lse would
+ * show in p, maximum and sum are found again from the logits, which takes longer.)  A row without a token has no first term; one with a
  * token >= V gets NaN (both as dlogp is given).  grad may be logits with grad_ld = ld. */
 int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
                         const int32_t* tokens, float temperature, const float* lse,

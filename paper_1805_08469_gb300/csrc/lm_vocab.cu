@@ -1678,19 +1678,88 @@ __global__ void __launch_bounds__(kShortWarps * 32) token_logp_short_kernel(cons
 //
 // lse and entropy come from the forward call, so an element is read, transformed and written: HBM
 // bound (2048 x 32000 fp32: 75 us, 6.3 TB/s of reads and writes under the profiler).
+//
+// p = exp(z / tau - lse) has the rounding of lse as its relative error: up to 2^-18 below kFarLse.  Rows
+// beyond it (low temperatures, logits with a common offset, an lse past fp32) are taken by their first block
+// alone, which finds their maximum and sum again and forms (z - m) / tau - log s, where nothing cancels
+// (2048 x 32000 fp32, every row such: 125 us; one row of 131072 bf16: 28.5 against 6.8).
 
 constexpr int kGradPieces = 4;   // of a thread
+constexpr float kFarLse = 128.0f;
+
+// log p = (z - ref) / tau - off
+struct GradRow {
+  float inv_tau, ref, off;
+  float none;        // 0: a row without mass, where p = 0
+  float dl, dh, H;   // dlogp, dentropy, entropy
+  int y;
+};
+
+// The gradients of elements j and j + 1.  FAR: ref is not 0.
+template <typename E, bool FAR>
+__device__ __forceinline__ Vec<2> score_grad(const GradRow& r, Vec<2> v, int j) {
+  if constexpr (FAR) v = v + splat<2>(-r.ref);
+  const Vec<2> lp = fma<2>(v, splat<2>(r.inv_tau), splat<2>(-r.off)), x = lp * splat<2>(kLog2e);
+  const Vec<2> e = Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])} * splat<2>(-r.none);
+  const Vec<2> bounded = {fmaxf(lp.v[0], -1000.0f), fmaxf(lp.v[1], -1000.0f)};
+  Vec<2> g = e * fma<2>(splat<2>(r.dh), bounded, splat<2>(fmaf(r.dh, r.H, r.dl)));
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+    if (j + m == r.y) g.v[m] += r.dl;
+  return g * splat<2>(r.inv_tau);
+}
+
+template <typename E, bool FAR>
+__device__ __forceinline__ void write_score_grad(const GradRow& r, const uint4& w, E* grad, int j, bool aligned) {
+  Vec<2> v[kPairs<E>];
+  unpack<E>(w, v);
+#pragma unroll
+  for (int k = 0; k < kPairs<E>; ++k) v[k] = score_grad<E, FAR>(r, v[k], j + 2 * k);
+  const uint4 o = pack<E>(v);
+  if (aligned) {
+    *reinterpret_cast<uint4*>(grad + j) = o;
+  } else {
+    const E* e = reinterpret_cast<const E*>(&o);
+#pragma unroll
+    for (int k = 0; k < kPer<E>; ++k) grad[j + k] = e[k];
+  }
+}
+
+// A whole row by one block.  grad may be the row itself: all have read it before the first store, and then
+// each thread reads a piece before it writes there.
+template <typename E>
+__device__ __noinline__ void far_row_grad(const E* z, int V, E* grad, GradRow r) {
+  __shared__ Stats all[kRowThreads / 32];
+  const int tid = threadIdx.x;
+  const Slice<E> s = slice_of(z, V, 0, 1);
+  const bool aligned = reinterpret_cast<uintptr_t>(grad + s.index(0)) % 16 == 0;
+  const float c = kLog2e * r.inv_tau;
+  const int je = tid < s.edges() ? s.edge(tid) : -1;
+  const float ze = je >= 0 ? to_f32(z[je]) : 0.0f;
+  Stats mine = no_stats();
+  mine.m = thread_max<E>(s.data(), s.pieces, tid, kRowThreads);
+  thread_sums<E, false, kNoLabels, false>(s.data(), s.pieces, tid, kRowThreads, c, mine, [](int) {});
+  if (je >= 0) join(mine, one_element(ze), c);
+  mine = warp_join(mine, c);
+  if (tid % 32 == 0) all[tid / 32] = mine;
+  __syncthreads();
+  const Stats row = collect_stats(all, 1, kRowThreads / 32, c);
+  r.ref = row.m == -INFINITY ? 0.0f : row.m;
+  r.off = row.s == 0.0f ? 0.0f : logf(row.s);
+  r.none = row.s == 0.0f ? 0.0f : 1.0f;
+  for (int i = tid; i < s.pieces; i += kRowThreads) write_score_grad<E, true>(r, s.data()[i], grad, s.index(i), aligned);
+  if (je >= 0) grad[je] = from_f32<E>(score_grad<E, true>(r, splat<2>(ze), je).v[0]);
+}
 
 template <typename E>
-__global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const LogpGradArgs p, int blocks_per_row) {
+__global__ void __launch_bounds__(kRowThreads, 8) token_logp_grad_kernel(const LogpGradArgs p, int blocks_per_row) {
   pdl_entry();
   const int64_t n = blockIdx.x / blocks_per_row;
   const int part = blockIdx.x % blocks_per_row;
   const E* z = static_cast<const E*>(p.logits) + n * p.ld;
   const Slice<E> s = slice_of(z, p.V, 0, 1);
   E* const grad = static_cast<E*>(p.grad) + n * p.grad_ld;
-  E* const out = grad + s.index(0);
-  const bool aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
+  const bool aligned = reinterpret_cast<uintptr_t>(grad + s.index(0)) % 16 == 0;
   const int first = part * kGradPieces * kRowThreads + threadIdx.x;
   uint4 w[kGradPieces];
 #pragma unroll
@@ -1698,7 +1767,6 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
     if (first + i * kRowThreads < s.pieces) w[i] = s.data()[first + i * kRowThreads];
   const int je = part == 0 && int(threadIdx.x) < s.edges() ? s.edge(threadIdx.x) : -1;
   const float ze = je >= 0 ? to_f32(z[je]) : 0.0f;
-  const float inv_tau = 1.0f / p.tau;
   const float lse = p.lse[n];
   int y = -1;
   float dl = 0.0f;
@@ -1706,39 +1774,18 @@ __global__ void __launch_bounds__(kRowThreads) token_logp_grad_kernel(const Logp
     y = p.tokens[n];
     if (y >= 0) dl = y < p.V ? p.dlogp[n] : NAN;
   }
-  const float dh = p.dentropy ? p.dentropy[n] : 0.0f;
-  const float H = p.dentropy ? p.entropy[n] : 0.0f;
-  const float none = lse == -INFINITY ? 0.0f : 1.0f;   // a row without mass: p = 0
-  const float off = lse == -INFINITY ? 0.0f : lse;
-  auto value = [&](Vec<2> v, int j) {
-    const Vec<2> lp = fma<2>(v, splat<2>(inv_tau), splat<2>(-off)), x = lp * splat<2>(kLog2e);
-    const Vec<2> e = Vec<2>{exp2_grad<E>(x.v[0]), exp2_grad<E>(x.v[1])} * splat<2>(-none);
-    const Vec<2> bounded = {fmaxf(lp.v[0], -1000.0f), fmaxf(lp.v[1], -1000.0f)};
-    Vec<2> g = e * fma<2>(splat<2>(dh), bounded, splat<2>(fmaf(dh, H, dl)));
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-      if (j + m == y) g.v[m] += dl;
-    return g * splat<2>(inv_tau);
-  };
+  const GradRow r = {1.0f / p.tau, 0.0f, lse, 1.0f, dl, p.dentropy ? p.dentropy[n] : 0.0f, p.dentropy ? p.entropy[n] : 0.0f, y};
+  if (fabsf(lse) >= kFarLse) {   // (not NaN)
+    if (part == 0) far_row_grad<E>(z, p.V, grad, r);
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < kGradPieces; ++i) {
     const int piece = first + i * kRowThreads;
     if (piece >= s.pieces) break;
-    const int j = s.index(piece);
-    Vec<2> v[kPairs<E>];
-    unpack<E>(w[i], v);
-#pragma unroll
-    for (int k = 0; k < kPairs<E>; ++k) v[k] = value(v[k], j + 2 * k);
-    const uint4 o = pack<E>(v);
-    if (aligned) {
-      *reinterpret_cast<uint4*>(grad + j) = o;
-    } else {
-      const E* e = reinterpret_cast<const E*>(&o);
-#pragma unroll
-      for (int k = 0; k < kPer<E>; ++k) grad[j + k] = e[k];
-    }
+    write_score_grad<E, false>(r, w[i], grad, s.index(piece), aligned);
   }
-  if (je >= 0) grad[je] = from_f32<E>(value(splat<2>(ze), je).v[0]);
+  if (je >= 0) grad[je] = from_f32<E>(score_grad<E, false>(r, splat<2>(ze), je).v[0]);
 }
 
 // How a row is held: blocks of a cluster, threads of a block (the side warps' too) and bytes of

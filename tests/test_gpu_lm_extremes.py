@@ -1,0 +1,88 @@
+"""The language-model operators at the ends of their ranges: logits with a common offset, temperatures down to
+the lowest one, a student far surer than its rest, losses of one term only, states that are infinite."""
+import numpy as np
+import pytest
+import torch
+
+import lm_reference as ref
+from lm_reference import U
+from paper_1805_08469_gb300 import lm
+from test_gpu_lm_glr import Case
+from test_gpu_lm_vocab import INF, distill_inputs, distill_run, floats, host, ints, logp_run, rows
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------------- the scores' gradient
+
+
+def grad_reference(z, y, tau, dl, dH, dtype):
+    """(value, bound) of the scores' gradient.  The bound has the errors of (z - max) / tau and of the entropy,
+    neither of which grows with max / tau; subnormal factors of a product add their step."""
+    N, V = z.shape
+    _, lp, p, err_lp, rel_p, _, _ = ref._softmax(z, tau)
+    H, eH = (v[:, None] for v in ref.token_logp(z, y, tau, 0)["entropy"])
+    dl, dH = dl.astype(np.float64)[:, None], dH.astype(np.float64)[:, None]
+    lp = np.where(p > 0, lp, 0)
+    hit = (np.arange(V)[None] == np.asarray(y)[:, None]).astype(np.float64)
+    dl = np.where(np.asarray(y)[:, None] < 0, 0, dl)
+    g = (hit * dl - p * (dl + dH * (lp + H))) / tau
+    size = np.abs(dl) + np.abs(dH) * (np.abs(lp) + np.abs(H))
+    e = p * ((rel_p + 8 * U) * size + np.abs(dH) * (err_lp + 4 * U * np.abs(lp) + eH)) + 2.0 ** -147 * (1 + size)
+    e = (e + 4 * U * hit * np.abs(dl)) / tau + 4 * U * np.abs(g)
+    return g, 1.01 * e + ref.rounded(g, dtype)
+
+
+def check_grad(v, dtype, tau, pad=1):
+    rng = np.random.default_rng(v.shape[1])
+    N, V = v.shape
+    z = rows(v, dtype, pad=pad)
+    y = rng.integers(-1, V, N)
+    dl, dH = floats(tau * rng.standard_normal(N)), floats(0.1 * tau * rng.standard_normal(N))
+    got = logp_run(z, ints(y), tau, 0, dl, dH)["grad"]
+    ref.check(got, grad_reference(host(z), y, float(np.float32(tau)), host(dl), host(dH), dtype), "grad")
+    assert np.array_equal(logp_run(z, ints(y), tau, 0, dl, dH, grad=z)["grad"], got)   # in place
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [9, 3000, 40001])
+@pytest.mark.parametrize("offset", [1e4, -1e4])
+def test_gradient_of_logits_with_a_common_offset(V, dtype, offset):
+    """Beside ordinary rows, whose values and places they leave alone."""
+    v = 2 * np.random.default_rng(V).standard_normal((6, V))
+    v[1::2] += offset
+    check_grad(v, dtype, 1.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [9, 3000, 40001])
+@pytest.mark.parametrize("tau", [1e-3, 1e-6, 1e-8, 1e-20])
+def test_gradient_at_low_temperatures(V, dtype, tau):
+    """Equal top logits share the mass; neighbouring fp32 numbers lie near tau apart for one of the temperatures."""
+    rng = np.random.default_rng(V)
+    v = rng.standard_normal((5, V))
+    v[0, [1, V - 1]] = 10.3
+    v[1] = -10.3
+    v[2] = np.float32(10.3) + 2.0 ** -20 * rng.integers(-6, 1, V)
+    v[3, V // 2] = 50.0
+    check_grad(v, dtype, tau)
+
+
+def test_gradient_where_the_log_sum_exp_is_past_fp32():
+    v = np.full((4, 700), -1e19)
+    v[0, [3, 600]] = 1e19
+    v[2] = -INF
+    v[3] = 1.0
+    check_grad(v, "f32", 1e-20)
+
+
+def test_gradient_of_rows_that_are_not_finite_beside_an_offset():
+    v = np.random.default_rng(1).standard_normal((4, 9001)) + 1e5
+    v[1, 7] = np.nan
+    v[2, 9000] = INF
+    z = rows(v, "f32")
+    y, one = np.array([3, 3, 3, 3]), np.ones(4)
+    got = logp_run(z, ints(y), 1.0, 0, floats(one), floats(one))["grad"]
+    assert np.isnan(got[1:3]).all()
+    value, bound = grad_reference(host(z)[[0, 3]], y[:2], 1.0, one[:2], one[:2], "f32")
+    ref.check(got[[0, 3]], (value, bound), "grad")
