@@ -146,24 +146,33 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
   row_stats(z, p.V, inv_tau, buf, m, s);
   const float ref = m == -INFINITY ? 0.0f : m;
   const float inv_s = s == 0.0f ? 0.0f : 1.0f / s;
+  const float log_s = logf(s == 0.0f ? 1.0f : s);
   const float zk = there ? to_f32(z[j]) : 0.0f;
-  const float logp = (zk - ref) * inv_tau - logf(s == 0.0f ? 1.0f : s);
+  const float logp = (zk - ref) * inv_tau - log_s;
   float kl = block_reduce(q > 0.0f ? q * (logq - logp) : 0.0f, buf, Sum());
-  float inside = mass, outside = mass;   // factors of p_j in the gradient
+  float inside = mass;             // the factor of p_j in the gradient
+  float low = ref, share = 0.0f;   // outside the entries also -share exp((z_j - low) / tau)
   if (p.teacher_lse) {
-    // the mass outside the entries, summed by itself: 1 - sum p_k would cancel
-    float r = 0.0f;
+    // the mass outside the entries, summed by itself (1 - sum p_k would cancel) and relative to the largest
+    // logit there (relative to the row's it may leave fp32)
+    float top_z = -INFINITY, r = 0.0f;
     for (int i = tid; i < p.V; i += blockDim.x) {
       bool top = false;
       for (int k = 0; k < p.K; ++k) top |= at[k] == i;
-      if (!top) r += expf((to_f32(z[i]) - ref) * inv_tau);
+      const float zi = to_f32(z[i]);
+      if (top || zi == -INFINITY) continue;
+      const float e = expf(-fabsf(zi - top_z) * inv_tau);
+      r = zi > top_z ? r * e + 1.0f : r + e;
+      top_z = fmaxf(top_z, zi);
     }
-    r = block_reduce(r, buf, Sum());
+    const float most = block_reduce(top_z, buf, Max());
+    if (most != -INFINITY) low = most;
+    r = block_reduce(r * expf((top_z - low) * inv_tau), buf, Sum());
     const float qr = r == 0.0f ? 0.0f : fmaxf(1.0f - mass, 0.0f);
     if (qr > 0.0f) {
-      kl += qr * (logf(qr) - logf(r * inv_s));
+      kl += qr * (logf(qr) - (logf(r) + (low - ref) * inv_tau - log_s));
       inside += qr;
-      outside = inside - qr * s / r;
+      share = qr / r;
     }
   }
   const float soft = (1.0f - p.alpha) * p.tau;
@@ -181,16 +190,16 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
   }
   if (tid == 0) p.loss[n] = loss;
   if (!grad) return;
-  auto value = [&](float zj, float factor, float qj, bool is_label) {
-    const float d = zj - ref;
-    float g = soft * (expf(d * inv_tau) * inv_s * factor - qj);
-    if (hard) g += p.alpha * (expf(d) * inv_s1 - (is_label ? 1.0f : 0.0f));
+  const float scale = expf((low - ref) * inv_tau) * inv_s * inside - share;
+  auto value = [&](float zj, bool top, float qj, bool is_label) {
+    float g = soft * (top ? expf((zj - ref) * inv_tau) * inv_s * inside - qj : expf((zj - low) * inv_tau) * scale);
+    if (hard) g += p.alpha * (expf(zj - ref) * inv_s1 - (is_label ? 1.0f : 0.0f));
     return from_f32<E>(w * g);
   };
   // the entries' logits are read before any of the row is replaced (grad may be logits)
-  const E top_grad = first ? value(zk, inside, q_here, j == label) : from_f32<E>(0.0f);
+  const E top_grad = first ? value(zk, true, q_here, j == label) : from_f32<E>(0.0f);
   __syncthreads();
-  for (int i = tid; i < p.V; i += blockDim.x) grad[i] = value(to_f32(z[i]), outside, 0.0f, i == label);
+  for (int i = tid; i < p.V; i += blockDim.x) grad[i] = value(to_f32(z[i]), false, 0.0f, i == label);
   __syncthreads();
   if (first) grad[j] = top_grad;
 }

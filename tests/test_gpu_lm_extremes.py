@@ -86,3 +86,28 @@ def test_gradient_of_rows_that_are_not_finite_beside_an_offset():
     assert np.isnan(got[1:3]).all()
     value, bound = grad_reference(host(z)[[0, 3]], y[:2], 1.0, one[:2], one[:2], "f32")
     ref.check(got[[0, 3]], (value, bound), "grad")
+
+
+# ---------------------------------------------------------------------- the rest as a class
+
+
+def check_distill(z, dtype, idx, top, shown, tau, alpha=0.0, lse=None, labels=None):
+    """shown: the teacher's logits as the 64-bit form gets them."""
+    want = ref.distill(host(z), idx, shown, float(np.float32(tau)), alpha, lse, labels, dtype=dtype)
+    got = distill_run(z, idx, top, tau, alpha, lse, labels)
+    for k in want:
+        ref.check(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 5000), ("f32", 50000), ("f32", 500009), ("bf16", 800001)])
+def test_a_student_far_surer_than_its_rest(dtype, V):
+    """The rest's mass is below fp32's range relative to the row's largest; its class counts all the same."""
+    rng = np.random.default_rng(V)
+    N, K = 5, 4
+    v = rng.standard_normal((N, V))
+    idx = np.stack([rng.choice(V, K, replace=False) for _ in range(N)]).astype(np.int32)
+    for n, gap in enumerate([20, 40, 48, 52, 60]):
+        v[n, idx[n]] = gap + rng.standard_normal(K)
+    top = rng.standard_normal((N, K)).astype(np.float32)
+    lse = (np.log(np.exp(2 * top.astype(np.float64)).sum(1)) - np.log1p(-np.array([0.3, 0.1, 0.02, 0.5, 0.2]))).astype(np.float32)
+    check_distill(rows(v, dtype), dtype, idx, top, top, 0.5, lse=lse)
