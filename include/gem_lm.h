@@ -25,7 +25,8 @@
  *   - Strides and row pitches count elements.  Tensors need the alignment of their element
  *     type, no more (aligned rows are read with wider loads).
  *   - No kernel waits on another.  Blocks of a cluster of gem_glr_* wait for one another's maps for at
- *     most two seconds; a wait that ran out shows as NaN in the states from there on.
+ *     most two seconds; where a wait ran out, every state and gradient that rests on what did not come, and
+ *     all that later steps hand on, are NaN, resets or not.
  *   - Outputs overlap neither inputs nor one another except where a call says so.  A size of
  *     zero is valid and leaves nothing to do.
  */

@@ -118,8 +118,8 @@ __device__ __forceinline__ Map<V> compose(const Map<V>& sofar, const Map<V>& m) 
 // that count their bytes on the receiver's mbarrier, so nothing else (a cluster barrier would wait for
 // all of a block's stores to memory) holds the round up.
 struct Exchange {
-  uint32_t full;   // shared address of two mbarriers, one for each parity of the round
-  bool gave_up;    // a wait passed its limit: the states are NaN from there on
+  uint64_t full[2];    // mbarriers, one for each parity of the round
+  uint32_t gave_up;    // a wait of the block passed its limit: no more of the exchange, and NaN from there on
 };
 
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
@@ -169,16 +169,15 @@ __device__ __forceinline__ bool wait_phase(uint32_t mbarrier, uint32_t parity) {
 
 // Sets the mbarriers up; all threads call.  No block sends before all have.
 template <bool CLUSTER>
-__device__ __forceinline__ Exchange start_exchange(uint64_t (&mbarriers)[2]) {
-  Exchange x = {shared_address(mbarriers), false};
+__device__ __forceinline__ void start_exchange(Exchange& x) {
   if constexpr (CLUSTER) {
     if (threadIdx.x == 0) {
-      for (int b = 0; b < 2; ++b) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(x.full + 8 * b) : "memory");
+      for (int b = 0; b < 2; ++b) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(shared_address(&x.full[b])) : "memory");
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      x.gave_up = 0;
     }
     cg::this_cluster().sync();
   }
-  return x;
 }
 
 // From every thread's map of a round: the state before the thread's chunk, and `state` moved on to
@@ -207,17 +206,21 @@ __device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int w
     if (w == warp) mine = all;
     all = compose<V, RESETS>(all, buf[w * 32]);
   }
+  // (a map that forgets the state must not bring back what rests on a map that did not come; the mbarriers'
+  // phases stay open, so nobody arrives on them again, and the other blocks give up in their turn)
+  volatile uint32_t& gave_up = x.gave_up;
+  if (gave_up) return state = splat<V>(NAN);
   // (a buffer is sent to again two rounds on: by then all have read it, or their maps of the round
   // between would not have come)
   Map<V>* in = blocks + (round & 1) * C * 32 + lane;
-  const uint32_t full = x.full + 8 * (round & 1), slot = shared_address(in + rank * 32);
+  const uint32_t full = shared_address(&x.full[round & 1]), slot = shared_address(in + rank * 32);
   for (int c = warp; c < C; c += warps) send<V>(in_block(slot, c), all, in_block(full, c));
   if (threadIdx.x == 0)
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full), "r"(uint32_t(C * 32 * sizeof(Map<V>)))
                  : "memory");
-  if (!x.gave_up && !wait_phase(full, uint32_t(round >> 1) & 1u)) {
-    x.gave_up = true;
-    state = splat<V>(NAN);
+  if (!wait_phase(full, uint32_t(round >> 1) & 1u)) {
+    gave_up = 1;
+    return state = splat<V>(NAN);
   }
   for (int c = 0; c < C; ++c) {
     if (c == rank) before = state;

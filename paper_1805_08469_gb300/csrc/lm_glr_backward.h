@@ -85,9 +85,9 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
   const int C = CLUSTER ? blocks_of_cluster : 1;
   extern __shared__ __align__(16) uint32_t tiles[];   // [warp][stage][x, f, dh][kTile], then the blocks' maps
   __shared__ Map<V> maps[2 * kMaxWarps * 32];
-  __shared__ uint64_t mbarriers[2];
+  __shared__ Exchange exchange;
   pdl_entry();
-  Exchange exchange = start_exchange<CLUSTER>(mbarriers);
+  start_exchange<CLUSTER>(exchange);
   const Place w = place_of<E, V, MODE>(p, C);
   constexpr int kStage = 3 * kTile<MODE>;
   uint32_t* const ring = tiles + w.warp * kBackwardStages * kStage;
