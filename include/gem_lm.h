@@ -111,7 +111,8 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *     entries has no teacher: its first term is 0.
  *   teacher_lse [N] fp32.  NULL: q = softmax of the row's K entries / tau, q_rest = 0.  Else
  *     q_k = exp(top_logits_k / tau - teacher_lse), where teacher_lse is the teacher's
- *     log-sum-exp of all logits / tau, and q_rest = max(0, 1 - sum q) is compared with p_rest,
+ *     log-sum-exp of all logits / tau (its rounding is q's relative error, |teacher_lse| 2^-24: give
+ *     logits without an offset), and q_rest = max(0, 1 - sum q) is compared with p_rest,
  *     the student's mass outside the entries, as one class; where p_rest is 0 that class is
  *     left out.
  *   labels [N] int32 (required when alpha > 0, not read otherwise): < 0: the row has no label

@@ -115,20 +115,19 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
   float t = -INFINITY;
   if (tid < p.K) {
     j = p.top_idx[n * p.K + tid];
-    if (j >= 0 && j < p.V) t = p.top_logits[n * p.K + tid] * inv_tau;
-    if (t == -INFINITY) j = -1;
+    if (j >= 0 && j < p.V) t = p.top_logits[n * p.K + tid];
+    if (t * inv_tau == -INFINITY) j = -1;
     at[tid] = j;
   }
   const bool there = tid < p.K && j >= 0;
-  float lse;
+  float logq;
   if (p.teacher_lse) {
-    lse = p.teacher_lse[n];
+    logq = t * inv_tau - p.teacher_lse[n];
   } else {
-    const float mt = block_reduce(t, buf, Max());
-    const float st = block_reduce(there ? expf(t - mt) : 0.0f, buf, Sum());
-    lse = mt + logf(st);
+    // (differences first: an offset that the logits share would round q away)
+    const float d = (t - block_reduce(there ? t : -INFINITY, buf, Max())) * inv_tau;
+    logq = d - logf(block_reduce(there ? expf(d) : 0.0f, buf, Sum()));
   }
-  const float logq = t - lse;
   const float q = there ? expf(logq) : 0.0f;
   if (tid < p.K) qs[tid] = q;
   const float mass = block_reduce(q, buf, Sum());   // (its barriers also publish at and qs)
@@ -594,16 +593,18 @@ __device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n,
   for (int e = 0; e < kPerLane; ++e) {
     if (j[e] < 0 || j[e] >= p.V || logq[e] == -INFINITY) j[e] = -1;
     zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
-    logq[e] = j[e] >= 0 ? logq[e] * inv_tau : -INFINITY;
-    if (logq[e] == -INFINITY) j[e] = -1;
-    most = fmaxf(most, logq[e]);
+    if (logq[e] * inv_tau == -INFINITY) j[e] = -1;
+    most = fmaxf(most, j[e] >= 0 ? logq[e] : -INFINITY);
     base = fmaxf(base, zk[e]);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) base = fmaxf(base, __shfl_xor_sync(~0u, base, o));
   if (base == -INFINITY) base = 0.0f;
+  // log q = (logit - most) / tau - lse: without the teacher's own log-sum-exp relative to the largest entry (an
+  // offset that the logits share would round q away)
   float lse;
   if (p.teacher_lse) {
+    most = 0.0f;
     lse = p.teacher_lse[n];
   } else {
 #pragma unroll
@@ -611,8 +612,8 @@ __device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n,
     float sum = 0.0f;
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e)
-      if (e * 32 < p.K && j[e] >= 0) sum += expf(logq[e] - most);
-    lse = most + logf(warp_sum(sum));
+      if (e * 32 < p.K && j[e] >= 0) sum += expf((logq[e] - most) * inv_tau);
+    lse = logf(warp_sum(sum));
   }
   Entries r = {0.0f, 0.0f, base, no_stats(), false, 0u};
 #pragma unroll
@@ -621,7 +622,7 @@ __device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n,
     const int k = e * 32 + lane;
     float q = 0.0f;
     if (j[e] >= 0) {
-      logq[e] -= lse;
+      logq[e] = (logq[e] - most) * inv_tau - lse;
       q = expf(logq[e]);
       r.mass += q;
       if (q != 0.0f) r.cross += q * (logq[e] - (zk[e] - base) * inv_tau);

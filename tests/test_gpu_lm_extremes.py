@@ -111,3 +111,20 @@ def test_a_student_far_surer_than_its_rest(dtype, V):
     top = rng.standard_normal((N, K)).astype(np.float32)
     lse = (np.log(np.exp(2 * top.astype(np.float64)).sum(1)) - np.log1p(-np.array([0.3, 0.1, 0.02, 0.5, 0.2]))).astype(np.float32)
     check_distill(rows(v, dtype), dtype, idx, top, top, 0.5, lse=lse)
+
+
+# ---------------------------------------------------------------------- the teacher's entries
+
+
+SIZES = [("f32", 500), ("bf16", 500), ("f16", 20001), ("f32", 50000), ("f32", 500009)]
+
+
+@pytest.mark.parametrize("dtype,V", SIZES)
+@pytest.mark.parametrize("tau,offset", [(1.0, 1e4), (1.0, -3e4), (1e-3, 10.3), (1e-5, 10.3)])
+def test_teacher_logits_with_a_common_offset(dtype, V, tau, offset):
+    """The softmax of the entries does not know the offset: neither does the bound, which gets the differences
+    from the largest (exact in 64 bits)."""
+    z, idx, top, _ = distill_inputs(V, 3, V, 12, dtype, absent=False)
+    top = (offset + tau * top).astype(np.float32)
+    exact = top.astype(np.float64)
+    check_distill(z, dtype, idx, top, exact - exact.max(1, keepdims=True), tau)
