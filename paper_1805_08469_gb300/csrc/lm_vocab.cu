@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
   if (tid < p.K) {
     j = p.top_idx[n * p.K + tid];
     if (j >= 0 && j < p.V) t = p.top_logits[n * p.K + tid];
-    if (t * inv_tau == -INFINITY) j = -1;
+    if (t == -INFINITY) j = -1;
     at[tid] = j;
   }
   const bool there = tid < p.K && j >= 0;
@@ -593,7 +593,6 @@ __device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n,
   for (int e = 0; e < kPerLane; ++e) {
     if (j[e] < 0 || j[e] >= p.V || logq[e] == -INFINITY) j[e] = -1;
     zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
-    if (logq[e] * inv_tau == -INFINITY) j[e] = -1;
     most = fmaxf(most, j[e] >= 0 ? logq[e] : -INFINITY);
     base = fmaxf(base, zk[e]);
   }
@@ -1500,8 +1499,9 @@ __device__ __forceinline__ void load_row(const Slice<E>& s, uint4* slots) {
   load_commit();
 }
 
+// (eight blocks an SM, 64 registers a thread: 8192 x 1000 bf16 with 8 entries 15.5 us; without that bound 16.4)
 template <typename E, Hard HARD>
-__global__ void __launch_bounds__(kShortWarps * 32) distill_short_kernel(const DistillArgs p, int64_t N, unsigned warp_bytes, int slots) {
+__global__ void __launch_bounds__(kShortWarps * 32, 8) distill_short_kernel(const DistillArgs p, int64_t N, unsigned warp_bytes, int slots) {
   extern __shared__ uint4 shared[];
   pdl_entry();
   const int64_t n = int64_t(blockIdx.x) * kShortWarps + threadIdx.x / 32;

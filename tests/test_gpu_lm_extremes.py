@@ -128,3 +128,13 @@ def test_teacher_logits_with_a_common_offset(dtype, V, tau, offset):
     top = (offset + tau * top).astype(np.float32)
     exact = top.astype(np.float64)
     check_distill(z, dtype, idx, top, exact - exact.max(1, keepdims=True), tau)
+
+
+@pytest.mark.parametrize("dtype,V", SIZES)
+def test_an_entry_of_the_lowest_value_stays_an_entry(dtype, V):
+    """A logit that is finite, but not after its division by tau, has no mass and is none of the rest."""
+    z, idx, top, lse = distill_inputs(V, 3, V, 6, dtype, tau=0.5, tail=True, absent=False)
+    top[:, 4] = np.finfo(np.float32).min
+    for n in range(3):
+        z[n, int(idx[n, 4])] = 6.0
+    check_distill(z, dtype, idx, top, top, 0.5, lse=lse)
