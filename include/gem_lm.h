@@ -117,6 +117,7 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *     left out.
  *   labels [N] int32 (required when alpha > 0, not read otherwise): < 0: the row has no label
  *     and no second term; >= V: the row's loss and gradient are NaN.
+ *   alpha = 1: labels only; the teacher's arrays are checked, but not read.
  *   row_scale [N] fp32, NULL: ones.  The gradient of row n is multiplied by row_scale[n]
  *     (1 / rows for a mean, a loss scale, a mask).  A row whose scale is 0 is not read: its loss
  *     is 0 and its gradient zeros.

@@ -1919,7 +1919,9 @@ int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
   if (!optional_ok(teacher_lse) || !optional_ok(row_scale) || !array_ok(loss)) return GEM_EINVAL;
   if (alpha > 0.0f && !array_ok(labels)) return GEM_EINVAL;
   if (grad && (!grad_ok(dtype, V, grad, grad_ld) || (grad == logits && grad_ld != ld))) return GEM_EINVAL;
-  const DistillArgs p = {logits, grad, ld, grad_ld, int(V), K, top_idx, top_logits, teacher_lse,
+  // labels only: 0 times a term that may be infinite is not 0, so the kernels get no teacher
+  const bool teacher = alpha < 1.0f;
+  const DistillArgs p = {logits, grad, ld, grad_ld, int(V), teacher ? K : 0, top_idx, top_logits, teacher ? teacher_lse : nullptr,
                          labels, row_scale, temperature, alpha, loss};
   return launch_status(BY_TYPE(launch_distill, p, dtype, N, static_cast<cudaStream_t>(stream)));
 }

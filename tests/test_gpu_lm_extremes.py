@@ -138,3 +138,22 @@ def test_an_entry_of_the_lowest_value_stays_an_entry(dtype, V):
     for n in range(3):
         z[n, int(idx[n, 4])] = 6.0
     check_distill(z, dtype, idx, top, top, 0.5, lse=lse)
+
+
+# ---------------------------------------------------------------------- losses of one term
+
+
+@pytest.mark.parametrize("dtype,V", SIZES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0])
+def test_labels_only(dtype, V, tail, tau):
+    """alpha = 1: the teacher's term is not there, whatever it would be."""
+    z, idx, top, lse = distill_inputs(V, 4, V, 6, dtype, tail=tail, absent=False)
+    for n in range(2):
+        z[n, int(idx[n, 2])] = -INF
+    top[2, 1] = np.nan
+    labels = [int(idx[0, 0]), 7, 3, -1]
+    want = ref.distill(host(z), np.full((4, 0), -1), np.zeros((4, 0)), tau, 1.0, None, labels, dtype=dtype)
+    got = distill_run(z, idx, top, tau, 1.0, lse, labels)
+    for k in want:
+        ref.check(got[k], want[k], k)
