@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
     }
   }
   const float soft = (1.0f - p.alpha) * p.tau;
-  float loss = soft * p.tau * kl;
+  float loss = soft * (p.tau * kl);   // (tau^2 may leave fp32)
   int label = -1;
   float inv_s1 = 0.0f;
   const bool hard = p.alpha > 0.0f && (label = p.labels[n]) >= 0;
@@ -808,7 +808,7 @@ __device__ __forceinline__ void write_entries(const DistillArgs& p, const Teache
 template <Hard HARD>
 __device__ __forceinline__ float row_loss(const DistillArgs& p, const Coefficients& k, const Entries& entries, int label, float zl) {
   const float kl = entries.mass == 0.0f ? 0.0f : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
-  float loss = (1.0f - p.alpha) * p.tau * p.tau * (kl + k.kl_rest);
+  float loss = (1.0f - p.alpha) * p.tau * (p.tau * (kl + k.kl_rest));   // (tau^2 may leave fp32)
   if (HARD && label >= 0)
     loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);
   return loss;

@@ -157,3 +157,15 @@ def test_labels_only(dtype, V, tail, tau):
     got = distill_run(z, idx, top, tau, 1.0, lse, labels)
     for k in want:
         ref.check(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("dtype,V", SIZES)
+@pytest.mark.parametrize("tau", [1e-20, 1e19, 5e19, 1e20])
+@pytest.mark.parametrize("alpha", [0.0, 0.5])
+def test_no_teacher_at_the_ends_of_the_temperatures(dtype, V, tau, alpha):
+    z, _, _, _ = distill_inputs(V, 3, V, 6, dtype, absent=False)
+    none, labels = np.full((3, 2), -1), [5, -1, V - 1]
+    want = ref.distill(host(z), none, np.zeros((3, 2)), float(np.float32(tau)), alpha, None, labels, dtype=dtype)
+    got = distill_run(z, none, np.zeros((3, 2)), tau, alpha, None, labels)
+    for k in want:
+        ref.check(got[k], want[k], k)
