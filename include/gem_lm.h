@@ -125,8 +125,8 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *   grad (row n at grad + n * grad_ld, type dtype), may be NULL and may be logits with grad_ld
  *     = ld: row_scale[n] dL/dlogits.
  * A student logit of -inf has p = 0: its gradient is that of the formula, and the loss is +inf
- * where the teacher gives it mass.  The first term's rounding, some 2^-20, is multiplied by tau^2 in the loss
- * and by tau (of p and q) in the gradient.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
+ * where the teacher gives it mass.  A logit of NaN or +inf makes its row's loss and gradient NaN.  The first
+ * term's rounding, some 2^-20, is multiplied by tau^2 in the loss and by tau (of p and q) in the gradient.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
  * temperature <= 1e20, 0 <= alpha <= 1, 1 <= V <= 2^30, N <= 2^27,
  * ld >= V (or 0: one row of logits for all), grad_ld >= V. */
 int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld, int K,

@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) distill_stream_kernel(const DistillA
   const float log_s = logf(s == 0.0f ? 1.0f : s);
   const float zk = there ? to_f32(z[j]) : 0.0f;
   const float logp = (zk - ref) * inv_tau - log_s;
-  float kl = block_reduce(q > 0.0f ? q * (logq - logp) : 0.0f, buf, Sum());
+  float kl = block_reduce(q > 0.0f ? q * (logq - logp) : 0.0f, buf, Sum()) + 0.0f * log_s;   // (NaN of a row without entries)
   float inside = mass;             // the factor of p_j in the gradient
   float low = ref, share = 0.0f;   // outside the entries also -share exp((z_j - low) / tau)
   if (p.teacher_lse) {
@@ -807,7 +807,8 @@ __device__ __forceinline__ void write_entries(const DistillArgs& p, const Teache
 // A row's loss.
 template <Hard HARD>
 __device__ __forceinline__ float row_loss(const DistillArgs& p, const Coefficients& k, const Entries& entries, int label, float zl) {
-  const float kl = entries.mass == 0.0f ? 0.0f : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
+  // (a NaN in the row makes log_s NaN, which a row without entries keeps)
+  const float kl = entries.mass == 0.0f ? 0.0f * k.log_s : entries.cross + entries.mass * ((k.ref - entries.base) * (1.0f / p.tau) + k.log_s);
   float loss = (1.0f - p.alpha) * p.tau * (p.tau * (kl + k.kl_rest));   // (tau^2 may leave fp32)
   if (HARD && label >= 0)
     loss -= p.alpha * (label < p.V ? (zl - k.ref) + (k.inv_s1 == 0.0f ? 0.0f : logf(k.inv_s1)) : NAN);

@@ -169,3 +169,18 @@ def test_no_teacher_at_the_ends_of_the_temperatures(dtype, V, tau, alpha):
     got = distill_run(z, none, np.zeros((3, 2)), tau, alpha, None, labels)
     for k in want:
         ref.check(got[k], want[k], k)
+
+
+@pytest.mark.parametrize("dtype,V", SIZES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("alpha", [0.0, 0.5])
+def test_a_row_of_nan_without_a_teacher(dtype, V, tail, alpha):
+    """What is not a number in a row shows in its loss as in its gradient, with entries or without."""
+    z, idx, top, lse = distill_inputs(V, 4, V, 6, dtype, tail=tail, absent=False)
+    idx[1:] = -1
+    z[1, V // 2] = float("nan")
+    z[2, 3] = INF
+    got = distill_run(z, idx, top, 1.0, alpha, lse, [-1] * 4)
+    for k in got:
+        assert np.isnan(got[k][1:3]).all() and np.isfinite(got[k][[0, 3]]).all(), k
+    assert got["loss"][3] == 0
