@@ -57,7 +57,8 @@ typedef struct {
  *   GEM_GLR_LERP   h_t = a_t h_{t-1} + (1 - a_t) x_t
  *   GEM_GLR_ADD    h_t = a_t h_{t-1} + x_t
  *
- * from h_{-1} = h0. */
+ * from h_{-1} = h0.  f below -80 counts as -80 (a = 2e-35), so that an infinite state, or gradient, stays
+ * infinite until a reset. */
 enum gem_glr_form { GEM_GLR_LERP = 0, GEM_GLR_ADD = 1 };
 
 /* Steps between the states that gem_glr_forward saves for gem_glr_backward. */

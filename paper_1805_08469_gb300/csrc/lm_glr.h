@@ -82,6 +82,9 @@ __device__ __forceinline__ void gate(Vec<V> f, Vec<V>& a, Vec<V>& b) {
 // forward), sums and products of two channels in one instruction, no spilled registers (backward
 // 173 -> 116).
 //
+// A is 2^-149 at least (at_least_some): gates are above 0, so that a state of infinity stays one, while 0 times
+// it is NaN.  (Of a finite state that lets through 5e-7 at the most.)
+//
 // A map whose steps contain a reset has A = -1: it forgets the state whatever that holds (0 times
 // an infinity would not).
 
@@ -92,6 +95,12 @@ template <int V>
 struct Map {
   Vec<V> A, H;
 };
+
+template <int V>
+__device__ __forceinline__ void at_least_some(Vec<V>& A) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) A.v[k] = A.v[k] == 0.0f ? __uint_as_float(1u) : A.v[k];
+}
 
 // h after the map m, and m after the maps composed so far.  RESETS: a map may forget.
 template <int V, bool RESETS>
@@ -206,6 +215,8 @@ __device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int w
     if (w == warp) mine = all;
     all = compose<V, RESETS>(all, buf[w * 32]);
   }
+  at_least_some<V>(all.A);
+  at_least_some<V>(mine.A);
   // (a map that forgets the state must not bring back what rests on a map that did not come; the mbarriers'
   // phases stay open, so nobody arrives on them again, and the other blocks give up in their turn)
   volatile uint32_t& gave_up = x.gave_up;

@@ -184,3 +184,43 @@ def test_a_row_of_nan_without_a_teacher(dtype, V, tail, alpha):
     for k in got:
         assert np.isnan(got[k][1:3]).all() and np.isfinite(got[k][[0, 3]]).all(), k
     assert got["loss"][3] == 0
+
+
+# ---------------------------------------------------------------------- infinite states
+
+
+@pytest.mark.parametrize("form", ["lerp", "add"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,T,D,resets", [(2, 700, 66, 0.0), (2, 700, 66, 0.004), (200, 70, 64, 0.0), (200, 70, 64, 0.03)])
+def test_an_infinite_state_stays_one(B, T, D, resets, dtype, form):
+    """However little the gates of a chunk let through, some of an infinity is one: as in calls of a step each."""
+    c = Case(B + T, B, T, D, dtype, form, resets=resets)
+    c.f.fill_(-12.0)
+    c.h0[0, ::2], c.h0[1, ::3] = INF, -INF
+    got, want = c.run(), c.reference()
+    for k in ("h", "h_last", "saved", "dx", "dh0"):
+        ref.check(got[k], want[k], k)
+    state = c.h0.clone()
+    one = torch.empty((B, 1, D), dtype=c.x.dtype, device="cuda")
+    for t in range(40):
+        lm.gem_glr_forward(c.x[:, t:t + 1], c.f[:, t:t + 1], one, form=lm.GEM_GLR_LERP if form == "lerp" else lm.GEM_GLR_ADD, h0=state,
+                           reset=None if c.reset is None else c.reset[:, t:t + 1].contiguous(), h_last=state)
+        h, step = got["h"][:, t], host(one)[:, 0]
+        assert np.array_equal(np.isinf(h), np.isinf(step)) and not np.isnan(h).any()
+
+
+@pytest.mark.parametrize("form", ["lerp", "add"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("B,T,D,resets", [(2, 700, 66, 0.0), (2, 700, 66, 0.004), (200, 70, 64, 0.0), (200, 70, 64, 0.03)])
+def test_an_infinite_gradient_stays_one(B, T, D, resets, dtype, form):
+    """From the last state's and from single steps', at the end, the middle and the start of a chunk."""
+    c = Case(B + T, B, T, D, dtype, form, resets=resets)
+    c.f.fill_(-12.0)
+    c.dh_last[0, ::2] = INF
+    for t, d in ((47, 1), (40, 5), (32, 9)):
+        c.dh[1, t, d] = -INF
+    c.dh[1, T - 1, 13] = INF
+    got, want = c.run(), c.reference()
+    for k in ("h", "dx", "dh0"):
+        ref.check(got[k], want[k], k)
+    assert np.array_equal(np.isfinite(got["df"]), np.isfinite(want["df"][0]))
