@@ -591,9 +591,12 @@ __device__ __forceinline__ Entries read_teacher(const DistillArgs& p, int64_t n,
   }
 #pragma unroll
   for (int e = 0; e < kPerLane; ++e) {
-    if (j[e] < 0 || j[e] >= p.V || logq[e] == -INFINITY) j[e] = -1;
+    if (j[e] < 0 || j[e] >= p.V || logq[e] == -INFINITY) {
+      j[e] = -1;
+      logq[e] = -INFINITY;
+    }
     zk[e] = j[e] >= 0 ? to_f32(z[j[e]]) : -INFINITY;
-    most = fmaxf(most, j[e] >= 0 ? logq[e] : -INFINITY);
+    most = fmaxf(most, logq[e]);
     base = fmaxf(base, zk[e]);
   }
 #pragma unroll
