@@ -504,11 +504,11 @@ __device__ __forceinline__ uint32_t reset_bits(uint8_t lane_byte, int m) {
 // SMs in three or more: no clusters, whose rounds take longer (bf16, forward: 128 slabs of 4,096 steps
 // 45 us without and 52 in clusters of two; 96 slabs of 8,000 steps 84 and 70 in threes).
 //
-// DIRECTION names the kernel, its tensors copied in, stages and blocks of an SM.
+// DIRECTION names the kernel, its tensors copied in and their stages.
 template <typename DIRECTION, typename E, int V, Mode MODE, bool LERP, bool RESETS>
 cudaError_t launch_form(const GlrArgs& p, cudaStream_t stream) {
-  constexpr int kSms = 152, kBlocks = DIRECTION::template blocks<MODE>();
-  constexpr size_t kWarpBytes = size_t(kTile<MODE>) * 4 * DIRECTION::kTensors * DIRECTION::template stages<MODE>();
+  constexpr int kSms = 152, kBlocks = 2;   // (of an SM)
+  constexpr size_t kWarpBytes = size_t(kTile<MODE>) * 4 * DIRECTION::kTensors * DIRECTION::kStages;
   const int64_t chunks = (p.T + kChunk - 1) / kChunk;
   const int64_t slabs = (p.D + 32 * V - 1) / (32 * V) * p.B;
   auto clip = [](int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; };

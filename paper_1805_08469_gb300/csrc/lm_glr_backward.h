@@ -200,10 +200,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_backward_kernel(const G
 
 struct Backward {
   static constexpr int kTensors = 3;
-  template <Mode MODE>
-  static constexpr int stages() { return kBackwardStages; }
-  template <Mode MODE>
-  static constexpr int blocks() { return 2; }
+  static constexpr int kStages = kBackwardStages;
   template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER, bool RESETS>
   static constexpr auto kernel() { return &glr_backward_kernel<E, V, MODE, LERP, CLUSTER, RESETS>; }
   static std::array<const gem_seq_t*, 5> tensors(const GlrArgs& p) { return {&p.x, &p.f, &p.dh, &p.dx, &p.df}; }

@@ -168,10 +168,7 @@ __global__ void __launch_bounds__(kMaxWarps * 32, 2) glr_forward_kernel(const Gl
 
 struct Forward {
   static constexpr int kTensors = 2;
-  template <Mode MODE>
-  static constexpr int stages() { return kForwardStages; }
-  template <Mode MODE>
-  static constexpr int blocks() { return 2; }
+  static constexpr int kStages = kForwardStages;
   template <typename E, int V, Mode MODE, bool LERP, bool CLUSTER, bool RESETS>
   static constexpr auto kernel() { return &glr_forward_kernel<E, V, MODE, LERP, CLUSTER, RESETS>; }
   static std::array<const gem_seq_t*, 3> tensors(const GlrArgs& p) { return {&p.x, &p.f, &p.h}; }
