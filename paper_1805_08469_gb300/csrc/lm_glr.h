@@ -96,10 +96,16 @@ struct Map {
   Vec<V> A, H;
 };
 
-template <int V>
+// (RESETS: A may be -1.  NaN stays)
+template <int V, bool RESETS>
 __device__ __forceinline__ void at_least_some(Vec<V>& A) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) A.v[k] = A.v[k] == 0.0f ? __uint_as_float(1u) : A.v[k];
+  for (int k = 0; k < V; ++k) {
+    if constexpr (RESETS)
+      A.v[k] = A.v[k] == 0.0f ? __uint_as_float(1u) : A.v[k];
+    else
+      asm("max.NaN.f32 %0, %0, 0f00000001;" : "+f"(A.v[k]));
+  }
 }
 
 // h after the map m, and m after the maps composed so far.  RESETS: a map may forget.
@@ -215,8 +221,8 @@ __device__ __forceinline__ Vec<V> scan_round(const Map<V>& own, int round, int w
     if (w == warp) mine = all;
     all = compose<V, RESETS>(all, buf[w * 32]);
   }
-  at_least_some<V>(all.A);
-  at_least_some<V>(mine.A);
+  at_least_some<V, RESETS>(all.A);
+  at_least_some<V, RESETS>(mine.A);
   // (a map that forgets the state must not bring back what rests on a map that did not come; the mbarriers'
   // phases stay open, so nobody arrives on them again, and the other blocks give up in their turn)
   volatile uint32_t& gave_up = x.gave_up;

@@ -23,19 +23,6 @@ struct Words {
 template <int V>
 constexpr int kKeep = V == 1 ? kChunk : 1;
 
-// What a chunk hands back of its own gradients, step by step from its end (or its first reset).
-template <typename E, int V, Mode MODE>
-__device__ __noinline__ Vec<V> handed_back(Words in, int m, uint32_t fresh) {
-  Vec<V> g = splat<V>(0.0f);
-  const int first_reset = fresh ? __ffs(fresh) - 1 : kChunk;
-  for (int k = min(m, first_reset) - 1; k >= 0; --k) {
-    Vec<V> a, b;
-    gate<E, V>(unpack<E, V>(read_word<MODE>(in.f, k, in.odd_f)), a, b);
-    g = a * (g + unpack<E, V>(read_word<MODE>(in.dh, k, in.odd_dh)));
-  }
-  return g;
-}
-
 template <typename E, int V, Mode MODE, bool LERP, bool PLAIN>
 __device__ __forceinline__ Map<V> backward_map(const Words& in, int m, uint32_t fresh,
                                                Vec<V> h, Vec<V> (&q)[kChunk], Vec<V> (&gates)[2][kKeep<V>]) {
@@ -59,15 +46,10 @@ __device__ __forceinline__ Map<V> backward_map(const Words& in, int m, uint32_t 
     if (r) counts = false;
     if (counts) {
       own.A = own.A * a;
+      at_least_some<V, false>(own.A);   // (at every step: any dh may be infinite)
       own.H = fma<V>(own.A, unpack<E, V>(read_word<MODE>(in.dh, k, in.odd_dh)), own.H);
     }
   }
-  // where the gates' product left fp32, an infinity among dh may have met a factor of 0
-  bool none_left = false;
-#pragma unroll
-  for (int v = 0; v < V; ++v) none_left |= own.A.v[v] == 0.0f;
-  if (none_left) own.H = handed_back<E, V, MODE>(in, PLAIN ? kChunk : m, PLAIN ? 0u : fresh);
-  at_least_some<V>(own.A);
   if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
   return own;
 }

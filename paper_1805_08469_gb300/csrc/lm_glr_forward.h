@@ -56,7 +56,7 @@ __device__ __forceinline__ Map<V> forward_map(const uint32_t* x, const uint32_t*
     own.H = !PLAIN && (fresh >> k & 1) ? u[k] : moved;
     own.A = own.A * a[k];
   }
-  at_least_some<V>(own.A);
+  at_least_some<V, false>(own.A);
   if (!PLAIN && fresh) own.A = splat<V>(-1.0f);
   return own;
 }
