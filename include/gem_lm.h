@@ -15,12 +15,15 @@
  * Conventions shared by every call:
  *   - Return value: GEM_OK (0) or a negative gem_status.  Arguments are checked on the host;
  *     a call that fails a check launches nothing.  Calls hold no handle, allocate nothing and
- *     keep nothing from one call for the next.
+ *     keep nothing of their data from one call for the next (only, for each kernel and device, that it may
+ *     use the shared memory that it does, and how many of its clusters fit).
  *   - All pointers are device memory of the current device.  Work is asynchronous and ordered
  *     on `stream` (a cudaStream_t; NULL is the legacy default stream); the caller orders
  *     buffers that other streams use.  Calls can be captured into a CUDA graph.
  *   - Elements are fp32, bf16 or fp16 (gem_dtype), statistics and states fp32.  All arithmetic
- *     is fp32, rounded once when an output of 16 bits is stored.  Results do not depend on
+ *     is fp32, rounded once when an output of 16 bits is stored; exponentials over rows, those of 16-bit
+ *     gates and the gates' quotients are the GPU's approximations (2 units in the last place and what rounding
+ *     the argument adds; a quotient 1).  Results do not depend on
  *     timing: sums are taken in an order that the sizes fix.
  *   - Strides and row pitches count elements.  Tensors need the alignment of their element
  *     type, no more (aligned rows are read with wider loads).
@@ -108,8 +111,8 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *
  * with p = softmax(logits / tau), p1 = softmax(logits), tau = temperature.
  *   top_idx, top_logits [N][K]: the teacher's entries; an index outside [0, V) or a logit of
- *     -inf is an entry that is absent.  Entries with the same index add up.  A row without
- *     entries has no teacher: its first term is 0.
+ *     -inf is an entry that is absent.  Entries with the same index add up in the gradient; the
+ *     loss has a term for each.  A row without entries has no teacher: its first term is 0.
  *   teacher_lse [N] fp32.  NULL: q = softmax of the row's K entries / tau, q_rest = 0.  Else
  *     q_k = exp(top_logits_k / tau - teacher_lse), where teacher_lse is the teacher's
  *     log-sum-exp of all logits / tau (its rounding is q's relative error, |teacher_lse| 2^-24: give
@@ -126,8 +129,9 @@ int gem_glr_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, const
  *   grad (row n at grad + n * grad_ld, type dtype), may be NULL and may be logits with grad_ld
  *     = ld: row_scale[n] dL/dlogits.
  * A student logit of -inf has p = 0: its gradient is that of the formula, and the loss is +inf
- * where the teacher gives it mass.  A logit of NaN or +inf makes its row's loss and gradient NaN.  The first
- * term's rounding, some 2^-20, is multiplied by tau^2 in the loss and by tau (of p and q) in the gradient.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
+ * where the teacher gives it mass.  A logit of NaN or +inf makes its row's loss and gradient NaN.
+ * The first term's rounding, some 2^-20, is multiplied by tau^2 in the loss and by tau (of p and q)
+ * in the gradient.  Requires 0 <= K <= GEM_TOP_MAX, 1e-20 <=
  * temperature <= 1e20, 0 <= alpha <= 1, 1 <= V <= 2^30, N <= 2^27,
  * ld >= V (or 0: one row of logits for all), grad_ld >= V. */
 int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld, int K,
@@ -144,7 +148,8 @@ int gem_distill(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
  *   top_idx, top_logp [N][K] (K = 0: not written): the K largest logits' indices, descending,
  *     equal ones by ascending index, and their log p.  NaN orders above everything.
  * A row whose logits are all -inf has lse -inf, entropy 0 and every log p -inf; in a row with a
- * NaN or +inf logit every value is NaN (the indices are those of the order above).  Requires 0
+ * NaN or +inf logit every value is NaN (logp stays 0 where there is no token; the indices are those of the
+ * order above).  Requires 0
  * <= K <= min(V, GEM_TOP_MAX), 1e-20 <= temperature <= 1e20, V >= 1, ld >= V or 0. */
 int gem_token_logp(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
                    const int32_t* tokens, float temperature, int K, float* logp,
@@ -156,8 +161,9 @@ int gem_token_logp(int dtype, int64_t N, int64_t V, const void* logits, int64_t 
  *
  * with dlogp [N] and dentropy [N] (either may be NULL: zeros), and lse [N] and, with dentropy,
  * entropy [N] as that call wrote them.  (In a row whose |lse| is 128 or more, where the rounding of lse would
- * show in p, maximum and sum are found again from the logits, which takes longer.)  A row without a token has no first term; one with a
- * token >= V gets NaN (both as dlogp is given).  grad may be logits with grad_ld = ld. */
+ * show in p, maximum and sum are found again from the logits, which takes longer.)  A row without a
+ * token has no first term; one with a token >= V gets NaN (both as dlogp is given).  grad may be
+ * logits with grad_ld = ld. */
 int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
                         const int32_t* tokens, float temperature, const float* lse,
                         const float* entropy, const float* dlogp, const float* dentropy,

@@ -76,11 +76,12 @@ __device__ __forceinline__ void gate(Vec<V> f, Vec<V>& a, Vec<V>& b) {
 //
 // Forward moves 3, backward 5 elements a step and channel and a 16th of a float of saved state each;
 // about 25 instructions an element of 16 bits are near what the SMs issue in that time.  Measured (bf16,
-// 8 x 4096 x 2048): 69 us and 115 us, 5.8 TB/s both; fp32, 1 x 100,003 x 1024: 267 and 379 us (4.6 and 5.4
-// TB/s), where a round's latency (2.7 us: scan in the block, exchange in a cluster of 8 or 9) shows.
+// 8 x 4096 x 2048): 69 us and 118 us, 5.8 and 5.7 TB/s; fp32, 1 x 100,003 x 1024 without resets: 243 and 342 us
+// (5.1 and 6.0 TB/s), 2.8 and 3.9 us a round of 72 chunks, of which scan and exchange are waited for (with a reset
+// in 700 steps 259 and 412: a chunk with one takes the path that tests every step).
 // Steps that made it so: 16-byte copies through the warp's tile instead of 4-byte ones (157 -> 75 us
-// forward), sums and products of two channels in one instruction, no spilled registers (backward
-// 173 -> 116).
+// forward), sums and products of two channels in one instruction, gates computed again instead of spilled
+// (backward 173 -> 116).
 //
 // A is 2^-149 at least (at_least_some): gates are above 0, so that a state of infinity stays one, while 0 times
 // it is NaN.  (Of a finite state that lets through 5e-7 at the most.)

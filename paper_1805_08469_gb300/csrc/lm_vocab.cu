@@ -280,8 +280,8 @@ __global__ void __launch_bounds__(kThreads) token_logp_stream_kernel(const LogpA
 //
 // The distillation reads and writes each logit once, the scores read it once.  Per element that is
 // about 18 instructions (scores: 10) and 2 exponentials (1), of which an SM issues 128 and 16 a cycle.
-// Measured, bf16, 4096 x 131072: distillation with 128 entries 420 us (5.1 TB/s), scores 207 us (5.2 TB/s)
-// without alternatives, 261 with 20 of them and 366 with 64, where a row's chain of barrier, search
+// Measured, bf16, 4096 x 131072: distillation with 128 entries 429 us (5.0 TB/s), scores 207 us (5.2 TB/s)
+// without alternatives, 255 with one, 259 with 20 and 356 with 64, where a row's chain of barrier, search
 // and sort is longer than its stream.  A block's slice of 64 KB and 256 threads was the best of 16 to
 // 64 KB and 128 to 256; one pass of blocks without prefetch took 672 and 260 us.
 //
@@ -461,7 +461,7 @@ __device__ __forceinline__ Stats warp_join(Stats a, float c) {
 
 // What the second softmax, that with tau = 1, costs: nothing where there are no labels or tau is 1 itself;
 // where tau is 2, exp(d) = exp(d / 2)^2; else exponentials of its own (4 a logit in both passes, at 16 a
-// cycle and SM: 132 us instead of 105 at 4096 x 32000).
+// cycle and SM: 124 us instead of 110 at 4096 x 32000 with 64 entries).
 enum Hard { kNoLabels, kOwnExponential, kTau1, kTau2 };
 
 template <Hard HARD>
@@ -1031,8 +1031,8 @@ __device__ __forceinline__ float group_bound(const float* values, int G, int K) 
   hi = __reduce_max_sync(~0u, hi);
   // K values reach lo; fewer than K reach hi + 1
   int reach = G;
-  // groups without an element (often the edges') would stretch the range: eight steps more, 400 us
-  // instead of 366 for 4096 x 131072 bf16 with 64 alternatives
+  // groups without an element (often the edges') would stretch the range: eight steps more, a tenth of the
+  // time of 4096 x 131072 bf16 with 64 alternatives
   const int least = order(-INFINITY);
   if (lo == least) {
     int n = 0, low = INT32_MAX;
@@ -1503,7 +1503,7 @@ __device__ __forceinline__ void load_row(const Slice<E>& s, uint4* slots) {
   load_commit();
 }
 
-// (eight blocks an SM, 64 registers a thread: 8192 x 1000 bf16 with 8 entries 15.5 us; without that bound 16.4)
+// (eight blocks an SM, 64 registers a thread: 8192 x 1000 bf16 with 8 entries 15.6 us; without that bound 16.6)
 template <typename E, Hard HARD>
 __global__ void __launch_bounds__(kShortWarps * 32, 8) distill_short_kernel(const DistillArgs p, int64_t N, unsigned warp_bytes, int slots) {
   extern __shared__ uint4 shared[];
@@ -1691,7 +1691,7 @@ __global__ void __launch_bounds__(kShortWarps * 32) token_logp_short_kernel(cons
 // ---- gradient of log probability and entropy: one pass over a row's pieces, cut over blocks ----
 //
 // lse and entropy come from the forward call, so an element is read, transformed and written: HBM
-// bound (2048 x 32000 fp32: 75 us, 6.3 TB/s of reads and writes under the profiler).
+// bound (2048 x 32000 fp32: 76 us, 6.2 TB/s of reads and writes under the profiler).
 //
 // p = exp(z / tau - lse) has the rounding of lse as its relative error: up to 2^-18 below kFarLse.  Rows
 // beyond it (low temperatures, logits with a common offset, an lse past fp32) are taken by their first block
