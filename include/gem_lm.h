@@ -1,10 +1,16 @@
 /* gem_lm.h -- operators of a language model that asynchronous workers train with GEM (C
- * ABI, sm_103a): the layer that mixes time, the loss over a vocabulary, and the scoring of
- * what the model answers.
+ * ABI, sm_103a): the embedding, the layers that mix time, the losses over a vocabulary, and the
+ * scoring of what the model answers.
  *
+ *   gem_embed, gem_embed_grad             rows of the embedding table for tokens, and the
+ *                                         table's gradient
+ *   gem_conv_forward, gem_conv_backward   a short causal convolution of each channel
+ *   gem_ssm_forward, gem_ssm_backward     a selective state space scan
  *   gem_glr_forward, gem_glr_backward     a gated linear recurrence over long sequences
  *   gem_distill                           the loss against a teacher's top logits, with its
  *                                         gradient
+ *   gem_policy                            the clipped policy loss of sampled tokens with a KL
+ *                                         term and an entropy bonus, with its gradient
  *   gem_token_logp, gem_token_logp_grad   log probabilities of given tokens with entropy and
  *                                         the top alternatives, and their gradient
  *
@@ -168,6 +174,155 @@ int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int
                         const int32_t* tokens, float temperature, const float* lse,
                         const float* entropy, const float* dlogp, const float* dentropy,
                         void* grad, int64_t grad_ld, void* stream);
+
+/* Clipped policy loss: for each of N rows of V logits, with p = softmax(logits / temperature),
+ * logp = log p of the row's token, H = -sum p log p and r = exp(logp - old_logp), the loss
+ *
+ *   L = max(-r A, -min(max(r, 1 - clip_low), 1 + clip_high) A) + kl (exp(d) - d - 1) - bonus H,
+ *       d = ref_logp - logp,
+ *
+ * and its gradient, with D = -r A where the first of the two terms is the larger or equal one, else 0, less
+ * kl (exp(d) - 1),
+ *
+ *   dL/dlogits_j = (D ([j = token] - p_j) + bonus p_j (log p_j + H)) / temperature.
+ *
+ *   tokens [N] int32: the sampled tokens; < 0: the row has none, its loss is 0 and its gradient zeros;
+ *     >= V: its loss, logp and gradient are NaN.
+ *   old_logp [N] fp32: the tokens' log probabilities when they were sampled (gem_token_logp);
+ *     advantage [N] fp32: A of each; ref_logp [N] fp32 (required when kl > 0, not read otherwise):
+ *     those under the reference model.
+ *   row_scale [N] fp32, NULL: ones.  The gradient of row n is multiplied by row_scale[n].  A row whose
+ *     scale is 0 (a prompt's, padding) is not read: its loss, logp and entropy are 0, its gradient zeros.
+ *   loss [N] fp32: L of each row (not multiplied by row_scale); logp, entropy [N] fp32, may be NULL: logp and H
+ *     (0 in a row without a token).
+ *   grad (row n at grad + n * grad_ld, type dtype), may be NULL and may be logits with grad_ld =
+ *     ld: row_scale[n] dL/dlogits.
+ * A logit of -inf has p = 0, and no gradient unless it is the token's; a logit of NaN or +inf, or a row of -inf
+ * alone, makes its row's loss and gradient NaN.  Requires 0 <= clip_low <= 1, 0 <= clip_high, kl and bonus finite and
+ * kl >= 0, 1e-20 <= temperature <= 1e20, 1 <= V <= 2^30, N <= 2^27, ld >= V (or 0), grad_ld >= V. */
+int gem_policy(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
+               const int32_t* tokens, const float* old_logp, const float* advantage,
+               const float* ref_logp, const float* row_scale, float temperature, float clip_low,
+               float clip_high, float kl, float bonus, float* loss, float* logp, float* entropy,
+               void* grad, int64_t grad_ld, void* stream);
+
+/* Embedding: out[n] = scale table[tokens[n]] for N tokens (int32), rows of D elements: row v of the
+ * table at table + v * table_ld (type table_dtype), row n of out at out + n * out_ld (type dtype; rounded
+ * once).  A token < 0 has no row: zeros; one >= V gives NaN. */
+int gem_embed(int table_dtype, int dtype, int64_t N, int64_t V, int64_t D, const void* table,
+              int64_t table_ld, const int32_t* tokens, float scale, void* out, int64_t out_ld,
+              void* stream);
+
+/* Bytes of gem_embed_grad's workspace; -1 for a size out of range. */
+int64_t gem_embed_workspace(int64_t N, int64_t V, int64_t D);
+
+/* Gradient of the embedding with respect to the table: dtable[v] = scale sum dout[n] over the n
+ * with tokens[n] = v, from dout (row n at dout + n * dout_ld, type dtype), into dtable (row v at
+ * dtable + v * dtable_ld, type grad_dtype).  Tokens outside [0, V) have no row and are left out, dout
+ * unread.
+ *   accumulate = 0: all V rows are written, those without a token with zeros.
+ *   accumulate = 1: the sum is added to what dtable holds (a table that is also the output layer);
+ *     rows without a token are not touched.
+ *   workspace: gem_embed_workspace bytes, 16-byte aligned, in use until the call's work is done.
+ * Sums are fp32, in the order of n and of pieces of it that the tokens alone fix. */
+int gem_embed_grad(int dtype, int grad_dtype, int64_t N, int64_t V, int64_t D, const void* dout,
+                   int64_t dout_ld, const int32_t* tokens, float scale, int accumulate,
+                   void* dtable, int64_t dtable_ld, void* workspace, void* stream);
+
+enum gem_conv_form { GEM_CONV_LINEAR = 0, GEM_CONV_SILU = 1 };
+
+/* Short causal convolution of each channel over time:
+ *
+ *   p_t = bias + sum_{k < W} weight_k x_{t - W + 1 + k},   y_t = p_t (GEM_CONV_LINEAR) or p_t sigmoid(p_t)
+ *
+ * over x (B sequences of T steps and D channels, of type dtype) into y; 2 <= W <= 4.
+ *   weight [D][W], bias [D] fp32 (NULL: zeros).
+ *   state [B][W - 1][D] fp32, NULL: zeros: the W - 1 inputs before the first step, oldest first.
+ *   lengths [B] int32, NULL: all T.  Sequence b has lengths[b] steps (clipped to 0..T): past
+ *     them x is not used and y is 0.
+ *   reset [B][T] bytes, NULL: none.  Where it is not 0, every input before the step counts as 0 from
+ *     then on, whatever it holds (packed documents).
+ *   state_last [B][W - 1][D] fp32, may be NULL and may be state: the last W - 1 inputs, so that a call
+ *     can go on where another ended (serving: T = 1 for each token). */
+int gem_conv_forward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W, const gem_seq_t* x,
+                     const float* weight, const float* bias, const float* state,
+                     const int32_t* lengths, const uint8_t* reset, const gem_seq_t* y,
+                     float* state_last, void* stream);
+
+/* Floats of gem_conv_backward's workspace; -1 for a size out of range. */
+int64_t gem_conv_workspace(int64_t B, int64_t T, int64_t D, int W);
+
+/* Gradients of the convolution: dy is the gradient with respect to y, dstate_last [B][W - 1][D] fp32
+ * (NULL: zeros) that with respect to state_last; x, weight, bias, state, lengths, reset and form are
+ * those of the forward call.  Writes dx (0 past lengths[b]), dweight [D][W], dbias [D] and dstate [B][W -
+ * 1][D] fp32 (any of the last three may be NULL; dstate may be dstate_last).  workspace: gem_conv_workspace floats, in
+ * use until the call's work is done. */
+int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W,
+                      const gem_seq_t* x, const float* weight, const float* bias,
+                      const float* state, const int32_t* lengths, const uint8_t* reset,
+                      const gem_seq_t* dy, const float* dstate_last, const gem_seq_t* dx,
+                      float* dweight, float* dbias, float* dstate, float* workspace, void* stream);
+
+/* Selective state space scan.  Each of D channels has N states; with step = softplus(dt + dt_bias)
+ * (softplus != 0) or dt + dt_bias, per channel and step,
+ *
+ *   h_t[n] = exp(step_t A[n]) h_{t-1}[n] + step_t x_t b_t[n]
+ *   y_t    = (sum_n c_t[n] h_t[n] + skip x_t) z_t sigmoid(z_t)
+ *
+ * from h_{-1} = h0.  b and c are shared by the D / G channels of each of G groups. */
+typedef struct {
+  int64_t B, T, D;
+  int32_t N, G;              /* 1 <= N <= GEM_SSM_STATES; G divides D */
+  int32_t softplus;
+  gem_seq_t x, dt;           /* [B][T][D] */
+  gem_seq_t b, c;            /* [B][T][G][N], the last two dimensions side by side */
+  gem_seq_t z;               /* [B][T][D]; data NULL: no gate, y is the sum alone */
+  const float* A;            /* [D][N] */
+  const float* skip;         /* [D], NULL: zeros */
+  const float* dt_bias;      /* [D], NULL: zeros */
+  const int32_t* lengths;    /* [B], NULL: all T; past lengths[b] (clipped to 0..T) x, dt, b, c and z are not used, y is 0
+                                and the state stays */
+  const uint8_t* reset;      /* [B][T], NULL: none; where it is not 0, the state before the step counts as 0,
+                                whatever it holds */
+} gem_ssm_t;
+
+/* Most states of a channel. */
+#define GEM_SSM_STATES 64
+/* Steps between the states that gem_ssm_forward saves for gem_ssm_backward. */
+#define GEM_SSM_CHUNK 16
+
+/* Floats of the `saved` buffer, [B][ceil(T / GEM_SSM_CHUNK)][D][N]; -1 for a size out of range. */
+int64_t gem_ssm_saved_count(int64_t B, int64_t T, int64_t D, int N);
+
+/* Floats of the workspace of gem_ssm_forward (backward = 0), or of one that serves both calls (backward =
+ * 1); may be 0; -1 for a size out of range. */
+int64_t gem_ssm_workspace(int64_t B, int64_t T, int64_t D, int N, int G, int backward);
+
+/* The scan into y [B][T][D], of type dtype as x, dt, b, c and z.
+ *   h0 [B][D][N] fp32, NULL: zeros.
+ *   h_last [B][D][N] fp32, may be NULL and may be h0: the state after the last step (serving is a call with
+ *     T = 1 for each token).
+ *   saved, may be NULL: gem_ssm_saved_count floats, the state before steps 0, 16, 32, ... for
+ *     gem_ssm_backward; those past a sequence's end are not written.
+ *   workspace: gem_ssm_workspace floats (NULL where that is 0), in use until the call's work is done.
+ * A state or step that is not finite stays so until a reset, but an infinite state becomes NaN where
+ * exp(step A) leaves fp32. */
+int gem_ssm_forward(int dtype, const gem_ssm_t* in, const float* h0, const gem_seq_t* y,
+                    float* h_last, float* saved, float* workspace, void* stream);
+
+/* What gem_ssm_backward writes: gradients of the inputs of the same names, [D], [D][N] and [B][D][N] ones
+ * fp32 (each may be NULL), those of sequences of type dtype, 0 past lengths[b] (dz only with a gate). */
+typedef struct {
+  gem_seq_t dx, ddt, db, dc, dz;
+  float *dA, *dskip, *ddt_bias, *dh0;
+} gem_ssm_grad_t;
+
+/* Gradients of the scan: dy is the gradient with respect to y, dh_last [B][D][N] fp32 (NULL: zeros) that
+ * with respect to h_last; in is that of the forward call and saved is what it saved.  dh0 may be
+ * dh_last. */
+int gem_ssm_backward(int dtype, const gem_ssm_t* in, const float* saved, const gem_seq_t* dy,
+                     const float* dh_last, const gem_ssm_grad_t* out, float* workspace,
+                     void* stream);
 
 #ifdef __cplusplus
 }

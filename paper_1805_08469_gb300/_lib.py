@@ -23,9 +23,23 @@ class GemSeq(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64)]
 
 
+class GemSsm(C.Structure):
+    """gem_ssm_t: sizes and inputs of the selective state space scan."""
+    _fields_ = [("B", C.c_int64), ("T", C.c_int64), ("D", C.c_int64), ("N", C.c_int32), ("G", C.c_int32), ("softplus", C.c_int32),
+                ("x", GemSeq), ("dt", GemSeq), ("b", GemSeq), ("c", GemSeq), ("z", GemSeq),
+                ("A", C.c_void_p), ("skip", C.c_void_p), ("dt_bias", C.c_void_p), ("lengths", C.c_void_p), ("reset", C.c_void_p)]
+
+
+class GemSsmGrad(C.Structure):
+    """gem_ssm_grad_t: what the scan's backward call writes."""
+    _fields_ = [("dx", GemSeq), ("ddt", GemSeq), ("db", GemSeq), ("dc", GemSeq), ("dz", GemSeq),
+                ("dA", C.c_void_p), ("dskip", C.c_void_p), ("ddt_bias", C.c_void_p), ("dh0", C.c_void_p)]
+
+
 def _declare(L):
     p, i, sz = C.c_void_p, C.c_int, C.c_size_t
     f, i64, seq = C.c_float, C.c_int64, C.POINTER(GemSeq)
+    ssm, ssm_grad = C.POINTER(GemSsm), C.POINTER(GemSsmGrad)
     sig = {
         "gem_create": ([sz, i, C.c_float, C.c_float, C.c_float, p], i),
         "gem_destroy": ([p], None),
@@ -88,6 +102,17 @@ def _declare(L):
         "gem_distill": ([i, i64, i64, p, i64, i, p, p, p, p, p, f, f, p, p, i64, p], i),
         "gem_token_logp": ([i, i64, i64, p, i64, p, f, i, p, p, p, p, p, p], i),
         "gem_token_logp_grad": ([i, i64, i64, p, i64, p, f, p, p, p, p, p, i64, p], i),
+        "gem_policy": ([i, i64, i64, p, i64, p, p, p, p, p, f, f, f, f, f, p, p, p, p, i64, p], i),
+        "gem_embed": ([i, i, i64, i64, i64, p, i64, p, f, p, i64, p], i),
+        "gem_embed_workspace": ([i64, i64, i64], i64),
+        "gem_embed_grad": ([i, i, i64, i64, i64, p, i64, p, f, i, p, i64, p, p], i),
+        "gem_conv_forward": ([i, i, i64, i64, i64, i, seq, p, p, p, p, p, seq, p, p], i),
+        "gem_conv_workspace": ([i64, i64, i64, i], i64),
+        "gem_conv_backward": ([i, i, i64, i64, i64, i, seq, p, p, p, p, p, seq, p, seq, p, p, p, p, p], i),
+        "gem_ssm_saved_count": ([i64, i64, i64, i], i64),
+        "gem_ssm_workspace": ([i64, i64, i64, i, i, i], i64),
+        "gem_ssm_forward": ([i, ssm, p, seq, p, p, p, p], i),
+        "gem_ssm_backward": ([i, ssm, p, seq, p, ssm_grad, p, p], i),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)

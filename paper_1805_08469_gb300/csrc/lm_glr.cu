@@ -12,26 +12,6 @@ bool sizes_ok(int dtype, int form, int64_t B, int64_t T, int64_t D) {
   return B == 0 || (D + 31) / 32 <= (int64_t(1) << 27) / B;   // a block at least for 32 channels of a sequence
 }
 
-// An input: any strides (0: one step or sequence for all).
-bool input_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64_t D) {
-  if (!s) return false;
-  if (B == 0 || T == 0 || D == 0) return true;
-  if (!s->data || !aligned_to(s->data, size_t(dtype_size(dtype)))) return false;
-  if (B > 1 && (s->stride_b < 0 || s->stride_b > kMaxStride / B)) return false;
-  if (T > 1 && (s->stride_t < 0 || s->stride_t > kMaxStride / T)) return false;
-  return true;
-}
-
-// An output: its elements also have places of their own.
-bool output_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64_t D) {
-  if (!input_ok(s, dtype, B, T, D)) return false;
-  if (B == 0 || T == 0 || D == 0) return true;
-  const int64_t sb = s->stride_b, st = s->stride_t;
-  if (T == 1) return B == 1 || sb >= D;
-  if (B == 1) return st >= D;
-  return (st >= D && sb >= (T - 1) * st + D) || (sb >= D && st >= (B - 1) * sb + D);
-}
-
 }  // namespace
 }  // namespace glr
 }  // namespace lm

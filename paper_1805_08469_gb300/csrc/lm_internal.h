@@ -105,6 +105,26 @@ constexpr int64_t kMaxStride = int64_t(1) << 46;
 
 inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 
+// An input: any strides (0: one step or sequence for all).
+inline bool input_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64_t D) {
+  if (!s) return false;
+  if (B == 0 || T == 0 || D == 0) return true;
+  if (!s->data || !aligned_to(s->data, size_t(dtype_size(dtype)))) return false;
+  if (B > 1 && (s->stride_b < 0 || s->stride_b > kMaxStride / B)) return false;
+  if (T > 1 && (s->stride_t < 0 || s->stride_t > kMaxStride / T)) return false;
+  return true;
+}
+
+// An output: its elements also have places of their own.
+inline bool output_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64_t D) {
+  if (!input_ok(s, dtype, B, T, D)) return false;
+  if (B == 0 || T == 0 || D == 0) return true;
+  const int64_t sb = s->stride_b, st = s->stride_t;
+  if (T == 1) return B == 1 || sb >= D;
+  if (B == 1) return st >= D;
+  return (st >= D && sb >= (T - 1) * st + D) || (sb >= D && st >= (B - 1) * sb + D);
+}
+
 // Most dynamic shared memory of a block of these kernels: 227 KB less their static shared memory (up to
 // 8.3 KB).
 constexpr size_t kMaxShared = 216 << 10;

@@ -1,0 +1,268 @@
+// Selective state space scan: what the forward and the backward kernels share (internal).
+//
+// Work is cut into blocks of one sequence, a split of its time, and up to CH channels of a group.  A block
+// goes over its split in tiles of 16 steps: its threads stage a tile (step and step x of every channel, b and c) in
+// shared memory as fp32, all once; then each thread takes four states of K channels through the tile in
+// registers.  The LS lanes of a channel add up what the states give together.
+//
+//   lane = (state quad g, channel lane c), c fastest: the lanes of a quarter warp read the same b and c
+//
+// Splits: time is one split where the channels fill the GPU.  Else a first pass takes each split from a state of 0
+// and leaves its last state and the sum of its steps; a block of the second pass composes the splits before its own,
+//   h = exp(A sum step) h + last,
+// and goes on from there.  A sum of +inf marks a split in which the state was dropped.
+#pragma once
+
+#include "lm_internal.h"
+
+namespace gem {
+namespace lm {
+namespace ssm {
+
+constexpr int kTile = GEM_SSM_CHUNK;
+static_assert(kTile == 16, "a reduction's lanes hold whole steps");
+constexpr int kWarps = 4, kSsmThreads = 32 * kWarps;
+constexpr int kQuad = 4;                        // states of a thread and channel
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct SsmArgs {
+  gem_ssm_t in;
+  gem_seq_t y, dy, dx, ddt, db, dc, dz;
+  const float* h0;         // backward: dh_last
+  float* h_last;           // backward: dh0
+  float* saved;
+  float *dA, *dskip, *ddt_bias;
+  float *states, *sums;    // [B][splits][D][N], [B][splits][D]
+  float* bc_part;          // [B][T][G][blocks][2][4 LS]
+  float* param_part;       // [B][splits][N + 2][D]
+  bool params;             // whether any of dA, dskip and ddt_bias is asked for
+  int splits, blocks;      // of a sequence's time, of a group's channels
+  int64_t steps;           // of a split
+  int vec;                 // bit per tensor: its pieces lie at multiples of their size
+};
+enum { kVecX = 1, kVecDt = 2, kVecZ = 4, kVecB = 8, kVecC = 16, kVecY = 32, kVecDy = 64, kVecDx = 128, kVecDdt = 256, kVecDz = 512,
+       kVecState = 1024, kVecSaved = 2048 };
+
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float sigmoid(float v) { return reciprocal(1.0f + ex2(-v * kLog2e)); }
+
+// max(v, 0) + log(1 + w), w = exp(-|v|): log(1 + w) = 2 artanh(s) with s = w / (2 + w) <= 1/3, by its
+// series in s^2, whose first term left out is 2e-8 of the sum.
+__device__ __forceinline__ float softplus(float v) {
+  const float w = ex2(-fabsf(v) * kLog2e), s = w * reciprocal(2.0f + w), q = s * s;
+  float r = fmaf(q, 1.0f / 13, 1.0f / 11);
+  r = fmaf(q, r, 1.0f / 9);
+  r = fmaf(q, r, 1.0f / 7);
+  r = fmaf(q, r, 1.0f / 5);
+  r = fmaf(q, r, 1.0f / 3);
+  r = fmaf(q, r, 1.0f);
+  return fmaf(2.0f * s, r, fmaxf(v, 0.0f));
+}
+
+// A decay's exponent step A log2(e), and a little more: the GPU's approximate exp2 gives on average 0.1 (next to 1) to
+// 0.45 of 2^-24 too little, which a state of small decay would add up over its whole memory.  With 2^-27 more the mean at
+// exponents above -0.002 is within 0.04 of 2^-24, and a step of 0 still decays by exactly 1.
+constexpr float kNudge = 1.0749e-8f;
+__device__ __forceinline__ Vec<2> decay(float step, const Vec<2>& A2) {
+  const Vec<2> x = fma<2>(splat<2>(step), A2, splat<2>(kNudge));
+  return {ex2(x.v[0]), ex2(x.v[1])};
+}
+// That over a split: above 0, so that an infinite state does not become NaN by leaving fp32.
+__device__ __forceinline__ float far_decay(float sum, float A2) { return fmaxf(ex2(sum * A2), 1.4e-45f); }
+
+// n neighbouring elements as they are in memory.
+template <typename E, int V>
+struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Piece {
+  E e[V];
+};
+
+// `there` (<= V) elements from p on, zeros past them.
+template <typename E, int V>
+__device__ __forceinline__ Piece<E, V> load_piece(const E* p, bool vec, int there) {
+  Piece<E, V> r;
+  if (vec && there >= V) return *reinterpret_cast<const Piece<E, V>*>(p);
+#pragma unroll
+  for (int k = 0; k < V; ++k) r.e[k] = k < there ? p[k] : from_f32<E>(0.0f);
+  return r;
+}
+template <typename E, int V>
+__device__ __forceinline__ void store_piece(E* p, bool vec, int there, const float (&v)[V]) {
+  Piece<E, V> r;
+#pragma unroll
+  for (int k = 0; k < V; ++k) r.e[k] = from_f32<E>(v[k]);
+  if (vec && there >= V) {
+    *reinterpret_cast<Piece<E, V>*>(p) = r;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (k < there) p[k] = r.e[k];
+}
+
+// Four states from p on, of which `there` exist.
+struct Quad {
+  Vec<2> a, b;
+};
+__device__ __forceinline__ Quad zeros() { return {splat<2>(0.0f), splat<2>(0.0f)}; }
+__device__ __forceinline__ Quad quad(const float4& v) { return {{v.x, v.y}, {v.z, v.w}}; }
+__device__ __forceinline__ Quad load_quad(const float* p, bool vec, int there) {
+  if (vec && there >= kQuad) return quad(*reinterpret_cast<const float4*>(p));
+  return {{there > 0 ? p[0] : 0.0f, there > 1 ? p[1] : 0.0f}, {there > 2 ? p[2] : 0.0f, there > 3 ? p[3] : 0.0f}};
+}
+__device__ __forceinline__ void store_quad(float* p, bool vec, int there, const Quad& q) {
+  if (vec && there >= kQuad) {
+    *reinterpret_cast<float4*>(p) = make_float4(q.a.v[0], q.a.v[1], q.b.v[0], q.b.v[1]);
+    return;
+  }
+  if (there > 0) p[0] = q.a.v[0];
+  if (there > 1) p[1] = q.a.v[1];
+  if (there > 2) p[2] = q.b.v[0];
+  if (there > 3) p[3] = q.b.v[1];
+}
+
+// How a block is laid out.
+template <int LS_, int K_>
+struct Shape {
+  static constexpr int LS = LS_, K = K_;
+  static constexpr int lanes = 32 / LS;            // channel lanes of a warp
+  static constexpr int CH = kWarps * lanes * K;    // channels
+  static constexpr int V = CH / 8;                 // channels of a staging thread (8 of them to a step)
+  static constexpr int row = CH + 8;               // of the tiles' rows: steps lie 8 banks (floats) apart
+  static constexpr int NP = kQuad * LS;            // states, padded
+};
+
+// The block's place, and a thread's in it.
+template <typename S>
+struct Place {
+  int64_t b, n;              // sequence, its steps
+  int64_t first, end;        // steps of the split
+  int split, group, part;    // part: block of the group's channels
+  int d0, channels;          // first channel and how many
+  int states;                // N
+  // staging: step and first channel of the piece
+  int s, o, c0, there;
+  // computing
+  int g, quads;              // state quad, how many of its states exist
+  int pos;                   // column of channel 0 in the tiles; channel k is k lanes further
+
+  __device__ Place(const SsmArgs& p) {
+    int64_t i = blockIdx.x;
+    part = int(i % p.blocks);
+    i /= p.blocks;
+    group = int(i % p.in.G);
+    i /= p.in.G;
+    split = int(i % p.splits);
+    b = i / p.splits;
+    n = p.in.lengths ? min(max(int64_t(p.in.lengths[b]), int64_t(0)), p.in.T) : p.in.T;
+    first = split * p.steps;
+    end = min(first + p.steps, p.in.T);
+    const int per = int(p.in.D / p.in.G);
+    d0 = group * per + part * S::CH;
+    channels = min(S::CH, per - part * S::CH);
+    states = p.in.N;
+    s = threadIdx.x / 8;
+    o = threadIdx.x % 8;
+    c0 = o * S::V;
+    there = min(max(channels - c0, 0), S::V);
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    g = lane / S::lanes;
+    quads = min(max(states - g * kQuad, 0), kQuad);
+    pos = warp * S::K * S::lanes + lane % S::lanes;
+  }
+  // Column i of the tiles holds channel (i % 8) V + i / 8, so that both ways of access are free of conflicts.
+  __device__ int channel(int k) const {
+    const int i = pos + k * S::lanes;
+    return i % 8 * S::V + i / 8;
+  }
+  __device__ bool has(int k) const { return channel(k) < channels; }
+  // Of a [..][D][N] array's row: where the thread's states of channel k begin.
+  __device__ int64_t state(int64_t row, int64_t D, int k) const { return (row * D + d0 + channel(k)) * states + g * kQuad; }
+};
+
+template <typename E>
+__device__ __forceinline__ E* at(const gem_seq_t& s, int64_t b, int64_t t, int d) {
+  return static_cast<E*>(s.data) + b * s.stride_b + t * s.stride_t + d;
+}
+
+// b and c of a tile, loaded ahead: a thread has quads of states of some steps.
+template <typename E, typename S, bool HAS_B, bool HAS_C>
+struct States {
+  static constexpr int each = (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS / kSsmThreads > 0 ? (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS / kSsmThreads : 1;
+  static constexpr int total = (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS;
+  Piece<E, kQuad> e[each];
+  __device__ __forceinline__ void load(const SsmArgs& p, const Place<S>& a, int64_t t0) {
+#pragma unroll
+    for (int i = 0; i < each; ++i) {
+      const int at_ = i * kSsmThreads + threadIdx.x, q = at_ % S::LS, s = at_ / S::LS % kTile;
+      const bool is_c = !HAS_B || (HAS_C && at_ >= kTile * S::LS);
+      const int there = at_ < total && t0 + s < a.n ? min(max(a.states - q * kQuad, 0), kQuad) : 0;
+      const gem_seq_t& from = is_c ? p.in.c : p.in.b;
+      e[i] = load_piece<E, kQuad>(at<E>(from, a.b, t0 + s, a.group * a.states + q * kQuad), p.vec & (is_c ? kVecC : kVecB), there);
+    }
+  }
+  // Into [HAS_B + HAS_C][kTile][LS] quads.
+  __device__ __forceinline__ void stage(float4* to) const {
+#pragma unroll
+    for (int i = 0; i < each; ++i) {
+      const int at_ = i * kSsmThreads + threadIdx.x;
+      if (at_ < total) to[at_] = make_float4(to_f32(e[i].e[0]), to_f32(e[i].e[1]), to_f32(e[i].e[2]), to_f32(e[i].e[3]));
+    }
+  }
+};
+
+// Bits of the tile's steps at which the state is dropped; steps past the end have none.
+__device__ __forceinline__ unsigned resets_of(const SsmArgs& p, int64_t b, int64_t t0, int64_t end) {
+  if (!p.in.reset) return 0u;
+  const int64_t t = t0 + threadIdx.x % 32;
+  return __ballot_sync(~0u, threadIdx.x % 32 < kTile && t < end && p.in.reset[b * p.in.T + t] != 0);
+}
+
+// Sums of v over the lanes that differ in the bits from `low` to `high` (lane masks): the first N / lanes values of v
+// are then those of the N sums from index N / lanes * (the lane's number among them) on.
+template <int N, int HIGH, int LOW>
+__device__ __forceinline__ void scatter_sums(float (&v)[N]) {
+  int count = N;
+#pragma unroll
+  for (int bit = HIGH; bit >= LOW; bit /= 2) {
+    const bool upper = threadIdx.x & bit;
+    count /= 2;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      if (i >= count) break;
+      const float keep = upper ? v[count + i] : v[i], give = upper ? v[i] : v[count + i];
+      v[i] = keep + __shfl_xor_sync(~0u, give, bit);
+    }
+  }
+}
+
+// The staging of one tensor element's step: step = softplus(dt + bias), or without it.
+__device__ __forceinline__ float step_of(const SsmArgs& p, float raw) { return p.in.softplus ? softplus(raw) : raw; }
+
+// How time and channels are cut (for kernels of CH channels a block).
+struct SsmCut {
+  int64_t blocks, splits, steps;
+};
+SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH);
+
+template <typename E>
+cudaError_t launch_forward(SsmArgs p, cudaStream_t stream);
+template <typename E>
+cudaError_t launch_backward(SsmArgs p, cudaStream_t stream);
+
+// Shapes by N: LS lanes for 4 LS states.
+inline int state_lanes(int N) { return N <= 16 ? 4 : N <= 32 ? 8 : 16; }
+constexpr int kForwardK = 2, kBackwardK = 1;
+inline int block_channels(int N, int K) { return kWarps * 32 / state_lanes(N) * K; }
+
+}  // namespace ssm
+}  // namespace lm
+}  // namespace gem

@@ -1,0 +1,377 @@
+// Selective state space scan, backward kernels (internal).
+//
+// With dy' = dy z sigmoid(z) and g_t the gradient of h_t, from the last step to the first
+//
+//   g += c_t dy'_t;  dc_t = sum_channels dy'_t h_t;  db_t = sum_channels g step_t x_t
+//   q = g exp(step_t A) h_{t-1};  dA += q step_t;  dstep_t = sum_n A q + x_t sum_n g b_t
+//   dx_t = step_t sum_n g b_t + skip dy'_t;  g = exp(step_t A) g
+//
+// A tile's states are computed again from the one saved before it and stay in registers.  db and dc are summed
+// over a warp's channels by exchanges, over the block's in shared memory, and over blocks by a second kernel;
+// the parameters' gradients over a split in registers, then by that kernel as well.  Splits are composed
+// from the last one back, as in the forward pass.
+#pragma once
+
+#include "lm_ssm.h"
+
+namespace gem {
+namespace lm {
+namespace ssm {
+
+__device__ __forceinline__ Vec<2> scaled(const Vec<2>& a, float b) { return a * splat<2>(b); }
+
+template <typename E, int LS, bool GATE, bool STATES>
+__global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kernel(const SsmArgs p) {
+  using S = Shape<LS, kBackwardK>;
+  constexpr int kSums = GATE ? 3 : 2;
+  __shared__ float2 steps[kTile][S::row];                  // (step, step x)
+  __shared__ float gys[kTile][S::row];                     // dy'
+  __shared__ float4 bc[(STATES ? 1 : 2) * kTile * LS];
+  __shared__ float sums[STATES ? 1 : kSums][kTile][S::row];   // sum A2 q, sum g b, sum c h
+  __shared__ float red[STATES ? 1 : kWarps][kTile][2 * S::NP];   // db, dc of a warp's channels
+  pdl_entry();
+  const Place<S> a(p);
+  if (STATES && a.split == 0) return;
+  const int64_t D = p.in.D, N = a.states;
+  const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
+  const bool vec = p.vec & kVecState, has = a.has(0);
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+
+  Quad A2 = has ? load_quad(p.in.A + a.state(0, D, 0), vec, a.quads) : zeros();
+  A2 = {scaled(A2.a, kLog2e), scaled(A2.b, kLog2e)};
+  Quad g = zeros();
+  if (has) {
+    if (p.splits == 1 || (STATES && a.split + 1 == p.splits)) {
+      if (p.h0) g = load_quad(p.h0 + a.state(a.b, D, 0), vec, a.quads);
+      // (the second pass's own copy: dh0 may be dh_last)
+      if (STATES) store_quad(p.states + a.state(a.b * p.splits, D, 0), vec, a.quads, g);
+    } else if (!STATES) {
+      if (a.split + 1 == p.splits) g = load_quad(p.states + a.state(a.b * p.splits, D, 0), vec, a.quads);
+#pragma unroll 4
+      for (int q = p.splits - 1; q > a.split; --q) {
+        const int64_t from = a.b * p.splits + q;
+        const Quad first = load_quad(p.states + a.state(from, D, 0), vec, a.quads);
+        const float sum = p.sums[from * D + a.d0 + a.channel(0)];
+        if (sum == INFINITY || q == p.splits - 1) {
+          g = first;
+        } else {
+          g.a = fma<2>({far_decay(sum, A2.a.v[0]), far_decay(sum, A2.a.v[1])}, g.a, first.a);
+          g.b = fma<2>({far_decay(sum, A2.b.v[0]), far_decay(sum, A2.b.v[1])}, g.b, first.b);
+        }
+      }
+    }
+  }
+
+  float bias[S::V], skip[S::V], dskip[S::V] = {}, dbias[S::V] = {};
+#pragma unroll
+  for (int j = 0; j < S::V; ++j) {
+    bias[j] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
+    skip[j] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
+  }
+  Quad dA = zeros();
+  float total = 0.0f;
+  bool dropped = false;
+
+  Piece<E, S::V> x, dt, z, dy, x_next, dt_next, z_next, dy_next;
+  States<E, S, !STATES, true> b_next;
+  Quad start_next = zeros();
+  const int64_t chunks = (p.in.T + kTile - 1) / kTile;
+  auto load = [&](int64_t t0) {
+    const int64_t t = t0 + a.s;
+    const int there = t < end ? a.there : 0, d = a.d0 + a.c0;
+    if (!STATES) x_next = load_piece<E, S::V>(at<E>(p.in.x, a.b, t, d), p.vec & kVecX, there);
+    dt_next = load_piece<E, S::V>(at<E>(p.in.dt, a.b, t, d), p.vec & kVecDt, there);
+    if (GATE) z_next = load_piece<E, S::V>(at<E>(p.in.z, a.b, t, d), p.vec & kVecZ, there);
+    dy_next = load_piece<E, S::V>(at<E>(p.dy, a.b, t, d), p.vec & kVecDy, there);
+    b_next.load(p, a, t0);
+    if (!STATES && has) start_next = load_quad(p.saved + a.state(a.b * chunks + t0 / kTile, D, 0), p.vec & kVecSaved, a.quads);
+  };
+  const int64_t tiles = end > a.first ? (end - a.first + kTile - 1) / kTile : 0;
+  if (tiles > 0) load(a.first + (tiles - 1) * kTile);
+  for (int64_t t0 = a.first + (tiles - 1) * kTile; t0 >= a.first; t0 -= kTile) {
+    if (!STATES) x = x_next;
+    dt = dt_next;
+    if (GATE) z = z_next;
+    dy = dy_next;
+    const Quad start = start_next;
+    const bool in = t0 + a.s < end;
+#pragma unroll
+    for (int j = 0; j < S::V; ++j) {
+      const float step = in ? step_of(p, to_f32(dt.e[j]) + bias[j]) : 0.0f;
+      steps[a.s][j * 8 + a.o] = {step, in && !STATES ? step * to_f32(x.e[j]) : 0.0f};
+      float gy = to_f32(dy.e[j]);
+      if (GATE) gy *= to_f32(z.e[j]) * sigmoid(to_f32(z.e[j]));
+      gys[a.s][j * 8 + a.o] = in ? gy : 0.0f;
+    }
+    b_next.stage(bc);
+    const unsigned resets = resets_of(p, a.b, t0, end);
+    __syncthreads();
+    if (t0 > a.first) load(t0 - kTile);
+    const int count = int(min(end - t0, int64_t(kTile)));
+    dropped |= resets != 0;
+
+    if constexpr (STATES) {
+      auto tile = [&](auto check) {
+#pragma unroll
+        for (int t = kTile - 1; t >= 0; --t) {
+          if (check.value && t >= count) continue;
+          const Quad c = quad(bc[t * LS + a.g]);
+          const float step = steps[t][a.pos].x, gy = gys[t][a.pos];
+          g.a = decay(step, A2.a) * fma<2>(c.a, splat<2>(gy), g.a);
+          g.b = decay(step, A2.b) * fma<2>(c.b, splat<2>(gy), g.b);
+          if (check.value && (resets >> t & 1)) g = zeros();
+          total += step;
+        }
+      };
+      if (count == kTile && resets == 0)
+        tile(std::false_type());
+      else
+        tile(std::true_type());
+      __syncthreads();
+    } else {
+      auto tile = [&](auto check) {
+        Quad h[kTile];
+        Quad now = start;
+#pragma unroll
+        for (int t = 0; t < kTile; ++t) {
+          if (check.value && t >= count) {
+            h[t] = now;
+            continue;
+          }
+          if (check.value && (resets >> t & 1)) now = zeros();
+          const Quad b = quad(bc[t * LS + a.g]);
+          const float2 v = steps[t][a.pos];
+          now.a = fma<2>(decay(v.x, A2.a), now.a, splat<2>(v.y) * b.a);
+          now.b = fma<2>(decay(v.x, A2.b), now.b, splat<2>(v.y) * b.b);
+          h[t] = now;
+        }
+        float sq[LS], sb[LS], sy[LS];
+#pragma unroll
+        for (int t = kTile - 1; t >= 0; --t) {
+          sq[t % LS] = sb[t % LS] = sy[t % LS] = 0.0f;
+          if (!check.value || t < count) {
+            const Quad b = quad(bc[t * LS + a.g]), c = quad(bc[(kTile + t) * LS + a.g]);
+            const float2 v = steps[t][a.pos];
+            const float gy = gys[t][a.pos];
+            if (GATE) {
+              const Vec<2> m = fma<2>(c.b, h[t].b, c.a * h[t].a);
+              sy[t % LS] = m.v[0] + m.v[1];
+            }
+            g.a = fma<2>(c.a, splat<2>(gy), g.a);
+            g.b = fma<2>(c.b, splat<2>(gy), g.b);
+            const Vec<2> db0 = scaled(g.a, v.y), db1 = scaled(g.b, v.y), dc0 = scaled(h[t].a, gy), dc1 = scaled(h[t].b, gy);
+            float w[8] = {db0.v[0], db0.v[1], db1.v[0], db1.v[1], dc0.v[0], dc0.v[1], dc1.v[0], dc1.v[1]};
+            const Vec<2> mb = fma<2>(g.b, b.b, g.a * b.a);
+            sb[t % LS] = mb.v[0] + mb.v[1];
+            Quad prev = t > 0 ? h[t > 0 ? t - 1 : 0] : start;
+            const Quad dec = {decay(v.x, A2.a), decay(v.x, A2.b)};
+            const bool drop = check.value && (resets >> t & 1);
+            if (drop) prev = zeros();
+            g.a = g.a * dec.a;
+            g.b = g.b * dec.b;
+            const Vec<2> q0 = g.a * prev.a, q1 = g.b * prev.b;
+            const Vec<2> mq = fma<2>(q1, A2.b, q0 * A2.a);
+            sq[t % LS] = mq.v[0] + mq.v[1];
+            dA.a = fma<2>(q0, splat<2>(v.x), dA.a);
+            dA.b = fma<2>(q1, splat<2>(v.x), dA.b);
+            if (drop) {
+              g = zeros();
+              sq[t % LS] = 0.0f;
+            }
+            scatter_sums<8, S::lanes / 2, 1>(w);
+#pragma unroll
+            for (int i = 0; i < 8 / S::lanes; ++i) {
+              const int k = lane % S::lanes * (8 / S::lanes) + i;
+              red[warp][t][k / kQuad * S::NP + a.g * kQuad + k % kQuad] = w[i];
+            }
+          }
+          if (t % LS == 0) {
+            scatter_sums<LS, 16, S::lanes>(sq);
+            scatter_sums<LS, 16, S::lanes>(sb);
+            sums[0][t + a.g][a.pos] = sq[0];
+            sums[1][t + a.g][a.pos] = sb[0];
+            if (GATE) {
+              scatter_sums<LS, 16, S::lanes>(sy);
+              sums[kSums - 1][t + a.g][a.pos] = sy[0];
+            }
+          }
+        }
+      };
+      if (count == kTile && resets == 0)
+        tile(std::false_type());
+      else
+        tile(std::true_type());
+      __syncthreads();
+
+      for (int i = threadIdx.x; i < count * 2 * S::NP; i += kSsmThreads) {
+        const int t = i / (2 * S::NP), k = i % (2 * S::NP);
+        float v = red[0][t][k];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) v += red[w][t][k];
+        if (p.blocks > 1) {
+          p.bc_part[(((a.b * p.in.T + t0 + t) * p.in.G + a.group) * p.blocks + a.part) * (2 * S::NP) + k] = v;
+        } else if (k % S::NP < N) {
+          *at<E>(k < S::NP ? p.db : p.dc, a.b, t0 + t, a.group * a.states + k % S::NP) = from_f32<E>(v);
+        }
+      }
+      if (t0 + a.s < a.end) {
+        float out[3][S::V];
+#pragma unroll
+        for (int j = 0; j < S::V; ++j) {
+          const int i = j * 8 + a.o;
+          const float xj = to_f32(x.e[j]), sg = sums[1][a.s][i], gy = gys[a.s][i];
+          float d = fmaf(sg, xj, sums[0][a.s][i] * kLn2);
+          if (p.in.softplus) d *= sigmoid(to_f32(dt.e[j]) + bias[j]);
+          out[0][j] = in ? fmaf(sg, steps[a.s][i].x, skip[j] * gy) : 0.0f;
+          out[1][j] = in ? d : 0.0f;
+          if (in) {
+            dskip[j] = fmaf(gy, xj, dskip[j]);
+            dbias[j] += d;
+          }
+          if (GATE) {
+            const float zj = to_f32(z.e[j]), sig = sigmoid(zj);
+            out[2][j] = in ? to_f32(dy.e[j]) * fmaf(skip[j], xj, sums[kSums - 1][a.s][i]) * (sig * fmaf(zj, 1.0f - sig, 1.0f)) : 0.0f;
+          }
+        }
+        const int64_t t = t0 + a.s;
+        const int d = a.d0 + a.c0;
+        store_piece<E, S::V>(at<E>(p.dx, a.b, t, d), p.vec & kVecDx, a.there, out[0]);
+        store_piece<E, S::V>(at<E>(p.ddt, a.b, t, d), p.vec & kVecDdt, a.there, out[1]);
+        if (GATE) store_piece<E, S::V>(at<E>(p.dz, a.b, t, d), p.vec & kVecDz, a.there, out[2]);
+      }
+      __syncthreads();   // (the next tile's steps replace these)
+    }
+  }
+  if constexpr (STATES) {
+    if (has) {
+      store_quad(p.states + a.state(row, D, 0), vec, a.quads, g);
+      if (a.g == 0) p.sums[row * D + a.d0 + a.channel(0)] = dropped ? INFINITY : total;
+    }
+    return;
+  } else {
+    if (has && a.split == 0 && p.h_last) store_quad(p.h_last + a.state(a.b, D, 0), vec, a.quads, g);
+    if (has && p.params) {
+      const float v[kQuad] = {dA.a.v[0], dA.a.v[1], dA.b.v[0], dA.b.v[1]};
+#pragma unroll
+      for (int i = 0; i < kQuad; ++i)
+        if (i < a.quads) p.param_part[(row * (N + 2) + a.g * kQuad + i) * D + a.d0 + a.channel(0)] = v[i];
+    }
+    if (p.params) {
+#pragma unroll
+      for (int j = 0; j < S::V; ++j) {
+        sums[0][a.s][j * 8 + a.o] = dskip[j];
+        sums[1][a.s][j * 8 + a.o] = dbias[j];
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < 2 * S::CH; i += kSsmThreads) {
+        const int which = i / S::CH, col = i % S::CH, c = col % 8 * S::V + col / 8;
+        float v = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kTile; ++s) v += sums[which][s][col];
+        if (c < a.channels) p.param_part[(row * (N + 2) + N + which) * D + a.d0 + c] = v;
+      }
+    }
+    // what is left of the split past the sequence's end
+    const int64_t past = a.first + tiles * kTile;
+    const float none[S::V] = {};
+    for (int64_t t = past + a.s; t < a.end; t += kTile) {
+      const int d = a.d0 + a.c0;
+      store_piece<E, S::V>(at<E>(p.dx, a.b, t, d), p.vec & kVecDx, a.there, none);
+      store_piece<E, S::V>(at<E>(p.ddt, a.b, t, d), p.vec & kVecDdt, a.there, none);
+      if (GATE) store_piece<E, S::V>(at<E>(p.dz, a.b, t, d), p.vec & kVecDz, a.there, none);
+    }
+    if (p.blocks == 1) {
+      const int64_t left = a.end - max(end, a.first);
+      for (int64_t i = threadIdx.x; i < left * N; i += kSsmThreads) {
+        const int64_t t = max(end, a.first) + i / N;
+        const int n = a.group * a.states + int(i % N);
+        *at<E>(p.db, a.b, t, n) = from_f32<E>(0.0f);
+        *at<E>(p.dc, a.b, t, n) = from_f32<E>(0.0f);
+      }
+    }
+  }
+}
+
+// db and dc from the blocks' parts, a thread for each value.
+template <typename E>
+__global__ void __launch_bounds__(256) ssm_join_states_kernel(const SsmArgs p, int NP, int64_t count) {
+  pdl_entry();
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= count) return;
+  const int k = int(i % (2 * NP)), n = k % NP;
+  if (n >= p.in.N) return;
+  const int64_t row = i / (2 * NP);
+  const int group = int(row % p.in.G);
+  const int64_t t = row / p.in.G % p.in.T, b = row / p.in.G / p.in.T;
+  float v = 0.0f;
+  if (!p.in.lengths || t < p.in.lengths[b])
+#pragma unroll 8
+    for (int j = 0; j < p.blocks; ++j) v += p.bc_part[(row * p.blocks + j) * (2 * NP) + k];
+  *at<E>(k < NP ? p.db : p.dc, b, t, group * p.in.N + n) = from_f32<E>(v);
+}
+
+// dA, dskip and ddt_bias from the splits' parts, a thread for each value.
+static __global__ void __launch_bounds__(128) ssm_join_params_kernel(const SsmArgs p) {
+  pdl_entry();
+  const int64_t d = int64_t(blockIdx.x) * 128 + threadIdx.x;
+  const int n = blockIdx.y, N = p.in.N;
+  if (d >= p.in.D) return;
+  float v = 0.0f;
+#pragma unroll 4
+  for (int64_t r = 0; r < p.in.B * p.splits; ++r) v += p.param_part[(r * (N + 2) + n) * p.in.D + d];
+  if (n < N) {
+    if (p.dA) p.dA[d * N + n] = v;
+  } else if (n == N) {
+    if (p.dskip) p.dskip[d] = v;
+  } else if (p.ddt_bias) {
+    p.ddt_bias[d] = v;
+  }
+}
+
+template <typename E, int LS>
+cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
+  using S = Shape<LS, kBackwardK>;
+  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
+  p.blocks = int(cut.blocks);
+  p.splits = int(cut.splits);
+  p.steps = cut.steps;
+  float* space = p.states;
+  if (cut.splits > 1) {
+    p.sums = space + p.in.B * cut.splits * p.in.D * p.in.N;
+    space = p.sums + p.in.B * cut.splits * p.in.D;
+  }
+  p.bc_part = space;
+  if (cut.blocks > 1) space += p.in.B * p.in.T * p.in.G * cut.blocks * 2 * S::NP;
+  p.param_part = space;
+  const dim3 grid(unsigned(p.in.B * cut.splits * p.in.G * cut.blocks)), block(kSsmThreads);
+  const bool gate = p.in.z.data;
+  cudaError_t e = cudaSuccess;
+  if (grid.x > 0) {
+    if (cut.splits > 1)
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, true, true>, grid, block, 0, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, false, true>, grid, block, 0, stream, p);
+    if (e == cudaSuccess)
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, true, false>, grid, block, 0, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, false, false>, grid, block, 0, stream, p);
+  }
+  if (e == cudaSuccess && cut.blocks > 1) {
+    const int64_t count = p.in.B * p.in.T * p.in.G * 2 * S::NP;
+    if (count > 0) e = launch_pdl(ssm_join_states_kernel<E>, dim3(unsigned((count + 255) / 256)), dim3(256), 0, stream, p, int(S::NP), count);
+  }
+  if (e == cudaSuccess && p.params)
+    e = launch_pdl(ssm_join_params_kernel, dim3(unsigned((p.in.D + 127) / 128), unsigned(p.in.N + 2)), block, 0, stream, p);
+  return e;
+}
+
+template <typename E>
+cudaError_t launch_backward(SsmArgs p, cudaStream_t stream) {
+  switch (state_lanes(p.in.N)) {
+    case 4: return launch_backward_as<E, 4>(p, stream);
+    case 8: return launch_backward_as<E, 8>(p, stream);
+    default: return launch_backward_as<E, 16>(p, stream);
+  }
+}
+
+}  // namespace ssm
+}  // namespace lm
+}  // namespace gem

@@ -1,0 +1,205 @@
+// Selective state space scan, forward kernels (internal).
+#pragma once
+
+#include "lm_ssm.h"
+
+namespace gem {
+namespace lm {
+namespace ssm {
+
+// Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.
+template <typename E, int LS, int K, bool STATES>
+__global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs p) {
+  using S = Shape<LS, K>;
+  __shared__ float2 steps[kTile][S::row];                          // (step, step x) of each channel
+  __shared__ float4 bc[(STATES ? 1 : 2) * kTile * LS];
+  __shared__ float mixed[STATES ? 1 : kTile][STATES ? 1 : S::row];   // sum c h
+  pdl_entry();
+  const Place<S> a(p);
+  const int64_t D = p.in.D, N = a.states;
+  const bool gate = p.in.z.data;
+  const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
+  const bool vec = p.vec & kVecState;
+
+  Quad A2[K], h[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    A2[k] = a.has(k) ? load_quad(p.in.A + a.state(0, D, k), vec, a.quads) : zeros();
+    A2[k] = {A2[k].a * splat<2>(kLog2e), A2[k].b * splat<2>(kLog2e)};
+    h[k] = zeros();
+  }
+  auto state0 = [&](int k) { return p.h0 ? load_quad(p.h0 + a.state(a.b, D, k), vec, a.quads) : zeros(); };
+  if (STATES) {
+    if (a.split == 0) {
+      // (the second pass's own copy: h_last may be h0)
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (a.has(k)) {
+          h[k] = state0(k);
+          store_quad(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), vec, a.quads, h[k]);
+        }
+    }
+  } else if (p.splits == 1) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (a.has(k)) h[k] = state0(k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!a.has(k)) continue;
+      if (a.split == 0) h[k] = load_quad(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), vec, a.quads);
+#pragma unroll 4
+      for (int q = 0; q < a.split; ++q) {
+        const int64_t from = a.b * p.splits + q;
+        const Quad last = load_quad(p.states + a.state(from, D, k), vec, a.quads);
+        const float sum = p.sums[from * D + a.d0 + a.channel(k)];
+        if (sum == INFINITY || q == 0) {
+          h[k] = last;
+        } else {
+          h[k].a = fma<2>({far_decay(sum, A2[k].a.v[0]), far_decay(sum, A2[k].a.v[1])}, h[k].a, last.a);
+          h[k].b = fma<2>({far_decay(sum, A2[k].b.v[0]), far_decay(sum, A2[k].b.v[1])}, h[k].b, last.b);
+        }
+      }
+    }
+  }
+
+  float bias[S::V], skip[S::V];
+#pragma unroll
+  for (int j = 0; j < S::V; ++j) {
+    bias[j] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
+    skip[j] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
+  }
+  float sum[K] = {};
+  bool dropped = false;
+
+  Piece<E, S::V> x, dt, z, x_next, dt_next, z_next;
+  States<E, S, true, !STATES> b_next;
+  auto load = [&](int64_t t0) {
+    const int64_t t = t0 + a.s;
+    const int there = t < end ? a.there : 0, d = a.d0 + a.c0;
+    x_next = load_piece<E, S::V>(at<E>(p.in.x, a.b, t, d), p.vec & kVecX, there);
+    dt_next = load_piece<E, S::V>(at<E>(p.in.dt, a.b, t, d), p.vec & kVecDt, there);
+    if (!STATES && gate) z_next = load_piece<E, S::V>(at<E>(p.in.z, a.b, t, d), p.vec & kVecZ, there);
+    b_next.load(p, a, t0);
+  };
+  if (a.first < end) load(a.first);
+  for (int64_t t0 = a.first; t0 < end; t0 += kTile) {
+    x = x_next;
+    dt = dt_next;
+    z = z_next;
+    const bool in = t0 + a.s < end;
+#pragma unroll
+    for (int j = 0; j < S::V; ++j) {
+      const float step = in ? step_of(p, to_f32(dt.e[j]) + bias[j]) : 0.0f;
+      steps[a.s][j * 8 + a.o] = {step, in ? step * to_f32(x.e[j]) : 0.0f};
+    }
+    b_next.stage(bc);
+    const unsigned resets = resets_of(p, a.b, t0, end);
+    __syncthreads();
+    if (t0 + kTile < end) load(t0 + kTile);
+    if (!STATES && p.saved) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (a.has(k)) store_quad(p.saved + a.state(a.b * ((p.in.T + kTile - 1) / kTile) + t0 / kTile, D, k), p.vec & kVecSaved, a.quads, h[k]);
+    }
+    float y[K][kTile];
+    auto tile = [&](auto check) {
+      const int count = int(min(end - t0, int64_t(kTile)));
+#pragma unroll
+      for (int t = 0; t < kTile; ++t) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) y[k][t] = 0.0f;
+        if (check.value && t >= count) continue;
+        const Quad b = quad(bc[t * LS + a.g]);
+        const Quad c = STATES ? b : quad(bc[(kTile + t) * LS + a.g]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          if (check.value && (resets >> t & 1)) h[k] = zeros();
+          const float2 v = steps[t][a.pos + k * S::lanes];
+          h[k].a = fma<2>(decay(v.x, A2[k].a), h[k].a, splat<2>(v.y) * b.a);
+          h[k].b = fma<2>(decay(v.x, A2[k].b), h[k].b, splat<2>(v.y) * b.b);
+          if (STATES) {
+            sum[k] += v.x;
+          } else {
+            const Vec<2> m = fma<2>(c.b, h[k].b, c.a * h[k].a);
+            y[k][t] = m.v[0] + m.v[1];
+          }
+        }
+      }
+    };
+    if (t0 + kTile <= end && resets == 0)
+      tile(std::false_type());
+    else
+      tile(std::true_type());
+    dropped |= resets != 0;
+    if (!STATES) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        scatter_sums<kTile, 16, S::lanes>(y[k]);
+#pragma unroll
+        for (int i = 0; i < kTile / LS; ++i) mixed[a.g * (kTile / LS) + i][a.pos + k * S::lanes] = y[k][i];
+      }
+    }
+    __syncthreads();
+    if (!STATES && t0 + a.s < a.end) {
+      float out[S::V];
+#pragma unroll
+      for (int j = 0; j < S::V; ++j) {
+        out[j] = fmaf(skip[j], to_f32(x.e[j]), mixed[a.s][j * 8 + a.o]);
+        if (gate) out[j] *= to_f32(z.e[j]) * sigmoid(to_f32(z.e[j]));
+        if (!in) out[j] = 0.0f;
+      }
+      store_piece<E, S::V>(at<E>(p.y, a.b, t0 + a.s, a.d0 + a.c0), p.vec & kVecY, a.there, out);
+    }
+  }
+  if (STATES) {
+    if (a.split + 1 < p.splits) {
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (a.has(k)) {
+          store_quad(p.states + a.state(row, D, k), vec, a.quads, h[k]);
+          if (a.g == 0) p.sums[row * D + a.d0 + a.channel(k)] = dropped ? INFINITY : sum[k];
+        }
+    }
+    return;
+  }
+  if (p.h_last && a.split + 1 == p.splits) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (a.has(k)) store_quad(p.h_last + a.state(a.b, D, k), vec, a.quads, h[k]);
+  }
+  // what is left of the split past the sequence's end
+  const int64_t past = a.first < end ? a.first + (end - a.first + kTile - 1) / kTile * kTile : a.first;
+  const float none[S::V] = {};
+  for (int64_t t = past + a.s; t < a.end; t += kTile)
+    store_piece<E, S::V>(at<E>(p.y, a.b, t, a.d0 + a.c0), p.vec & kVecY, a.there, none);
+}
+
+template <typename E, int LS>
+cudaError_t launch_forward_as(SsmArgs p, cudaStream_t stream) {
+  using S = Shape<LS, kForwardK>;
+  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
+  p.blocks = int(cut.blocks);
+  p.splits = int(cut.splits);
+  p.steps = cut.steps;
+  p.sums = p.states + p.in.B * cut.splits * p.in.D * p.in.N;
+  const dim3 grid(unsigned(p.in.B * cut.splits * p.in.G * cut.blocks));
+  if (cut.splits > 1) {
+    const cudaError_t e = launch_pdl(ssm_forward_kernel<E, LS, kForwardK, true>, grid, dim3(kSsmThreads), 0, stream, p);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(ssm_forward_kernel<E, LS, kForwardK, false>, grid, dim3(kSsmThreads), 0, stream, p);
+}
+
+template <typename E>
+cudaError_t launch_forward(SsmArgs p, cudaStream_t stream) {
+  switch (state_lanes(p.in.N)) {
+    case 4: return launch_forward_as<E, 4>(p, stream);
+    case 8: return launch_forward_as<E, 8>(p, stream);
+    default: return launch_forward_as<E, 16>(p, stream);
+  }
+}
+
+}  // namespace ssm
+}  // namespace lm
+}  // namespace gem

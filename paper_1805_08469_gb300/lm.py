@@ -1,5 +1,6 @@
-"""Binding of the language-model operators (include/gem_lm.h): the gated linear recurrence,
-the distillation loss and the log probabilities of tokens.
+"""Binding of the language-model operators (include/gem_lm.h): embedding, short causal convolution,
+selective state space scan, gated linear recurrence, the distillation and the policy loss, and the log
+probabilities of tokens.
 
 Argument marshalling only: tensors are checked for type, layout and size, and their addresses
 go to the CUDA library.  Outputs are the caller's tensors.  ``stream`` is a torch stream or a
@@ -9,12 +10,14 @@ from __future__ import annotations
 
 import torch
 
-from ._lib import GemSeq, check, lib
+from ._lib import GemSeq, GemSsm, GemSsmGrad, check, lib
 
 GEM_F32, GEM_BF16, GEM_F16 = 0, 1, 2
 GEM_GLR_LERP, GEM_GLR_ADD = 0, 1
 GEM_GLR_CHUNK = 16
 GEM_TOP_MAX = 256
+GEM_CONV_LINEAR, GEM_CONV_SILU = 0, 1
+GEM_SSM_STATES, GEM_SSM_CHUNK = 64, 16
 
 _DTYPES = {torch.float32: GEM_F32, torch.bfloat16: GEM_BF16, torch.float16: GEM_F16}
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
@@ -164,3 +167,173 @@ def gem_token_logp_grad(logits, tokens, lse, entropy, dlogp, dentropy, grad, *,
         0 if dlogp is None else _dense(dlogp, "dlogp", _F32, (N,)),
         0 if dentropy is None else _dense(dentropy, "dentropy", _F32, (N,)), grad.data_ptr(),
         _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_token_logp_grad")
+
+
+def gem_policy(logits, tokens, old_logp, advantage, loss, grad=None, *, ref_logp=None, row_scale=None,
+               temperature: float = 1.0, clip_low: float = 0.2, clip_high: float = 0.2, kl: float = 0.0,
+               bonus: float = 0.0, logp=None, entropy=None, stream=None) -> None:
+    """logits and grad [N, V] (rows contiguous; grad may be logits or None); tokens [N] int32; old_logp,
+    advantage, ref_logp, row_scale, loss, logp, entropy [N] float32."""
+    N, V, ld = _rows(logits, "logits")
+    check(lib().gem_policy(
+        _dtype(logits, "logits"), N, V, logits.data_ptr(), ld, _dense(tokens, "tokens", _I32, (N,)),
+        _dense(old_logp, "old_logp", _F32, (N,)), _dense(advantage, "advantage", _F32, (N,)),
+        0 if ref_logp is None else _dense(ref_logp, "ref_logp", _F32, (N,)),
+        0 if row_scale is None else _dense(row_scale, "row_scale", _F32, (N,)), temperature, clip_low, clip_high, kl, bonus,
+        _dense(loss, "loss", _F32, (N,)), 0 if logp is None else _dense(logp, "logp", _F32, (N,)),
+        0 if entropy is None else _dense(entropy, "entropy", _F32, (N,)), 0 if grad is None else grad.data_ptr(),
+        V if grad is None else _grad_rows(grad, logits), _stream(stream, logits.device)), "gem_policy")
+
+
+def _matrix(t, what: str, shape):
+    """Address and row pitch of a matrix with contiguous rows."""
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected the shape {shape}, got {tuple(t.shape)}")
+    N, D, ld = _rows(t, what)
+    return t.data_ptr(), ld
+
+
+def gem_embed(table, tokens, out, *, scale: float = 1.0, stream=None) -> None:
+    """out [N, D] = scale table[tokens] from table [V, D] (rows contiguous, any two types); tokens [N]
+    int32."""
+    V, D, ld = _rows(table, "table")
+    N = tokens.shape[0]
+    data, out_ld = _matrix(out, "out", (N, D))
+    check(lib().gem_embed(_dtype(table, "table"), _dtype(out, "out"), N, V, D, table.data_ptr(), ld,
+                          _dense(tokens, "tokens", _I32, (N,)), scale, data, out_ld, _stream(stream, table.device)), "gem_embed")
+
+
+def gem_embed_workspace(N: int, V: int, D: int) -> int:
+    return int(lib().gem_embed_workspace(N, V, D))
+
+
+def _space(t, what: str, size: int, dtype) -> int:
+    """Address of a workspace of at least this many elements (None where it takes none)."""
+    if t is None:
+        if size > 0:
+            raise ValueError(f"{what}: expected {size} elements")
+        return 0
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{what}: expected a contiguous {dtype} CUDA tensor")
+    if t.numel() < size:
+        raise ValueError(f"{what}: expected {size} elements, got {t.numel()}")
+    return t.data_ptr()
+
+
+def gem_embed_grad(dout, tokens, dtable, workspace, *, scale: float = 1.0, accumulate: bool = False,
+                   stream=None) -> None:
+    """dtable [V, D] (written, or with accumulate added to) from dout [N, D] (rows contiguous, any two
+    types); tokens [N] int32; workspace uint8, gem_embed_workspace(N, V, D) of it."""
+    V, D, ld = _rows(dtable, "dtable")
+    N = tokens.shape[0]
+    data, dout_ld = _matrix(dout, "dout", (N, D))
+    check(lib().gem_embed_grad(
+        _dtype(dout, "dout"), _dtype(dtable, "dtable"), N, V, D, data, dout_ld, _dense(tokens, "tokens", _I32, (N,)), scale,
+        int(accumulate), dtable.data_ptr(), ld, _space(workspace, "workspace", gem_embed_workspace(N, V, D), _U8),
+        _stream(stream, dout.device)), "gem_embed_grad")
+
+
+def _optional(t, what: str, shape, dtype=_F32) -> int:
+    return 0 if t is None else _dense(t, what, dtype, shape)
+
+
+def _bytes(t, what: str, shape) -> int:
+    return 0 if t is None else _dense(t.view(_U8) if t.dtype is torch.bool else t, what, _U8, shape)
+
+
+def gem_conv_forward(x, weight, y, *, form: int = GEM_CONV_SILU, bias=None, state=None, lengths=None, reset=None,
+                     state_last=None, stream=None) -> None:
+    """x, y [B, T, D] (channels contiguous, any batch and time strides); weight [D, W], bias [D], state and
+    state_last [B, W - 1, D] float32; lengths [B] int32; reset [B, T] uint8 or bool."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x, weight: expected [B, T, D] and [D, W] tensors")
+    B, T, D = x.shape
+    W = weight.shape[1]
+    check(lib().gem_conv_forward(
+        _dtype(x, "x"), form, B, T, D, W, _seq(x, "x", x), _dense(weight, "weight", _F32, (D, W)), _optional(bias, "bias", (D,)),
+        _optional(state, "state", (B, W - 1, D)), _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)),
+        _seq(y, "y", x), _optional(state_last, "state_last", (B, W - 1, D)), _stream(stream, x.device)), "gem_conv_forward")
+
+
+def gem_conv_workspace(B: int, T: int, D: int, W: int) -> int:
+    return int(lib().gem_conv_workspace(B, T, D, W))
+
+
+def gem_conv_backward(x, weight, dy, dx, dweight, workspace, *, form: int = GEM_CONV_SILU, bias=None, dbias=None, state=None,
+                      lengths=None, reset=None, dstate_last=None, dstate=None, stream=None) -> None:
+    """dx [B, T, D], dweight [D, W], dbias [D] and dstate [B, W - 1, D] (the last three may be None) from dy
+    [B, T, D] and dstate_last [B, W - 1, D]; workspace float32, gem_conv_workspace(B, T, D, W) of it."""
+    if x.dim() != 3 or weight.dim() != 2:
+        raise ValueError("x, weight: expected [B, T, D] and [D, W] tensors")
+    B, T, D = x.shape
+    W = weight.shape[1]
+    size = gem_conv_workspace(B, T, D, W) if dweight is not None or dbias is not None else 0
+    check(lib().gem_conv_backward(
+        _dtype(x, "x"), form, B, T, D, W, _seq(x, "x", x), _dense(weight, "weight", _F32, (D, W)), _optional(bias, "bias", (D,)),
+        _optional(state, "state", (B, W - 1, D)), _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)),
+        _seq(dy, "dy", x), _optional(dstate_last, "dstate_last", (B, W - 1, D)), _seq(dx, "dx", x),
+        _optional(dweight, "dweight", (D, W)), _optional(dbias, "dbias", (D,)), _optional(dstate, "dstate", (B, W - 1, D)),
+        _space(workspace, "workspace", size, _F32), _stream(stream, x.device)), "gem_conv_backward")
+
+
+def _states(t, what: str, like, B, T, G, N):
+    """gem_seq_t of a [B, T, G, N] tensor whose last two dimensions lie side by side."""
+    if t.dtype is not like.dtype or not t.is_cuda:
+        raise TypeError(f"{what}: expected a {like.dtype} CUDA tensor")
+    if t.shape != (B, T, G, N):
+        raise ValueError(f"{what}: expected the shape {(B, T, G, N)}, got {tuple(t.shape)}")
+    sb, st, sg, sn = t.stride()
+    if (sn != 1 and N > 1) or (sg != N and G > 1):
+        raise TypeError(f"{what}: groups and states must be contiguous")
+    return GemSeq(t.data_ptr(), sb, st)
+
+
+def _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset):
+    if x.dim() != 3 or b.dim() != 4:
+        raise ValueError("x, b: expected [B, T, D] and [B, T, G, N] tensors")
+    (B, T, D), (G, N) = x.shape, b.shape[2:]
+    return GemSsm(B, T, D, N, G, int(softplus), _seq(x, "x", x), _seq(dt, "dt", x), _states(b, "b", x, B, T, G, N),
+                  _states(c, "c", x, B, T, G, N), GemSeq() if z is None else _seq(z, "z", x), _dense(A, "A", _F32, (D, N)),
+                  _optional(skip, "skip", (D,)), _optional(dt_bias, "dt_bias", (D,)), _optional(lengths, "lengths", (B,), _I32),
+                  _bytes(reset, "reset", (B, T)))
+
+
+def gem_ssm_saved_count(B: int, T: int, D: int, N: int) -> int:
+    return int(lib().gem_ssm_saved_count(B, T, D, N))
+
+
+def gem_ssm_workspace(B: int, T: int, D: int, N: int, G: int = 1, *, backward: bool = False) -> int:
+    return int(lib().gem_ssm_workspace(B, T, D, N, G, int(backward)))
+
+
+def gem_ssm_forward(x, dt, A, b, c, y, *, z=None, skip=None, dt_bias=None, softplus: bool = True, h0=None, lengths=None,
+                    reset=None, h_last=None, saved=None, workspace=None, stream=None) -> None:
+    """x, dt, z, y [B, T, D] (channels contiguous, any batch and time strides); b, c [B, T, G, N] (the last two
+    dimensions contiguous); A [D, N], skip, dt_bias [D], h0, h_last [B, D, N], saved [B, ceil(T / 16), D, N]
+    float32; lengths [B] int32; reset [B, T] uint8 or bool; workspace float32, gem_ssm_workspace(B, T, D, N, G)
+    of it."""
+    p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
+    B, T, D, N = p.B, p.T, p.D, p.N
+    check(lib().gem_ssm_forward(
+        _dtype(x, "x"), p, _optional(h0, "h0", (B, D, N)), _seq(y, "y", x), _optional(h_last, "h_last", (B, D, N)),
+        _optional(saved, "saved", (B, -(-T // GEM_SSM_CHUNK), D, N)),
+        _space(workspace, "workspace", lib().gem_ssm_workspace(B, T, D, N, p.G, 0), _F32), _stream(stream, x.device)), "gem_ssm_forward")
+
+
+def gem_ssm_backward(x, dt, A, b, c, saved, dy, dx, ddt, dA, db, dc, *, z=None, dz=None, skip=None, dskip=None, dt_bias=None,
+                     ddt_bias=None, softplus: bool = True, lengths=None, reset=None, dh_last=None, dh0=None, workspace=None,
+                     stream=None) -> None:
+    """Gradients of what gem_ssm_forward takes from dy [B, T, D] and dh_last [B, D, N]; saved is what the
+    forward call saved; dA, dskip, ddt_bias and dh0 may be None; workspace float32,
+    gem_ssm_workspace(B, T, D, N, G, backward=True) of it."""
+    p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
+    B, T, D, N, G = p.B, p.T, p.D, p.N, p.G
+    if (z is None) != (dz is None):
+        raise ValueError("z and dz come together")
+    out = GemSsmGrad(_seq(dx, "dx", x), _seq(ddt, "ddt", x), _states(db, "db", x, B, T, G, N), _states(dc, "dc", x, B, T, G, N),
+                     GemSeq() if dz is None else _seq(dz, "dz", x), _optional(dA, "dA", (D, N)), _optional(dskip, "dskip", (D,)),
+                     _optional(ddt_bias, "ddt_bias", (D,)), _optional(dh0, "dh0", (B, D, N)))
+    check(lib().gem_ssm_backward(
+        _dtype(x, "x"), p, _dense(saved, "saved", _F32, (B, -(-T // GEM_SSM_CHUNK), D, N)), _seq(dy, "dy", x),
+        _optional(dh_last, "dh_last", (B, D, N)), out,
+        _space(workspace, "workspace", lib().gem_ssm_workspace(B, T, D, N, G, 1), _F32), _stream(stream, x.device)), "gem_ssm_backward")
