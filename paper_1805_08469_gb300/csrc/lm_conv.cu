@@ -5,6 +5,8 @@
 // as well: step t's dp_t goes to the gradients of the W inputs it used, the oldest of which is then complete; it
 // goes W - 1 steps past the segment for that.  Sums for the weights are taken in registers over the
 // segment, in shared memory over the block's warps, and by a second kernel over the blocks, in that order.
+#include <type_traits>
+
 #include "lm_internal.h"
 
 namespace gem {
@@ -13,7 +15,7 @@ namespace {
 
 constexpr int kConvWarps = 4;       // most segments of time of a block, a warp each
 constexpr int kSegment = 64;        // steps of a segment
-constexpr int kAhead = 4;           // steps whose loads are in flight together
+constexpr int kGroup = 4;           // steps whose loads are in flight together; two groups are
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct ConvArgs {
@@ -30,18 +32,77 @@ struct ConvArgs {
   int D, columns, blocks;  // blocks along the channels, along a sequence's time
 };
 
-__device__ __forceinline__ float sigmoid(float v) {
-  float e, r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(-v * kLog2e));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+template <int V>
+__device__ __forceinline__ Vec<V> sigmoid(const Vec<V>& v) {
+  Vec<V> e = v * splat<V>(-kLog2e);
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.v[k]) : "f"(e.v[k]));
+  e = e + splat<V>(1.0f);
+#pragma unroll
+  for (int k = 0; k < V; ++k) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(e.v[k]) : "f"(e.v[k]));
+  return e;
+}
+
+// A thread's K channels: four as two pairs, or one.
+template <int K>
+constexpr int kVec = K == 4 ? 2 : 1;
+template <int K>
+struct Channels {
+  static constexpr int V = kVec<K>, P = K / V;
+  Vec<V> c[P];
+};
+template <int K>
+__device__ __forceinline__ Channels<K> none() {
+  Channels<K> r;
+#pragma unroll
+  for (int i = 0; i < Channels<K>::P; ++i) r.c[i] = splat<Channels<K>::V>(0.0f);
   return r;
 }
 
 // K neighbouring elements as they are in memory (K = 1: any alignment, K = 4: aligned to all four).
 template <typename E, int K>
-struct alignas(sizeof(E) * K) Piece {
-  E e[K];
+struct Raw;
+template <typename E>
+struct Raw<E, 1> {
+  E x;
+  __device__ __forceinline__ void read(const E* p) { x = *p; }
+  __device__ __forceinline__ void clear() { x = from_f32<E>(0.0f); }
+  __device__ __forceinline__ Channels<1> floats() const { return {{{to_f32(x)}}}; }
 };
+template <>
+struct Raw<float, 4> {
+  float4 x;
+  __device__ __forceinline__ void read(const float* p) { x = *reinterpret_cast<const float4*>(p); }
+  __device__ __forceinline__ void clear() { x = make_float4(0, 0, 0, 0); }
+  __device__ __forceinline__ Channels<4> floats() const { return {{{x.x, x.y}, {x.z, x.w}}}; }
+};
+template <typename E>
+__device__ __forceinline__ Vec<2> two(uint32_t w) {
+  if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+    return {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+  } else {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    return {f.x, f.y};
+  }
+}
+template <typename E>
+struct Raw<E, 4> {
+  uint2 x;
+  __device__ __forceinline__ void read(const E* p) { x = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void clear() { x = make_uint2(0, 0); }
+  __device__ __forceinline__ Channels<4> floats() const { return {{two<E>(x.x), two<E>(x.y)}}; }
+};
+template <typename E, int K>
+__device__ __forceinline__ void write_step(E* at, const Channels<K>& v) {
+  if constexpr (K == 1) {
+    *at = from_f32<E>(v.c[0].v[0]);
+  } else if constexpr (sizeof(E) == 4) {
+    *reinterpret_cast<float4*>(at) = make_float4(v.c[0].v[0], v.c[0].v[1], v.c[1].v[0], v.c[1].v[1]);
+  } else {
+    alignas(8) E e[4] = {from_f32<E>(v.c[0].v[0]), from_f32<E>(v.c[0].v[1]), from_f32<E>(v.c[1].v[0]), from_f32<E>(v.c[1].v[1])};
+    *reinterpret_cast<uint2*>(at) = *reinterpret_cast<const uint2*>(e);
+  }
+}
 
 // What a warp works on.
 struct ConvPlace {
@@ -63,15 +124,40 @@ __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& p) {
   return a;
 }
 
+// The steps of a segment, and those around it that it looks at, at which the state is dropped.  One warp calls.
+struct Resets {
+  static constexpr int kBefore = 4;
+  uint32_t bits[3];   // of steps first - kBefore + 32 i and on
+  int64_t from;
+  __device__ __forceinline__ Resets(const ConvArgs& p, const ConvPlace& a) : from(a.first - kBefore) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int64_t t = from + 32 * i + threadIdx.x % 32;
+      bits[i] = p.reset ? __ballot_sync(~0u, t >= 0 && t < a.n && p.reset[a.b * p.T + t] != 0) : 0u;
+    }
+  }
+  // Of steps t to t + kGroup - 1, the lowest bit that of t.
+  __device__ __forceinline__ unsigned group(int64_t t) const {
+    const int i = int(t - from);
+    const uint32_t low = i < 32 ? bits[0] : i < 64 ? bits[1] : bits[2], high = i < 32 ? bits[1] : i < 64 ? bits[2] : 0u;
+    return __funnelshift_r(low, high, i % 32) & ((1u << kGroup) - 1);
+  }
+  __device__ __forceinline__ bool at(int64_t t) const { return group(t) & 1; }
+};
+
 template <int W, int K>
 struct Taps {
-  float w[W][K], bias[K];
+  Channels<K> w[W], bias;
   __device__ __forceinline__ void read(const ConvArgs& p, const ConvPlace& a) {
+    bias = none<K>();
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j] = none<K>();
+    if (!a.on) return;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      bias[k] = p.bias && a.on ? p.bias[a.d + k] : 0.0f;
+      if (p.bias) bias.c[k / kVec<K>].v[k % kVec<K>] = p.bias[a.d + k];
 #pragma unroll
-      for (int j = 0; j < W; ++j) w[j][k] = a.on ? p.weight[int64_t(a.d + k) * W + j] : 0.0f;
+      for (int j = 0; j < W; ++j) w[j].c[k / kVec<K>].v[k % kVec<K>] = p.weight[int64_t(a.d + k) * W + j];
     }
   }
 };
@@ -80,73 +166,64 @@ struct Taps {
 // step's own document.
 template <typename E, int W, int K>
 struct Window {
-  float x[W][K];
+  Channels<K> x[W];
   int age;
 
   // The inputs before the segment's first step (which lie in the sequence, or in its state).
-  __device__ __forceinline__ void start(const ConvArgs& p, const ConvPlace& a, const E* row) {
+  __device__ __forceinline__ void start(const ConvArgs& p, const ConvPlace& a, const Resets& resets, const E* row) {
     age = W;
 #pragma unroll
-    for (int j = 0; j < W; ++j)
-#pragma unroll
-      for (int k = 0; k < K; ++k) x[j][k] = 0.0f;
+    for (int j = 0; j < W; ++j) x[j] = none<K>();
 #pragma unroll
     for (int j = 1; j < W; ++j) {
       const int64_t t = a.first - W + j;
+      if (t >= 0 && t < a.n && resets.at(t)) drop();
+      age = min(age + 1, W);
+      if (!a.on) continue;
       if (t >= 0) {
-        next(p, a, t);
-        if (a.on) {
-          const Piece<E, K> piece = *reinterpret_cast<const Piece<E, K>*>(row + t * p.x.stride_t);
+        Raw<E, K> raw;
+        raw.read(row + t * p.x.stride_t);
+        x[j] = raw.floats();
+      } else if (p.state) {
 #pragma unroll
-          for (int k = 0; k < K; ++k) x[j][k] = to_f32(piece.e[k]);
-        }
-      } else if (p.state && a.on) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) x[j][k] = p.state[(a.b * (W - 1) + t + W - 1) * p.D + a.d + k];
+        for (int k = 0; k < K; ++k) x[j].c[k / kVec<K>].v[k % kVec<K>] = p.state[(a.b * (W - 1) + t + W - 1) * p.D + a.d + k];
       }
     }
   }
-  __device__ __forceinline__ void next(const ConvArgs& p, const ConvPlace& a, int64_t t) {
-    age = p.reset && p.reset[a.b * p.T + t] ? 0 : min(age + 1, W);
+  // Every input so far counts as 0 from now on.
+  __device__ __forceinline__ void drop() {
+    age = -1;
+#pragma unroll
+    for (int j = 0; j < W; ++j) x[j] = none<K>();
   }
-  __device__ __forceinline__ void push(const ConvArgs& p, const ConvPlace& a, int64_t t, const Piece<E, K>& piece) {
-    next(p, a, t);
+  __device__ __forceinline__ void push(const Raw<E, K>& raw) {
 #pragma unroll
-    for (int j = 0; j + 1 < W; ++j)
-#pragma unroll
-      for (int k = 0; k < K; ++k) x[j][k] = x[j + 1][k];
-#pragma unroll
-    for (int k = 0; k < K; ++k) x[W - 1][k] = to_f32(piece.e[k]);
-    if (age < W - 1) {   // dropped inputs count as 0, whatever they hold
-#pragma unroll
-      for (int j = 0; j < W; ++j)
-#pragma unroll
-        for (int k = 0; k < K; ++k) x[j][k] = W - 1 - j > age ? 0.0f : x[j][k];
-    }
+    for (int j = 0; j + 1 < W; ++j) x[j] = x[j + 1];
+    x[W - 1] = raw.floats();
   }
 };
 
-// The pieces of steps [t, t + kAhead) below `end` (zeros for a thread without channels).
+// The elements of the group of steps from t on that lie below `end` (zeros for a thread without channels).
 template <typename E, int K>
-__device__ __forceinline__ void read_ahead(Piece<E, K> (&to)[kAhead], const E* row, int64_t stride, int64_t t, int64_t end, bool on) {
+__device__ __forceinline__ void read_group(Raw<E, K> (&to)[kGroup], const E* row, int64_t stride, int64_t t, int64_t end, bool on) {
 #pragma unroll
-  for (int u = 0; u < kAhead; ++u) {
-    to[u] = Piece<E, K>{};
-    if (on && t + u < end) to[u] = *reinterpret_cast<const Piece<E, K>*>(row + (t + u) * stride);
+  for (int u = 0; u < kGroup; ++u) {
+    to[u].clear();
+    if (on && t + u < end) to[u].read(row + (t + u) * stride);
   }
-}
-template <typename E, int K>
-__device__ __forceinline__ void write_step(E* at, const float (&v)[K]) {
-  Piece<E, K> piece;
-#pragma unroll
-  for (int k = 0; k < K; ++k) piece.e[k] = from_f32<E>(v[k]);
-  *reinterpret_cast<Piece<E, K>*>(at) = piece;
 }
 template <typename E, int K>
 __device__ __forceinline__ void write_zeros(E* row, int64_t stride, const ConvPlace& a) {
   if (!a.on) return;
-  const float none[K] = {};
-  for (int64_t t = max(a.first, a.n); t < a.end; ++t) write_step<E, K>(row + t * stride, none);
+  for (int64_t t = max(a.first, a.n); t < a.end; ++t) write_step<E, K>(row + t * stride, none<K>());
+}
+
+template <int W, int K>
+__device__ __forceinline__ Vec<kVec<K>> pre_activation(const Taps<W, K>& taps, const Channels<K> (&x)[W], int i) {
+  Vec<kVec<K>> v = taps.bias.c[i];
+#pragma unroll
+  for (int j = 0; j < W; ++j) v = fma<kVec<K>>(taps.w[j].c[i], x[j].c[i], v);
+  return v;
 }
 
 // A sequence's last inputs, by the warp whose segment it ends in (state_last may be state: only where one warp has
@@ -158,37 +235,50 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const Con
   const int64_t end = min(a.end, a.n);
   const E* const row = static_cast<const E*>(p.x.data) + a.b * p.x.stride_b + a.d;
   E* const out = static_cast<E*>(p.y.data) + a.b * p.y.stride_b + a.d;
+  const Resets resets(p, a);
   if (a.first < end || a.first == 0) {
+    constexpr int V = kVec<K>, P = Channels<K>::P;
     Taps<W, K> taps;
     taps.read(p, a);
     Window<E, W, K> win;
-    win.start(p, a, row);
-    Piece<E, K> ahead[kAhead], now[kAhead];
-    read_ahead<E, K>(ahead, row, p.x.stride_t, a.first, end, a.on);
-    for (int64_t t = a.first; t < end; t += kAhead) {
+    win.start(p, a, resets, row);
+    Raw<E, K> xs[2][kGroup];
+    auto step = [&](int64_t t, const Raw<E, K>& raw) {
+      win.push(raw);
+      Channels<K> y;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) now[u] = ahead[u];
-      read_ahead<E, K>(ahead, row, p.x.stride_t, t + kAhead, end, a.on);
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (t + u >= end) break;
-        win.push(p, a, t + u, now[u]);
-        float y[K];
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          float v = taps.bias[k];
-#pragma unroll
-          for (int j = 0; j < W; ++j) v = fmaf(taps.w[j][k], win.x[j][k], v);
-          y[k] = SILU ? v * sigmoid(v) : v;
-        }
-        if (a.on) write_step<E, K>(out + (t + u) * p.y.stride_t, y);
+      for (int i = 0; i < P; ++i) {
+        y.c[i] = pre_activation<W, K>(taps, win.x, i);
+        if (SILU) y.c[i] = y.c[i] * sigmoid<V>(y.c[i]);
       }
+      if (a.on) write_step<E, K>(out + t * p.y.stride_t, y);
+    };
+    auto group = [&](int64_t t, const Raw<E, K> (&raw)[kGroup]) {
+      const unsigned drops = resets.group(t);
+      if (t + kGroup <= end && drops == 0) {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) step(t + u, raw[u]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) {
+          if (t + u >= end) break;
+          if (drops >> u & 1) win.drop();
+          step(t + u, raw[u]);
+        }
+      }
+    };
+    read_group<E, K>(xs[0], row, p.x.stride_t, a.first, end, a.on);
+    for (int64_t t = a.first; t < end; t += 2 * kGroup) {
+      read_group<E, K>(xs[1], row, p.x.stride_t, t + kGroup, end, a.on);
+      group(t, xs[0]);
+      read_group<E, K>(xs[0], row, p.x.stride_t, t + 2 * kGroup, end, a.on);
+      if (t + kGroup < end) group(t + kGroup, xs[1]);
     }
     if (p.state_last && a.on) {
 #pragma unroll
       for (int j = 1; j < W; ++j)
 #pragma unroll
-        for (int k = 0; k < K; ++k) p.state_last[(a.b * (W - 1) + j - 1) * p.D + a.d + k] = win.x[j][k];
+        for (int k = 0; k < K; ++k) p.state_last[(a.b * (W - 1) + j - 1) * p.D + a.d + k] = win.x[j].c[k / kVec<K>].v[k % kVec<K>];
     }
   }
   write_zeros<E, K>(out, p.y.stride_t, a);
@@ -225,67 +315,87 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
   const E* const row = static_cast<const E*>(p.x.data) + a.b * p.x.stride_b + a.d;
   const E* const dy = static_cast<const E*>(p.dy.data) + a.b * p.dy.stride_b + a.d;
   E* const out = static_cast<E*>(p.y.data) + a.b * p.y.stride_b + a.d;
-  float dw[W + 1][K] = {};
+  const Resets resets(p, a);
+  constexpr int V = kVec<K>, P = Channels<K>::P;
+  Channels<K> dw[W + 1];
+#pragma unroll
+  for (int j = 0; j <= W; ++j) dw[j] = none<K>();
   if (a.first < end || a.first == 0) {
     Taps<W, K> taps;
     taps.read(p, a);
     Window<E, W, K> win;
-    win.start(p, a, row);
-    float dx[W][K] = {};   // gradients of the window's inputs
+    win.start(p, a, resets, row);
+    Channels<K> dx[W];   // gradients of the window's inputs
+#pragma unroll
+    for (int j = 0; j < W; ++j) dx[j] = none<K>();
     // the complete gradient of input t, which is the segment's, or the state's for the first one
-    auto put = [&](int64_t t, const float (&v)[K]) {
+    auto put = [&](int64_t t, const Channels<K>& v) {
       if (!a.on || t >= a.end) return;
       if (t >= a.first) {
         write_step<E, K>(out + t * p.y.stride_t, v);
       } else if (t < 0 && a.first == 0 && p.dstate) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) p.dstate[(a.b * (W - 1) + t + W - 1) * p.D + a.d + k] = v[k];
+        for (int k = 0; k < K; ++k) p.dstate[(a.b * (W - 1) + t + W - 1) * p.D + a.d + k] = v.c[k / V].v[k % V];
       }
     };
-    Piece<E, K> xs[kAhead], gs[kAhead], x_now[kAhead], g_now[kAhead];
-    read_ahead<E, K>(xs, row, p.x.stride_t, a.first, reach, a.on);
-    read_ahead<E, K>(gs, dy, p.dy.stride_t, a.first, reach, a.on);
-    for (int64_t t0 = a.first; t0 < reach; t0 += kAhead) {
+    // one step: `all` of its taps lie in its document, and it is the segment's `own`
+    auto step = [&](const Raw<E, K>& raw_x, const Raw<E, K>& raw_g, bool all, bool own) {
+      win.push(raw_x);
+      const Channels<K> dy = raw_g.floats();
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        x_now[u] = xs[u];
-        g_now[u] = gs[u];
-      }
-      read_ahead<E, K>(xs, row, p.x.stride_t, t0 + kAhead, reach, a.on);
-      read_ahead<E, K>(gs, dy, p.dy.stride_t, t0 + kAhead, reach, a.on);
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int64_t t = t0 + u;
-        if (t >= reach) break;
-        win.push(p, a, t, x_now[u]);
-        const bool own = t < end;   // (steps past the segment only complete its inputs' gradients)
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          float g = to_f32(g_now[u].e[k]);
-          if (SILU) {
-            float v = taps.bias[k];
-#pragma unroll
-            for (int j = 0; j < W; ++j) v = fmaf(taps.w[j][k], win.x[j][k], v);
-            const float s = sigmoid(v);
-            g *= s * fmaf(v, 1.0f - s, 1.0f);
-          }
-#pragma unroll
-          for (int j = 0; j < W; ++j) {
-            dx[j][k] = j + 1 < W ? dx[j + 1][k] : 0.0f;
-            if (W - 1 - j <= win.age) dx[j][k] = fmaf(g, taps.w[j][k], dx[j][k]);
-            if (own) dw[j][k] = fmaf(g, win.x[j][k], dw[j][k]);
-          }
-          if (own) dw[W][k] += g;
+      for (int i = 0; i < P; ++i) {
+        Vec<V> g = dy.c[i];
+        if (SILU) {
+          const Vec<V> v = pre_activation<W, K>(taps, win.x, i), s = sigmoid<V>(v), one = splat<V>(1.0f);
+          g = g * (s * fma<V>(v, one - s, one));
         }
-        put(t - W + 1, dx[0]);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+          dx[j].c[i] = j + 1 < W ? dx[j + 1].c[i] : splat<V>(0.0f);
+          if (all || W - 1 - j <= win.age) dx[j].c[i] = fma<V>(g, taps.w[j].c[i], dx[j].c[i]);
+          if (own) dw[j].c[i] = fma<V>(g, win.x[j].c[i], dw[j].c[i]);
+        }
+        if (own) dw[W].c[i] = dw[W].c[i] + g;
       }
+    };
+    auto group = [&](int64_t t, const Raw<E, K> (&raw_x)[kGroup], const Raw<E, K> (&raw_g)[kGroup]) {
+      const unsigned drops = resets.group(t);
+      if (t + kGroup <= end && drops == 0 && win.age >= W - 2 && t >= a.first + W - 1) {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) {
+          step(raw_x[u], raw_g[u], true, true);
+          if (a.on) write_step<E, K>(out + (t + u - W + 1) * p.y.stride_t, dx[0]);
+        }
+        win.age = W;
+      } else {
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u) {
+          if (t + u >= reach) break;
+          if (drops >> u & 1) win.drop();
+          win.age = min(win.age + 1, W);
+          step(raw_x[u], raw_g[u], false, t + u < end);   // (steps past the segment only complete its inputs' gradients)
+          put(t + u - W + 1, dx[0]);
+        }
+      }
+    };
+    Raw<E, K> xs[2][kGroup], gs[2][kGroup];
+    auto read = [&](int i, int64_t t) {
+      read_group<E, K>(xs[i], row, p.x.stride_t, t, reach, a.on);
+      read_group<E, K>(gs[i], dy, p.dy.stride_t, t, reach, a.on);
+    };
+    read(0, a.first);
+    for (int64_t t = a.first; t < reach; t += 2 * kGroup) {
+      read(1, t + kGroup);
+      group(t, xs[0], gs[0]);
+      read(0, t + 2 * kGroup);
+      if (t + kGroup < reach) group(t + kGroup, xs[1], gs[1]);
     }
     if (reach == a.n) {   // the sequence ends here: no later step completes its last inputs
 #pragma unroll
       for (int j = 1; j < W; ++j) {
         if (p.dstate_last && a.on && (a.n == 0 || W - 1 - j <= win.age)) {
 #pragma unroll
-          for (int k = 0; k < K; ++k) dx[j][k] += p.dstate_last[(a.b * (W - 1) + j - 1) * p.D + a.d + k];
+          for (int k = 0; k < K; ++k) dx[j].c[k / V].v[k % V] += p.dstate_last[(a.b * (W - 1) + j - 1) * p.D + a.d + k];
         }
         put(a.n - W + j, dx[j]);
       }
@@ -296,14 +406,14 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
 #pragma unroll
   for (int j = 0; j <= W; ++j)
 #pragma unroll
-    for (int k = 0; k < K; ++k) sums[warp][j][k][lane] = dw[j][k];
+    for (int k = 0; k < K; ++k) sums[warp][j][k][lane] = dw[j].c[k / V].v[k % V];
   __syncthreads();
   if (warp != 0 || !a.on) return;
 #pragma unroll
   for (int j = 0; j <= W; ++j)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      float v = dw[j][k];
+      float v = dw[j].c[k / V].v[k % V];
       for (int q = 1; q < int(blockDim.x) / 32; ++q) v += sums[q][j][k][lane];
       p.partial[(a.row * (W + 1) + j) * p.D + a.d + k] = v;
     }

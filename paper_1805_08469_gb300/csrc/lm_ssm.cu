@@ -1,4 +1,6 @@
 // Selective state space scan: the calls of include/gem_lm.h (argument checks, cuts and dispatch).
+#include <algorithm>
+
 #include "lm_ssm.h"
 
 namespace gem {
@@ -47,15 +49,15 @@ bool inputs_ok(int dtype, const gem_ssm_t* in) {
   return optional_ok(in->skip) && optional_ok(in->dt_bias) && optional_ok(in->lengths);
 }
 
-// Whether the pieces of V elements that blocks of CH channels read lie at multiples of their size (16 bytes at most).
+// Whether the pieces of V channels, or states, that blocks read lie at multiples of their size (16 bytes at most).
 bool in_pieces(const gem_seq_t& s, int dtype, const gem_ssm_t& in, int V) {
   const int64_t e = dtype_size(dtype), bytes = std::min(int64_t(16), V * e), per = bytes / e;
-  return aligned_to(s.data, size_t(bytes)) && (in.D / in.G) % per == 0 && (in.B <= 1 || s.stride_b % per == 0) &&
-         (in.T <= 1 || s.stride_t % per == 0);
+  return aligned_to(s.data, size_t(bytes)) && (in.B <= 1 || s.stride_b % per == 0) && (in.T <= 1 || s.stride_t % per == 0);
 }
-bool in_quads(const gem_seq_t& s, int dtype, const gem_ssm_t& in) {
-  return aligned_to(s.data, size_t(4 * dtype_size(dtype))) && in.N % 4 == 0 && (in.B <= 1 || s.stride_b % 4 == 0) &&
-         (in.T <= 1 || s.stride_t % 4 == 0);
+bool inputs_wide(const gem_ssm_t& in, int dtype, int V) {
+  return in.N % kQuad == 0 && in.D / in.G % V == 0 && in_pieces(in.x, dtype, in, V) && in_pieces(in.dt, dtype, in, V) &&
+         (!in.z.data || in_pieces(in.z, dtype, in, V)) && in_pieces(in.b, dtype, in, kQuad) && in_pieces(in.c, dtype, in, kQuad) &&
+         aligned_to(in.A, 16);
 }
 
 int64_t split_floats(const gem_ssm_t& in, const SsmCut& c) { return c.splits > 1 ? in.B * c.splits * in.D * (int64_t(in.N) + 1) : 0; }
@@ -109,13 +111,8 @@ int gem_ssm_forward(int dtype, const gem_ssm_t* in, const float* h0, const gem_s
   p.saved = saved;
   p.states = workspace;
   const int V = block_channels(in->N, kForwardK) / 8;
-  p.vec = (in_pieces(in->x, dtype, *in, V) ? kVecX : 0) | (in_pieces(in->dt, dtype, *in, V) ? kVecDt : 0) |
-          (in_pieces(in->z, dtype, *in, V) ? kVecZ : 0) | (in_pieces(*y, dtype, *in, V) ? kVecY : 0) |
-          (in_quads(in->b, dtype, *in) ? kVecB : 0) | (in_quads(in->c, dtype, *in) ? kVecC : 0);
-  if (in->N % 4 == 0) {
-    if (aligned_to(in->A, 16) && aligned_to(h0, 16) && aligned_to(h_last, 16) && aligned_to(workspace, 16)) p.vec |= kVecState;
-    if (aligned_to(saved, 16)) p.vec |= kVecSaved;
-  }
+  p.wide = inputs_wide(*in, dtype, V) && in_pieces(*y, dtype, *in, V) && aligned_to(h0, 16) && aligned_to(h_last, 16) && aligned_to(saved, 16) &&
+           aligned_to(workspace, 16);
   return launch_status(BY_TYPE(launch_forward, p, static_cast<cudaStream_t>(stream)));
 }
 
@@ -149,15 +146,9 @@ int gem_ssm_backward(int dtype, const gem_ssm_t* in, const float* saved, const g
   p.states = workspace;
   p.params = params;
   const int V = block_channels(in->N, kBackwardK) / 8;
-  p.vec = (in_pieces(in->x, dtype, *in, V) ? kVecX : 0) | (in_pieces(in->dt, dtype, *in, V) ? kVecDt : 0) |
-          (in_pieces(in->z, dtype, *in, V) ? kVecZ : 0) | (in_pieces(*dy, dtype, *in, V) ? kVecDy : 0) |
-          (in_pieces(out->dx, dtype, *in, V) ? kVecDx : 0) | (in_pieces(out->ddt, dtype, *in, V) ? kVecDdt : 0) |
-          (in_pieces(out->dz, dtype, *in, V) ? kVecDz : 0) | (in_quads(in->b, dtype, *in) ? kVecB : 0) |
-          (in_quads(in->c, dtype, *in) ? kVecC : 0);
-  if (in->N % 4 == 0) {
-    if (aligned_to(in->A, 16) && aligned_to(dh_last, 16) && aligned_to(out->dh0, 16) && aligned_to(workspace, 16)) p.vec |= kVecState;
-    if (aligned_to(saved, 16)) p.vec |= kVecSaved;
-  }
+  p.wide = inputs_wide(*in, dtype, V) && in_pieces(*dy, dtype, *in, V) && in_pieces(out->dx, dtype, *in, V) && in_pieces(out->ddt, dtype, *in, V) &&
+           (!in->z.data || in_pieces(out->dz, dtype, *in, V)) && aligned_to(dh_last, 16) && aligned_to(out->dh0, 16) && aligned_to(saved, 16) &&
+           aligned_to(workspace, 16);
   return launch_status(BY_TYPE(launch_backward, p, static_cast<cudaStream_t>(stream)));
 }
 

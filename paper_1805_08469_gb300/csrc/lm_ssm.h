@@ -38,10 +38,8 @@ struct SsmArgs {
   bool params;             // whether any of dA, dskip and ddt_bias is asked for
   int splits, blocks;      // of a sequence's time, of a group's channels
   int64_t steps;           // of a split
-  int vec;                 // bit per tensor: its pieces lie at multiples of their size
+  bool wide;               // pieces of all tensors are whole and lie at multiples of their size (16 bytes at most)
 };
-enum { kVecX = 1, kVecDt = 2, kVecZ = 4, kVecB = 8, kVecC = 16, kVecY = 32, kVecDy = 64, kVecDx = 128, kVecDdt = 256, kVecDz = 512,
-       kVecState = 1024, kVecSaved = 2048 };
 
 __device__ __forceinline__ float ex2(float x) {
   float r;
@@ -79,54 +77,103 @@ __device__ __forceinline__ Vec<2> decay(float step, const Vec<2>& A2) {
 // That over a split: above 0, so that an infinite state does not become NaN by leaving fp32.
 __device__ __forceinline__ float far_decay(float sum, float A2) { return fmaxf(ex2(sum * A2), 1.4e-45f); }
 
-// n neighbouring elements as they are in memory.
-template <typename E, int V>
-struct alignas(sizeof(E) * V < 16 ? sizeof(E) * V : 16) Piece {
-  E e[V];
-};
-
-// `there` (<= V) elements from p on, zeros past them.
-template <typename E, int V>
-__device__ __forceinline__ Piece<E, V> load_piece(const E* p, bool vec, int there) {
-  Piece<E, V> r;
-  if (vec && there >= V) return *reinterpret_cast<const Piece<E, V>*>(p);
+// V neighbouring elements as they are in memory: in words where WIDE (all of them exist or none), else one by one, of which
+// `there` exist.  (Loads that pack single elements would wait for each.)
+template <typename E, int V, bool WIDE>
+struct Raw {
+  static constexpr bool kInWords = WIDE && V * sizeof(E) >= 4;
+  static constexpr int kWords = kInWords ? V * int(sizeof(E)) / 4 : 1, kSingles = kInWords ? 1 : V;
+  uint32_t w[kWords];
+  E x[kSingles];
+  __device__ __forceinline__ void read(const E* p, int there) {
+    if constexpr (kInWords) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) r.e[k] = k < there ? p[k] : from_f32<E>(0.0f);
-  return r;
-}
-template <typename E, int V>
-__device__ __forceinline__ void store_piece(E* p, bool vec, int there, const float (&v)[V]) {
-  Piece<E, V> r;
+      for (int i = 0; i < kWords; ++i) w[i] = 0;
+      if (there <= 0) return;
+      if constexpr (kWords >= 4) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) r.e[k] = from_f32<E>(v[k]);
-  if (vec && there >= V) {
-    *reinterpret_cast<Piece<E, V>*>(p) = r;
-    return;
+        for (int i = 0; i < kWords; i += 4) {
+          const uint4 q = *reinterpret_cast<const uint4*>(p + i * 4 / int(sizeof(E)));
+          w[i] = q.x, w[i + 1] = q.y, w[i + 2] = q.z, w[i + 3] = q.w;
+        }
+      } else if constexpr (kWords == 2) {
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        w[0] = q.x, w[1] = q.y;
+      } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        x[k] = from_f32<E>(0.0f);
+        if (k < there) x[k] = p[k];
+      }
+    }
   }
+  __device__ __forceinline__ float operator[](int k) const {
+    if constexpr (!kInWords) {
+      return to_f32(x[k]);
+    } else if constexpr (sizeof(E) == 4) {
+      return __uint_as_float(w[k]);
+    } else {
+      const uint16_t half = uint16_t(w[k / 2] >> (k % 2 * 16));
+      return to_f32(*reinterpret_cast<const E*>(&half));
+    }
+  }
+};
+template <typename E, int V, bool WIDE>
+__device__ __forceinline__ void store_piece(E* p, int there, const float (&v)[V]) {
+  if constexpr (Raw<E, V, WIDE>::kInWords) {
+    constexpr int kBytes = V * int(sizeof(E)) < 16 ? V * int(sizeof(E)) : 16, kEach = kBytes / int(sizeof(E));
+    if (there <= 0) return;
 #pragma unroll
-  for (int k = 0; k < V; ++k)
-    if (k < there) p[k] = r.e[k];
+    for (int i = 0; i < V; i += kEach) {
+      alignas(16) E e[kEach];
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) e[k] = from_f32<E>(v[i + k]);
+      if constexpr (kBytes == 16)
+        *reinterpret_cast<uint4*>(p + i) = *reinterpret_cast<const uint4*>(e);
+      else if constexpr (kBytes == 8)
+        *reinterpret_cast<uint2*>(p + i) = *reinterpret_cast<const uint2*>(e);
+      else
+        *reinterpret_cast<uint32_t*>(p + i) = *reinterpret_cast<const uint32_t*>(e);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      if (k < there) p[k] = from_f32<E>(v[k]);
+  }
 }
 
-// Four states from p on, of which `there` exist.
+// Four states from p on, of which `there` exist (WIDE: all or none).
 struct Quad {
   Vec<2> a, b;
 };
 __device__ __forceinline__ Quad zeros() { return {splat<2>(0.0f), splat<2>(0.0f)}; }
 __device__ __forceinline__ Quad quad(const float4& v) { return {{v.x, v.y}, {v.z, v.w}}; }
-__device__ __forceinline__ Quad load_quad(const float* p, bool vec, int there) {
-  if (vec && there >= kQuad) return quad(*reinterpret_cast<const float4*>(p));
-  return {{there > 0 ? p[0] : 0.0f, there > 1 ? p[1] : 0.0f}, {there > 2 ? p[2] : 0.0f, there > 3 ? p[3] : 0.0f}};
-}
-__device__ __forceinline__ void store_quad(float* p, bool vec, int there, const Quad& q) {
-  if (vec && there >= kQuad) {
-    *reinterpret_cast<float4*>(p) = make_float4(q.a.v[0], q.a.v[1], q.b.v[0], q.b.v[1]);
-    return;
+template <bool WIDE>
+__device__ __forceinline__ Quad load_quad(const float* p, int there) {
+  float4 v = make_float4(0, 0, 0, 0);
+  if constexpr (WIDE) {
+    if (there > 0) v = *reinterpret_cast<const float4*>(p);
+  } else {
+    if (there > 0) v.x = p[0];
+    if (there > 1) v.y = p[1];
+    if (there > 2) v.z = p[2];
+    if (there > 3) v.w = p[3];
   }
-  if (there > 0) p[0] = q.a.v[0];
-  if (there > 1) p[1] = q.a.v[1];
-  if (there > 2) p[2] = q.b.v[0];
-  if (there > 3) p[3] = q.b.v[1];
+  return quad(v);
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_quad(float* p, int there, const Quad& q) {
+  if constexpr (WIDE) {
+    if (there > 0) *reinterpret_cast<float4*>(p) = make_float4(q.a.v[0], q.a.v[1], q.b.v[0], q.b.v[1]);
+  } else {
+    if (there > 0) p[0] = q.a.v[0];
+    if (there > 1) p[1] = q.a.v[1];
+    if (there > 2) p[2] = q.b.v[0];
+    if (there > 3) p[3] = q.b.v[1];
+  }
 }
 
 // How a block is laid out.
@@ -194,11 +241,11 @@ __device__ __forceinline__ E* at(const gem_seq_t& s, int64_t b, int64_t t, int d
 }
 
 // b and c of a tile, loaded ahead: a thread has quads of states of some steps.
-template <typename E, typename S, bool HAS_B, bool HAS_C>
+template <typename E, typename S, bool WIDE, bool HAS_B, bool HAS_C>
 struct States {
   static constexpr int each = (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS / kSsmThreads > 0 ? (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS / kSsmThreads : 1;
   static constexpr int total = (HAS_B && HAS_C ? 2 : 1) * kTile * S::LS;
-  Piece<E, kQuad> e[each];
+  Raw<E, kQuad, WIDE> e[each];
   __device__ __forceinline__ void load(const SsmArgs& p, const Place<S>& a, int64_t t0) {
 #pragma unroll
     for (int i = 0; i < each; ++i) {
@@ -206,7 +253,7 @@ struct States {
       const bool is_c = !HAS_B || (HAS_C && at_ >= kTile * S::LS);
       const int there = at_ < total && t0 + s < a.n ? min(max(a.states - q * kQuad, 0), kQuad) : 0;
       const gem_seq_t& from = is_c ? p.in.c : p.in.b;
-      e[i] = load_piece<E, kQuad>(at<E>(from, a.b, t0 + s, a.group * a.states + q * kQuad), p.vec & (is_c ? kVecC : kVecB), there);
+      e[i].read(at<E>(from, a.b, t0 + s, a.group * a.states + q * kQuad), there);
     }
   }
   // Into [HAS_B + HAS_C][kTile][LS] quads.
@@ -214,7 +261,7 @@ struct States {
 #pragma unroll
     for (int i = 0; i < each; ++i) {
       const int at_ = i * kSsmThreads + threadIdx.x;
-      if (at_ < total) to[at_] = make_float4(to_f32(e[i].e[0]), to_f32(e[i].e[1]), to_f32(e[i].e[2]), to_f32(e[i].e[3]));
+      if (at_ < total) to[at_] = make_float4(e[i][0], e[i][1], e[i][2], e[i][3]);
     }
   }
 };

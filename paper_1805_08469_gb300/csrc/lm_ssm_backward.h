@@ -20,7 +20,7 @@ namespace ssm {
 
 __device__ __forceinline__ Vec<2> scaled(const Vec<2>& a, float b) { return a * splat<2>(b); }
 
-template <typename E, int LS, bool GATE, bool STATES>
+template <typename E, int LS, bool WIDE, bool GATE, bool STATES>
 __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kernel(const SsmArgs p) {
   using S = Shape<LS, kBackwardK>;
   constexpr int kSums = GATE ? 3 : 2;
@@ -34,23 +34,23 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
   if (STATES && a.split == 0) return;
   const int64_t D = p.in.D, N = a.states;
   const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
-  const bool vec = p.vec & kVecState, has = a.has(0);
+  const bool has = a.has(0);
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
 
-  Quad A2 = has ? load_quad(p.in.A + a.state(0, D, 0), vec, a.quads) : zeros();
+  Quad A2 = has ? load_quad<WIDE>(p.in.A + a.state(0, D, 0), a.quads) : zeros();
   A2 = {scaled(A2.a, kLog2e), scaled(A2.b, kLog2e)};
   Quad g = zeros();
   if (has) {
     if (p.splits == 1 || (STATES && a.split + 1 == p.splits)) {
-      if (p.h0) g = load_quad(p.h0 + a.state(a.b, D, 0), vec, a.quads);
+      if (p.h0) g = load_quad<WIDE>(p.h0 + a.state(a.b, D, 0), a.quads);
       // (the second pass's own copy: dh0 may be dh_last)
-      if (STATES) store_quad(p.states + a.state(a.b * p.splits, D, 0), vec, a.quads, g);
+      if (STATES) store_quad<WIDE>(p.states + a.state(a.b * p.splits, D, 0), a.quads, g);
     } else if (!STATES) {
-      if (a.split + 1 == p.splits) g = load_quad(p.states + a.state(a.b * p.splits, D, 0), vec, a.quads);
+      if (a.split + 1 == p.splits) g = load_quad<WIDE>(p.states + a.state(a.b * p.splits, D, 0), a.quads);
 #pragma unroll 4
       for (int q = p.splits - 1; q > a.split; --q) {
         const int64_t from = a.b * p.splits + q;
-        const Quad first = load_quad(p.states + a.state(from, D, 0), vec, a.quads);
+        const Quad first = load_quad<WIDE>(p.states + a.state(from, D, 0), a.quads);
         const float sum = p.sums[from * D + a.d0 + a.channel(0)];
         if (sum == INFINITY || q == p.splits - 1) {
           g = first;
@@ -72,19 +72,19 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
   float total = 0.0f;
   bool dropped = false;
 
-  Piece<E, S::V> x, dt, z, dy, x_next, dt_next, z_next, dy_next;
-  States<E, S, !STATES, true> b_next;
+  Raw<E, S::V, WIDE> x, dt, z, dy, x_next, dt_next, z_next, dy_next;
+  States<E, S, WIDE, !STATES, true> b_next;
   Quad start_next = zeros();
   const int64_t chunks = (p.in.T + kTile - 1) / kTile;
   auto load = [&](int64_t t0) {
     const int64_t t = t0 + a.s;
     const int there = t < end ? a.there : 0, d = a.d0 + a.c0;
-    if (!STATES) x_next = load_piece<E, S::V>(at<E>(p.in.x, a.b, t, d), p.vec & kVecX, there);
-    dt_next = load_piece<E, S::V>(at<E>(p.in.dt, a.b, t, d), p.vec & kVecDt, there);
-    if (GATE) z_next = load_piece<E, S::V>(at<E>(p.in.z, a.b, t, d), p.vec & kVecZ, there);
-    dy_next = load_piece<E, S::V>(at<E>(p.dy, a.b, t, d), p.vec & kVecDy, there);
+    if (!STATES) x_next.read(at<E>(p.in.x, a.b, t, d), there);
+    dt_next.read(at<E>(p.in.dt, a.b, t, d), there);
+    if (GATE) z_next.read(at<E>(p.in.z, a.b, t, d), there);
+    dy_next.read(at<E>(p.dy, a.b, t, d), there);
     b_next.load(p, a, t0);
-    if (!STATES && has) start_next = load_quad(p.saved + a.state(a.b * chunks + t0 / kTile, D, 0), p.vec & kVecSaved, a.quads);
+    if (!STATES && has) start_next = load_quad<WIDE>(p.saved + a.state(a.b * chunks + t0 / kTile, D, 0), a.quads);
   };
   const int64_t tiles = end > a.first ? (end - a.first + kTile - 1) / kTile : 0;
   if (tiles > 0) load(a.first + (tiles - 1) * kTile);
@@ -97,10 +97,10 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
     const bool in = t0 + a.s < end;
 #pragma unroll
     for (int j = 0; j < S::V; ++j) {
-      const float step = in ? step_of(p, to_f32(dt.e[j]) + bias[j]) : 0.0f;
-      steps[a.s][j * 8 + a.o] = {step, in && !STATES ? step * to_f32(x.e[j]) : 0.0f};
-      float gy = to_f32(dy.e[j]);
-      if (GATE) gy *= to_f32(z.e[j]) * sigmoid(to_f32(z.e[j]));
+      const float step = in ? step_of(p, dt[j] + bias[j]) : 0.0f;
+      steps[a.s][j * 8 + a.o] = {step, in && !STATES ? step * x[j] : 0.0f};
+      float gy = dy[j];
+      if (GATE) gy *= z[j] * sigmoid(z[j]);
       gys[a.s][j * 8 + a.o] = in ? gy : 0.0f;
     }
     b_next.stage(bc);
@@ -144,6 +144,12 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
           now.a = fma<2>(decay(v.x, A2.a), now.a, splat<2>(v.y) * b.a);
           now.b = fma<2>(decay(v.x, A2.b), now.b, splat<2>(v.y) * b.b);
           h[t] = now;
+        }
+        // (the decays are computed again: kept from the first loop they would take the registers of as many states)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          asm volatile("" : "+f"(A2.a.v[i]));
+          asm volatile("" : "+f"(A2.b.v[i]));
         }
         float sq[LS], sb[LS], sy[LS];
 #pragma unroll
@@ -219,9 +225,9 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
 #pragma unroll
         for (int j = 0; j < S::V; ++j) {
           const int i = j * 8 + a.o;
-          const float xj = to_f32(x.e[j]), sg = sums[1][a.s][i], gy = gys[a.s][i];
+          const float xj = x[j], sg = sums[1][a.s][i], gy = gys[a.s][i];
           float d = fmaf(sg, xj, sums[0][a.s][i] * kLn2);
-          if (p.in.softplus) d *= sigmoid(to_f32(dt.e[j]) + bias[j]);
+          if (p.in.softplus) d *= sigmoid(dt[j] + bias[j]);
           out[0][j] = in ? fmaf(sg, steps[a.s][i].x, skip[j] * gy) : 0.0f;
           out[1][j] = in ? d : 0.0f;
           if (in) {
@@ -229,27 +235,27 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
             dbias[j] += d;
           }
           if (GATE) {
-            const float zj = to_f32(z.e[j]), sig = sigmoid(zj);
-            out[2][j] = in ? to_f32(dy.e[j]) * fmaf(skip[j], xj, sums[kSums - 1][a.s][i]) * (sig * fmaf(zj, 1.0f - sig, 1.0f)) : 0.0f;
+            const float zj = z[j], sig = sigmoid(zj);
+            out[2][j] = in ? dy[j] * fmaf(skip[j], xj, sums[kSums - 1][a.s][i]) * (sig * fmaf(zj, 1.0f - sig, 1.0f)) : 0.0f;
           }
         }
         const int64_t t = t0 + a.s;
         const int d = a.d0 + a.c0;
-        store_piece<E, S::V>(at<E>(p.dx, a.b, t, d), p.vec & kVecDx, a.there, out[0]);
-        store_piece<E, S::V>(at<E>(p.ddt, a.b, t, d), p.vec & kVecDdt, a.there, out[1]);
-        if (GATE) store_piece<E, S::V>(at<E>(p.dz, a.b, t, d), p.vec & kVecDz, a.there, out[2]);
+        store_piece<E, S::V, WIDE>(at<E>(p.dx, a.b, t, d), a.there, out[0]);
+        store_piece<E, S::V, WIDE>(at<E>(p.ddt, a.b, t, d), a.there, out[1]);
+        if (GATE) store_piece<E, S::V, WIDE>(at<E>(p.dz, a.b, t, d), a.there, out[2]);
       }
       __syncthreads();   // (the next tile's steps replace these)
     }
   }
   if constexpr (STATES) {
     if (has) {
-      store_quad(p.states + a.state(row, D, 0), vec, a.quads, g);
+      store_quad<WIDE>(p.states + a.state(row, D, 0), a.quads, g);
       if (a.g == 0) p.sums[row * D + a.d0 + a.channel(0)] = dropped ? INFINITY : total;
     }
     return;
   } else {
-    if (has && a.split == 0 && p.h_last) store_quad(p.h_last + a.state(a.b, D, 0), vec, a.quads, g);
+    if (has && a.split == 0 && p.h_last) store_quad<WIDE>(p.h_last + a.state(a.b, D, 0), a.quads, g);
     if (has && p.params) {
       const float v[kQuad] = {dA.a.v[0], dA.a.v[1], dA.b.v[0], dA.b.v[1]};
 #pragma unroll
@@ -276,9 +282,9 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
     const float none[S::V] = {};
     for (int64_t t = past + a.s; t < a.end; t += kTile) {
       const int d = a.d0 + a.c0;
-      store_piece<E, S::V>(at<E>(p.dx, a.b, t, d), p.vec & kVecDx, a.there, none);
-      store_piece<E, S::V>(at<E>(p.ddt, a.b, t, d), p.vec & kVecDdt, a.there, none);
-      if (GATE) store_piece<E, S::V>(at<E>(p.dz, a.b, t, d), p.vec & kVecDz, a.there, none);
+      store_piece<E, S::V, WIDE>(at<E>(p.dx, a.b, t, d), a.there, none);
+      store_piece<E, S::V, WIDE>(at<E>(p.ddt, a.b, t, d), a.there, none);
+      if (GATE) store_piece<E, S::V, WIDE>(at<E>(p.dz, a.b, t, d), a.there, none);
     }
     if (p.blocks == 1) {
       const int64_t left = a.end - max(end, a.first);
@@ -328,7 +334,7 @@ static __global__ void __launch_bounds__(128) ssm_join_params_kernel(const SsmAr
   }
 }
 
-template <typename E, int LS>
+template <typename E, int LS, bool WIDE>
 cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
   using S = Shape<LS, kBackwardK>;
   const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
@@ -348,11 +354,11 @@ cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   if (grid.x > 0) {
     if (cut.splits > 1)
-      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, true, true>, grid, block, 0, stream, p)
-               : launch_pdl(ssm_backward_kernel<E, LS, false, true>, grid, block, 0, stream, p);
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, true>, grid, block, 0, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, true>, grid, block, 0, stream, p);
     if (e == cudaSuccess)
-      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, true, false>, grid, block, 0, stream, p)
-               : launch_pdl(ssm_backward_kernel<E, LS, false, false>, grid, block, 0, stream, p);
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, false>, grid, block, 0, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, false>, grid, block, 0, stream, p);
   }
   if (e == cudaSuccess && cut.blocks > 1) {
     const int64_t count = p.in.B * p.in.T * p.in.G * 2 * S::NP;
@@ -366,9 +372,9 @@ cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
 template <typename E>
 cudaError_t launch_backward(SsmArgs p, cudaStream_t stream) {
   switch (state_lanes(p.in.N)) {
-    case 4: return launch_backward_as<E, 4>(p, stream);
-    case 8: return launch_backward_as<E, 8>(p, stream);
-    default: return launch_backward_as<E, 16>(p, stream);
+    case 4: return p.wide ? launch_backward_as<E, 4, true>(p, stream) : launch_backward_as<E, 4, false>(p, stream);
+    case 8: return p.wide ? launch_backward_as<E, 8, true>(p, stream) : launch_backward_as<E, 8, false>(p, stream);
+    default: return p.wide ? launch_backward_as<E, 16, true>(p, stream) : launch_backward_as<E, 16, false>(p, stream);
   }
 }
 

@@ -8,7 +8,7 @@ namespace lm {
 namespace ssm {
 
 // Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.
-template <typename E, int LS, int K, bool STATES>
+template <typename E, int LS, int K, bool WIDE, bool STATES>
 __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs p) {
   using S = Shape<LS, K>;
   __shared__ float2 steps[kTile][S::row];                          // (step, step x) of each channel
@@ -16,19 +16,19 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
   __shared__ float mixed[STATES ? 1 : kTile][STATES ? 1 : S::row];   // sum c h
   pdl_entry();
   const Place<S> a(p);
-  const int64_t D = p.in.D, N = a.states;
+  if (STATES && a.split + 1 == p.splits) return;
+  const int64_t D = p.in.D;
   const bool gate = p.in.z.data;
   const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
-  const bool vec = p.vec & kVecState;
 
   Quad A2[K], h[K];
 #pragma unroll
   for (int k = 0; k < K; ++k) {
-    A2[k] = a.has(k) ? load_quad(p.in.A + a.state(0, D, k), vec, a.quads) : zeros();
+    A2[k] = a.has(k) ? load_quad<WIDE>(p.in.A + a.state(0, D, k), a.quads) : zeros();
     A2[k] = {A2[k].a * splat<2>(kLog2e), A2[k].b * splat<2>(kLog2e)};
     h[k] = zeros();
   }
-  auto state0 = [&](int k) { return p.h0 ? load_quad(p.h0 + a.state(a.b, D, k), vec, a.quads) : zeros(); };
+  auto state0 = [&](int k) { return p.h0 ? load_quad<WIDE>(p.h0 + a.state(a.b, D, k), a.quads) : zeros(); };
   if (STATES) {
     if (a.split == 0) {
       // (the second pass's own copy: h_last may be h0)
@@ -36,7 +36,7 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
       for (int k = 0; k < K; ++k)
         if (a.has(k)) {
           h[k] = state0(k);
-          store_quad(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), vec, a.quads, h[k]);
+          store_quad<WIDE>(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), a.quads, h[k]);
         }
     }
   } else if (p.splits == 1) {
@@ -47,11 +47,11 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if (!a.has(k)) continue;
-      if (a.split == 0) h[k] = load_quad(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), vec, a.quads);
+      if (a.split == 0) h[k] = load_quad<WIDE>(p.states + a.state(a.b * p.splits + p.splits - 1, D, k), a.quads);
 #pragma unroll 4
       for (int q = 0; q < a.split; ++q) {
         const int64_t from = a.b * p.splits + q;
-        const Quad last = load_quad(p.states + a.state(from, D, k), vec, a.quads);
+        const Quad last = load_quad<WIDE>(p.states + a.state(from, D, k), a.quads);
         const float sum = p.sums[from * D + a.d0 + a.channel(k)];
         if (sum == INFINITY || q == 0) {
           h[k] = last;
@@ -72,14 +72,14 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
   float sum[K] = {};
   bool dropped = false;
 
-  Piece<E, S::V> x, dt, z, x_next, dt_next, z_next;
-  States<E, S, true, !STATES> b_next;
+  Raw<E, S::V, WIDE> x, dt, z, x_next, dt_next, z_next;
+  States<E, S, WIDE, true, !STATES> b_next;
   auto load = [&](int64_t t0) {
     const int64_t t = t0 + a.s;
     const int there = t < end ? a.there : 0, d = a.d0 + a.c0;
-    x_next = load_piece<E, S::V>(at<E>(p.in.x, a.b, t, d), p.vec & kVecX, there);
-    dt_next = load_piece<E, S::V>(at<E>(p.in.dt, a.b, t, d), p.vec & kVecDt, there);
-    if (!STATES && gate) z_next = load_piece<E, S::V>(at<E>(p.in.z, a.b, t, d), p.vec & kVecZ, there);
+    x_next.read(at<E>(p.in.x, a.b, t, d), there);
+    dt_next.read(at<E>(p.in.dt, a.b, t, d), there);
+    if (!STATES && gate) z_next.read(at<E>(p.in.z, a.b, t, d), there);
     b_next.load(p, a, t0);
   };
   if (a.first < end) load(a.first);
@@ -90,8 +90,8 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     const bool in = t0 + a.s < end;
 #pragma unroll
     for (int j = 0; j < S::V; ++j) {
-      const float step = in ? step_of(p, to_f32(dt.e[j]) + bias[j]) : 0.0f;
-      steps[a.s][j * 8 + a.o] = {step, in ? step * to_f32(x.e[j]) : 0.0f};
+      const float step = in ? step_of(p, dt[j] + bias[j]) : 0.0f;
+      steps[a.s][j * 8 + a.o] = {step, in ? step * x[j] : 0.0f};
     }
     b_next.stage(bc);
     const unsigned resets = resets_of(p, a.b, t0, end);
@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     if (!STATES && p.saved) {
 #pragma unroll
       for (int k = 0; k < K; ++k)
-        if (a.has(k)) store_quad(p.saved + a.state(a.b * ((p.in.T + kTile - 1) / kTile) + t0 / kTile, D, k), p.vec & kVecSaved, a.quads, h[k]);
+        if (a.has(k)) store_quad<WIDE>(p.saved + a.state(a.b * ((p.in.T + kTile - 1) / kTile) + t0 / kTile, D, k), a.quads, h[k]);
     }
     float y[K][kTile];
     auto tile = [&](auto check) {
@@ -145,37 +145,35 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
       float out[S::V];
 #pragma unroll
       for (int j = 0; j < S::V; ++j) {
-        out[j] = fmaf(skip[j], to_f32(x.e[j]), mixed[a.s][j * 8 + a.o]);
-        if (gate) out[j] *= to_f32(z.e[j]) * sigmoid(to_f32(z.e[j]));
+        out[j] = fmaf(skip[j], x[j], mixed[a.s][j * 8 + a.o]);
+        if (gate) out[j] *= z[j] * sigmoid(z[j]);
         if (!in) out[j] = 0.0f;
       }
-      store_piece<E, S::V>(at<E>(p.y, a.b, t0 + a.s, a.d0 + a.c0), p.vec & kVecY, a.there, out);
+      store_piece<E, S::V, WIDE>(at<E>(p.y, a.b, t0 + a.s, a.d0 + a.c0), a.there, out);
     }
   }
   if (STATES) {
-    if (a.split + 1 < p.splits) {
 #pragma unroll
-      for (int k = 0; k < K; ++k)
-        if (a.has(k)) {
-          store_quad(p.states + a.state(row, D, k), vec, a.quads, h[k]);
-          if (a.g == 0) p.sums[row * D + a.d0 + a.channel(k)] = dropped ? INFINITY : sum[k];
-        }
-    }
+    for (int k = 0; k < K; ++k)
+      if (a.has(k)) {
+        store_quad<WIDE>(p.states + a.state(row, D, k), a.quads, h[k]);
+        if (a.g == 0) p.sums[row * D + a.d0 + a.channel(k)] = dropped ? INFINITY : sum[k];
+      }
     return;
   }
   if (p.h_last && a.split + 1 == p.splits) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (a.has(k)) store_quad(p.h_last + a.state(a.b, D, k), vec, a.quads, h[k]);
+      if (a.has(k)) store_quad<WIDE>(p.h_last + a.state(a.b, D, k), a.quads, h[k]);
   }
   // what is left of the split past the sequence's end
   const int64_t past = a.first < end ? a.first + (end - a.first + kTile - 1) / kTile * kTile : a.first;
   const float none[S::V] = {};
   for (int64_t t = past + a.s; t < a.end; t += kTile)
-    store_piece<E, S::V>(at<E>(p.y, a.b, t, a.d0 + a.c0), p.vec & kVecY, a.there, none);
+    store_piece<E, S::V, WIDE>(at<E>(p.y, a.b, t, a.d0 + a.c0), a.there, none);
 }
 
-template <typename E, int LS>
+template <typename E, int LS, bool WIDE>
 cudaError_t launch_forward_as(SsmArgs p, cudaStream_t stream) {
   using S = Shape<LS, kForwardK>;
   const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
@@ -185,18 +183,18 @@ cudaError_t launch_forward_as(SsmArgs p, cudaStream_t stream) {
   p.sums = p.states + p.in.B * cut.splits * p.in.D * p.in.N;
   const dim3 grid(unsigned(p.in.B * cut.splits * p.in.G * cut.blocks));
   if (cut.splits > 1) {
-    const cudaError_t e = launch_pdl(ssm_forward_kernel<E, LS, kForwardK, true>, grid, dim3(kSsmThreads), 0, stream, p);
+    const cudaError_t e = launch_pdl(ssm_forward_kernel<E, LS, kForwardK, WIDE, true>, grid, dim3(kSsmThreads), 0, stream, p);
     if (e != cudaSuccess) return e;
   }
-  return launch_pdl(ssm_forward_kernel<E, LS, kForwardK, false>, grid, dim3(kSsmThreads), 0, stream, p);
+  return launch_pdl(ssm_forward_kernel<E, LS, kForwardK, WIDE, false>, grid, dim3(kSsmThreads), 0, stream, p);
 }
 
 template <typename E>
 cudaError_t launch_forward(SsmArgs p, cudaStream_t stream) {
   switch (state_lanes(p.in.N)) {
-    case 4: return launch_forward_as<E, 4>(p, stream);
-    case 8: return launch_forward_as<E, 8>(p, stream);
-    default: return launch_forward_as<E, 16>(p, stream);
+    case 4: return p.wide ? launch_forward_as<E, 4, true>(p, stream) : launch_forward_as<E, 4, false>(p, stream);
+    case 8: return p.wide ? launch_forward_as<E, 8, true>(p, stream) : launch_forward_as<E, 8, false>(p, stream);
+    default: return p.wide ? launch_forward_as<E, 16, true>(p, stream) : launch_forward_as<E, 16, false>(p, stream);
   }
 }
 
