@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kConvWarps = 4;       // most segments of time of a block, a warp each
 constexpr int kSegment = 64;        // steps of a segment
-constexpr int kGroup = 4;           // steps whose loads are in flight together; two groups are
+constexpr int kGroup = 4;           // steps that are taken together
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct ConvArgs {
@@ -203,15 +203,77 @@ struct Window {
   }
 };
 
-// The elements of the group of steps from t on that lie below `end` (zeros for a thread without channels).
-template <typename E, int K>
-__device__ __forceinline__ void read_group(Raw<E, K> (&to)[kGroup], const E* row, int64_t stride, int64_t t, int64_t end, bool on) {
+// Feeds a thread the elements of N sequences' steps [t, end), a group of steps at a time, loaded ahead.  Four channels: by
+// asynchronous copies into places of the thread's own in shared memory (its registers are taken by sums and taps); one:
+// into registers, two groups in turn.  What lies past `end`, or a thread without channels gets, is not defined.
+template <typename E, int N>
+constexpr int kStages = sizeof(E) == 2 ? 4 : 2;
+template <typename E, int K, int N>
+struct Feed {
+  using Shared = Raw<E, K>[kStages<E, N>][N][kGroup][kConvWarps * 32];
+  Shared& ring;
+  const E* row[N];
+  int64_t stride[N];
+  int64_t next, end;
+  int stage = 0;
+  bool on;
+  __device__ __forceinline__ void issue(int to) {
+    if (on) {
 #pragma unroll
-  for (int u = 0; u < kGroup; ++u) {
-    to[u].clear();
-    if (on && t + u < end) to[u].read(row + (t + u) * stride);
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int u = 0; u < kGroup; ++u)
+          if (next + u < end) {
+            const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(&ring[to][i][u][threadIdx.x]));
+            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(row[i] + (next + u) * stride[i]), "n"(int(sizeof(Raw<E, K>)))
+                         : "memory");
+          }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    next += kGroup;
   }
-}
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int i = 0; i + 1 < kStages<E, N>; ++i) issue(i);
+  }
+  __device__ __forceinline__ void take(Raw<E, K> (&to)[N][kGroup]) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages<E, N> - 2) : "memory");
+    issue(stage == 0 ? kStages<E, N> - 1 : stage - 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) to[i][u] = ring[stage][i][u][threadIdx.x];
+    stage = stage + 1 == kStages<E, N> ? 0 : stage + 1;
+  }
+};
+template <typename E, int N>
+struct Feed<E, 1, N> {
+  using Shared = int;
+  Shared& ring;
+  const E* row[N];
+  int64_t stride[N];
+  int64_t next, end;
+  int stage = 0;
+  bool on;
+  Raw<E, 1> ahead[N][kGroup];
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) {
+        ahead[i][u].clear();
+        if (on && next + u < end) ahead[i][u].read(row[i] + (next + u) * stride[i]);
+      }
+    next += kGroup;
+  }
+  __device__ __forceinline__ void take(Raw<E, 1> (&to)[N][kGroup]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int u = 0; u < kGroup; ++u) to[i][u] = ahead[i][u];
+    start();
+  }
+};
 template <typename E, int K>
 __device__ __forceinline__ void write_zeros(E* row, int64_t stride, const ConvPlace& a) {
   if (!a.on) return;
@@ -230,6 +292,7 @@ __device__ __forceinline__ Vec<kVec<K>> pre_activation(const Taps<W, K>& taps, c
 // the whole sequence, else conv_state_kernel writes them).
 template <typename E, int W, int K, bool SILU>
 __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const ConvArgs p) {
+  __shared__ typename Feed<E, K, 1>::Shared ring;
   pdl_entry();
   const ConvPlace a = conv_place<K>(p);
   const int64_t end = min(a.end, a.n);
@@ -242,7 +305,8 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const Con
     taps.read(p, a);
     Window<E, W, K> win;
     win.start(p, a, resets, row);
-    Raw<E, K> xs[2][kGroup];
+    Feed<E, K, 1> feed{ring, {row}, {p.x.stride_t}, a.first, end, 0, a.on};
+    feed.start();
     auto step = [&](int64_t t, const Raw<E, K>& raw) {
       win.push(raw);
       Channels<K> y;
@@ -267,12 +331,10 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const Con
         }
       }
     };
-    read_group<E, K>(xs[0], row, p.x.stride_t, a.first, end, a.on);
-    for (int64_t t = a.first; t < end; t += 2 * kGroup) {
-      read_group<E, K>(xs[1], row, p.x.stride_t, t + kGroup, end, a.on);
-      group(t, xs[0]);
-      read_group<E, K>(xs[0], row, p.x.stride_t, t + 2 * kGroup, end, a.on);
-      if (t + kGroup < end) group(t + kGroup, xs[1]);
+    for (int64_t t = a.first; t < end; t += kGroup) {
+      Raw<E, K> raw[1][kGroup];
+      feed.take(raw);
+      group(t, raw[0]);
     }
     if (p.state_last && a.on) {
 #pragma unroll
@@ -308,6 +370,7 @@ __global__ void __launch_bounds__(128) conv_state_kernel(const ConvArgs p, int64
 template <typename E, int W, int K, bool SILU>
 __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const ConvArgs p) {
   pdl_entry();
+  __shared__ typename Feed<E, K, 2>::Shared ring;
   __shared__ float sums[kConvWarps][W + 1][K][32];
   const ConvPlace a = conv_place<K>(p);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -325,6 +388,8 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
     taps.read(p, a);
     Window<E, W, K> win;
     win.start(p, a, resets, row);
+    Feed<E, K, 2> feed{ring, {row, dy}, {p.x.stride_t, p.dy.stride_t}, a.first, reach, 0, a.on};
+    feed.start();
     Channels<K> dx[W];   // gradients of the window's inputs
 #pragma unroll
     for (int j = 0; j < W; ++j) dx[j] = none<K>();
@@ -378,17 +443,10 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
         }
       }
     };
-    Raw<E, K> xs[2][kGroup], gs[2][kGroup];
-    auto read = [&](int i, int64_t t) {
-      read_group<E, K>(xs[i], row, p.x.stride_t, t, reach, a.on);
-      read_group<E, K>(gs[i], dy, p.dy.stride_t, t, reach, a.on);
-    };
-    read(0, a.first);
-    for (int64_t t = a.first; t < reach; t += 2 * kGroup) {
-      read(1, t + kGroup);
-      group(t, xs[0], gs[0]);
-      read(0, t + 2 * kGroup);
-      if (t + kGroup < reach) group(t + kGroup, xs[1], gs[1]);
+    for (int64_t t = a.first; t < reach; t += kGroup) {
+      Raw<E, K> raw[2][kGroup];
+      feed.take(raw);
+      group(t, raw[0], raw[1]);
     }
     if (reach == a.n) {   // the sequence ends here: no later step completes its last inputs
 #pragma unroll
@@ -419,13 +477,21 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
     }
 }
 
-// Sums of the blocks' partial sums, a thread for each value.
-__global__ void __launch_bounds__(128) conv_join_kernel(const float* partial, int64_t rows, int D, int W, float* dweight, float* dbias) {
+// Sums of the blocks' partial sums: 32 channels of a tap by a block, whose warps take every eighth row each.
+constexpr int kJoinWarps = 8;
+__global__ void __launch_bounds__(kJoinWarps * 32) conv_join_kernel(const float* partial, int64_t rows, int D, int W, float* dweight, float* dbias) {
+  __shared__ float sums[kJoinWarps][32];
   pdl_entry();
-  const int d = blockIdx.x * 128 + threadIdx.x, j = blockIdx.y;
-  if (d >= D) return;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, d = blockIdx.x * 32 + lane, j = blockIdx.y;
   float v = 0.0f;
-  for (int64_t i = 0; i < rows; ++i) v += partial[(i * (W + 1) + j) * D + d];
+  if (d < D)
+#pragma unroll 8
+    for (int64_t i = warp; i < rows; i += kJoinWarps) v += partial[(i * (W + 1) + j) * D + d];
+  sums[warp][lane] = v;
+  __syncthreads();
+  if (warp != 0 || d >= D) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWarps; ++w) v += sums[w][lane];
   if (j < W) {
     if (dweight) dweight[int64_t(d) * W + j] = v;
   } else if (dbias) {
@@ -557,7 +623,7 @@ int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int 
     e = BY_TYPE(launch_conv, p, form, B, W, fours, true, on);
   }
   if (e == cudaSuccess && sums)
-    e = launch_pdl(conv_join_kernel, dim3(unsigned((D + 127) / 128), unsigned(W + 1)), dim3(128), 0, on,
+    e = launch_pdl(conv_join_kernel, dim3(unsigned((D + 31) / 32), unsigned(W + 1)), dim3(kJoinWarps * 32), 0, on,
                    static_cast<const float*>(workspace), B * conv_cut(T).blocks, int(D), W, dweight, dbias);
   return launch_status(e);
 }
