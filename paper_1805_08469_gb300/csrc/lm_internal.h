@@ -129,19 +129,19 @@ inline bool output_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64
 // 8.3 KB).
 constexpr size_t kMaxShared = 216 << 10;
 
-// Lets a kernel be launched with up to kMaxShared of dynamic shared memory (LARGE: and in clusters of
+// Lets a kernel be launched with up to MOST of dynamic shared memory (LARGE: and in clusters of
 // more than 8 blocks).  Asked of the runtime once for each kernel and device.
-template <auto KERNEL, bool LARGE = false>
+template <auto KERNEL, bool LARGE = false, size_t MOST = kMaxShared>
 cudaError_t allow_shared(size_t bytes) {
-  if (bytes > kMaxShared) return cudaErrorInvalidValue;
-  if (!LARGE && bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
+  if (bytes > MOST) return cudaErrorInvalidValue;
+  if (!LARGE && MOST == kMaxShared && bytes <= 32 << 10) return cudaSuccess;   // within the 48 KB that need no permission
   static std::atomic<uint64_t> allowed{0};
   int device = 0;
   cudaError_t e = cudaGetDevice(&device);
   if (e != cudaSuccess) return e;
   const uint64_t bit = uint64_t(1) << (device & 63);
   if (device < 64 && (allowed.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
-  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMaxShared));
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, int(MOST));
   if (LARGE && e == cudaSuccess) e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess && device < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
   return e;

@@ -13,6 +13,8 @@
 // and goes on from there.  A sum of +inf marks a split in which the state was dropped.
 #pragma once
 
+#include <type_traits>
+
 #include "lm_internal.h"
 
 namespace gem {
@@ -51,19 +53,39 @@ __device__ __forceinline__ float reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float sigmoid(float v) { return reciprocal(1.0f + ex2(-v * kLog2e)); }
+template <int V>
+__device__ __forceinline__ Vec<V> ex2(Vec<V> x) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) x.v[k] = ex2(x.v[k]);
+  return x;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> reciprocal(Vec<V> x) {
+#pragma unroll
+  for (int k = 0; k < V; ++k) x.v[k] = reciprocal(x.v[k]);
+  return x;
+}
+template <int V>
+__device__ __forceinline__ Vec<V> sigmoid(const Vec<V>& v) { return reciprocal<V>(ex2<V>(v * splat<V>(-kLog2e)) + splat<V>(1.0f)); }
 
 // max(v, 0) + log(1 + w), w = exp(-|v|): log(1 + w) = 2 artanh(s) with s = w / (2 + w) <= 1/3, by its
 // series in s^2, whose first term left out is 2e-8 of the sum.
-__device__ __forceinline__ float softplus(float v) {
-  const float w = ex2(-fabsf(v) * kLog2e), s = w * reciprocal(2.0f + w), q = s * s;
-  float r = fmaf(q, 1.0f / 13, 1.0f / 11);
-  r = fmaf(q, r, 1.0f / 9);
-  r = fmaf(q, r, 1.0f / 7);
-  r = fmaf(q, r, 1.0f / 5);
-  r = fmaf(q, r, 1.0f / 3);
-  r = fmaf(q, r, 1.0f);
-  return fmaf(2.0f * s, r, fmaxf(v, 0.0f));
+template <int V>
+__device__ __forceinline__ Vec<V> softplus(const Vec<V>& v) {
+  Vec<V> w, most;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    w.v[k] = ex2(fabsf(v.v[k]) * -kLog2e);
+    most.v[k] = fmaxf(v.v[k], 0.0f);
+  }
+  const Vec<V> s = w * reciprocal<V>(w + splat<V>(2.0f)), q = s * s;
+  Vec<V> r = fma<V>(q, splat<V>(1.0f / 13), splat<V>(1.0f / 11));
+  r = fma<V>(q, r, splat<V>(1.0f / 9));
+  r = fma<V>(q, r, splat<V>(1.0f / 7));
+  r = fma<V>(q, r, splat<V>(1.0f / 5));
+  r = fma<V>(q, r, splat<V>(1.0f / 3));
+  r = fma<V>(q, r, splat<V>(1.0f));
+  return fma<V>(s + s, r, most);
 }
 
 // A decay's exponent step A log2(e), and a little more: the GPU's approximate exp2 gives on average 0.1 (next to 1) to
@@ -115,10 +137,19 @@ struct Raw {
       return to_f32(x[k]);
     } else if constexpr (sizeof(E) == 4) {
       return __uint_as_float(w[k]);
+    } else if constexpr (std::is_same_v<E, __nv_bfloat16>) {
+      return __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
     } else {
-      const uint16_t half = uint16_t(w[k / 2] >> (k % 2 * 16));
-      return to_f32(*reinterpret_cast<const E*>(&half));
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k / 2]));
+      return k % 2 ? f.y : f.x;
     }
+  }
+  template <int U>
+  __device__ __forceinline__ Vec<U> at(int k) const {
+    Vec<U> r;
+#pragma unroll
+    for (int i = 0; i < U; ++i) r.v[i] = (*this)[k + i];
+    return r;
   }
 };
 template <typename E, int V, bool WIDE>
@@ -182,7 +213,8 @@ struct Shape {
   static constexpr int LS = LS_, K = K_;
   static constexpr int lanes = 32 / LS;            // channel lanes of a warp
   static constexpr int CH = kWarps * lanes * K;    // channels
-  static constexpr int V = CH / 8;                 // channels of a staging thread (8 of them to a step)
+  static constexpr int V = CH / 8;                 // channels of a staging thread (8 of them to a step),
+  static constexpr int U = V > 1 ? 2 : 1;          // taken two at a time
   static constexpr int row = CH + 8;               // of the tiles' rows: steps lie 8 banks (floats) apart
   static constexpr int NP = kQuad * LS;            // states, padded
 };
@@ -273,13 +305,18 @@ __device__ __forceinline__ unsigned resets_of(const SsmArgs& p, int64_t b, int64
   return __ballot_sync(~0u, threadIdx.x % 32 < kTile && t < end && p.in.reset[b * p.in.T + t] != 0);
 }
 
-// Sums of v over the lanes that differ in the bits from `low` to `high` (lane masks): the first N / lanes values of v
-// are then those of the N sums from index N / lanes * (the lane's number among them) on.
+// Sums of v over the lanes that differ in the bits from LOW to HIGH (lane masks): the first N / lanes values of v
+// are then those of the N sums from index N / lanes * (the lane's number among them) on; with more lanes than values,
+// lanes with neighbouring numbers have the same one.
 template <int N, int HIGH, int LOW>
 __device__ __forceinline__ void scatter_sums(float (&v)[N]) {
   int count = N;
 #pragma unroll
   for (int bit = HIGH; bit >= LOW; bit /= 2) {
+    if (count == 1) {
+      v[0] += __shfl_xor_sync(~0u, v[0], bit);
+      continue;
+    }
     const bool upper = threadIdx.x & bit;
     count /= 2;
 #pragma unroll
@@ -290,9 +327,6 @@ __device__ __forceinline__ void scatter_sums(float (&v)[N]) {
     }
   }
 }
-
-// The staging of one tensor element's step: step = softplus(dt + bias), or without it.
-__device__ __forceinline__ float step_of(const SsmArgs& p, float raw) { return p.in.softplus ? softplus(raw) : raw; }
 
 // How time and channels are cut (for kernels of CH channels a block).
 struct SsmCut {
@@ -307,7 +341,7 @@ cudaError_t launch_backward(SsmArgs p, cudaStream_t stream);
 
 // Shapes by N: LS lanes for 4 LS states.
 inline int state_lanes(int N) { return N <= 16 ? 4 : N <= 32 ? 8 : 16; }
-constexpr int kForwardK = 2, kBackwardK = 1;
+constexpr int kForwardK = 1, kBackwardK = 1;
 inline int block_channels(int N, int K) { return kWarps * 32 / state_lanes(N) * K; }
 
 }  // namespace ssm

@@ -6,10 +6,12 @@
 //   q = g exp(step_t A) h_{t-1};  dA += q step_t;  dstep_t = sum_n A q + x_t sum_n g b_t
 //   dx_t = step_t sum_n g b_t + skip dy'_t;  g = exp(step_t A) g
 //
-// A tile's states are computed again from the one saved before it and stay in registers.  db and dc are summed
-// over a warp's channels by exchanges, over the block's in shared memory, and over blocks by a second kernel;
-// the parameters' gradients over a split in registers, then by that kernel as well.  Splits are composed
-// from the last one back, as in the forward pass.
+// A tile is taken in two halves, the later one first: its states are computed again from the one saved before the tile and
+// stay in registers (all sixteen would leave fewer warps on an SM: 1.07 ms instead of ...).  What a step gives to db and dc goes
+// through shared memory, where a thread adds up the block's channels for an output (exchanges between lanes, two
+// selections, a shuffle and a sum for each value, took twice the instructions); a second kernel adds up the
+// blocks.  The parameters' gradients are summed over a split in registers, then by that kernel as well.  Splits are
+// composed from the last one back, as in the forward pass.
 #pragma once
 
 #include "lm_ssm.h"
@@ -20,22 +22,37 @@ namespace ssm {
 
 __device__ __forceinline__ Vec<2> scaled(const Vec<2>& a, float b) { return a * splat<2>(b); }
 
+constexpr int kHalf = kTile / 2;
+
+// What a step gives to db and dc, [kHalf][channel][2 LS] quads of states, rotated by LS / 4 quads a channel: the eight lanes that
+// store together then lie in different banks.
+template <typename S>
+struct Given {
+  static constexpr int kQuads = 2 * S::LS, kTurn = S::LS / 4, kFloats = kHalf * S::CH * kQuads * kQuad;
+  static __device__ __forceinline__ int place(int t, int channel, int q) {
+    return ((t * S::CH + channel) * kQuads + (q + kTurn * channel) % kQuads) * kQuad;
+  }
+};
+
 template <typename E, int LS, bool WIDE, bool GATE, bool STATES>
-__global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kernel(const SsmArgs p) {
+__global__ void __launch_bounds__(kSsmThreads, 4) ssm_backward_kernel(const SsmArgs p) {
   using S = Shape<LS, kBackwardK>;
-  constexpr int kSums = GATE ? 3 : 2;
+  constexpr int kSums = GATE ? 3 : 2, U = S::U;
+  extern __shared__ float4 shared[];
+  float* const given = reinterpret_cast<float*>(shared);
   __shared__ float2 steps[kTile][S::row];                  // (step, step x)
   __shared__ float gys[kTile][S::row];                     // dy'
   __shared__ float4 bc[(STATES ? 1 : 2) * kTile * LS];
   __shared__ float sums[STATES ? 1 : kSums][kTile][S::row];   // sum A2 q, sum g b, sum c h
-  __shared__ float red[STATES ? 1 : kWarps][kTile][2 * S::NP];   // db, dc of a warp's channels
   pdl_entry();
   const Place<S> a(p);
   if (STATES && a.split == 0) return;
   const int64_t D = p.in.D, N = a.states;
   const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
   const bool has = a.has(0);
-  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  // the places of the thread's channel, and from one step to the next
+  constexpr int kGivenStep = S::CH * Given<S>::kQuads * kQuad;
+  const int to_db = Given<S>::place(0, a.pos, a.g), to_dc = Given<S>::place(0, a.pos, S::LS + a.g);
 
   Quad A2 = has ? load_quad<WIDE>(p.in.A + a.state(0, D, 0), a.quads) : zeros();
   A2 = {scaled(A2.a, kLog2e), scaled(A2.b, kLog2e)};
@@ -62,11 +79,12 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
     }
   }
 
-  float bias[S::V], skip[S::V], dskip[S::V] = {}, dbias[S::V] = {};
+  Vec<U> bias[S::V / U], skip[S::V / U], dskip[S::V / U], dbias[S::V / U];
 #pragma unroll
   for (int j = 0; j < S::V; ++j) {
-    bias[j] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
-    skip[j] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
+    bias[j / U].v[j % U] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
+    skip[j / U].v[j % U] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
+    dskip[j / U].v[j % U] = dbias[j / U].v[j % U] = 0.0f;
   }
   Quad dA = zeros();
   float total = 0.0f;
@@ -96,12 +114,22 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
     const Quad start = start_next;
     const bool in = t0 + a.s < end;
 #pragma unroll
-    for (int j = 0; j < S::V; ++j) {
-      const float step = in ? step_of(p, dt[j] + bias[j]) : 0.0f;
-      steps[a.s][j * 8 + a.o] = {step, in && !STATES ? step * x[j] : 0.0f};
-      float gy = dy[j];
-      if (GATE) gy *= z[j] * sigmoid(z[j]);
-      gys[a.s][j * 8 + a.o] = in ? gy : 0.0f;
+    for (int j = 0; j < S::V; j += U) {
+      Vec<U> step = dt.template at<U>(j) + bias[j / U];
+      if (p.in.softplus) step = softplus<U>(step);
+      if (!in) step = splat<U>(0.0f);
+      Vec<U> gy = dy.template at<U>(j);   // (x, z and dy are 0 past the end)
+      if (GATE) {
+        const Vec<U> zj = z.template at<U>(j);
+        gy = gy * (zj * sigmoid<U>(zj));
+      }
+      Vec<U> input = splat<U>(0.0f);
+      if (!STATES) input = step * x.template at<U>(j);
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        steps[a.s][(j + i) * 8 + a.o] = {step.v[i], input.v[i]};
+        gys[a.s][(j + i) * 8 + a.o] = gy.v[i];
+      }
     }
     b_next.stage(bc);
     const unsigned resets = resets_of(p, a.b, t0, end);
@@ -129,21 +157,21 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
         tile(std::true_type());
       __syncthreads();
     } else {
-      auto tile = [&](auto check) {
-        Quad h[kTile];
-        Quad now = start;
+      // half: steps from t1 on, whose states are computed again into h from the one before them
+      auto half = [&](int t1, const Quad& before, auto check) {
+        Quad h[kHalf];
+        Quad now = before;
 #pragma unroll
-        for (int t = 0; t < kTile; ++t) {
-          if (check.value && t >= count) {
-            h[t] = now;
-            continue;
+        for (int i = 0; i < kHalf; ++i) {
+          const int t = t1 + i;
+          if (!check.value || t < count) {
+            if (check.value && (resets >> t & 1)) now = zeros();
+            const Quad b = quad(bc[t * LS + a.g]);
+            const float2 v = steps[t][a.pos];
+            now.a = fma<2>(decay(v.x, A2.a), now.a, splat<2>(v.y) * b.a);
+            now.b = fma<2>(decay(v.x, A2.b), now.b, splat<2>(v.y) * b.b);
           }
-          if (check.value && (resets >> t & 1)) now = zeros();
-          const Quad b = quad(bc[t * LS + a.g]);
-          const float2 v = steps[t][a.pos];
-          now.a = fma<2>(decay(v.x, A2.a), now.a, splat<2>(v.y) * b.a);
-          now.b = fma<2>(decay(v.x, A2.b), now.b, splat<2>(v.y) * b.b);
-          h[t] = now;
+          h[i] = now;
         }
         // (the decays are computed again: kept from the first loop they would take the registers of as many states)
 #pragma unroll
@@ -151,92 +179,130 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
           asm volatile("" : "+f"(A2.a.v[i]));
           asm volatile("" : "+f"(A2.b.v[i]));
         }
-        float sq[LS], sb[LS], sy[LS];
+        constexpr int kSet = LS < kHalf ? LS : kHalf;   // steps whose sums over the states' lanes are taken together
+        float sq[kSet], sb[kSet], sy[kSet];
 #pragma unroll
-        for (int t = kTile - 1; t >= 0; --t) {
-          sq[t % LS] = sb[t % LS] = sy[t % LS] = 0.0f;
+        for (int i = kHalf - 1; i >= 0; --i) {
+          const int t = t1 + i;
+          sq[i % kSet] = sb[i % kSet] = sy[i % kSet] = 0.0f;
           if (!check.value || t < count) {
             const Quad b = quad(bc[t * LS + a.g]), c = quad(bc[(kTile + t) * LS + a.g]);
             const float2 v = steps[t][a.pos];
             const float gy = gys[t][a.pos];
             if (GATE) {
-              const Vec<2> m = fma<2>(c.b, h[t].b, c.a * h[t].a);
-              sy[t % LS] = m.v[0] + m.v[1];
+              const Vec<2> m = fma<2>(c.b, h[i].b, c.a * h[i].a);
+              sy[i % kSet] = m.v[0] + m.v[1];
             }
             g.a = fma<2>(c.a, splat<2>(gy), g.a);
             g.b = fma<2>(c.b, splat<2>(gy), g.b);
-            const Vec<2> db0 = scaled(g.a, v.y), db1 = scaled(g.b, v.y), dc0 = scaled(h[t].a, gy), dc1 = scaled(h[t].b, gy);
-            float w[8] = {db0.v[0], db0.v[1], db1.v[0], db1.v[1], dc0.v[0], dc0.v[1], dc1.v[0], dc1.v[1]};
+            const Vec<2> db0 = scaled(g.a, v.y), db1 = scaled(g.b, v.y), dc0 = scaled(h[i].a, gy), dc1 = scaled(h[i].b, gy);
+            *reinterpret_cast<float4*>(given + to_db + i * kGivenStep) = make_float4(db0.v[0], db0.v[1], db1.v[0], db1.v[1]);
+            *reinterpret_cast<float4*>(given + to_dc + i * kGivenStep) = make_float4(dc0.v[0], dc0.v[1], dc1.v[0], dc1.v[1]);
             const Vec<2> mb = fma<2>(g.b, b.b, g.a * b.a);
-            sb[t % LS] = mb.v[0] + mb.v[1];
-            Quad prev = t > 0 ? h[t > 0 ? t - 1 : 0] : start;
-            const Quad dec = {decay(v.x, A2.a), decay(v.x, A2.b)};
+            sb[i % kSet] = mb.v[0] + mb.v[1];
+            Quad prev = i > 0 ? h[i > 0 ? i - 1 : 0] : before;
             const bool drop = check.value && (resets >> t & 1);
             if (drop) prev = zeros();
-            g.a = g.a * dec.a;
-            g.b = g.b * dec.b;
+            g.a = g.a * decay(v.x, A2.a);
+            g.b = g.b * decay(v.x, A2.b);
             const Vec<2> q0 = g.a * prev.a, q1 = g.b * prev.b;
             const Vec<2> mq = fma<2>(q1, A2.b, q0 * A2.a);
-            sq[t % LS] = mq.v[0] + mq.v[1];
-            dA.a = fma<2>(q0, splat<2>(v.x), dA.a);
-            dA.b = fma<2>(q1, splat<2>(v.x), dA.b);
+            sq[i % kSet] = drop ? 0.0f : mq.v[0] + mq.v[1];
             if (drop) {
               g = zeros();
-              sq[t % LS] = 0.0f;
-            }
-            scatter_sums<8, S::lanes / 2, 1>(w);
-#pragma unroll
-            for (int i = 0; i < 8 / S::lanes; ++i) {
-              const int k = lane % S::lanes * (8 / S::lanes) + i;
-              red[warp][t][k / kQuad * S::NP + a.g * kQuad + k % kQuad] = w[i];
+            } else {
+              dA.a = fma<2>(q0, splat<2>(v.x), dA.a);
+              dA.b = fma<2>(q1, splat<2>(v.x), dA.b);
             }
           }
-          if (t % LS == 0) {
-            scatter_sums<LS, 16, S::lanes>(sq);
-            scatter_sums<LS, 16, S::lanes>(sb);
-            sums[0][t + a.g][a.pos] = sq[0];
-            sums[1][t + a.g][a.pos] = sb[0];
-            if (GATE) {
-              scatter_sums<LS, 16, S::lanes>(sy);
-              sums[kSums - 1][t + a.g][a.pos] = sy[0];
-            }
+          if (i % kSet == 0) {
+            // (with more lanes than steps of a half, the lanes that end up with the same step write the same)
+            scatter_sums<kSet, 16, S::lanes>(sq);
+            scatter_sums<kSet, 16, S::lanes>(sb);
+            if (GATE) scatter_sums<kSet, 16, S::lanes>(sy);
+            const int s = t + a.g * kSet / LS;
+            sums[0][s][a.pos] = sq[0];
+            sums[1][s][a.pos] = sb[0];
+            if (GATE) sums[kSums - 1][s][a.pos] = sy[0];
           }
         }
+      };
+      // the half's db and dc of all the block's channels
+      auto collect = [&](int t1) {
+        constexpr int kOutputs = 2 * S::NP;
+#pragma unroll
+        for (int i = 0; i < kHalf * kOutputs / kSsmThreads; ++i) {
+          const int o = i * kSsmThreads + threadIdx.x, t = o / kOutputs, k = o % kOutputs;
+          if (t1 + t >= count) break;
+          float v[4] = {};
+          const float* const from = given + t * kGivenStep + k % kQuad;
+#pragma unroll
+          for (int c = 0; c < S::CH; ++c) v[c % 4] += from[Given<S>::place(0, c, k / kQuad)];
+          const float sum = (v[0] + v[1]) + (v[2] + v[3]);
+          if (p.blocks > 1) {
+            p.bc_part[(((a.b * p.in.T + t0 + t1 + t) * p.in.G + a.group) * p.blocks + a.part) * kOutputs + k] = sum;
+          } else if (k % S::NP < N) {
+            *at<E>(k < S::NP ? p.db : p.dc, a.b, t0 + t1 + t, a.group * a.states + k % S::NP) = from_f32<E>(sum);
+          }
+        }
+      };
+      auto tile = [&](auto check) {
+        if (!check.value || count > kHalf) {
+          Quad middle = start;
+#pragma unroll
+          for (int t = 0; t < kHalf; ++t) {
+            if (check.value && (resets >> t & 1)) middle = zeros();
+            const Quad b = quad(bc[t * LS + a.g]);
+            const float2 v = steps[t][a.pos];
+            middle.a = fma<2>(decay(v.x, A2.a), middle.a, splat<2>(v.y) * b.a);
+            middle.b = fma<2>(decay(v.x, A2.b), middle.b, splat<2>(v.y) * b.b);
+          }
+          half(kHalf, middle, check);
+          __syncthreads();
+          collect(kHalf);
+          __syncthreads();
+        }
+        half(0, start, check);
       };
       if (count == kTile && resets == 0)
         tile(std::false_type());
       else
         tile(std::true_type());
       __syncthreads();
+      collect(0);
 
-      for (int i = threadIdx.x; i < count * 2 * S::NP; i += kSsmThreads) {
-        const int t = i / (2 * S::NP), k = i % (2 * S::NP);
-        float v = red[0][t][k];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) v += red[w][t][k];
-        if (p.blocks > 1) {
-          p.bc_part[(((a.b * p.in.T + t0 + t) * p.in.G + a.group) * p.blocks + a.part) * (2 * S::NP) + k] = v;
-        } else if (k % S::NP < N) {
-          *at<E>(k < S::NP ? p.db : p.dc, a.b, t0 + t, a.group * a.states + k % S::NP) = from_f32<E>(v);
-        }
-      }
       if (t0 + a.s < a.end) {
         float out[3][S::V];
 #pragma unroll
-        for (int j = 0; j < S::V; ++j) {
-          const int i = j * 8 + a.o;
-          const float xj = x[j], sg = sums[1][a.s][i], gy = gys[a.s][i];
-          float d = fmaf(sg, xj, sums[0][a.s][i] * kLn2);
-          if (p.in.softplus) d *= sigmoid(dt[j] + bias[j]);
-          out[0][j] = in ? fmaf(sg, steps[a.s][i].x, skip[j] * gy) : 0.0f;
-          out[1][j] = in ? d : 0.0f;
-          if (in) {
-            dskip[j] = fmaf(gy, xj, dskip[j]);
-            dbias[j] += d;
+        for (int j = 0; j < S::V; j += U) {
+          Vec<U> sq, sb, sy, gy, step;
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            const int i = (j + k) * 8 + a.o;
+            sq.v[k] = sums[0][a.s][i];
+            sb.v[k] = sums[1][a.s][i];
+            sy.v[k] = sums[kSums - 1][a.s][i];
+            gy.v[k] = gys[a.s][i];
+            step.v[k] = steps[a.s][i].x;
           }
+          const Vec<U> xj = x.template at<U>(j);
+          Vec<U> d = fma<U>(sb, xj, sq * splat<U>(kLn2));
+          if (p.in.softplus) d = d * sigmoid<U>(dt.template at<U>(j) + bias[j / U]);
+          const Vec<U> dx = fma<U>(sb, step, skip[j / U] * gy);
+          Vec<U> dz = d;
           if (GATE) {
-            const float zj = z[j], sig = sigmoid(zj);
-            out[2][j] = in ? dy[j] * fmaf(skip[j], xj, sums[kSums - 1][a.s][i]) * (sig * fmaf(zj, 1.0f - sig, 1.0f)) : 0.0f;
+            const Vec<U> zj = z.template at<U>(j), s = sigmoid<U>(zj), one = splat<U>(1.0f);
+            dz = dy.template at<U>(j) * fma<U>(skip[j / U], xj, sy) * (s * fma<U>(zj, one - s, one));
+          }
+          if (in) {
+            dskip[j / U] = fma<U>(gy, xj, dskip[j / U]);
+            dbias[j / U] = dbias[j / U] + d;
+          }
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            out[0][j + k] = in ? dx.v[k] : 0.0f;
+            out[1][j + k] = in ? d.v[k] : 0.0f;
+            out[2][j + k] = in ? dz.v[k] : 0.0f;
           }
         }
         const int64_t t = t0 + a.s;
@@ -265,8 +331,8 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : 3) ssm_backward_kern
     if (p.params) {
 #pragma unroll
       for (int j = 0; j < S::V; ++j) {
-        sums[0][a.s][j * 8 + a.o] = dskip[j];
-        sums[1][a.s][j * 8 + a.o] = dbias[j];
+        sums[0][a.s][j * 8 + a.o] = dskip[j / U].v[j % U];
+        sums[1][a.s][j * 8 + a.o] = dbias[j / U].v[j % U];
       }
       __syncthreads();
       for (int i = threadIdx.x; i < 2 * S::CH; i += kSsmThreads) {
@@ -353,12 +419,15 @@ cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
   const bool gate = p.in.z.data;
   cudaError_t e = cudaSuccess;
   if (grid.x > 0) {
-    if (cut.splits > 1)
+    constexpr size_t kShared = size_t(Given<S>::kFloats) * 4;
+    e = gate ? allow_shared<ssm_backward_kernel<E, LS, WIDE, true, false>, false, kShared>(kShared)
+             : allow_shared<ssm_backward_kernel<E, LS, WIDE, false, false>, false, kShared>(kShared);
+    if (e == cudaSuccess && cut.splits > 1)
       e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, true>, grid, block, 0, stream, p)
                : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, true>, grid, block, 0, stream, p);
     if (e == cudaSuccess)
-      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, false>, grid, block, 0, stream, p)
-               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, false>, grid, block, 0, stream, p);
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, false>, grid, block, kShared, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, false>, grid, block, kShared, stream, p);
   }
   if (e == cudaSuccess && cut.blocks > 1) {
     const int64_t count = p.in.B * p.in.T * p.in.G * 2 * S::NP;

@@ -63,11 +63,12 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     }
   }
 
-  float bias[S::V], skip[S::V];
+  constexpr int U = S::U;
+  Vec<U> bias[S::V / U], skip[S::V / U];
 #pragma unroll
   for (int j = 0; j < S::V; ++j) {
-    bias[j] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
-    skip[j] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
+    bias[j / U].v[j % U] = p.in.dt_bias && j < a.there ? p.in.dt_bias[a.d0 + a.c0 + j] : 0.0f;
+    skip[j / U].v[j % U] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
   }
   float sum[K] = {};
   bool dropped = false;
@@ -89,9 +90,13 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     z = z_next;
     const bool in = t0 + a.s < end;
 #pragma unroll
-    for (int j = 0; j < S::V; ++j) {
-      const float step = in ? step_of(p, dt[j] + bias[j]) : 0.0f;
-      steps[a.s][j * 8 + a.o] = {step, in ? step * x[j] : 0.0f};
+    for (int j = 0; j < S::V; j += U) {
+      Vec<U> step = dt.template at<U>(j) + bias[j / U];
+      if (p.in.softplus) step = softplus<U>(step);
+      if (!in) step = splat<U>(0.0f);
+      const Vec<U> input = step * x.template at<U>(j);   // (x is 0 past the end)
+#pragma unroll
+      for (int i = 0; i < U; ++i) steps[a.s][(j + i) * 8 + a.o] = {step.v[i], input.v[i]};
     }
     b_next.stage(bc);
     const unsigned resets = resets_of(p, a.b, t0, end);
@@ -144,10 +149,17 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     if (!STATES && t0 + a.s < a.end) {
       float out[S::V];
 #pragma unroll
-      for (int j = 0; j < S::V; ++j) {
-        out[j] = fmaf(skip[j], x[j], mixed[a.s][j * 8 + a.o]);
-        if (gate) out[j] *= z[j] * sigmoid(z[j]);
-        if (!in) out[j] = 0.0f;
+      for (int j = 0; j < S::V; j += U) {
+        Vec<U> v;
+#pragma unroll
+        for (int i = 0; i < U; ++i) v.v[i] = mixed[a.s][(j + i) * 8 + a.o];
+        v = fma<U>(skip[j / U], x.template at<U>(j), v);
+        if (gate) {
+          const Vec<U> zj = z.template at<U>(j);
+          v = v * (zj * sigmoid<U>(zj));
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) out[j + i] = in ? v.v[i] : 0.0f;
       }
       store_piece<E, S::V, WIDE>(at<E>(p.y, a.b, t0 + a.s, a.d0 + a.c0), a.there, out);
     }
