@@ -6,6 +6,7 @@ from __future__ import annotations
 
 import ctypes as C
 from pathlib import Path
+from struct import Struct
 
 LIB_PATH = Path(__file__).resolve().parent / "libgem.so"
 
@@ -36,10 +37,15 @@ class GemSsmGrad(C.Structure):
                 ("dA", C.c_void_p), ("dskip", C.c_void_p), ("ddt_bias", C.c_void_p), ("dh0", C.c_void_p)]
 
 
+# The same as bytes, in a third of the time that a Structure takes to build.
+pack_seq = Struct("=3q").pack
+pack_ssm = Struct("=3q3i4x20q").pack
+pack_ssm_grad = Struct("=19q").pack
+
+
 def _declare(L):
     p, i, sz = C.c_void_p, C.c_int, C.c_size_t
     f, i64, seq = C.c_float, C.c_int64, C.POINTER(GemSeq)
-    ssm, ssm_grad = C.POINTER(GemSsm), C.POINTER(GemSsmGrad)
     sig = {
         "gem_create": ([sz, i, C.c_float, C.c_float, C.c_float, p], i),
         "gem_destroy": ([p], None),
@@ -111,8 +117,8 @@ def _declare(L):
         "gem_conv_backward": ([i, i, i64, i64, i64, i, seq, p, p, p, p, p, seq, p, seq, p, p, p, p, p], i),
         "gem_ssm_saved_count": ([i64, i64, i64, i], i64),
         "gem_ssm_workspace": ([i64, i64, i64, i, i, i], i64),
-        "gem_ssm_forward": ([i, ssm, p, seq, p, p, p, p], i),
-        "gem_ssm_backward": ([i, ssm, p, seq, p, ssm_grad, p, p], i),
+        "gem_ssm_forward": ([i, p, p, p, p, p, p, p], i),
+        "gem_ssm_backward": ([i, p, p, p, p, p, p, p], i),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)

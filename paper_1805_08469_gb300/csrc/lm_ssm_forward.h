@@ -185,8 +185,60 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     store_piece<E, S::V, WIDE>(at<E>(p.y, a.b, t, a.d0 + a.c0), a.there, none);
 }
 
+// One step: a thread for four states of a channel, the LS lanes of a channel side by side, so that states are read and written
+// in the order of memory.  (16 x 2048 x 16: 3 us; the kernel above, most of whose tile would be empty, 8.)
+template <typename E, int LS, bool WIDE>
+__global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs p) {
+  pdl_entry();
+  const int64_t i = int64_t(blockIdx.x) * kSsmThreads + threadIdx.x, D = p.in.D, N = p.in.N;
+  const int q = threadIdx.x % LS;
+  const int64_t row = i / LS;
+  const bool on = row < p.in.B * D;
+  const int64_t b = on ? row / D : 0, d = on ? row % D : 0;
+  const int there = on ? min(max(int(N) - q * kQuad, 0), kQuad) : 0;
+  const int64_t state = (b * D + d) * N + q * kQuad;
+  const int first = int(d / (D / p.in.G) * N) + q * kQuad;
+  const bool live = !p.in.lengths || p.in.lengths[b] > 0, gate = p.in.z.data;
+  Quad h = zeros();
+  if (p.h0) h = load_quad<WIDE>(p.h0 + state, there);
+  if (p.saved && live) store_quad<WIDE>(p.saved + state, there, h);
+  Raw<E, kQuad, WIDE> bs, cs;
+  bs.read(at<E>(p.in.b, b, 0, first), live ? there : 0);
+  cs.read(at<E>(p.in.c, b, 0, first), live ? there : 0);
+  Quad A2 = load_quad<WIDE>(p.in.A + d * N + q * kQuad, there);
+  float x = 0.0f, dt = 0.0f, z = 0.0f;
+  if (live) {
+    x = to_f32(*at<E>(p.in.x, b, 0, int(d)));
+    dt = to_f32(*at<E>(p.in.dt, b, 0, int(d)));
+    if (gate) z = to_f32(*at<E>(p.in.z, b, 0, int(d)));
+  }
+  const float skip = p.in.skip ? p.in.skip[d] : 0.0f;
+  float step = dt + (p.in.dt_bias ? p.in.dt_bias[d] : 0.0f);
+  if (p.in.softplus) step = softplus<1>({step}).v[0];
+  float y = 0.0f;
+  if (live) {
+    if (p.in.reset && p.in.reset[b]) h = zeros();
+    A2 = {A2.a * splat<2>(kLog2e), A2.b * splat<2>(kLog2e)};
+    const Vec<2> in = splat<2>(step * x);
+    h.a = fma<2>(decay(step, A2.a), h.a, in * bs.template at<2>(0));
+    h.b = fma<2>(decay(step, A2.b), h.b, in * bs.template at<2>(2));
+    const Vec<2> m = fma<2>(cs.template at<2>(2), h.b, cs.template at<2>(0) * h.a);
+    y = m.v[0] + m.v[1];
+  }
+  if (p.h_last) store_quad<WIDE>(p.h_last + state, there, h);
+#pragma unroll
+  for (int bit = LS / 2; bit > 0; bit /= 2) y += __shfl_xor_sync(~0u, y, bit);
+  if (!on || q != 0) return;
+  y = fmaf(skip, x, y);
+  if (gate) y *= z * sigmoid<1>({z}).v[0];
+  *at<E>(p.y, b, 0, int(d)) = from_f32<E>(live ? y : 0.0f);
+}
+
 template <typename E, int LS, bool WIDE>
 cudaError_t launch_forward_as(SsmArgs p, cudaStream_t stream) {
+  if (p.in.T == 1)
+    return launch_pdl(ssm_step_kernel<E, LS, WIDE>, dim3(unsigned((p.in.B * p.in.D * LS + kSsmThreads - 1) / kSsmThreads)), dim3(kSsmThreads), 0,
+                      stream, p);
   using S = Shape<LS, kForwardK>;
   const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
   p.blocks = int(cut.blocks);

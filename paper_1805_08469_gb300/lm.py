@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import torch
 
-from ._lib import GemSeq, GemSsm, GemSsmGrad, check, lib
+from ._lib import GemSeq, check, lib, pack_seq, pack_ssm, pack_ssm_grad
 
 GEM_F32, GEM_BF16, GEM_F16 = 0, 1, 2
 GEM_GLR_LERP, GEM_GLR_ADD = 0, 1
@@ -276,26 +276,42 @@ def gem_conv_backward(x, weight, dy, dx, dweight, workspace, *, form: int = GEM_
         _space(workspace, "workspace", size, _F32), _stream(stream, x.device)), "gem_conv_backward")
 
 
-def _states(t, what: str, like, B, T, G, N):
-    """gem_seq_t of a [B, T, G, N] tensor whose last two dimensions lie side by side."""
+def _place(t, what: str, like):
+    """Address, batch and time stride of a [B, T, D] tensor of like's type and shape (None: of no tensor)."""
+    if t is None:
+        return 0, 0, 0
+    sb, st, sd = t.stride()
     if t.dtype is not like.dtype or not t.is_cuda:
         raise TypeError(f"{what}: expected a {like.dtype} CUDA tensor")
-    if t.shape != (B, T, G, N):
-        raise ValueError(f"{what}: expected the shape {(B, T, G, N)}, got {tuple(t.shape)}")
+    if t.shape != like.shape:
+        raise ValueError(f"{what}: expected the shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    if sd != 1 and t.shape[2] > 1:
+        raise TypeError(f"{what}: the channels must be contiguous")
+    return t.data_ptr(), sb, st
+
+
+def _states(t, what: str, like, shape):
+    """The same of a [B, T, G, N] tensor of like's type, whose last two dimensions lie side by side."""
+    if t.dtype is not like.dtype or not t.is_cuda:
+        raise TypeError(f"{what}: expected a {like.dtype} CUDA tensor")
+    if t.shape != shape:
+        raise ValueError(f"{what}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
     sb, st, sg, sn = t.stride()
-    if (sn != 1 and N > 1) or (sg != N and G > 1):
+    if (sn != 1 and shape[3] > 1) or (sg != shape[3] and shape[2] > 1):
         raise TypeError(f"{what}: groups and states must be contiguous")
-    return GemSeq(t.data_ptr(), sb, st)
+    return t.data_ptr(), sb, st
 
 
 def _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset):
+    """The sizes, and gem_ssm_t."""
     if x.dim() != 3 or b.dim() != 4:
         raise ValueError("x, b: expected [B, T, D] and [B, T, G, N] tensors")
     (B, T, D), (G, N) = x.shape, b.shape[2:]
-    return GemSsm(B, T, D, N, G, int(softplus), _seq(x, "x", x), _seq(dt, "dt", x), _states(b, "b", x, B, T, G, N),
-                  _states(c, "c", x, B, T, G, N), GemSeq() if z is None else _seq(z, "z", x), _dense(A, "A", _F32, (D, N)),
-                  _optional(skip, "skip", (D,)), _optional(dt_bias, "dt_bias", (D,)), _optional(lengths, "lengths", (B,), _I32),
-                  _bytes(reset, "reset", (B, T)))
+    shape = (B, T, G, N)
+    return B, T, D, N, G, pack_ssm(
+        B, T, D, N, G, bool(softplus), *_place(x, "x", x), *_place(dt, "dt", x), *_states(b, "b", x, shape), *_states(c, "c", x, shape),
+        *_place(z, "z", x), _dense(A, "A", _F32, (D, N)), _optional(skip, "skip", (D,)), _optional(dt_bias, "dt_bias", (D,)),
+        _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)))
 
 
 def gem_ssm_saved_count(B: int, T: int, D: int, N: int) -> int:
@@ -311,13 +327,14 @@ def gem_ssm_forward(x, dt, A, b, c, y, *, z=None, skip=None, dt_bias=None, softp
     """x, dt, z, y [B, T, D] (channels contiguous, any batch and time strides); b, c [B, T, G, N] (the last two
     dimensions contiguous); A [D, N], skip, dt_bias [D], h0, h_last [B, D, N], saved [B, ceil(T / 16), D, N]
     float32; lengths [B] int32; reset [B, T] uint8 or bool; workspace float32, gem_ssm_workspace(B, T, D, N, G)
-    of it."""
-    p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
-    B, T, D, N = p.B, p.T, p.D, p.N
+    of it (one step takes none)."""
+    B, T, D, N, G, p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
+    state = (B, D, N)
     check(lib().gem_ssm_forward(
-        _dtype(x, "x"), p, _optional(h0, "h0", (B, D, N)), _seq(y, "y", x), _optional(h_last, "h_last", (B, D, N)),
+        _dtype(x, "x"), p, _optional(h0, "h0", state), pack_seq(*_place(y, "y", x)), _optional(h_last, "h_last", state),
         _optional(saved, "saved", (B, -(-T // GEM_SSM_CHUNK), D, N)),
-        _space(workspace, "workspace", lib().gem_ssm_workspace(B, T, D, N, p.G, 0), _F32), _stream(stream, x.device)), "gem_ssm_forward")
+        _space(workspace, "workspace", 0 if T == 1 else lib().gem_ssm_workspace(B, T, D, N, G, 0), _F32), _stream(stream, x.device)),
+        "gem_ssm_forward")
 
 
 def gem_ssm_backward(x, dt, A, b, c, saved, dy, dx, ddt, dA, db, dc, *, z=None, dz=None, skip=None, dskip=None, dt_bias=None,
@@ -326,14 +343,14 @@ def gem_ssm_backward(x, dt, A, b, c, saved, dy, dx, ddt, dA, db, dc, *, z=None, 
     """Gradients of what gem_ssm_forward takes from dy [B, T, D] and dh_last [B, D, N]; saved is what the
     forward call saved; dA, dskip, ddt_bias and dh0 may be None; workspace float32,
     gem_ssm_workspace(B, T, D, N, G, backward=True) of it."""
-    p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
-    B, T, D, N, G = p.B, p.T, p.D, p.N, p.G
+    B, T, D, N, G, p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
     if (z is None) != (dz is None):
         raise ValueError("z and dz come together")
-    out = GemSsmGrad(_seq(dx, "dx", x), _seq(ddt, "ddt", x), _states(db, "db", x, B, T, G, N), _states(dc, "dc", x, B, T, G, N),
-                     GemSeq() if dz is None else _seq(dz, "dz", x), _optional(dA, "dA", (D, N)), _optional(dskip, "dskip", (D,)),
-                     _optional(ddt_bias, "ddt_bias", (D,)), _optional(dh0, "dh0", (B, D, N)))
+    shape, state = (B, T, G, N), (B, D, N)
+    out = pack_ssm_grad(
+        *_place(dx, "dx", x), *_place(ddt, "ddt", x), *_states(db, "db", x, shape), *_states(dc, "dc", x, shape), *_place(dz, "dz", x),
+        _optional(dA, "dA", (D, N)), _optional(dskip, "dskip", (D,)), _optional(ddt_bias, "ddt_bias", (D,)), _optional(dh0, "dh0", state))
     check(lib().gem_ssm_backward(
-        _dtype(x, "x"), p, _dense(saved, "saved", _F32, (B, -(-T // GEM_SSM_CHUNK), D, N)), _seq(dy, "dy", x),
-        _optional(dh_last, "dh_last", (B, D, N)), out,
+        _dtype(x, "x"), p, _dense(saved, "saved", _F32, (B, -(-T // GEM_SSM_CHUNK), D, N)), pack_seq(*_place(dy, "dy", x)),
+        _optional(dh_last, "dh_last", state), out,
         _space(workspace, "workspace", lib().gem_ssm_workspace(B, T, D, N, G, 1), _F32), _stream(stream, x.device)), "gem_ssm_backward")

@@ -97,12 +97,12 @@ def ssm_in(B=2, T=4, D=10, N=4, G=1, x=None, dt=None, b=None, c=None, z=None, A=
 
 
 def ssm(L, dtype=0, h0=0, y=None, last=0, saved=0, space=0, **kw):
-    return L.gem_ssm_forward(dtype, ssm_in(**kw), h0, y or seq(), last, saved, space, 0)
+    return L.gem_ssm_forward(dtype, C.byref(ssm_in(**kw)), h0, C.byref(y or seq()), last, saved, space, 0)
 
 
 def ssm_back(L, dtype=0, saved=PTR, dy=None, dlast=0, dx=None, ddt=None, db=None, dc=None, dz=None, dA=0, dskip=0, dbias=0, dh0=0, space=PTR, **kw):
     out = _lib.GemSsmGrad(dx or seq(), ddt or seq(), db or seq(), dc or seq(), dz or seq(), dA, dskip, dbias, dh0)
-    return L.gem_ssm_backward(dtype, ssm_in(**kw), saved, dy or seq(), dlast, out, space, 0)
+    return L.gem_ssm_backward(dtype, C.byref(ssm_in(**kw)), saved, C.byref(dy or seq()), dlast, C.byref(out), space, 0)
 
 
 SSM = SIZES + [dict(N=0), dict(N=65), dict(G=0), dict(G=3), dict(G=-1), dict(dt=seq(0)), dict(b=seq(0)), dict(c=seq(PTR + 2)), dict(b=seq(st=-1)),
@@ -124,11 +124,12 @@ def test_ssm_backward_refuses(L, bad):
 
 def test_null_structures_are_refused(L):
     one = seq()
-    assert L.gem_ssm_forward(0, None, 0, one, 0, 0, 0, 0) == EINVAL
-    assert L.gem_ssm_forward(0, ssm_in(), 0, None, 0, 0, 0, 0) == EINVAL
-    assert L.gem_ssm_backward(0, None, PTR, one, 0, _lib.GemSsmGrad(), PTR, 0) == EINVAL
-    assert L.gem_ssm_backward(0, ssm_in(), PTR, one, 0, None, PTR, 0) == EINVAL
-    assert L.gem_ssm_backward(0, ssm_in(), PTR, None, 0, _lib.GemSsmGrad(one, one, one, one, one), PTR, 0) == EINVAL
+    ref_one, ref_in, ref_out = C.byref(one), C.byref(ssm_in()), C.byref(_lib.GemSsmGrad(one, one, one, one, one))
+    assert L.gem_ssm_forward(0, None, 0, ref_one, 0, 0, 0, 0) == EINVAL
+    assert L.gem_ssm_forward(0, ref_in, 0, None, 0, 0, 0, 0) == EINVAL
+    assert L.gem_ssm_backward(0, None, PTR, ref_one, 0, ref_out, PTR, 0) == EINVAL
+    assert L.gem_ssm_backward(0, ref_in, PTR, ref_one, 0, None, PTR, 0) == EINVAL
+    assert L.gem_ssm_backward(0, ref_in, PTR, None, 0, ref_out, PTR, 0) == EINVAL
     assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, None, PTR, 0, 0, 0, 0, one, 0, 0) == EINVAL
     assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, one, PTR, 0, 0, 0, 0, None, 0, 0) == EINVAL
 
@@ -174,7 +175,13 @@ def test_the_binding_checks_its_tensors():
 
 
 def test_structure_layouts():
+    """The structures' sizes, and that they packed into bytes are the same."""
     assert C.sizeof(_lib.GemSsm) == 24 + 16 + 5 * 24 + 5 * 8 and C.sizeof(_lib.GemSsmGrad) == 5 * 24 + 4 * 8
+    s = [_lib.GemSeq(10 * k, 10 * k + 1, 10 * k + 2) for k in range(1, 6)]
+    flat = [v for q in s for v in (q.data, q.stride_b, q.stride_t)]
+    assert bytes(s[0]) == _lib.pack_seq(*flat[:3])
+    assert bytes(_lib.GemSsm(1, 2, 3, 4, 5, 1, *s, 6, 7, 8, 9, 10)) == _lib.pack_ssm(1, 2, 3, 4, 5, True, *flat, 6, 7, 8, 9, 10)
+    assert bytes(_lib.GemSsmGrad(*s, 6, 7, 8, 9)) == _lib.pack_ssm_grad(*flat, 6, 7, 8, 9)
 
 
 # ---------------------------------------------------------------------- the definitions themselves
