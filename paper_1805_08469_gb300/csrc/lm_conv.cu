@@ -128,21 +128,19 @@ __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& p) {
 struct Resets {
   static constexpr int kBefore = 4;
   uint32_t bits[3];   // of steps first - kBefore + 32 i and on
-  int64_t from;
-  __device__ __forceinline__ Resets(const ConvArgs& p, const ConvPlace& a) : from(a.first - kBefore) {
+  __device__ __forceinline__ Resets(const ConvArgs& p, const ConvPlace& a) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      const int64_t t = from + 32 * i + threadIdx.x % 32;
+      const int64_t t = a.first - kBefore + 32 * i + threadIdx.x % 32;
       bits[i] = p.reset ? __ballot_sync(~0u, t >= 0 && t < a.n && p.reset[a.b * p.T + t] != 0) : 0u;
     }
   }
-  // Of steps t to t + kGroup - 1, the lowest bit that of t.
-  __device__ __forceinline__ unsigned group(int64_t t) const {
-    const int i = int(t - from);
+  // Of the segment's steps i to i + kGroup - 1, the lowest bit that of i.
+  __device__ __forceinline__ unsigned group(int i) const {
+    i += kBefore;
     const uint32_t low = i < 32 ? bits[0] : i < 64 ? bits[1] : bits[2], high = i < 32 ? bits[1] : i < 64 ? bits[2] : 0u;
     return __funnelshift_r(low, high, i % 32) & ((1u << kGroup) - 1);
   }
-  __device__ __forceinline__ bool at(int64_t t) const { return group(t) & 1; }
 };
 
 template <int W, int K>
@@ -177,7 +175,7 @@ struct Window {
 #pragma unroll
     for (int j = 1; j < W; ++j) {
       const int64_t t = a.first - W + j;
-      if (t >= 0 && t < a.n && resets.at(t)) drop();
+      if (resets.group(j - W) & 1) drop();   // (none before step 0 or past the end)
       age = min(age + 1, W);
       if (!a.on) continue;
       if (t >= 0) {
@@ -203,34 +201,31 @@ struct Window {
   }
 };
 
-// Feeds a thread the elements of N sequences' steps [t, end), a group of steps at a time, loaded ahead.  Four channels: by
+// Feeds a thread the elements of N sequences, a group of steps at a time, loaded ahead.  Four channels: by
 // asynchronous copies into places of the thread's own in shared memory (its registers are taken by sums and taps); one:
-// into registers, two groups in turn.  What lies past `end`, or a thread without channels gets, is not defined.
+// into registers.  What lies past the last step, or a thread without channels gets, is not defined.
 template <typename E, int N>
 constexpr int kStages = sizeof(E) == 2 ? 4 : 2;
 template <typename E, int K, int N>
 struct Feed {
   using Shared = Raw<E, K>[kStages<E, N>][N][kGroup][kConvWarps * 32];
   Shared& ring;
-  const E* row[N];
+  const E* at[N];      // the next step to load
   int64_t stride[N];
-  int64_t next, end;
+  int left;            // steps not loaded yet (0 or less: none; of a thread without channels always)
   int stage = 0;
-  bool on;
   __device__ __forceinline__ void issue(int to) {
-    if (on) {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
-        for (int u = 0; u < kGroup; ++u)
-          if (next + u < end) {
-            const uint32_t at = static_cast<uint32_t>(__cvta_generic_to_shared(&ring[to][i][u][threadIdx.x]));
-            asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(row[i] + (next + u) * stride[i]), "n"(int(sizeof(Raw<E, K>)))
-                         : "memory");
-          }
-    }
+      for (int u = 0; u < kGroup; ++u) {
+        const uint32_t slot = static_cast<uint32_t>(__cvta_generic_to_shared(&ring[to][i][u][threadIdx.x]));
+        if (u < left)
+          asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(slot), "l"(at[i]), "n"(int(sizeof(Raw<E, K>))) : "memory");
+        at[i] += stride[i];
+      }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    next += kGroup;
+    left -= kGroup;
   }
   __device__ __forceinline__ void start() {
 #pragma unroll
@@ -250,11 +245,10 @@ template <typename E, int N>
 struct Feed<E, 1, N> {
   using Shared = int;
   Shared& ring;
-  const E* row[N];
+  const E* at[N];
   int64_t stride[N];
-  int64_t next, end;
+  int left;
   int stage = 0;
-  bool on;
   Raw<E, 1> ahead[N][kGroup];
   __device__ __forceinline__ void start() {
 #pragma unroll
@@ -262,9 +256,10 @@ struct Feed<E, 1, N> {
 #pragma unroll
       for (int u = 0; u < kGroup; ++u) {
         ahead[i][u].clear();
-        if (on && next + u < end) ahead[i][u].read(row[i] + (next + u) * stride[i]);
+        if (u < left) ahead[i][u].read(at[i]);
+        at[i] += stride[i];
       }
-    next += kGroup;
+    left -= kGroup;
   }
   __device__ __forceinline__ void take(Raw<E, 1> (&to)[N][kGroup]) {
 #pragma unroll
@@ -305,9 +300,11 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const Con
     taps.read(p, a);
     Window<E, W, K> win;
     win.start(p, a, resets, row);
-    Feed<E, K, 1> feed{ring, {row}, {p.x.stride_t}, a.first, end, 0, a.on};
+    const int own = int(end - a.first);
+    Feed<E, K, 1> feed{ring, {row + a.first * p.x.stride_t}, {p.x.stride_t}, a.on ? own : 0};
     feed.start();
-    auto step = [&](int64_t t, const Raw<E, K>& raw) {
+    E* to = out + a.first * p.y.stride_t;
+    auto step = [&](const Raw<E, K>& raw) {
       win.push(raw);
       Channels<K> y;
 #pragma unroll
@@ -315,26 +312,24 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_forward_kernel(const Con
         y.c[i] = pre_activation<W, K>(taps, win.x, i);
         if (SILU) y.c[i] = y.c[i] * sigmoid<V>(y.c[i]);
       }
-      if (a.on) write_step<E, K>(out + t * p.y.stride_t, y);
+      if (a.on) write_step<E, K>(to, y);
+      to += p.y.stride_t;
     };
-    auto group = [&](int64_t t, const Raw<E, K> (&raw)[kGroup]) {
-      const unsigned drops = resets.group(t);
-      if (t + kGroup <= end && drops == 0) {
+    for (int i = 0; i < own; i += kGroup) {
+      Raw<E, K> raw[1][kGroup];
+      feed.take(raw);
+      const unsigned drops = resets.group(i);
+      if (i + kGroup <= own && drops == 0) {
 #pragma unroll
-        for (int u = 0; u < kGroup; ++u) step(t + u, raw[u]);
+        for (int u = 0; u < kGroup; ++u) step(raw[0][u]);
       } else {
 #pragma unroll
         for (int u = 0; u < kGroup; ++u) {
-          if (t + u >= end) break;
+          if (i + u >= own) break;
           if (drops >> u & 1) win.drop();
-          step(t + u, raw[u]);
+          step(raw[0][u]);
         }
       }
-    };
-    for (int64_t t = a.first; t < end; t += kGroup) {
-      Raw<E, K> raw[1][kGroup];
-      feed.take(raw);
-      group(t, raw[0]);
     }
     if (p.state_last && a.on) {
 #pragma unroll
@@ -388,7 +383,8 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
     taps.read(p, a);
     Window<E, W, K> win;
     win.start(p, a, resets, row);
-    Feed<E, K, 2> feed{ring, {row, dy}, {p.x.stride_t, p.dy.stride_t}, a.first, reach, 0, a.on};
+    const int own = int(end - a.first), all = int(reach - a.first);
+    Feed<E, K, 2> feed{ring, {row + a.first * p.x.stride_t, dy + a.first * p.dy.stride_t}, {p.x.stride_t, p.dy.stride_t}, a.on ? all : 0};
     feed.start();
     Channels<K> dx[W];   // gradients of the window's inputs
 #pragma unroll
@@ -403,8 +399,8 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
         for (int k = 0; k < K; ++k) p.dstate[(a.b * (W - 1) + t + W - 1) * p.D + a.d + k] = v.c[k / V].v[k % V];
       }
     };
-    // one step: `all` of its taps lie in its document, and it is the segment's `own`
-    auto step = [&](const Raw<E, K>& raw_x, const Raw<E, K>& raw_g, bool all, bool own) {
+    // one step: `whole`, all of its taps lie in its document; `mine`, it is the segment's own
+    auto step = [&](const Raw<E, K>& raw_x, const Raw<E, K>& raw_g, bool whole, bool mine) {
       win.push(raw_x);
       const Channels<K> dy = raw_g.floats();
 #pragma unroll
@@ -417,36 +413,36 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
 #pragma unroll
         for (int j = 0; j < W; ++j) {
           dx[j].c[i] = j + 1 < W ? dx[j + 1].c[i] : splat<V>(0.0f);
-          if (all || W - 1 - j <= win.age) dx[j].c[i] = fma<V>(g, taps.w[j].c[i], dx[j].c[i]);
-          if (own) dw[j].c[i] = fma<V>(g, win.x[j].c[i], dw[j].c[i]);
+          if (whole || W - 1 - j <= win.age) dx[j].c[i] = fma<V>(g, taps.w[j].c[i], dx[j].c[i]);
+          if (mine) dw[j].c[i] = fma<V>(g, win.x[j].c[i], dw[j].c[i]);
         }
-        if (own) dw[W].c[i] = dw[W].c[i] + g;
+        if (mine) dw[W].c[i] = dw[W].c[i] + g;
       }
     };
-    auto group = [&](int64_t t, const Raw<E, K> (&raw_x)[kGroup], const Raw<E, K> (&raw_g)[kGroup]) {
-      const unsigned drops = resets.group(t);
-      if (t + kGroup <= end && drops == 0 && win.age >= W - 2 && t >= a.first + W - 1) {
+    E* to = out + (a.first - W + 1) * p.y.stride_t;   // where the input goes that a step completes
+    for (int i = 0; i < all; i += kGroup) {
+      Raw<E, K> raw[2][kGroup];
+      feed.take(raw);
+      const unsigned drops = resets.group(i);
+      if (i + kGroup <= own && drops == 0 && win.age >= W - 2 && i >= W - 1) {
 #pragma unroll
         for (int u = 0; u < kGroup; ++u) {
-          step(raw_x[u], raw_g[u], true, true);
-          if (a.on) write_step<E, K>(out + (t + u - W + 1) * p.y.stride_t, dx[0]);
+          step(raw[0][u], raw[1][u], true, true);
+          if (a.on) write_step<E, K>(to, dx[0]);
+          to += p.y.stride_t;
         }
         win.age = W;
       } else {
 #pragma unroll
         for (int u = 0; u < kGroup; ++u) {
-          if (t + u >= reach) break;
+          if (i + u >= all) break;
           if (drops >> u & 1) win.drop();
           win.age = min(win.age + 1, W);
-          step(raw_x[u], raw_g[u], false, t + u < end);   // (steps past the segment only complete its inputs' gradients)
-          put(t + u - W + 1, dx[0]);
+          step(raw[0][u], raw[1][u], false, i + u < own);   // (steps past the segment only complete its inputs' gradients)
+          put(a.first + i + u - W + 1, dx[0]);
+          to += p.y.stride_t;
         }
       }
-    };
-    for (int64_t t = a.first; t < reach; t += kGroup) {
-      Raw<E, K> raw[2][kGroup];
-      feed.take(raw);
-      group(t, raw[0], raw[1]);
     }
     if (reach == a.n) {   // the sequence ends here: no later step completes its last inputs
 #pragma unroll
