@@ -192,16 +192,26 @@ __device__ void sort_tokens(const EmbedGradArgs& p, SortShared& s, int rank, int
     };
     auto digit_of = [&](int key) { return unsigned(key) >> shift & (radix - 1); };
     for (int i = tid; i < kSortWarps * kRadix / 4; i += kSortThreads) reinterpret_cast<uint4*>(s.counts)[i] = make_uint4(0, 0, 0, 0);
-    __syncthreads();
-    for (int64_t i0 = begin; i0 < end; i0 += 32 * kBatch) {
-      int key[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) key[u] = i0 + 32 * u + lane < end ? key_at(i0 + 32 * u + lane) : 0;
-      unsigned same[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) same[u] = alike(digit_of(key[u]), p.bits, __ballot_sync(~0u, i0 + 32 * u + lane < end));
+    int key[kBatch], place[kBatch];
+    unsigned same[kBatch];   // the lanes with the same digit
+    auto load = [&](int64_t i0) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
+        const int64_t i = i0 + 32 * u + lane;
+        key[u] = i < end ? key_at(i) : 0;
+        place[u] = i < end ? pass == 0 ? int(i) : places[i] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (i0 + 32 * u < end) same[u] = alike(digit_of(key[u]), p.bits, __ballot_sync(~0u, i0 + 32 * u + lane < end));
+    };
+    load(begin);
+    __syncthreads();
+    for (int64_t i0 = begin; i0 < end; i0 += 32 * kBatch) {
+      if (i0 > begin) load(i0);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        if (i0 + 32 * u >= end) break;
         const bool in = i0 + 32 * u + lane < end;
         if (in && lane == __ffs(same[u]) - 1) s.counts[warp][digit_of(key[u])] += __popc(same[u]);
         __syncwarp();
@@ -252,18 +262,10 @@ __device__ void sort_tokens(const EmbedGradArgs& p, SortShared& s, int rank, int
     int32_t* const keys_out = pass & 1 ? p.keys[1] : p.keys[0];
     int32_t* const places_out = pass & 1 ? p.places[1] : p.places[0];
     for (int64_t i0 = begin; i0 < end; i0 += 32 * kBatch) {
-      int key[kBatch], place[kBatch];
+      if (end - begin > 32 * kBatch) load(i0);   // (else the only batch is still there)
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
-        const int64_t i = i0 + 32 * u + lane;
-        key[u] = i < end ? key_at(i) : 0;
-        place[u] = i < end ? pass == 0 ? int(i) : places[i] : 0;
-      }
-      unsigned same[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) same[u] = alike(digit_of(key[u]), p.bits, __ballot_sync(~0u, i0 + 32 * u + lane < end));
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
+        if (i0 + 32 * u >= end) break;
         const bool in = i0 + 32 * u + lane < end;
         const unsigned digit = digit_of(key[u]);
         unsigned to = 0;
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sums_kernel(const EmbedGr
 // `slabs` warps, 128 columns each; share q takes every shares-th partial row from the q-th on, and the first adds theirs up.
 constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinSlabs = 8;
 template <typename G, bool WIDE>
-__global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedGradArgs p, int slabs) {
+__global__ void __launch_bounds__(kJoinThreads, 3) embed_join_kernel(const EmbedGradArgs p, int slabs) {
   __shared__ float parts[kJoinWarps][kSlab<float>];
   pdl_entry();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, share = warp / slabs, shares = kJoinWarps / slabs;
@@ -454,7 +456,7 @@ __global__ void __launch_bounds__(kJoinThreads) embed_join_kernel(const EmbedGra
         const unsigned all = __ballot_sync(~0u, on[q]);
         if (count == q * 32) count += all == ~0u ? 32 : __ffs(~all) - 1;
       }
-#pragma unroll 16
+#pragma unroll 8
       for (int i = share; i < count; i += shares) add(at + i, 0);
       if (count < 128) break;
     }
@@ -488,7 +490,7 @@ bool wide(const void* p, int element, int64_t ld, int64_t D, int per) {
 int chunk_of(int64_t N) { return N < 2048 ? 8 : N < 16384 ? 16 : 32; }
 
 // Blocks of the sort's cluster.
-unsigned sort_blocks(int64_t N) { return N <= 8192 ? 1 : N <= 32768 ? 8 : 16; }
+unsigned sort_blocks(int64_t N) { return N <= 2048 ? 1 : N <= 16384 ? 8 : 16; }
 
 // Parts of the workspace, each a multiple of 16 bytes.
 int64_t list_bytes(int64_t N) { return (N * 4 + 15) / 16 * 16; }
