@@ -112,9 +112,9 @@ def _declare(L):
         "gem_embed": ([i, i, i64, i64, i64, p, i64, p, f, p, i64, p], i),
         "gem_embed_workspace": ([i64, i64, i64], i64),
         "gem_embed_grad": ([i, i, i64, i64, i64, p, i64, p, f, i, p, i64, p, p], i),
-        "gem_conv_forward": ([i, i, i64, i64, i64, i, seq, p, p, p, p, p, seq, p, p], i),
+        "gem_conv_forward": ([i, i, i64, i64, i64, i, p, p, p, p, p, p, p, p, p], i),
         "gem_conv_workspace": ([i64, i64, i64, i], i64),
-        "gem_conv_backward": ([i, i, i64, i64, i64, i, seq, p, p, p, p, p, seq, p, seq, p, p, p, p, p], i),
+        "gem_conv_backward": ([i, i, i64, i64, i64, i, p, p, p, p, p, p, p, p, p, p, p, p, p, p], i),
         "gem_ssm_saved_count": ([i64, i64, i64, i], i64),
         "gem_ssm_workspace": ([i64, i64, i64, i, i, i], i64),
         "gem_ssm_forward": ([i, p, p, p, p, p, p, p], i),

@@ -233,12 +233,18 @@ def gem_embed_grad(dout, tokens, dtable, workspace, *, scale: float = 1.0, accum
         _stream(stream, dout.device)), "gem_embed_grad")
 
 
-def _optional(t, what: str, shape, dtype=_F32) -> int:
-    return 0 if t is None else _dense(t, what, dtype, shape)
-
-
-def _bytes(t, what: str, shape) -> int:
-    return 0 if t is None else _dense(t.view(_U8) if t.dtype is torch.bool else t, what, _U8, shape)
+def _place(t, what: str, like):
+    """Address, batch and time stride of a [B, T, D] tensor of like's type and shape (None: of no tensor)."""
+    if t is None:
+        return 0, 0, 0
+    if t.dtype is not like.dtype or not t.is_cuda:
+        raise TypeError(f"{what}: expected a {like.dtype} CUDA tensor")
+    if t.shape != like.shape:
+        raise ValueError(f"{what}: expected the shape {tuple(like.shape)}, got {tuple(t.shape)}")
+    sb, st, sd = t.stride()
+    if sd != 1 and t.shape[2] > 1:
+        raise TypeError(f"{what}: the channels must be contiguous")
+    return t.data_ptr(), sb, st
 
 
 def gem_conv_forward(x, weight, y, *, form: int = GEM_CONV_SILU, bias=None, state=None, lengths=None, reset=None,
@@ -250,9 +256,11 @@ def gem_conv_forward(x, weight, y, *, form: int = GEM_CONV_SILU, bias=None, stat
     B, T, D = x.shape
     W = weight.shape[1]
     check(lib().gem_conv_forward(
-        _dtype(x, "x"), form, B, T, D, W, _seq(x, "x", x), _dense(weight, "weight", _F32, (D, W)), _optional(bias, "bias", (D,)),
-        _optional(state, "state", (B, W - 1, D)), _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)),
-        _seq(y, "y", x), _optional(state_last, "state_last", (B, W - 1, D)), _stream(stream, x.device)), "gem_conv_forward")
+        _dtype(x, "x"), form, B, T, D, W, pack_seq(*_place(x, "x", x)), _dense(weight, "weight", _F32, (D, W)),
+        0 if bias is None else _dense(bias, "bias", _F32, (D,)), 0 if state is None else _dense(state, "state", _F32, (B, W - 1, D)),
+        0 if lengths is None else _dense(lengths, "lengths", _I32, (B,)), 0 if reset is None else _reset(reset, B, T),
+        pack_seq(*_place(y, "y", x)), 0 if state_last is None else _dense(state_last, "state_last", _F32, (B, W - 1, D)),
+        _stream(stream, x.device)), "gem_conv_forward")
 
 
 def gem_conv_workspace(B: int, T: int, D: int, W: int) -> int:
@@ -269,25 +277,13 @@ def gem_conv_backward(x, weight, dy, dx, dweight, workspace, *, form: int = GEM_
     W = weight.shape[1]
     size = gem_conv_workspace(B, T, D, W) if dweight is not None or dbias is not None else 0
     check(lib().gem_conv_backward(
-        _dtype(x, "x"), form, B, T, D, W, _seq(x, "x", x), _dense(weight, "weight", _F32, (D, W)), _optional(bias, "bias", (D,)),
-        _optional(state, "state", (B, W - 1, D)), _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)),
-        _seq(dy, "dy", x), _optional(dstate_last, "dstate_last", (B, W - 1, D)), _seq(dx, "dx", x),
-        _optional(dweight, "dweight", (D, W)), _optional(dbias, "dbias", (D,)), _optional(dstate, "dstate", (B, W - 1, D)),
+        _dtype(x, "x"), form, B, T, D, W, pack_seq(*_place(x, "x", x)), _dense(weight, "weight", _F32, (D, W)),
+        0 if bias is None else _dense(bias, "bias", _F32, (D,)), 0 if state is None else _dense(state, "state", _F32, (B, W - 1, D)),
+        0 if lengths is None else _dense(lengths, "lengths", _I32, (B,)), 0 if reset is None else _reset(reset, B, T),
+        pack_seq(*_place(dy, "dy", x)), 0 if dstate_last is None else _dense(dstate_last, "dstate_last", _F32, (B, W - 1, D)),
+        pack_seq(*_place(dx, "dx", x)), 0 if dweight is None else _dense(dweight, "dweight", _F32, (D, W)),
+        0 if dbias is None else _dense(dbias, "dbias", _F32, (D,)), 0 if dstate is None else _dense(dstate, "dstate", _F32, (B, W - 1, D)),
         _space(workspace, "workspace", size, _F32), _stream(stream, x.device)), "gem_conv_backward")
-
-
-def _place(t, what: str, like):
-    """Address, batch and time stride of a [B, T, D] tensor of like's type and shape (None: of no tensor)."""
-    if t is None:
-        return 0, 0, 0
-    sb, st, sd = t.stride()
-    if t.dtype is not like.dtype or not t.is_cuda:
-        raise TypeError(f"{what}: expected a {like.dtype} CUDA tensor")
-    if t.shape != like.shape:
-        raise ValueError(f"{what}: expected the shape {tuple(like.shape)}, got {tuple(t.shape)}")
-    if sd != 1 and t.shape[2] > 1:
-        raise TypeError(f"{what}: the channels must be contiguous")
-    return t.data_ptr(), sb, st
 
 
 def _states(t, what: str, like, shape):
@@ -310,8 +306,9 @@ def _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset):
     shape = (B, T, G, N)
     return B, T, D, N, G, pack_ssm(
         B, T, D, N, G, bool(softplus), *_place(x, "x", x), *_place(dt, "dt", x), *_states(b, "b", x, shape), *_states(c, "c", x, shape),
-        *_place(z, "z", x), _dense(A, "A", _F32, (D, N)), _optional(skip, "skip", (D,)), _optional(dt_bias, "dt_bias", (D,)),
-        _optional(lengths, "lengths", (B,), _I32), _bytes(reset, "reset", (B, T)))
+        *_place(z, "z", x), _dense(A, "A", _F32, (D, N)), 0 if skip is None else _dense(skip, "skip", _F32, (D,)),
+        0 if dt_bias is None else _dense(dt_bias, "dt_bias", _F32, (D,)),
+        0 if lengths is None else _dense(lengths, "lengths", _I32, (B,)), 0 if reset is None else _reset(reset, B, T))
 
 
 def gem_ssm_saved_count(B: int, T: int, D: int, N: int) -> int:
@@ -331,8 +328,9 @@ def gem_ssm_forward(x, dt, A, b, c, y, *, z=None, skip=None, dt_bias=None, softp
     B, T, D, N, G, p = _ssm(x, dt, A, b, c, z, skip, dt_bias, softplus, lengths, reset)
     state = (B, D, N)
     check(lib().gem_ssm_forward(
-        _dtype(x, "x"), p, _optional(h0, "h0", state), pack_seq(*_place(y, "y", x)), _optional(h_last, "h_last", state),
-        _optional(saved, "saved", (B, -(-T // GEM_SSM_CHUNK), D, N)),
+        _dtype(x, "x"), p, 0 if h0 is None else _dense(h0, "h0", _F32, state), pack_seq(*_place(y, "y", x)),
+        0 if h_last is None else _dense(h_last, "h_last", _F32, state),
+        0 if saved is None else _dense(saved, "saved", _F32, (B, -(-T // GEM_SSM_CHUNK), D, N)),
         _space(workspace, "workspace", 0 if T == 1 else lib().gem_ssm_workspace(B, T, D, N, G, 0), _F32), _stream(stream, x.device)),
         "gem_ssm_forward")
 
@@ -349,8 +347,9 @@ def gem_ssm_backward(x, dt, A, b, c, saved, dy, dx, ddt, dA, db, dc, *, z=None, 
     shape, state = (B, T, G, N), (B, D, N)
     out = pack_ssm_grad(
         *_place(dx, "dx", x), *_place(ddt, "ddt", x), *_states(db, "db", x, shape), *_states(dc, "dc", x, shape), *_place(dz, "dz", x),
-        _optional(dA, "dA", (D, N)), _optional(dskip, "dskip", (D,)), _optional(ddt_bias, "ddt_bias", (D,)), _optional(dh0, "dh0", state))
+        0 if dA is None else _dense(dA, "dA", _F32, (D, N)), 0 if dskip is None else _dense(dskip, "dskip", _F32, (D,)),
+        0 if ddt_bias is None else _dense(ddt_bias, "ddt_bias", _F32, (D,)), 0 if dh0 is None else _dense(dh0, "dh0", _F32, state))
     check(lib().gem_ssm_backward(
         _dtype(x, "x"), p, _dense(saved, "saved", _F32, (B, -(-T // GEM_SSM_CHUNK), D, N)), pack_seq(*_place(dy, "dy", x)),
-        _optional(dh_last, "dh_last", state), out,
+        0 if dh_last is None else _dense(dh_last, "dh_last", _F32, state), out,
         _space(workspace, "workspace", lib().gem_ssm_workspace(B, T, D, N, G, 1), _F32), _stream(stream, x.device)), "gem_ssm_backward")

@@ -65,12 +65,13 @@ def test_embed_grad_refuses(L, bad):
 
 
 def conv(L, dtype=0, form=1, B=2, T=4, D=10, W=4, x=None, weight=PTR, bias=0, state=0, lengths=0, y=None, last=0):
-    return L.gem_conv_forward(dtype, form, B, T, D, W, x or seq(), weight, bias, state, lengths, 0, y or seq(), last, 0)
+    return L.gem_conv_forward(dtype, form, B, T, D, W, C.byref(x or seq()), weight, bias, state, lengths, 0, C.byref(y or seq()), last, 0)
 
 
 def conv_back(L, dtype=0, form=1, B=2, T=4, D=10, W=4, x=None, weight=PTR, bias=0, state=0, lengths=0, dy=None, dlast=0, dx=None, dw=PTR, db=0, ds=0,
               space=PTR):
-    return L.gem_conv_backward(dtype, form, B, T, D, W, x or seq(), weight, bias, state, lengths, 0, dy or seq(), dlast, dx or seq(), dw, db, ds, space, 0)
+    x, dy, dx = (C.byref(t or seq()) for t in (x, dy, dx))
+    return L.gem_conv_backward(dtype, form, B, T, D, W, x, weight, bias, state, lengths, 0, dy, dlast, dx, dw, db, ds, space, 0)
 
 
 SIZES = [dict(dtype=3), dict(dtype=-1), dict(B=-1), dict(T=-1), dict(D=-1), dict(B=1 << 31), dict(T=1 << 31), dict(x=seq(0)), dict(x=seq(PTR + 2)),
@@ -130,8 +131,8 @@ def test_null_structures_are_refused(L):
     assert L.gem_ssm_backward(0, None, PTR, ref_one, 0, ref_out, PTR, 0) == EINVAL
     assert L.gem_ssm_backward(0, ref_in, PTR, ref_one, 0, None, PTR, 0) == EINVAL
     assert L.gem_ssm_backward(0, ref_in, PTR, None, 0, ref_out, PTR, 0) == EINVAL
-    assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, None, PTR, 0, 0, 0, 0, one, 0, 0) == EINVAL
-    assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, one, PTR, 0, 0, 0, 0, None, 0, 0) == EINVAL
+    assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, None, PTR, 0, 0, 0, 0, ref_one, 0, 0) == EINVAL
+    assert L.gem_conv_forward(0, 0, 1, 1, 1, 4, ref_one, PTR, 0, 0, 0, 0, None, 0, 0) == EINVAL
 
 
 def test_empty_sizes_leave_nothing_to_do(L):
