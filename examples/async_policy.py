@@ -129,7 +129,7 @@ def loss_and_gradient(model, flat, read, sampled, old_logp, advantage, bonus: fl
     return loss.mean(), model.backward(flat, read, kept, logits)
 
 
-def main(commits: int = 300, n: int = 4, V: int = 200, B: int = 32, T: int = 24, eta: float = 0.5, seed: int = 5, verbose: bool = True):
+def main(commits: int = 300, n: int = 4, V: int = 200, B: int = 32, T: int = 24, eta: float = 0.002, seed: int = 5, verbose: bool = True):
     """Returns the mean rewards and losses of the commits."""
     g = torch.Generator(device="cuda")
     g.manual_seed(seed)
@@ -137,7 +137,9 @@ def main(commits: int = 300, n: int = 4, V: int = 200, B: int = 32, T: int = 24,
     order, _ = sim.gem_schedule_uniform(seed, n, commits)
     rewards, losses = torch.empty(commits, device="cuda"), torch.empty(commits, device="cuda")
     with gem.Gem(model.P, n, eta=eta, mu=0.9, eps=1e-8, stream=torch.cuda.current_stream()) as G:
-        G.set_theta(model.init(g))
+        theta = model.init(g)
+        model.views(theta)["outward"].mul_(0.02)              # (nearly even chances to begin with)
+        G.set_theta(theta)
         for t, w in enumerate(order.tolist()):
             flat = G.snapshot(w)                              # the worker's stale parameters
             first = torch.randint(0, V, (B,), device="cuda", generator=g, dtype=torch.int32)

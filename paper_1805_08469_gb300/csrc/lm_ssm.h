@@ -332,7 +332,7 @@ __device__ __forceinline__ void scatter_sums(float (&v)[N]) {
 struct SsmCut {
   int64_t blocks, splits, steps;
 };
-SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH);
+SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH, bool backward);
 
 template <typename E>
 cudaError_t launch_forward(SsmArgs p, cudaStream_t stream);

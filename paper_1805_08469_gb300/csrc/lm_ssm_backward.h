@@ -403,7 +403,7 @@ static __global__ void __launch_bounds__(128) ssm_join_params_kernel(const SsmAr
 template <typename E, int LS, bool WIDE>
 cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
   using S = Shape<LS, kBackwardK>;
-  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH);
+  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH, true);
   p.blocks = int(cut.blocks);
   p.splits = int(cut.splits);
   p.steps = cut.steps;
