@@ -75,7 +75,7 @@ int64_t workspace_floats(const gem_ssm_t& in, bool backward) {
   const int64_t forward = split_floats(in, ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, kForwardK), false));
   if (!backward) return forward;
   const SsmCut c = ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, kBackwardK), true);
-  const int64_t parts = c.blocks > 1 ? in.B * in.T * in.G * c.blocks * 2 * kQuad * state_lanes(in.N) : 0;
+  const int64_t parts = c.blocks > 1 ? in.B * in.T * in.G * c.blocks * 2 * kQuad * state_lanes(in.N) + 3 : 0;   // (and to a multiple of 16 bytes)
   return std::max(forward, split_floats(in, c) + parts + in.B * c.splits * in.D * (int64_t(in.N) + 2));
 }
 

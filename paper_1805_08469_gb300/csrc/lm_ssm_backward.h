@@ -227,22 +227,38 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_backward_kernel(const SsmA
           }
         }
       };
-      // the half's db and dc of all the block's channels
+      // the half's db and dc of all the block's channels: a thread for a quad of states of a step, or kShare of them
+      // with a share of the channels each, which begin a rotation apart
       auto collect = [&](int t1) {
-        constexpr int kOutputs = 2 * S::NP;
+        constexpr int kQuads = Given<S>::kQuads, kShare = LS < 8 ? 8 / LS : 1, kEach = S::CH / kShare;
 #pragma unroll
-        for (int i = 0; i < kHalf * kOutputs / kSsmThreads; ++i) {
-          const int o = i * kSsmThreads + threadIdx.x, t = o / kOutputs, k = o % kOutputs;
-          if (t1 + t >= count) break;
-          float v[4] = {};
-          const float* const from = given + t * kGivenStep + k % kQuad;
+        for (int i = 0; i < kHalf * kQuads * kShare / kSsmThreads; ++i) {
+          const int o = (i * kSsmThreads + threadIdx.x) / kShare, share = threadIdx.x % kShare, t = o / kQuads, q = o % kQuads;
+          Quad v = zeros();
 #pragma unroll
-          for (int c = 0; c < S::CH; ++c) v[c % 4] += from[Given<S>::place(0, c, k / kQuad)];
-          const float sum = (v[0] + v[1]) + (v[2] + v[3]);
+          for (int c = 0; c < kEach; ++c) {
+            const int channel = share * kEach + (c + share * (kQuads / kShare)) % kEach;
+            const Quad w = quad(*reinterpret_cast<const float4*>(given + Given<S>::place(t, channel, q)));
+            v = {v.a + w.a, v.b + w.b};
+          }
+#pragma unroll
+          for (int bit = 1; bit < kShare; bit *= 2)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              v.a.v[k] += __shfl_xor_sync(~0u, v.a.v[k], bit);
+              v.b.v[k] += __shfl_xor_sync(~0u, v.b.v[k], bit);
+            }
+          if (share != 0 || t1 + t >= count) continue;
+          const int64_t step = t0 + t1 + t;
           if (p.blocks > 1) {
-            p.bc_part[(((a.b * p.in.T + t0 + t1 + t) * p.in.G + a.group) * p.blocks + a.part) * kOutputs + k] = sum;
-          } else if (k % S::NP < N) {
-            *at<E>(k < S::NP ? p.db : p.dc, a.b, t0 + t1 + t, a.group * a.states + k % S::NP) = from_f32<E>(sum);
+            store_quad<true>(p.bc_part + ((((a.b * p.in.T + step) * p.in.G + a.group) * p.blocks + a.part) * kQuads + q) * kQuad, kQuad, v);
+          } else {
+            E* const to = at<E>(q < LS ? p.db : p.dc, a.b, step, a.group * a.states + q % LS * kQuad);
+            const int there = a.states - q % LS * kQuad;
+            const float out[kQuad] = {v.a.v[0], v.a.v[1], v.b.v[0], v.b.v[1]};
+#pragma unroll
+            for (int k = 0; k < kQuad; ++k)
+              if (k < there) to[k] = from_f32<E>(out[k]);
           }
         }
       };
@@ -412,8 +428,10 @@ cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
     p.sums = space + p.in.B * cut.splits * p.in.D * p.in.N;
     space = p.sums + p.in.B * cut.splits * p.in.D;
   }
-  p.bc_part = space;
-  if (cut.blocks > 1) space += p.in.B * p.in.T * p.in.G * cut.blocks * 2 * S::NP;
+  if (cut.blocks > 1) {
+    p.bc_part = space + (16 - reinterpret_cast<uintptr_t>(space) % 16) % 16 / 4;   // (quads are stored to it)
+    space += p.in.B * p.in.T * p.in.G * cut.blocks * 2 * S::NP + 3;
+  }
   p.param_part = space;
   const dim3 grid(unsigned(p.in.B * cut.splits * p.in.G * cut.blocks)), block(kSsmThreads);
   const bool gate = p.in.z.data;
