@@ -35,7 +35,7 @@ struct Given {
 };
 
 template <typename E, int LS, bool WIDE, bool GATE, bool STATES>
-__global__ void __launch_bounds__(kSsmThreads, 4) ssm_backward_kernel(const SsmArgs p) {
+__global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_kernel(const SsmArgs p) {
   using S = Shape<LS, kBackwardK>;
   constexpr int kSums = GATE ? 3 : 2, U = S::U;
   extern __shared__ float4 shared[];
