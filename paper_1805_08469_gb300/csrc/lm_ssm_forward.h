@@ -9,7 +9,7 @@ namespace ssm {
 
 // Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.
 template <typename E, int LS, int K, bool WIDE, bool STATES>
-__global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs p) {
+__global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmArgs p) {
   using S = Shape<LS, K>;
   __shared__ float2 steps[kTile][S::row];                          // (step, step x) of each channel
   __shared__ float4 bc[(STATES ? 1 : 2) * kTile * LS];
@@ -110,24 +110,38 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_forward_kernel(const SsmArgs 
     float y[K][kTile];
     auto tile = [&](auto check) {
       const int count = int(min(end - t0, int64_t(kTile)));
+      // steps in sets: what a set reads and its decays come first, so that their latencies overlap
+      constexpr int kSet = 4;
 #pragma unroll
-      for (int t = 0; t < kTile; ++t) {
+      for (int t1 = 0; t1 < kTile; t1 += kSet) {
+        Quad b[kSet], c[kSet];
+        float2 v[kSet][K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) y[k][t] = 0.0f;
-        if (check.value && t >= count) continue;
-        const Quad b = quad(bc[t * LS + a.g]);
-        const Quad c = STATES ? b : quad(bc[(kTile + t) * LS + a.g]);
+        for (int i = 0; i < kSet; ++i) {
+          b[i] = quad(bc[(t1 + i) * LS + a.g]);
+          if (!STATES) c[i] = quad(bc[(kTile + t1 + i) * LS + a.g]);
+#pragma unroll
+          for (int k = 0; k < K; ++k) v[i][k] = steps[t1 + i][a.pos + k * S::lanes];
+        }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-          if (check.value && (resets >> t & 1)) h[k] = zeros();
-          const float2 v = steps[t][a.pos + k * S::lanes];
-          h[k].a = fma<2>(decay(v.x, A2[k].a), h[k].a, splat<2>(v.y) * b.a);
-          h[k].b = fma<2>(decay(v.x, A2[k].b), h[k].b, splat<2>(v.y) * b.b);
-          if (STATES) {
-            sum[k] += v.x;
-          } else {
-            const Vec<2> m = fma<2>(c.b, h[k].b, c.a * h[k].a);
-            y[k][t] = m.v[0] + m.v[1];
+          Quad dec[kSet];
+#pragma unroll
+          for (int i = 0; i < kSet; ++i) dec[i] = {decay(v[i][k].x, A2[k].a), decay(v[i][k].x, A2[k].b)};
+#pragma unroll
+          for (int i = 0; i < kSet; ++i) {
+            const int t = t1 + i;
+            if (!STATES) y[k][t] = 0.0f;
+            if (check.value && t >= count) continue;
+            if (check.value && (resets >> t & 1)) h[k] = zeros();
+            h[k].a = fma<2>(dec[i].a, h[k].a, splat<2>(v[i][k].y) * b[i].a);
+            h[k].b = fma<2>(dec[i].b, h[k].b, splat<2>(v[i][k].y) * b[i].b);
+            if (STATES) {
+              sum[k] += v[i][k].x;
+            } else {
+              const Vec<2> m = fma<2>(c[i].b, h[k].b, c[i].a * h[k].a);
+              y[k][t] = m.v[0] + m.v[1];
+            }
           }
         }
       }
