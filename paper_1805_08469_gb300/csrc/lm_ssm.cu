@@ -9,20 +9,21 @@ namespace ssm {
 
 // Time is split where a block for every sequence and its channels would leave too few warps on an SM.  A split's first pass
 // costs 60% of the forward one's second, 20% of the backward one's, so the forward pass is split below one and a half
-// blocks an SM, the backward one below two and a half; then into whole turns of the four blocks that an SM holds, up to three
+// blocks an SM, the backward one below two and a half of four; then into whole turns of the blocks that an SM holds, up to three
 // while a block has no more than 40 splits to compose, but not into splits of less than 128 steps.  Both calls, bf16, 16
 // states, in us with 1, 4, 8, 16 and 32 splits: 4 x 2048 x 2048 739, 639, 621, 650, 771; 1 x 16,384 x 2048 4711, 1930, 1433,
 // 1275, 1258; 8 x 2048 x 2048 1125, 1180, 1178, 1259, 1510.  1 x 50,021 x 512 with 38 (one turn) 955, with 64 1012.
-SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH, bool backward) {
-  constexpr int64_t kSms = 152, kTurn = 4 * kSms, kMostComposed = 40, kMostSplits = 64, kLeastSteps = 128;
+SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH, bool backward, int resident) {
+  constexpr int64_t kSms = 152, kMostComposed = 40, kMostSplits = 64, kLeastSteps = 128;
   SsmCut c;
   c.blocks = (D / G + CH - 1) / CH;
-  const int64_t base = B * G * c.blocks, enough = backward ? 5 * kSms / 2 : 3 * kSms / 2;
+  const int64_t base = B * G * c.blocks, turn = resident * kSms;
+  const int64_t enough = backward && resident > 2 ? 5 * kSms / 2 : 3 * kSms / 2;
   int64_t splits = 1;
   if (base > 0 && base < enough) {
     int64_t turns = 3;
-    while (turns > 1 && turns * kTurn / base > kMostComposed) --turns;
-    splits = std::min(turns * kTurn / base, kMostSplits);
+    while (turns > 1 && turns * turn / base > kMostComposed) --turns;
+    splits = std::min(turns * turn / base, kMostSplits);
   }
   splits = std::max(std::min(splits, (T + kLeastSteps - 1) / kLeastSteps), int64_t(1));
   c.steps = ((T + splits - 1) / splits + kTile - 1) / kTile * kTile;
@@ -72,9 +73,10 @@ int64_t split_floats(const gem_ssm_t& in, const SsmCut& c) { return c.splits > 1
 
 int64_t workspace_floats(const gem_ssm_t& in, bool backward) {
   if (in.B == 0 || in.D == 0) return 0;
-  const int64_t forward = split_floats(in, ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, kForwardK), false));
+  const int64_t forward = split_floats(in, ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, kForwardK), false, 4));
   if (!backward) return forward;
-  const SsmCut c = ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, kBackwardK), true);
+  const int LS = state_lanes(in.N);
+  const SsmCut c = ssm_cut(in.B, in.T, in.D, in.G, block_channels(in.N, backward_k(LS)), true, backward_resident(LS));
   const int64_t parts = c.blocks > 1 ? in.B * in.T * in.G * c.blocks * 2 * kQuad * state_lanes(in.N) + 3 : 0;   // (and to a multiple of 16 bytes)
   return std::max(forward, split_floats(in, c) + parts + in.B * c.splits * in.D * (int64_t(in.N) + 2));
 }
@@ -153,7 +155,7 @@ int gem_ssm_backward(int dtype, const gem_ssm_t* in, const float* saved, const g
   p.ddt_bias = out->ddt_bias;
   p.states = workspace;
   p.params = params;
-  const int V = block_channels(in->N, kBackwardK) / 8;
+  const int V = block_channels(in->N, backward_k(state_lanes(in->N))) / 8;
   p.wide = inputs_wide(*in, dtype, V) && in_pieces(*dy, dtype, *in, V) && in_pieces(out->dx, dtype, *in, V) && in_pieces(out->ddt, dtype, *in, V) &&
            (!in->z.data || in_pieces(out->dz, dtype, *in, V)) && aligned_to(dh_last, 16) && aligned_to(out->dh0, 16) && aligned_to(saved, 16) &&
            aligned_to(workspace, 16);

@@ -28,15 +28,15 @@ constexpr int kHalf = kTile / 2;
 // store together then lie in different banks.
 template <typename S>
 struct Given {
-  static constexpr int kQuads = 2 * S::LS, kTurn = S::LS / 4, kFloats = kHalf * S::CH * kQuads * kQuad;
-  static __device__ __forceinline__ int place(int t, int channel, int q) {
-    return ((t * S::CH + channel) * kQuads + (q + kTurn * channel) % kQuads) * kQuad;
+  static constexpr int kRows = S::CH / S::K, kQuads = 2 * S::LS, kTurn = S::LS / 4, kFloats = kHalf * kRows * kQuads * kQuad;
+  static __device__ __forceinline__ int place(int t, int row, int q) {
+    return ((t * kRows + row) * kQuads + (q + kTurn * row) % kQuads) * kQuad;
   }
 };
 
-template <typename E, int LS, bool WIDE, bool GATE, bool STATES>
-__global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_kernel(const SsmArgs p) {
-  using S = Shape<LS, kBackwardK>;
+template <typename E, int LS, int K, bool WIDE, bool GATE, bool STATES>
+__global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS>) ssm_backward_kernel(const SsmArgs p) {
+  using S = Shape<LS, K>;
   constexpr int kSums = GATE ? 3 : 2, U = S::U;
   extern __shared__ float4 shared[];
   float* const given = reinterpret_cast<float*>(shared);
@@ -49,31 +49,34 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
   if (STATES && a.split == 0) return;
   const int64_t D = p.in.D, N = a.states;
   const int64_t end = min(a.end, a.n), row = a.b * p.splits + a.split;
-  const bool has = a.has(0);
-  // the places of the thread's channel, and from one step to the next
-  constexpr int kGivenStep = S::CH * Given<S>::kQuads * kQuad;
-  const int to_db = Given<S>::place(0, a.pos, a.g), to_dc = Given<S>::place(0, a.pos, S::LS + a.g);
+  // the places of what the thread gives, and from one step to the next
+  constexpr int kGivenStep = Given<S>::kRows * Given<S>::kQuads * kQuad;
+  const int given_row = threadIdx.x / 32 * S::lanes + threadIdx.x % S::lanes;
+  const int to_db = Given<S>::place(0, given_row, a.g), to_dc = Given<S>::place(0, given_row, S::LS + a.g);
 
-  Quad A2 = has ? load_quad<WIDE>(p.in.A + a.state(0, D, 0), a.quads) : zeros();
-  A2 = {scaled(A2.a, kLog2e), scaled(A2.b, kLog2e)};
-  Quad g = zeros();
-  if (has) {
+  Quad A2[K], g[K], dA[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) {
+    A2[k] = a.has(k) ? load_quad<WIDE>(p.in.A + a.state(0, D, k), a.quads) : zeros();
+    A2[k] = {scaled(A2[k].a, kLog2e), scaled(A2[k].b, kLog2e)};
+    g[k] = dA[k] = zeros();
+    if (!a.has(k)) continue;
     if (p.splits == 1 || (STATES && a.split + 1 == p.splits)) {
-      if (p.h0) g = load_quad<WIDE>(p.h0 + a.state(a.b, D, 0), a.quads);
+      if (p.h0) g[k] = load_quad<WIDE>(p.h0 + a.state(a.b, D, k), a.quads);
       // (the second pass's own copy: dh0 may be dh_last)
-      if (STATES) store_quad<WIDE>(p.states + a.state(a.b * p.splits, D, 0), a.quads, g);
+      if (STATES) store_quad<WIDE>(p.states + a.state(a.b * p.splits, D, k), a.quads, g[k]);
     } else if (!STATES) {
-      if (a.split + 1 == p.splits) g = load_quad<WIDE>(p.states + a.state(a.b * p.splits, D, 0), a.quads);
+      if (a.split + 1 == p.splits) g[k] = load_quad<WIDE>(p.states + a.state(a.b * p.splits, D, k), a.quads);
 #pragma unroll 4
       for (int q = p.splits - 1; q > a.split; --q) {
         const int64_t from = a.b * p.splits + q;
-        const Quad first = load_quad<WIDE>(p.states + a.state(from, D, 0), a.quads);
-        const float sum = p.sums[from * D + a.d0 + a.channel(0)];
+        const Quad first = load_quad<WIDE>(p.states + a.state(from, D, k), a.quads);
+        const float sum = p.sums[from * D + a.d0 + a.channel(k)];
         if (sum == INFINITY || q == p.splits - 1) {
-          g = first;
+          g[k] = first;
         } else {
-          g.a = fma<2>({far_decay(sum, A2.a.v[0]), far_decay(sum, A2.a.v[1])}, g.a, first.a);
-          g.b = fma<2>({far_decay(sum, A2.b.v[0]), far_decay(sum, A2.b.v[1])}, g.b, first.b);
+          g[k].a = fma<2>({far_decay(sum, A2[k].a.v[0]), far_decay(sum, A2[k].a.v[1])}, g[k].a, first.a);
+          g[k].b = fma<2>({far_decay(sum, A2[k].b.v[0]), far_decay(sum, A2[k].b.v[1])}, g[k].b, first.b);
         }
       }
     }
@@ -86,13 +89,14 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
     skip[j / U].v[j % U] = !STATES && p.in.skip && j < a.there ? p.in.skip[a.d0 + a.c0 + j] : 0.0f;
     dskip[j / U].v[j % U] = dbias[j / U].v[j % U] = 0.0f;
   }
-  Quad dA = zeros();
-  float total = 0.0f;
+  float total[K] = {};
   bool dropped = false;
 
   Raw<E, S::V, WIDE> x, dt, z, dy, x_next, dt_next, z_next, dy_next;
   States<E, S, WIDE, !STATES, true> b_next;
-  Quad start_next = zeros();
+  Quad start[K], start_next[K];
+#pragma unroll
+  for (int k = 0; k < K; ++k) start_next[k] = zeros();
   const int64_t chunks = (p.in.T + kTile - 1) / kTile;
   auto load = [&](int64_t t0) {
     const int64_t t = t0 + a.s;
@@ -102,7 +106,10 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
     if (GATE) z_next.read(at<E>(p.in.z, a.b, t, d), there);
     dy_next.read(at<E>(p.dy, a.b, t, d), there);
     b_next.load(p, a, t0);
-    if (!STATES && has) start_next = load_quad<WIDE>(p.saved + a.state(a.b * chunks + t0 / kTile, D, 0), a.quads);
+    if (!STATES)
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+        if (a.has(k)) start_next[k] = load_quad<WIDE>(p.saved + a.state(a.b * chunks + t0 / kTile, D, k), a.quads);
   };
   const int64_t tiles = end > a.first ? (end - a.first + kTile - 1) / kTile : 0;
   if (tiles > 0) load(a.first + (tiles - 1) * kTile);
@@ -111,7 +118,8 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
     dt = dt_next;
     if (GATE) z = z_next;
     dy = dy_next;
-    const Quad start = start_next;
+#pragma unroll
+    for (int k = 0; k < K; ++k) start[k] = start_next[k];
     const bool in = t0 + a.s < end;
 #pragma unroll
     for (int j = 0; j < S::V; j += U) {
@@ -144,11 +152,14 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
         for (int t = kTile - 1; t >= 0; --t) {
           if (check.value && t >= count) continue;
           const Quad c = quad(bc[t * LS + a.g]);
-          const float step = steps[t][a.pos].x, gy = gys[t][a.pos];
-          g.a = decay(step, A2.a) * fma<2>(c.a, splat<2>(gy), g.a);
-          g.b = decay(step, A2.b) * fma<2>(c.b, splat<2>(gy), g.b);
-          if (check.value && (resets >> t & 1)) g = zeros();
-          total += step;
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            const float step = steps[t][a.pos + k * S::lanes].x, gy = gys[t][a.pos + k * S::lanes];
+            g[k].a = decay(step, A2[k].a) * fma<2>(c.a, splat<2>(gy), g[k].a);
+            g[k].b = decay(step, A2[k].b) * fma<2>(c.b, splat<2>(gy), g[k].b);
+            if (check.value && (resets >> t & 1)) g[k] = zeros();
+            total[k] += step;
+          }
         }
       };
       if (count == kTile && resets == 0)
@@ -157,80 +168,104 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
         tile(std::true_type());
       __syncthreads();
     } else {
+      // a step forward
+      auto forward = [&](int t, Quad (&now)[K], auto check) {
+        const Quad b = quad(bc[t * LS + a.g]);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+          if (check.value && (resets >> t & 1)) now[k] = zeros();
+          const float2 v = steps[t][a.pos + k * S::lanes];
+          now[k].a = fma<2>(decay(v.x, A2[k].a), now[k].a, splat<2>(v.y) * b.a);
+          now[k].b = fma<2>(decay(v.x, A2[k].b), now[k].b, splat<2>(v.y) * b.b);
+        }
+      };
       // half: steps from t1 on, whose states are computed again into h from the one before them
-      auto half = [&](int t1, const Quad& before, auto check) {
-        Quad h[kHalf];
-        Quad now = before;
+      auto half = [&](int t1, const Quad (&before)[K], auto check) {
+        Quad h[kHalf][K], now[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) now[k] = before[k];
 #pragma unroll
         for (int i = 0; i < kHalf; ++i) {
-          const int t = t1 + i;
-          if (!check.value || t < count) {
-            if (check.value && (resets >> t & 1)) now = zeros();
-            const Quad b = quad(bc[t * LS + a.g]);
-            const float2 v = steps[t][a.pos];
-            now.a = fma<2>(decay(v.x, A2.a), now.a, splat<2>(v.y) * b.a);
-            now.b = fma<2>(decay(v.x, A2.b), now.b, splat<2>(v.y) * b.b);
-          }
-          h[i] = now;
+          if (!check.value || t1 + i < count) forward(t1 + i, now, check);
+#pragma unroll
+          for (int k = 0; k < K; ++k) h[i][k] = now[k];
         }
         // (the decays are computed again: kept from the first loop they would take the registers of as many states)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          asm volatile("" : "+f"(A2.a.v[i]));
-          asm volatile("" : "+f"(A2.b.v[i]));
-        }
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            asm volatile("" : "+f"(A2[k].a.v[i]));
+            asm volatile("" : "+f"(A2[k].b.v[i]));
+          }
         constexpr int kSet = LS < kHalf ? LS : kHalf;   // steps whose sums over the states' lanes are taken together
-        float sq[kSet], sb[kSet], sy[kSet];
+        float sq[K][kSet], sb[K][kSet], sy[K][kSet];
 #pragma unroll
         for (int i = kHalf - 1; i >= 0; --i) {
           const int t = t1 + i;
-          sq[i % kSet] = sb[i % kSet] = sy[i % kSet] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < K; ++k) sq[k][i % kSet] = sb[k][i % kSet] = sy[k][i % kSet] = 0.0f;
           if (!check.value || t < count) {
             const Quad b = quad(bc[t * LS + a.g]), c = quad(bc[(kTile + t) * LS + a.g]);
-            const float2 v = steps[t][a.pos];
-            const float gy = gys[t][a.pos];
-            if (GATE) {
-              const Vec<2> m = fma<2>(c.b, h[i].b, c.a * h[i].a);
-              sy[i % kSet] = m.v[0] + m.v[1];
-            }
-            g.a = fma<2>(c.a, splat<2>(gy), g.a);
-            g.b = fma<2>(c.b, splat<2>(gy), g.b);
-            const Vec<2> db0 = scaled(g.a, v.y), db1 = scaled(g.b, v.y), dc0 = scaled(h[i].a, gy), dc1 = scaled(h[i].b, gy);
-            *reinterpret_cast<float4*>(given + to_db + i * kGivenStep) = make_float4(db0.v[0], db0.v[1], db1.v[0], db1.v[1]);
-            *reinterpret_cast<float4*>(given + to_dc + i * kGivenStep) = make_float4(dc0.v[0], dc0.v[1], dc1.v[0], dc1.v[1]);
-            const Vec<2> mb = fma<2>(g.b, b.b, g.a * b.a);
-            sb[i % kSet] = mb.v[0] + mb.v[1];
-            Quad prev = i > 0 ? h[i > 0 ? i - 1 : 0] : before;
             const bool drop = check.value && (resets >> t & 1);
-            if (drop) prev = zeros();
-            g.a = g.a * decay(v.x, A2.a);
-            g.b = g.b * decay(v.x, A2.b);
-            const Vec<2> q0 = g.a * prev.a, q1 = g.b * prev.b;
-            const Vec<2> mq = fma<2>(q1, A2.b, q0 * A2.a);
-            sq[i % kSet] = drop ? 0.0f : mq.v[0] + mq.v[1];
-            if (drop) {
-              g = zeros();
-            } else {
-              dA.a = fma<2>(q0, splat<2>(v.x), dA.a);
-              dA.b = fma<2>(q1, splat<2>(v.x), dA.b);
+            Quad db = zeros(), dc = zeros();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+              const float2 v = steps[t][a.pos + k * S::lanes];
+              const float gy = gys[t][a.pos + k * S::lanes];
+              const Quad now_h = h[i][k];
+              if (GATE) {
+                const Vec<2> m = fma<2>(c.b, now_h.b, c.a * now_h.a);
+                sy[k][i % kSet] = m.v[0] + m.v[1];
+              }
+              g[k].a = fma<2>(c.a, splat<2>(gy), g[k].a);
+              g[k].b = fma<2>(c.b, splat<2>(gy), g[k].b);
+              if (k == 0) {
+                db = {scaled(g[k].a, v.y), scaled(g[k].b, v.y)};
+                dc = {scaled(now_h.a, gy), scaled(now_h.b, gy)};
+              } else {
+                db = {fma<2>(g[k].a, splat<2>(v.y), db.a), fma<2>(g[k].b, splat<2>(v.y), db.b)};
+                dc = {fma<2>(now_h.a, splat<2>(gy), dc.a), fma<2>(now_h.b, splat<2>(gy), dc.b)};
+              }
+              const Vec<2> mb = fma<2>(g[k].b, b.b, g[k].a * b.a);
+              sb[k][i % kSet] = mb.v[0] + mb.v[1];
+              Quad prev = before[k];
+              if (i > 0) prev = h[i > 0 ? i - 1 : 0][k];
+              if (drop) prev = zeros();
+              g[k].a = g[k].a * decay(v.x, A2[k].a);
+              g[k].b = g[k].b * decay(v.x, A2[k].b);
+              const Vec<2> q0 = g[k].a * prev.a, q1 = g[k].b * prev.b;
+              const Vec<2> mq = fma<2>(q1, A2[k].b, q0 * A2[k].a);
+              sq[k][i % kSet] = drop ? 0.0f : mq.v[0] + mq.v[1];
+              if (drop) {
+                g[k] = zeros();
+              } else {
+                dA[k].a = fma<2>(q0, splat<2>(v.x), dA[k].a);
+                dA[k].b = fma<2>(q1, splat<2>(v.x), dA[k].b);
+              }
             }
+            *reinterpret_cast<float4*>(given + to_db + i * kGivenStep) = make_float4(db.a.v[0], db.a.v[1], db.b.v[0], db.b.v[1]);
+            *reinterpret_cast<float4*>(given + to_dc + i * kGivenStep) = make_float4(dc.a.v[0], dc.a.v[1], dc.b.v[0], dc.b.v[1]);
           }
           if (i % kSet == 0) {
             // (with more lanes than steps of a half, the lanes that end up with the same step write the same)
-            scatter_sums<kSet, 16, S::lanes>(sq);
-            scatter_sums<kSet, 16, S::lanes>(sb);
-            if (GATE) scatter_sums<kSet, 16, S::lanes>(sy);
             const int s = t + a.g * kSet / LS;
-            sums[0][s][a.pos] = sq[0];
-            sums[1][s][a.pos] = sb[0];
-            if (GATE) sums[kSums - 1][s][a.pos] = sy[0];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+              scatter_sums<kSet, 16, S::lanes>(sq[k]);
+              scatter_sums<kSet, 16, S::lanes>(sb[k]);
+              if (GATE) scatter_sums<kSet, 16, S::lanes>(sy[k]);
+              sums[0][s][a.pos + k * S::lanes] = sq[k][0];
+              sums[1][s][a.pos + k * S::lanes] = sb[k][0];
+              if (GATE) sums[kSums - 1][s][a.pos + k * S::lanes] = sy[k][0];
+            }
           }
         }
       };
       // the half's db and dc of all the block's channels: a thread for a quad of states of a step, or kShare of them
       // with a share of the channels each, which begin a rotation apart
       auto collect = [&](int t1) {
-        constexpr int kQuads = Given<S>::kQuads, kShare = LS < 8 ? 8 / LS : 1, kEach = S::CH / kShare;
+        constexpr int kQuads = Given<S>::kQuads, kShare = LS < 8 ? 8 / LS : 1, kEach = Given<S>::kRows / kShare;
 #pragma unroll
         for (int i = 0; i < kHalf * kQuads * kShare / kSsmThreads; ++i) {
           const int o = (i * kSsmThreads + threadIdx.x) / kShare, share = threadIdx.x % kShare, t = o / kQuads, q = o % kQuads;
@@ -264,15 +299,11 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
       };
       auto tile = [&](auto check) {
         if (!check.value || count > kHalf) {
-          Quad middle = start;
+          Quad middle[K];
 #pragma unroll
-          for (int t = 0; t < kHalf; ++t) {
-            if (check.value && (resets >> t & 1)) middle = zeros();
-            const Quad b = quad(bc[t * LS + a.g]);
-            const float2 v = steps[t][a.pos];
-            middle.a = fma<2>(decay(v.x, A2.a), middle.a, splat<2>(v.y) * b.a);
-            middle.b = fma<2>(decay(v.x, A2.b), middle.b, splat<2>(v.y) * b.b);
-          }
+          for (int k = 0; k < K; ++k) middle[k] = start[k];
+#pragma unroll
+          for (int t = 0; t < kHalf; ++t) forward(t, middle, check);
           half(kHalf, middle, check);
           __syncthreads();
           collect(kHalf);
@@ -331,18 +362,22 @@ __global__ void __launch_bounds__(kSsmThreads, LS == 16 ? 5 : 4) ssm_backward_ke
     }
   }
   if constexpr (STATES) {
-    if (has) {
-      store_quad<WIDE>(p.states + a.state(row, D, 0), a.quads, g);
-      if (a.g == 0) p.sums[row * D + a.d0 + a.channel(0)] = dropped ? INFINITY : total;
-    }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (a.has(k)) {
+        store_quad<WIDE>(p.states + a.state(row, D, k), a.quads, g[k]);
+        if (a.g == 0) p.sums[row * D + a.d0 + a.channel(k)] = dropped ? INFINITY : total[k];
+      }
     return;
   } else {
-    if (has && a.split == 0 && p.h_last) store_quad<WIDE>(p.h_last + a.state(a.b, D, 0), a.quads, g);
-    if (has && p.params) {
-      const float v[kQuad] = {dA.a.v[0], dA.a.v[1], dA.b.v[0], dA.b.v[1]};
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!a.has(k)) continue;
+      if (a.split == 0 && p.h_last) store_quad<WIDE>(p.h_last + a.state(a.b, D, k), a.quads, g[k]);
+      const float v[kQuad] = {dA[k].a.v[0], dA[k].a.v[1], dA[k].b.v[0], dA[k].b.v[1]};
 #pragma unroll
       for (int i = 0; i < kQuad; ++i)
-        if (i < a.quads) p.param_part[(row * (N + 2) + a.g * kQuad + i) * D + a.d0 + a.channel(0)] = v[i];
+        if (p.params && i < a.quads) p.param_part[(row * (N + 2) + a.g * kQuad + i) * D + a.d0 + a.channel(k)] = v[i];
     }
     if (p.params) {
 #pragma unroll
@@ -418,8 +453,8 @@ static __global__ void __launch_bounds__(128) ssm_join_params_kernel(const SsmAr
 
 template <typename E, int LS, bool WIDE>
 cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
-  using S = Shape<LS, kBackwardK>;
-  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH, true);
+  using S = Shape<LS, kBackwardK<LS>>;
+  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH, true, kBackwardResident<LS>);
   p.blocks = int(cut.blocks);
   p.splits = int(cut.splits);
   p.steps = cut.steps;
@@ -438,14 +473,14 @@ cudaError_t launch_backward_as(SsmArgs p, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   if (grid.x > 0) {
     constexpr size_t kShared = size_t(Given<S>::kFloats) * 4;
-    e = gate ? allow_shared<ssm_backward_kernel<E, LS, WIDE, true, false>, false, kShared>(kShared)
-             : allow_shared<ssm_backward_kernel<E, LS, WIDE, false, false>, false, kShared>(kShared);
+    e = gate ? allow_shared<ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, true, false>, false, kShared>(kShared)
+             : allow_shared<ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, false, false>, false, kShared>(kShared);
     if (e == cudaSuccess && cut.splits > 1)
-      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, true>, grid, block, 0, stream, p)
-               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, true>, grid, block, 0, stream, p);
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, true, true>, grid, block, 0, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, false, true>, grid, block, 0, stream, p);
     if (e == cudaSuccess)
-      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, WIDE, true, false>, grid, block, kShared, stream, p)
-               : launch_pdl(ssm_backward_kernel<E, LS, WIDE, false, false>, grid, block, kShared, stream, p);
+      e = gate ? launch_pdl(ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, true, false>, grid, block, kShared, stream, p)
+               : launch_pdl(ssm_backward_kernel<E, LS, kBackwardK<LS>, WIDE, false, false>, grid, block, kShared, stream, p);
   }
   if (e == cudaSuccess && cut.blocks > 1) {
     const int64_t count = p.in.B * p.in.T * p.in.G * 2 * S::NP;

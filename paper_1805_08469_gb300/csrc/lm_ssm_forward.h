@@ -254,7 +254,7 @@ cudaError_t launch_forward_as(SsmArgs p, cudaStream_t stream) {
     return launch_pdl(ssm_step_kernel<E, LS, WIDE>, dim3(unsigned((p.in.B * p.in.D * LS + kSsmThreads - 1) / kSsmThreads)), dim3(kSsmThreads), 0,
                       stream, p);
   using S = Shape<LS, kForwardK>;
-  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH, false);
+  const SsmCut cut = ssm_cut(p.in.B, p.in.T, p.in.D, p.in.G, S::CH, false, 4);
   p.blocks = int(cut.blocks);
   p.splits = int(cut.splits);
   p.steps = cut.steps;
