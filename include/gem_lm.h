@@ -208,7 +208,7 @@ int gem_policy(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
 
 /* Embedding: out[n] = scale table[tokens[n]] for N tokens (int32), rows of D elements: row v of the
  * table at table + v * table_ld (type table_dtype), row n of out at out + n * out_ld (type dtype; rounded
- * once).  A token < 0 has no row: zeros; one >= V gives NaN. */
+ * once).  A token < 0 has no row: zeros; one >= V gives NaN.  Requires N <= 2^27, 1 <= V <= 2^30, D <= 2^23. */
 int gem_embed(int table_dtype, int dtype, int64_t N, int64_t V, int64_t D, const void* table,
               int64_t table_ld, const int32_t* tokens, float scale, void* out, int64_t out_ld,
               void* stream);
@@ -224,7 +224,8 @@ int64_t gem_embed_workspace(int64_t N, int64_t V, int64_t D);
  *   accumulate = 1: the sum is added to what dtable holds (a table that is also the output layer);
  *     rows without a token are not touched.
  *   workspace: gem_embed_workspace bytes, 16-byte aligned, in use until the call's work is done.
- * Sums are fp32, in the order of n and of pieces of it that the tokens alone fix. */
+ * Sums are fp32, in the order of n and of pieces of it that the tokens alone fix.  What is added to an fp32 dtable
+ * counts as 0 below 2^-126. */
 int gem_embed_grad(int dtype, int grad_dtype, int64_t N, int64_t V, int64_t D, const void* dout,
                    int64_t dout_ld, const int32_t* tokens, float scale, int accumulate,
                    void* dtable, int64_t dtable_ld, void* workspace, void* stream);
@@ -235,7 +236,7 @@ enum gem_conv_form { GEM_CONV_LINEAR = 0, GEM_CONV_SILU = 1 };
  *
  *   p_t = bias + sum_{k < W} weight_k x_{t - W + 1 + k},   y_t = p_t (GEM_CONV_LINEAR) or p_t sigmoid(p_t)
  *
- * over x (B sequences of T steps and D channels, of type dtype) into y; 2 <= W <= 4.
+ * over x (B sequences of T steps and D channels, of type dtype) into y; 2 <= W <= 4, D <= 2^30.
  *   weight [D][W], bias [D] fp32 (NULL: zeros).
  *   state [B][W - 1][D] fp32, NULL: zeros: the W - 1 inputs before the first step, oldest first.
  *   lengths [B] int32, NULL: all T.  Sequence b has lengths[b] steps (clipped to 0..T): past
@@ -272,7 +273,7 @@ int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int 
  * from h_{-1} = h0.  b and c are shared by the D / G channels of each of G groups. */
 typedef struct {
   int64_t B, T, D;
-  int32_t N, G;              /* 1 <= N <= GEM_SSM_STATES; G divides D */
+  int32_t N, G;              /* 1 <= N <= GEM_SSM_STATES; G divides D; D, G N <= 2^30 */
   int32_t softplus;
   gem_seq_t x, dt;           /* [B][T][D] */
   gem_seq_t b, c;            /* [B][T][G][N], the last two dimensions side by side */

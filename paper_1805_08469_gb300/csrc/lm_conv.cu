@@ -505,7 +505,7 @@ ConvCut conv_cut(int64_t T) {
 }
 
 bool conv_sizes_ok(int64_t B, int64_t T, int64_t D, int W) {
-  if (W < 2 || W > 4 || !extent_ok(B) || !extent_ok(T) || !extent_ok(D)) return false;
+  if (W < 2 || W > 4 || !extent_ok(B) || !extent_ok(T) || !channels_ok(D)) return false;
   const int64_t columns = (D + 31) / 32, blocks = conv_cut(T).blocks;
   return B == 0 || D == 0 || columns <= (kMaxExtent - 1) / blocks / B;   // a block at least for 32 channels and the steps of its warps
 }

@@ -105,6 +105,9 @@ constexpr int64_t kMaxStride = int64_t(1) << 46;
 
 inline bool extent_ok(int64_t n) { return n >= 0 && n < kMaxExtent; }
 
+// Channels of which 32-bit indices hold those of a whole block past the last.
+inline bool channels_ok(int64_t D) { return D >= 0 && D <= int64_t(1) << 30; }
+
 // An input: any strides (0: one step or sequence for all).
 inline bool input_ok(const gem_seq_t* s, int dtype, int64_t B, int64_t T, int64_t D) {
   if (!s) return false;

@@ -35,7 +35,8 @@ SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH, bool backward, in
 namespace {
 
 bool ssm_sizes_ok(int64_t B, int64_t T, int64_t D, int N, int G) {
-  if (!extent_ok(B) || !extent_ok(T) || !extent_ok(D) || N < 1 || N > GEM_SSM_STATES || G < 1 || D % G != 0) return false;
+  if (!extent_ok(B) || !extent_ok(T) || !channels_ok(D) || N < 1 || N > GEM_SSM_STATES || G < 1 || D % G != 0) return false;
+  if (!channels_ok(int64_t(G) * N)) return false;
   if (G > D && D > 0) return false;
   if (B == 0 || D == 0) return true;
   // grids: a block at least for 8 channels of a group (and few more where time is split), a thread for each

@@ -88,12 +88,29 @@ __device__ __forceinline__ Vec<V> softplus(const Vec<V>& v) {
   return fma<V>(s + s, r, most);
 }
 
-// A decay's exponent step A log2(e), and a little more: the GPU's approximate exp2 gives on average 0.1 (next to 1) to
-// 0.45 of 2^-24 too little, which a state of small decay would add up over its whole memory.  With 2^-27 more the mean at
-// exponents above -0.002 is within 0.04 of 2^-24, and a step of 0 still decays by exactly 1.
-constexpr float kNudge = 1.0749e-8f;
-__device__ __forceinline__ Vec<2> decay(float step, const Vec<2>& A2) {
-  const Vec<2> x = fma<2>(splat<2>(step), A2, splat<2>(kNudge));
+// Four states.
+struct Quad {
+  Vec<2> a, b;
+};
+__device__ __forceinline__ Quad zeros() { return {splat<2>(0.0f), splat<2>(0.0f)}; }
+__device__ __forceinline__ Quad quad(const float4& v) { return {{v.x, v.y}, {v.z, v.w}}; }
+
+// A decay is exp2 of step A log2(e) and a little more, the nudge.  The GPU's approximate exp2 gives too little on average, which
+// a state of slow decay adds up over its memory of 1 / |step A| steps.  Measured on the GB300, in 2^-24 of the result: 0.11
+// at exponents of size below 0.002, 0.28 to 0.004, 0.44 to 0.016, 0.3 falling to 0.14 at 0.5; so much more in the exponent
+// leaves a mean of some 0.05.  The size is taken at the first step of a tile.  (One nudge of 0.125 for all left three times the
+// error of an exact exponential in dA at exponents of 0.005.)  A step of 0 still decays by exactly 1: what is added there is below
+// half a unit.
+__device__ __forceinline__ float nudge(float x) {
+  constexpr float kUnit = 5.9604645e-8f * kLog2e;
+  const float size = fabsf(x);
+  return size < 0.002f * kLog2e ? 0.11f * kUnit : size < 0.004f * kLog2e || size > 0.016f * kLog2e ? 0.28f * kUnit : 0.44f * kUnit;
+}
+__device__ __forceinline__ Quad nudges(float step, const Quad& A2) {
+  return {{nudge(step * A2.a.v[0]), nudge(step * A2.a.v[1])}, {nudge(step * A2.b.v[0]), nudge(step * A2.b.v[1])}};
+}
+__device__ __forceinline__ Vec<2> decay(float step, const Vec<2>& A2, const Vec<2>& more) {
+  const Vec<2> x = fma<2>(splat<2>(step), A2, more);
   return {ex2(x.v[0]), ex2(x.v[1])};
 }
 // That over a split: above 0, so that an infinite state does not become NaN by leaving fp32.
@@ -177,11 +194,6 @@ __device__ __forceinline__ void store_piece(E* p, int there, const float (&v)[V]
 }
 
 // Four states from p on, of which `there` exist (WIDE: all or none).
-struct Quad {
-  Vec<2> a, b;
-};
-__device__ __forceinline__ Quad zeros() { return {splat<2>(0.0f), splat<2>(0.0f)}; }
-__device__ __forceinline__ Quad quad(const float4& v) { return {{v.x, v.y}, {v.z, v.w}}; }
 template <bool WIDE>
 __device__ __forceinline__ Quad load_quad(const float* p, int there) {
   float4 v = make_float4(0, 0, 0, 0);

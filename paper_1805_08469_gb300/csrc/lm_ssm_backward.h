@@ -145,6 +145,9 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
     if (t0 > a.first) load(t0 - kTile);
     const int count = int(min(end - t0, int64_t(kTile)));
     dropped |= resets != 0;
+    Quad more[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) more[k] = nudges(steps[0][a.pos + k * S::lanes].x, A2[k]);
 
     if constexpr (STATES) {
       auto tile = [&](auto check) {
@@ -155,8 +158,8 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
 #pragma unroll
           for (int k = 0; k < K; ++k) {
             const float step = steps[t][a.pos + k * S::lanes].x, gy = gys[t][a.pos + k * S::lanes];
-            g[k].a = decay(step, A2[k].a) * fma<2>(c.a, splat<2>(gy), g[k].a);
-            g[k].b = decay(step, A2[k].b) * fma<2>(c.b, splat<2>(gy), g[k].b);
+            g[k].a = decay(step, A2[k].a, more[k].a) * fma<2>(c.a, splat<2>(gy), g[k].a);
+            g[k].b = decay(step, A2[k].b, more[k].b) * fma<2>(c.b, splat<2>(gy), g[k].b);
             if (check.value && (resets >> t & 1)) g[k] = zeros();
             total[k] += step;
           }
@@ -175,8 +178,8 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
         for (int k = 0; k < K; ++k) {
           if (check.value && (resets >> t & 1)) now[k] = zeros();
           const float2 v = steps[t][a.pos + k * S::lanes];
-          now[k].a = fma<2>(decay(v.x, A2[k].a), now[k].a, splat<2>(v.y) * b.a);
-          now[k].b = fma<2>(decay(v.x, A2[k].b), now[k].b, splat<2>(v.y) * b.b);
+          now[k].a = fma<2>(decay(v.x, A2[k].a, more[k].a), now[k].a, splat<2>(v.y) * b.a);
+          now[k].b = fma<2>(decay(v.x, A2[k].b, more[k].b), now[k].b, splat<2>(v.y) * b.b);
         }
       };
       // half: steps from t1 on, whose states are computed again into h from the one before them
@@ -232,8 +235,8 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
               Quad prev = before[k];
               if (i > 0) prev = h[i > 0 ? i - 1 : 0][k];
               if (drop) prev = zeros();
-              g[k].a = g[k].a * decay(v.x, A2[k].a);
-              g[k].b = g[k].b * decay(v.x, A2[k].b);
+              g[k].a = g[k].a * decay(v.x, A2[k].a, more[k].a);
+              g[k].b = g[k].b * decay(v.x, A2[k].b, more[k].b);
               const Vec<2> q0 = g[k].a * prev.a, q1 = g[k].b * prev.b;
               const Vec<2> mq = fma<2>(q1, A2[k].b, q0 * A2[k].a);
               sq[k][i % kSet] = drop ? 0.0f : mq.v[0] + mq.v[1];

@@ -108,6 +108,9 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmAr
         if (a.has(k)) store_quad<WIDE>(p.saved + a.state(a.b * ((p.in.T + kTile - 1) / kTile) + t0 / kTile, D, k), a.quads, h[k]);
     }
     float y[K][kTile];
+    Quad more[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) more[k] = nudges(steps[0][a.pos + k * S::lanes].x, A2[k]);
     auto tile = [&](auto check) {
       const int count = int(min(end - t0, int64_t(kTile)));
       // steps in sets: what a set reads and its decays come first, so that their latencies overlap
@@ -127,7 +130,7 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmAr
         for (int k = 0; k < K; ++k) {
           Quad dec[kSet];
 #pragma unroll
-          for (int i = 0; i < kSet; ++i) dec[i] = {decay(v[i][k].x, A2[k].a), decay(v[i][k].x, A2[k].b)};
+          for (int i = 0; i < kSet; ++i) dec[i] = {decay(v[i][k].x, A2[k].a, more[k].a), decay(v[i][k].x, A2[k].b, more[k].b)};
 #pragma unroll
           for (int i = 0; i < kSet; ++i) {
             const int t = t1 + i;
@@ -234,8 +237,9 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs p) 
     if (p.in.reset && p.in.reset[b]) h = zeros();
     A2 = {A2.a * splat<2>(kLog2e), A2.b * splat<2>(kLog2e)};
     const Vec<2> in = splat<2>(step * x);
-    h.a = fma<2>(decay(step, A2.a), h.a, in * bs.template at<2>(0));
-    h.b = fma<2>(decay(step, A2.b), h.b, in * bs.template at<2>(2));
+    const Quad more = nudges(step, A2);
+    h.a = fma<2>(decay(step, A2.a, more.a), h.a, in * bs.template at<2>(0));
+    h.b = fma<2>(decay(step, A2.b, more.b), h.b, in * bs.template at<2>(2));
     const Vec<2> m = fma<2>(cs.template at<2>(2), h.b, cs.template at<2>(0) * h.a);
     y = m.v[0] + m.v[1];
   }

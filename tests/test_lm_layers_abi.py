@@ -79,7 +79,7 @@ SIZES = [dict(dtype=3), dict(dtype=-1), dict(B=-1), dict(T=-1), dict(D=-1), dict
 
 
 @pytest.mark.parametrize("bad", SIZES + [
-    dict(form=2), dict(form=-1), dict(W=1), dict(W=5), dict(W=0), dict(B=1 << 20, T=1 << 20), dict(weight=0), dict(weight=PTR + 2), dict(bias=PTR + 1),
+    dict(form=2), dict(form=-1), dict(W=1), dict(W=5), dict(W=0), dict(B=1 << 20, T=1 << 20), dict(B=1, T=1, D=(1 << 30) + 1), dict(weight=0), dict(weight=PTR + 2), dict(bias=PTR + 1),
     dict(state=PTR + 2), dict(last=PTR + 2), dict(y=seq(0)), dict(y=seq(st=9)), dict(y=seq(sb=39)), dict(y=seq(st=0))])
 def test_conv_refuses(L, bad):
     assert conv(L, **bad) == EINVAL
@@ -106,7 +106,7 @@ def ssm_back(L, dtype=0, saved=PTR, dy=None, dlast=0, dx=None, ddt=None, db=None
     return L.gem_ssm_backward(dtype, C.byref(ssm_in(**kw)), saved, C.byref(dy or seq()), dlast, C.byref(out), space, 0)
 
 
-SSM = SIZES + [dict(N=0), dict(N=65), dict(G=0), dict(G=3), dict(G=-1), dict(dt=seq(0)), dict(b=seq(0)), dict(c=seq(PTR + 2)), dict(b=seq(st=-1)),
+SSM = SIZES + [dict(N=0), dict(N=65), dict(B=1, T=1, D=(1 << 30) + 4), dict(B=1, T=1, D=1 << 26, G=1 << 25, N=64), dict(G=0), dict(G=3), dict(G=-1), dict(dt=seq(0)), dict(b=seq(0)), dict(c=seq(PTR + 2)), dict(b=seq(st=-1)),
                dict(z=seq(PTR + 1)), dict(A=0), dict(A=PTR + 2), dict(skip=PTR + 1), dict(bias=PTR + 2)]
 
 
