@@ -43,9 +43,9 @@ __device__ __forceinline__ Vec<V> sigmoid(const Vec<V>& v) {
   return e;
 }
 
-// A thread's K channels: four as two pairs, or one.
+// A thread's K channels: four or two as pairs, or one.
 template <int K>
-constexpr int kVec = K == 4 ? 2 : 1;
+constexpr int kVec = K > 1 ? 2 : 1;
 template <int K>
 struct Channels {
   static constexpr int V = kVec<K>, P = K / V;
@@ -59,7 +59,7 @@ __device__ __forceinline__ Channels<K> none() {
   return r;
 }
 
-// K neighbouring elements as they are in memory (K = 1: any alignment, K = 4: aligned to all four).
+// K neighbouring elements as they are in memory, aligned to all K.
 template <typename E, int K>
 struct Raw;
 template <typename E>
@@ -92,10 +92,29 @@ struct Raw<E, 4> {
   __device__ __forceinline__ void clear() { x = make_uint2(0, 0); }
   __device__ __forceinline__ Channels<4> floats() const { return {{two<E>(x.x), two<E>(x.y)}}; }
 };
+template <>
+struct Raw<float, 2> {
+  float2 x;
+  __device__ __forceinline__ void read(const float* p) { x = *reinterpret_cast<const float2*>(p); }
+  __device__ __forceinline__ void clear() { x = make_float2(0, 0); }
+  __device__ __forceinline__ Channels<2> floats() const { return {{{x.x, x.y}}}; }
+};
+template <typename E>
+struct Raw<E, 2> {
+  uint32_t x;
+  __device__ __forceinline__ void read(const E* p) { x = *reinterpret_cast<const uint32_t*>(p); }
+  __device__ __forceinline__ void clear() { x = 0; }
+  __device__ __forceinline__ Channels<2> floats() const { return {{two<E>(x)}}; }
+};
 template <typename E, int K>
 __device__ __forceinline__ void write_step(E* at, const Channels<K>& v) {
   if constexpr (K == 1) {
     *at = from_f32<E>(v.c[0].v[0]);
+  } else if constexpr (K == 2 && sizeof(E) == 4) {
+    *reinterpret_cast<float2*>(at) = make_float2(v.c[0].v[0], v.c[0].v[1]);
+  } else if constexpr (K == 2) {
+    alignas(4) E e[2] = {from_f32<E>(v.c[0].v[0]), from_f32<E>(v.c[0].v[1])};
+    *reinterpret_cast<uint32_t*>(at) = *reinterpret_cast<const uint32_t*>(e);
   } else if constexpr (sizeof(E) == 4) {
     *reinterpret_cast<float4*>(at) = make_float4(v.c[0].v[0], v.c[0].v[1], v.c[1].v[0], v.c[1].v[1]);
   } else {
@@ -201,7 +220,7 @@ struct Window {
   }
 };
 
-// Feeds a thread the elements of N sequences, a group of steps at a time, loaded ahead.  Four channels: by
+// Feeds a thread the elements of N sequences, a group of steps at a time, loaded ahead.  Four or two channels: by
 // asynchronous copies into places of the thread's own in shared memory (its registers are taken by sums and taps); one:
 // into registers.  What lies past the last step, or a thread without channels gets, is not defined.
 template <typename E, int N>
@@ -510,13 +529,13 @@ bool conv_sizes_ok(int64_t B, int64_t T, int64_t D, int W) {
   return B == 0 || D == 0 || columns <= (kMaxExtent - 1) / blocks / B;   // a block at least for 32 channels and the steps of its warps
 }
 
-// Whether pieces of four channels of every step lie at multiples of their size.
-bool in_fours(const gem_seq_t& s, int dtype, int64_t B, int64_t T, int64_t D) {
-  return D % 4 == 0 && aligned_to(s.data, 4 * dtype_size(dtype)) && (B <= 1 || s.stride_b % 4 == 0) && (T <= 1 || s.stride_t % 4 == 0);
+// Whether pieces of K channels of every step lie at multiples of their size.
+bool in_pieces(const gem_seq_t& s, int dtype, int64_t B, int64_t T, int64_t D, int K) {
+  return D % K == 0 && aligned_to(s.data, size_t(K * dtype_size(dtype))) && (B <= 1 || s.stride_b % K == 0) && (T <= 1 || s.stride_t % K == 0);
 }
 
 template <typename E, int W, int K>
-cudaError_t launch_conv_as(ConvArgs p, int form, int64_t B, bool backward, cudaStream_t stream) {
+cudaError_t launch_forward_as(ConvArgs p, int form, int64_t B, cudaStream_t stream) {
   const ConvCut cut = conv_cut(p.T);
   const bool whole = p.T <= kSegment;   // a warp has the whole sequence
   float* const state_last = p.state_last;
@@ -524,26 +543,37 @@ cudaError_t launch_conv_as(ConvArgs p, int form, int64_t B, bool backward, cudaS
   p.columns = (p.D + 32 * K - 1) / (32 * K);
   p.blocks = int(cut.blocks);
   const dim3 grid(unsigned(B * p.blocks * p.columns)), block(unsigned(cut.warps * 32));
-  const bool silu = form == GEM_CONV_SILU;
-  if (backward)
-    return silu ? launch_pdl(conv_backward_kernel<E, W, K, true>, grid, block, 0, stream, p)
-                : launch_pdl(conv_backward_kernel<E, W, K, false>, grid, block, 0, stream, p);
-  const cudaError_t e = silu ? launch_pdl(conv_forward_kernel<E, W, K, true>, grid, block, 0, stream, p)
-                             : launch_pdl(conv_forward_kernel<E, W, K, false>, grid, block, 0, stream, p);
+  const cudaError_t e = form == GEM_CONV_SILU ? launch_pdl(conv_forward_kernel<E, W, K, true>, grid, block, 0, stream, p)
+                                              : launch_pdl(conv_forward_kernel<E, W, K, false>, grid, block, 0, stream, p);
   if (e != cudaSuccess || whole || !state_last) return e;
   p.state_last = state_last;
   return launch_pdl(conv_state_kernel<E, W>, dim3(unsigned((B * p.D + 127) / 128)), dim3(128), 0, stream, p, B * p.D);
 }
+template <typename E, int W, int K>
+cudaError_t launch_backward_as(ConvArgs p, int form, int64_t B, cudaStream_t stream) {
+  const ConvCut cut = conv_cut(p.T);
+  p.columns = (p.D + 32 * K - 1) / (32 * K);
+  p.blocks = int(cut.blocks);
+  const dim3 grid(unsigned(B * p.blocks * p.columns)), block(unsigned(cut.warps * 32));
+  return form == GEM_CONV_SILU ? launch_pdl(conv_backward_kernel<E, W, K, true>, grid, block, 0, stream, p)
+                               : launch_pdl(conv_backward_kernel<E, W, K, false>, grid, block, 0, stream, p);
+}
 
+// Channels of a thread: pieces: the most that the tensors' rows allow, 4, 2 or 1.  The backward pass takes no more than two: its sums, taps and
+// windows of four fill the registers.
+template <typename E, int W>
+cudaError_t launch_conv_of(const ConvArgs& p, int form, int64_t B, int pieces, bool backward, cudaStream_t stream) {
+  if (backward)
+    return pieces > 1 ? launch_backward_as<E, W, 2>(p, form, B, stream) : launch_backward_as<E, W, 1>(p, form, B, stream);
+  return pieces == 4   ? launch_forward_as<E, W, 4>(p, form, B, stream)
+         : pieces == 2 ? launch_forward_as<E, W, 2>(p, form, B, stream)
+                       : launch_forward_as<E, W, 1>(p, form, B, stream);
+}
 template <typename E>
-cudaError_t launch_conv(const ConvArgs& p, int form, int64_t B, int W, bool fours, bool backward, cudaStream_t stream) {
-  if (fours)
-    return W == 2   ? launch_conv_as<E, 2, 4>(p, form, B, backward, stream)
-           : W == 3 ? launch_conv_as<E, 3, 4>(p, form, B, backward, stream)
-                    : launch_conv_as<E, 4, 4>(p, form, B, backward, stream);
-  return W == 2   ? launch_conv_as<E, 2, 1>(p, form, B, backward, stream)
-         : W == 3 ? launch_conv_as<E, 3, 1>(p, form, B, backward, stream)
-                  : launch_conv_as<E, 4, 1>(p, form, B, backward, stream);
+cudaError_t launch_conv(const ConvArgs& p, int form, int64_t B, int W, int pieces, bool backward, cudaStream_t stream) {
+  return W == 2   ? launch_conv_of<E, 2>(p, form, B, pieces, backward, stream)
+         : W == 3 ? launch_conv_of<E, 3>(p, form, B, pieces, backward, stream)
+                  : launch_conv_of<E, 4>(p, form, B, pieces, backward, stream);
 }
 
 }  // namespace
@@ -575,8 +605,9 @@ int gem_conv_forward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W
   p.reset = reset;
   p.T = T;
   p.D = int(D);
-  const bool fours = in_fours(p.x, dtype, B, T, D) && in_fours(p.y, dtype, B, T, D);
-  return launch_status(BY_TYPE(launch_conv, p, form, B, W, fours, false, static_cast<cudaStream_t>(stream)));
+  int pieces = 4;
+  while (pieces > 1 && !(in_pieces(p.x, dtype, B, T, D, pieces) && in_pieces(p.y, dtype, B, T, D, pieces))) pieces /= 2;
+  return launch_status(BY_TYPE(launch_conv, p, form, B, W, pieces, false, static_cast<cudaStream_t>(stream)));
 }
 
 int64_t gem_conv_workspace(int64_t B, int64_t T, int64_t D, int W) {
@@ -615,8 +646,8 @@ int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int 
   const cudaStream_t on = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (B > 0) {
-    const bool fours = in_fours(p.x, dtype, B, T, D) && in_fours(p.dy, dtype, B, T, D) && in_fours(p.y, dtype, B, T, D);
-    e = BY_TYPE(launch_conv, p, form, B, W, fours, true, on);
+    const bool pairs = in_pieces(p.x, dtype, B, T, D, 2) && in_pieces(p.dy, dtype, B, T, D, 2) && in_pieces(p.y, dtype, B, T, D, 2);
+    e = BY_TYPE(launch_conv, p, form, B, W, pairs ? 2 : 1, true, on);
   }
   if (e == cudaSuccess && sums)
     e = launch_pdl(conv_join_kernel, dim3(unsigned((D + 31) / 32), unsigned(W + 1)), dim3(kJoinWarps * 32), 0, on,
