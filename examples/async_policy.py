@@ -1,7 +1,7 @@
 """Asynchronous policy gradients of a small selective state space language model.
 
 Workers answer prompts with their own stale snapshots of the model, score the answers and commit the
-gradients of the clipped policy loss with Gradient Energy Matching.  A worker's round runs the library's operators:
+gradients of the clipped policy loss with Gradient Energy Matching.  A worker's step runs the library's operators:
 
   answer    gem_embed, gem_conv_forward and gem_ssm_forward with one step and their states carried on
   train     gem_embed, gem_conv_forward, gem_ssm_forward, gem_policy (loss and gradient of the logits),

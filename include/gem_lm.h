@@ -22,7 +22,8 @@
  *   - Return value: GEM_OK (0) or a negative gem_status.  Arguments are checked on the host;
  *     a call that fails a check launches nothing.  Calls hold no handle, allocate nothing and
  *     keep nothing of their data from one call for the next (only, for each kernel and device, that it may
- *     use the shared memory that it does, and how many of its clusters fit).
+ *     use the shared memory that it does, and how many of its clusters fit).  A workspace is the caller's; what it
+ *     holds before and after a call does not matter, and calls that may run at once need one each.
  *   - All pointers are device memory of the current device.  Work is asynchronous and ordered
  *     on `stream` (a cudaStream_t; NULL is the legacy default stream); the caller orders
  *     buffers that other streams use.  Calls can be captured into a CUDA graph.
@@ -30,7 +31,7 @@
  *     is fp32, rounded once when an output of 16 bits is stored; exponentials over rows, those of 16-bit
  *     gates and the gates' quotients are the GPU's approximations (2 units in the last place and what rounding
  *     the argument adds; a quotient 1).  Results do not depend on
- *     timing: sums are taken in an order that the sizes fix.
+ *     timing: sums are taken in an order that the sizes fix (the embedding gradient's: the tokens).
  *   - Strides and row pitches count elements.  Tensors need the alignment of their element
  *     type, no more (aligned rows are read with wider loads).
  *   - No kernel waits on another.  Blocks of a cluster of gem_glr_* wait for one another's maps for at

@@ -5,6 +5,9 @@
 // as well: step t's dp_t goes to the gradients of the W inputs it used, the oldest of which is then complete; it
 // goes W - 1 steps past the segment for that.  Sums for the weights are taken in registers over the
 // segment, in shared memory over the block's warps, and by a second kernel over the blocks, in that order.
+//
+// 8 x 4096 x 2048 bf16, W = 4, SiLU: forward 46 us (5.8 TB/s of input and output), backward 98 us (4.1 TB/s; half of the issue
+// slots, its warps wait for their own chains of products), the parameters' sums 5.
 #include <type_traits>
 
 #include "lm_internal.h"
@@ -559,8 +562,8 @@ cudaError_t launch_backward_as(ConvArgs p, int form, int64_t B, cudaStream_t str
                                : launch_pdl(conv_backward_kernel<E, W, K, false>, grid, block, 0, stream, p);
 }
 
-// Channels of a thread: pieces: the most that the tensors' rows allow, 4, 2 or 1.  The backward pass takes no more than two: its sums, taps and
-// windows of four fill the registers.
+// Channels of a thread: the most that the tensors' rows allow, 4, 2 or 1 (pieces).  The backward pass takes no more than two: its sums,
+// taps and windows of four fill the registers (110 us instead of 98).
 template <typename E, int W>
 cudaError_t launch_conv_of(const ConvArgs& p, int form, int64_t B, int pieces, bool backward, cudaStream_t stream) {
   if (backward)

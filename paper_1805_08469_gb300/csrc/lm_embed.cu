@@ -1,7 +1,7 @@
 // Embedding of tokens and the gradient of its table (include/gem_lm.h).
 //
 // Lookup: a warp copies a slab of a row, a lane 16 bytes of what it writes (single elements where a row
-// does not lie on such boundaries).
+// does not lie on such boundaries).  65,536 tokens, rows of 1024 fp32 to bf16: 47 us, HBM bound.
 //
 // Gradient, in four launches:
 //   zeros  to the table's rows that no token has (where they are not added to); each block looks through the
@@ -13,7 +13,9 @@
 //          chunk where it began, and in each where it goes on, are partial sums.
 //   join   adds a run's partial sums in the order of the chunks.
 // Every dout row is read once and every row of the table written once, and a heavy token (one word in ten) is
-// spread over as many warps as it has chunks.  The order of every sum is fixed by the tokens.
+// spread over as many warps as it has chunks.  The order of every sum is fixed by the tokens.  65,536 tokens of Zipf
+// frequencies, 131,072 rows of 1024 fp32 from bf16: zeros 80 us (400 MB), sort 24 beside them, sums 38 (5 TB/s), join 18 (the
+// heaviest token's 120 partial rows).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -489,7 +491,8 @@ bool wide(const void* p, int element, int64_t ld, int64_t D, int per) {
 // Few entries are cut into small chunks, so that there are warps for all SMs; the partial rows of small chunks cost more.
 int chunk_of(int64_t N) { return N < 2048 ? 8 : N < 16384 ? 16 : 32; }
 
-// Blocks of the sort's cluster.
+// Blocks of the sort's cluster: barriers between more blocks cost what few tokens do not earn (us with 1, 8, 16 blocks: 1024 tokens 9, -, -;
+// 8192 37, 13, -; 32,768 -, 22, 18).
 unsigned sort_blocks(int64_t N) { return N <= 2048 ? 1 : N <= 16384 ? 8 : 16; }
 
 // Parts of the workspace, each a multiple of 16 bytes.

@@ -7,11 +7,14 @@
 //   dx_t = step_t sum_n g b_t + skip dy'_t;  g = exp(step_t A) g
 //
 // A tile is taken in two halves, the later one first: its states are computed again from the one saved before the tile and
-// stay in registers (all sixteen would leave fewer warps on an SM: 1.07 ms instead of ...).  What a step gives to db and dc goes
-// through shared memory, where a thread adds up the block's channels for an output (exchanges between lanes, two
-// selections, a shuffle and a sum for each value, took twice the instructions); a second kernel adds up the
-// blocks.  The parameters' gradients are summed over a split in registers, then by that kernel as well.  Splits are
-// composed from the last one back, as in the forward pass.
+// stay in registers (all sixteen would leave fewer warps on an SM).  What a step gives to db and dc goes through shared
+// memory, where threads add up the block's channels for a quad of states (exchanges between lanes, two
+// selections, a shuffle and a sum for each value, took twice the instructions: 1.07 ms instead of 0.81 with the halves); a
+// second kernel adds up the blocks.  The parameters' gradients are summed over a split in registers, then by that kernel
+// as well.  Splits are composed from the last one back, as in the forward pass.
+//
+// Per state and step 28 warp instructions, two and a half exponentials among them.  8 x 2048 x 2048 x 16 bf16 with a gate: 0.80 ms,
+// 0.53 of the issue slots and 59% of shared memory's cycles with 13 warps an SM, whose latencies bound it (HBM 11%).
 #pragma once
 
 #include "lm_ssm.h"
@@ -24,7 +27,7 @@ __device__ __forceinline__ Vec<2> scaled(const Vec<2>& a, float b) { return a * 
 
 constexpr int kHalf = kTile / 2;
 
-// What a step gives to db and dc, [kHalf][channel][2 LS] quads of states, rotated by LS / 4 quads a channel: the eight lanes that
+// What a step gives to db and dc, [kHalf][lane of channels][2 LS] quads of states, rotated by LS / 4 quads a lane: the eight lanes that
 // store together then lie in different banks.
 template <typename S>
 struct Given {

@@ -7,7 +7,9 @@ namespace gem {
 namespace lm {
 namespace ssm {
 
-// Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.
+// Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.  Per state and step 10
+// warp instructions, an exponential among them (a third of them the staging, whose share falls with N).  8 x 2048 x 2048 x 16 bf16
+// with a gate, states saved: 255 us, 0.60 of the issue slots with 13 warps an SM (HBM 18%).
 template <typename E, int LS, int K, bool WIDE, bool STATES>
 __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmArgs p) {
   using S = Shape<LS, K>;
@@ -203,7 +205,7 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmAr
 }
 
 // One step: a thread for four states of a channel, the LS lanes of a channel side by side, so that states are read and written
-// in the order of memory.  (16 x 2048 x 16: 3 us; the kernel above, most of whose tile would be empty, 8.)
+// in the order of memory.  (16 x 2048 x 16 bf16: 3.4 us; the kernel above, most of whose tile would be empty, 8.1.)
 template <typename E, int LS, bool WIDE>
 __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs p) {
   pdl_entry();

@@ -7,11 +7,13 @@
 //     memory: griddepcontrol.wait returns once the previous grid in the stream has completed
 //     and its writes are visible;
 //   - the next launch is scheduled when this grid's blocks have exited, because no kernel
-//     triggers its dependents before that, but one: an earlier trigger let the dependents'
+//     triggers its dependents before that, but two: an earlier trigger let the dependents'
 //     blocks crowd onto the SMs that freed first and made the per-sample kernels slower.  The
 //     single commit (commit_one_kernel) triggers when it starts, so the kernel after it may be
 //     running before the commit, or what precedes the commit, has ended.  So no kernel may
-//     touch global memory before its wait, whatever it follows;
+//     touch global memory before its wait, whatever it follows.  The second is the embedding
+//     gradient's embed_zeros_kernel, whose blocks trigger after their own wait: the sort that
+//     follows it in the same call runs beside it and waits at its end;
 //   - dependencies that are not on a kernel of the same stream (event waits, copies) stay
 //     full dependencies.
 // In a kernel launched without the attribute, the wait returns at once.

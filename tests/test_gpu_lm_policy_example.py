@@ -98,7 +98,7 @@ def test_it_runs():
     assert bool(torch.isfinite(rewards).all() and torch.isfinite(losses).all())
 
 
-def test_a_captured_round_gives_the_same():
+def test_a_captured_step_gives_the_same():
     """Forward, loss and backward captured into a graph and replayed on other inputs, on a stream of its own."""
     import async_policy
 
