@@ -113,8 +113,17 @@ __device__ __forceinline__ Vec<2> decay(float step, const Vec<2>& A2, const Vec<
   const Vec<2> x = fma<2>(splat<2>(step), A2, more);
   return {ex2(x.v[0]), ex2(x.v[1])};
 }
-// That over a split: above 0, so that an infinite state does not become NaN by leaving fp32.
-__device__ __forceinline__ float far_decay(float sum, float A2) { return fmaxf(ex2(sum * A2), 1.4e-45f); }
+// A state, or its gradient, after a split with this sum of steps: exp(sum A) state + last.  In two factors, which leave fp32 only
+// where the product does (growing states).  They are kept above 0, so that an infinite state does not become NaN; nor does
+// a state of 0 by growing.
+__device__ __forceinline__ Quad after_split(float sum, const Quad& A2, const Quad& state, const Quad& last) {
+  auto one = [sum](float a, float h, float more) {
+    const float f = fmaxf(ex2(0.5f * sum * a), 1.4e-45f);
+    return h == 0.0f ? more : fmaf(f, f * h, more);
+  };
+  return {{one(A2.a.v[0], state.a.v[0], last.a.v[0]), one(A2.a.v[1], state.a.v[1], last.a.v[1])},
+          {one(A2.b.v[0], state.b.v[0], last.b.v[0]), one(A2.b.v[1], state.b.v[1], last.b.v[1])}};
+}
 
 // V neighbouring elements as they are in memory: in words where WIDE (all of them exist or none), else one by one, of which
 // `there` exist.  (Loads that pack single elements would wait for each.)

@@ -75,12 +75,7 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
         const int64_t from = a.b * p.splits + q;
         const Quad first = load_quad<WIDE>(p.states + a.state(from, D, k), a.quads);
         const float sum = p.sums[from * D + a.d0 + a.channel(k)];
-        if (sum == INFINITY || q == p.splits - 1) {
-          g[k] = first;
-        } else {
-          g[k].a = fma<2>({far_decay(sum, A2[k].a.v[0]), far_decay(sum, A2[k].a.v[1])}, g[k].a, first.a);
-          g[k].b = fma<2>({far_decay(sum, A2[k].b.v[0]), far_decay(sum, A2[k].b.v[1])}, g[k].b, first.b);
-        }
+        g[k] = sum == INFINITY || q == p.splits - 1 ? first : after_split(sum, A2[k], g[k], first);
       }
     }
   }

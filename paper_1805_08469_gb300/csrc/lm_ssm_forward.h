@@ -55,12 +55,7 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmAr
         const int64_t from = a.b * p.splits + q;
         const Quad last = load_quad<WIDE>(p.states + a.state(from, D, k), a.quads);
         const float sum = p.sums[from * D + a.d0 + a.channel(k)];
-        if (sum == INFINITY || q == 0) {
-          h[k] = last;
-        } else {
-          h[k].a = fma<2>({far_decay(sum, A2[k].a.v[0]), far_decay(sum, A2[k].a.v[1])}, h[k].a, last.a);
-          h[k].b = fma<2>({far_decay(sum, A2[k].b.v[0]), far_decay(sum, A2[k].b.v[1])}, h[k].b, last.b);
-        }
+        h[k] = sum == INFINITY || q == 0 ? last : after_split(sum, A2[k], h[k], last);
       }
     }
   }

@@ -204,6 +204,40 @@ def test_an_infinite_state_stays_not_finite():
         assert not np.isfinite(got["h_last"]).any()
 
 
+def test_growing_states():
+    """Negative steps let states grow, over many splits by more than fp32 holds as one factor; a state of 0 stays 0."""
+    B, T, D, N = 1, 3000, 24, 2
+    c = Case(14, B, T, D, N, 1, "f32", softplus=False, bias=False)
+    c.dt.copy_(-0.02 * torch.rand((B, T, D), device="cuda") - 0.001)      # growth by e^30 and e^60
+    c.h0.mul_(1e-20)
+    got, want = c.run(backward=False), c.reference()
+    for k in got:
+        check(got[k], want[k], k)
+    c.dt.fill_(-1.0)
+    c.x.zero_()
+    c.h0.zero_()
+    got = c.run(backward=False)
+    assert (got["h_last"] == 0).all() and (got["y"] == 0).all()
+
+
+def test_offsets_past_32_bits():
+    """Steps, states and outputs that lie more than 2^31 elements apart."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    T, D, N, far = 3, 40, 16, 1 << 30
+    c = Case(15, 1, T, D, N, 1, "bf16")
+    want = c.run()
+    stretch = lambda t: torch.empty(far * (T - 1) + t.shape[2:].numel(), dtype=t.dtype, device="cuda").as_strided(  # noqa: E731
+        t.shape, (far * T, far) + t.stride()[2:])
+    for name in ("x", "b"):
+        t = stretch(getattr(c, name))
+        t.copy_(getattr(c, name))
+        setattr(c, name, t)
+    y = stretch(c.dy)
+    lm.gem_ssm_forward(c.x, c.dt, c.A, c.b, c.c, y, z=c.z, skip=c.skip, dt_bias=c.bias, h0=c.h0)
+    assert np.array_equal(host(y), want["y"])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_extreme_steps(dtype):
     """Steps from 0 to ones that forget everything; nothing but the formula's values."""
@@ -217,7 +251,7 @@ def test_extreme_steps(dtype):
     for k, (value, bound) in want.items():
         if dtype == "f16" and k in ("y", "dx", "ddt", "dz", "db", "dc"):
             # the largest fp16 is 65504, and what lies half a step (16) above it or further rounds to infinity
-            value = np.where(np.abs(value) >= 65520, np.sign(value) * np.inf, value)
+            value = np.where(np.abs(value) >= 65520, np.copysign(np.inf, value), value)
         check(got[k], (value, bound + 1e-30), k)
 
 
