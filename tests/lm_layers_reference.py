@@ -265,8 +265,8 @@ def policy(z, tokens, old, A, ref=None, scale=None, tau=1.0, low=0.2, high=0.2, 
     """{name: (value, bound)} of loss, logp, entropy and grad; rows without NaN and +inf, ratios apart from the bounds."""
     N, V = z.shape
     d, lp, p, err_lp, rel_p, _, _ = _softmax(z, tau)
-    logs = np.where(np.isfinite(d), d - lp, 0).max(1)
     with np.errstate(invalid="ignore"):
+        logs = np.where(np.isfinite(d), d - lp, 0).max(1)
         terms = np.where(p > 0, p * lp, 0)
     H = -terms.sum(1)
     eH = ((np.abs(terms) * rel_p).sum(1) + (p * err_lp).sum(1) + err_lp.min(1) + U * (64 + V / 32) * np.abs(terms).sum(1) + 6 * U * (np.abs(H) + np.abs(logs)))

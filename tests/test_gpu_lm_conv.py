@@ -169,6 +169,24 @@ def test_no_steps():
     assert bool((dw == 0).all())
 
 
+def test_offsets_past_32_bits():
+    """Steps and outputs that lie more than 2^31 elements apart."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    T, D, far = 4, 66, 1 << 30
+    c = Case(15, 1, T, D, 4, "bf16")
+    want = c.run()
+    stretch = lambda t: torch.empty(far * (T - 1) + D, dtype=t.dtype, device="cuda").as_strided(t.shape, (far * T, far, 1))  # noqa: E731
+    x, y = stretch(c.x), stretch(c.x)
+    x.copy_(c.x)
+    lm.gem_conv_forward(x, c.w, y, bias=c.bias, state=c.state)
+    assert np.array_equal(host(y), want["y"])
+    dw = torch.empty_like(c.w)
+    lm.gem_conv_backward(x, c.w, c.dy, y, dw, torch.empty(lm.gem_conv_workspace(1, T, D, 4), device="cuda"), bias=c.bias, state=c.state,
+                         dstate_last=c.dlast)
+    assert np.array_equal(host(y), want["dx"]) and np.array_equal(host(dw), want["dweight"])
+
+
 def test_parts_of_the_gradient():
     c = Case(12, 2, 90, 30, 3, "f32")
     full = c.run()

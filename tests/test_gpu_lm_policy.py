@@ -205,6 +205,20 @@ def test_a_common_offset_changes_nothing(offset, V):
         assert np.array_equal(got[k], want[k]), k
 
 
+@pytest.mark.parametrize("V", [900, 20000, 1000003])
+def test_offsets_past_32_bits(V):
+    """Rows that begin more than 2^31 elements apart."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB")
+    c = Case(7, 4, V, "bf16", masked=False)
+    want = c.run()
+    far = torch.empty(3 * (1 << 30) + V, dtype=torch.bfloat16, device="cuda").as_strided((4, V), (1 << 30, 1))
+    far.copy_(c.z)
+    got = c.run(z=far, in_place=True)
+    for k in got:
+        assert np.array_equal(got[k], want[k]), k
+
+
 def test_one_row_of_logits_for_all():
     c = Case(5, 7, 4000, "f32", masked=False)
     z = c.z[:1].expand(7, 4000)
