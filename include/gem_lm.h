@@ -257,8 +257,8 @@ int64_t gem_conv_workspace(int64_t B, int64_t T, int64_t D, int W);
 /* Gradients of the convolution: dy is the gradient with respect to y, dstate_last [B][W - 1][D] fp32
  * (NULL: zeros) that with respect to state_last; x, weight, bias, state, lengths, reset and form are
  * those of the forward call.  Writes dx (0 past lengths[b]), dweight [D][W], dbias [D] and dstate [B][W -
- * 1][D] fp32 (any of the last three may be NULL; dstate may be dstate_last).  workspace: gem_conv_workspace floats, in
- * use until the call's work is done. */
+ * 1][D] fp32 (any of the last three may be NULL; dstate must not be dstate_last).  workspace: gem_conv_workspace floats,
+ * in use until the call's work is done. */
 int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W,
                       const gem_seq_t* x, const float* weight, const float* bias,
                       const float* state, const int32_t* lengths, const uint8_t* reset,
