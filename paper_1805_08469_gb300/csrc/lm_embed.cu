@@ -14,7 +14,7 @@
 //   join   adds a run's partial sums in the order of the chunks.
 // Every dout row is read once and every row of the table written once, and a heavy token (one word in ten) is
 // spread over as many warps as it has chunks.  The order of every sum is fixed by the tokens.  65,536 tokens of Zipf
-// frequencies, 131,072 rows of 1024 fp32 from bf16: zeros 80 us (400 MB), sort 24 beside them, sums 38 (5 TB/s), join 18 (the
+// frequencies, 131,072 rows of 1024 fp32 from bf16: zeros 80 us (400 MB), sort 24 beside them, sums 38 (5 TB/s), join 13 (the
 // heaviest token's 120 partial rows).
 #include <cooperative_groups.h>
 
@@ -421,56 +421,87 @@ __global__ void __launch_bounds__(kEmbedThreads) embed_sums_kernel(const EmbedGr
   }
 }
 
-// A block per chunk and up to 1024 columns: the run that began in the chunk and goes on past it.  The warps are shares of
-// `slabs` warps, 128 columns each; share q takes every shares-th partial row from the q-th on, and the first adds theirs up.
-constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinSlabs = 8;
+// The runs that go on past the chunk where they began.  A block has up to kJoinSlabs slabs of 128 columns and looks at 32 chunks
+// gridDim.x apart at a time; its warps are shares of `slabs` warps.  A run that ends in the next chunk is a share's own; of a longer
+// one share q takes every shares-th partial row from the q-th on, and the first adds theirs up.  65,536 tokens, rows of 1024, in us for
+// Zipf frequencies and for one token in all places (the whole call): 13.0, 112; a block for each chunk instead, most of which found
+// nothing, 17.7, 187; two slabs of a block 18.9, 112; eight 17.6, 247.
+constexpr int kJoinThreads = 512, kJoinWarps = kJoinThreads / 32, kJoinSlabs = 4, kJoinBlocks = 152 * 3;
 template <typename G, bool WIDE>
-__global__ void __launch_bounds__(kJoinThreads, 3) embed_join_kernel(const EmbedGradArgs p, int slabs) {
+__global__ void __launch_bounds__(kJoinThreads, 2) embed_join_kernel(const EmbedGradArgs p, int slabs) {
   __shared__ float parts[kJoinWarps][kSlab<float>];
   pdl_entry();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, share = warp / slabs, shares = kJoinWarps / slabs;
-  const int64_t chunk = blockIdx.x;
   const int32_t* const keys = p.sorted_keys;
-  const int64_t first = chunk * p.chunk, next = first + p.chunk;
-  const int key = keys[next - 1], after = keys[next], start = keys[first], before = first > 0 ? keys[first - 1] : -1;
-  if (key >= p.V || after != key || (start == key && before == key)) return;   // none, or it began earlier
   const Columns<float, WIDE> c(int(blockIdx.y) * slabs + warp % slabs, p.D);
-  float sum[4] = {};
-  if (share < shares) {
-    auto add = [&](int64_t at, int slot) {
-      Row<float, WIDE, float> v = {};
-      v.read(c, p.parts + (at * 2 + slot) * p.pitch);
+  auto part = [&](int64_t at, int slot) {
+    Row<float, WIDE, float> v = {};
+    v.read(c, p.parts + (at * 2 + slot) * p.pitch);
+    return v;
+  };
+  for (int64_t base = blockIdx.x; base < p.chunks - 1; base += 32 * int64_t(gridDim.x)) {
+    const int64_t mine = base + lane * int64_t(gridDim.x), first = mine * p.chunk, next = first + p.chunk;
+    int key = p.V, beyond = p.V;
+    if (mine < p.chunks - 1) {
+      const int start = keys[first], before = first > 0 ? keys[first - 1] : -1, after = keys[next];
+      key = keys[next - 1];
+      beyond = mine + 2 < p.chunks ? keys[next + p.chunk] : p.V;
+      if (after != key || (start == key && before == key)) key = p.V;   // none, or it began earlier
+    }
+    unsigned runs = __ballot_sync(~0u, key < p.V && beyond != key);
+    for (int i = 0; runs != 0; ++i, runs &= runs - 1) {
+      if (i % shares != share) continue;
+      const int from = __ffs(runs) - 1;
+      const int64_t at = base + from * int64_t(gridDim.x);
+      const Row<float, WIDE, float> v = part(at, 1), w = part(at + 1, 0);
+      float sum[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sum[k] += v[k];
-    };
-    if (share == 0) add(chunk, 1);
-    // chunks from here on that begin with the run's token, 128 looked up at a time
-    for (int64_t at = chunk + 1;; at += 128) {
-      int count = 0;
-      bool on[4];
+      for (int k = 0; k < 4; ++k) sum[k] = v[k] + w[k];
+      finish_row<float, WIDE, G>(p, c, __shfl_sync(~0u, key, from), sum);
+    }
+    runs = __ballot_sync(~0u, key < p.V && beyond == key);
+    for (; runs != 0; runs &= runs - 1) {
+      const int from = __ffs(runs) - 1, run = __shfl_sync(~0u, key, from);
+      const int64_t chunk = base + from * int64_t(gridDim.x);
+      float sum[4] = {};
+      if (share < shares) {
+        auto add = [&](int64_t at, int slot) {
+          const Row<float, WIDE, float> v = part(at, slot);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t mine = at + q * 32 + lane;
-        on[q] = mine < p.chunks && keys[mine * p.chunk] == key;
-      }
+          for (int k = 0; k < 4; ++k) sum[k] += v[k];
+        };
+        if (share == 0) add(chunk, 1);
+        // chunks from here on that begin with the run's token, 128 looked up at a time
+        for (int64_t at = chunk + 1;; at += 128) {
+          int count = 0;
+          bool on[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const unsigned all = __ballot_sync(~0u, on[q]);
-        if (count == q * 32) count += all == ~0u ? 32 : __ffs(~all) - 1;
-      }
+          for (int q = 0; q < 4; ++q) {
+            const int64_t i = at + q * 32 + lane;
+            on[q] = i < p.chunks && keys[i * p.chunk] == run;
+          }
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const unsigned all = __ballot_sync(~0u, on[q]);
+            if (count == q * 32) count += all == ~0u ? 32 : __ffs(~all) - 1;
+          }
 #pragma unroll 8
-      for (int i = share; i < count; i += shares) add(at + i, 0);
-      if (count < 128) break;
+          for (int i = share; i < count; i += shares) add(at + i, 0);
+          if (count < 128) break;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) parts[warp][k * 32 + lane] = sum[k];
+      __syncthreads();
+      if (share == 0) {
+        for (int q = 1; q < shares; ++q)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum[k] += parts[q * slabs + warp][k * 32 + lane];
+        finish_row<float, WIDE, G>(p, c, run, sum);
+      }
+      __syncthreads();
     }
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k) parts[warp][k * 32 + lane] = sum[k];
-  __syncthreads();
-  if (share != 0) return;
-  for (int q = 1; q < shares; ++q)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] += parts[q * slabs + warp][k * 32 + lane];
-  finish_row<float, WIDE, G>(p, c, key, sum);
 }
 
 constexpr int64_t kMaxTokens = int64_t(1) << 27, kMaxRowsOfTable = int64_t(1) << 30, kMaxWidth = int64_t(1) << 23;
@@ -537,7 +568,8 @@ cudaError_t launch_embed_grad_as(EmbedGradArgs p, cudaStream_t stream) {
           : launch_pdl(embed_sums_kernel<E, G, false>, grid, dim3(kEmbedThreads), 0, stream, p);
   if (e != cudaSuccess || p.chunks == 1) return e;
   const int columns = kSlab<float>, slabs = std::min((p.D + columns - 1) / columns, kJoinSlabs);
-  const dim3 joins(unsigned(p.chunks - 1), unsigned((p.D + columns * slabs - 1) / (columns * slabs)));   // (the second: at most 2^16 - 1)
+  const int groups = (p.D + columns * slabs - 1) / (columns * slabs);   // (at most 2^14)
+  const dim3 joins(unsigned(std::min(p.chunks - 1, std::max(kJoinBlocks / groups, 1))), unsigned(groups));
   return wide(p.dtable, sizeof(G), p.dtable_ld, p.D, kCols<float>) ? launch_pdl(embed_join_kernel<G, true>, joins, dim3(kJoinThreads), 0, stream, p, slabs)
                                                                    : launch_pdl(embed_join_kernel<G, false>, joins, dim3(kJoinThreads), 0, stream, p, slabs);
 }

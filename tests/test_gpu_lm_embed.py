@@ -109,6 +109,16 @@ def test_large_tables(V):
     both(V, len(t), V, 16 if V > 1000000 else 40, "bf16", tokens=t)
 
 
+@pytest.mark.parametrize("D", [3, 8])
+def test_many_tokens(D):
+    """More chunks than the blocks look at once, with runs of one chunk, of two and of thousands."""
+    rng = np.random.default_rng(D)
+    N, V = 480001, 150000
+    t = np.minimum(rng.integers(0, V, N), (V * rng.random(N) ** 4).astype(np.int64))
+    t[rng.random(N) < 0.2] = 77777
+    both(D, N, V, D, "bf16", tokens=t, accumulate=D == 8)
+
+
 def test_tokens_out_of_range():
     """Negative ones have no row; those past the table give NaN, and no gradient; what dout holds there is not used."""
     tokens = np.array([0, -1, 5, 6, -2**31, 2**31 - 1, 3, 3])
