@@ -4,9 +4,10 @@
 // registers, so x is read once but for the W - 1 steps before a segment.  The backward pass walks forward
 // as well: step t's dp_t goes to the gradients of the W inputs it used, the oldest of which is then complete; it
 // goes W - 1 steps past the segment for that.  Sums for the weights are taken in registers over the
-// segment, in shared memory over the block's warps, and by a second kernel over the blocks, in that order.
+// segment, in shared memory over the block's warps, which may have several short sequences, and by a second kernel over the blocks, in that
+// order.
 //
-// 8 x 4096 x 2048 bf16, W = 4, SiLU: forward 46 us (5.8 TB/s of input and output), backward 98 us (4.1 TB/s; half of the issue
+// 8 x 4096 x 2048 bf16, W = 4, SiLU: forward 46 us (5.8 TB/s of input and output), backward 101 us (4.0 TB/s; half of the issue
 // slots, its warps wait for their own chains of products), the parameters' sums 5.
 #include <type_traits>
 
@@ -16,7 +17,7 @@ namespace gem {
 namespace lm {
 namespace {
 
-constexpr int kConvWarps = 4;       // most segments of time of a block, a warp each
+constexpr int kConvWarps = 4;       // most segments of a block, a warp each
 constexpr int kSegment = 64;        // steps of a segment
 constexpr int kGroup = 4;           // steps that are taken together
 constexpr float kLog2e = 1.4426950408889634f;
@@ -28,11 +29,12 @@ struct ConvArgs {
   float* state_last;
   const float* dstate_last;
   float* dstate;
-  float* partial;          // [B blocks][W + 1][D]
+  float* partial;          // [rows of blocks][W + 1][D]
   const int32_t* lengths;
   const uint8_t* reset;
   int64_t T;
-  int D, columns, blocks;  // blocks along the channels, along a sequence's time
+  int D, columns;          // blocks along the channels
+  unsigned segments, total;   // of a sequence, of all
 };
 
 template <int V>
@@ -129,7 +131,7 @@ __device__ __forceinline__ void write_step(E* at, const Channels<K>& v) {
 // What a warp works on.
 struct ConvPlace {
   int64_t b, first, end, n;   // its steps [first, end) of the sequence's n
-  int64_t row;                // the block's number along sequences and time
+  int64_t row;                // the block's number along the segments of all sequences
   int d;                      // the thread's first channel
   bool on;
 };
@@ -137,12 +139,14 @@ template <int K>
 __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& p) {
   ConvPlace a;
   a.row = blockIdx.x / p.columns;
-  a.b = a.row / p.blocks;
-  a.first = ((a.row % p.blocks) * (blockDim.x / 32) + threadIdx.x / 32) * kSegment;
-  a.end = min(a.first + kSegment, p.T);
-  a.n = p.lengths ? min(max(int64_t(p.lengths[a.b]), int64_t(0)), p.T) : p.T;
   a.d = ((blockIdx.x % p.columns) * 32 + threadIdx.x % 32) * K;
-  a.on = a.d < p.D;
+  const unsigned segment = unsigned(a.row) * (blockDim.x / 32) + threadIdx.x / 32;
+  const bool live = segment < p.total;   // (a block's other warps have no channels, and no steps)
+  a.b = segment / p.segments;
+  a.first = int64_t(segment % p.segments) * kSegment;
+  a.end = min(a.first + kSegment, p.T);
+  a.n = !live ? 0 : p.lengths ? min(max(int64_t(p.lengths[a.b]), int64_t(0)), p.T) : p.T;
+  a.on = live && a.d < p.D;
   return a;
 }
 
@@ -495,21 +499,24 @@ __global__ void __launch_bounds__(kConvWarps * 32) conv_backward_kernel(const Co
     }
 }
 
-// Sums of the blocks' partial sums: 32 channels of a tap by a block, whose warps take every eighth row each.
-constexpr int kJoinWarps = 8;
-__global__ void __launch_bounds__(kJoinWarps * 32) conv_join_kernel(const float* partial, int64_t rows, int D, int W, float* dweight, float* dbias) {
-  __shared__ float sums[kJoinWarps][32];
+// Sums of the blocks' partial sums: 32 channels of a tap by a block, of whose WARPS each takes every WARPS-th row.  Many rows
+// want many warps: 1024 of them (1 x 262,144 x 256 bf16) 106 us for the whole backward call with 32 and 123 with 8; 128 (8 x 4096 x 2048) 5
+// us with 8 and 9.5 with 32 for this kernel.
+constexpr int64_t kManyRows = 256;
+template <int WARPS>
+__global__ void __launch_bounds__(WARPS * 32) conv_join_kernel(const float* partial, int64_t rows, int D, int W, float* dweight, float* dbias) {
+  __shared__ float sums[WARPS][32];
   pdl_entry();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, d = blockIdx.x * 32 + lane, j = blockIdx.y;
   float v = 0.0f;
   if (d < D)
 #pragma unroll 8
-    for (int64_t i = warp; i < rows; i += kJoinWarps) v += partial[(i * (W + 1) + j) * D + d];
+    for (int64_t i = warp; i < rows; i += WARPS) v += partial[(i * (W + 1) + j) * D + d];
   sums[warp][lane] = v;
   __syncthreads();
   if (warp != 0 || d >= D) return;
 #pragma unroll
-  for (int w = 1; w < kJoinWarps; ++w) v += sums[w][lane];
+  for (int w = 1; w < WARPS; ++w) v += sums[w][lane];
   if (j < W) {
     if (dweight) dweight[int64_t(d) * W + j] = v;
   } else if (dbias) {
@@ -517,19 +524,27 @@ __global__ void __launch_bounds__(kJoinWarps * 32) conv_join_kernel(const float*
   }
 }
 
-// How time is cut: warps of a block, blocks of a sequence.
+// How sequences are cut: segments of one, of all, warps of a block, rows of blocks.  A block has the segments of one or several sequences,
+// but one alone where blocks of four would not give every SM one (in a graph, bf16, us with one and with four: 16 x 1 x 2048 2.0, 2.3, backward 4.1,
+// 4.8; 1 x 1000 x 2048 5.9, 6.1, backward 9.8, 10.5).  Blocks of one sequence each left short ones a row of sums for every sequence: 4096 x 64
+// x 256, backward 192 instead of 100.
 struct ConvCut {
-  int64_t warps, blocks;
+  int64_t segments, total, warps, rows;
 };
-ConvCut conv_cut(int64_t T) {
-  const int64_t segments = T < 1 ? 1 : (T + kSegment - 1) / kSegment, warps = segments < kConvWarps ? segments : kConvWarps;
-  return {warps, (segments + warps - 1) / warps};
+ConvCut conv_cut(int64_t B, int64_t T, int64_t D) {
+  ConvCut c;
+  c.segments = T < 1 ? 1 : (T + kSegment - 1) / kSegment;
+  c.total = B * c.segments;
+  c.warps = c.total * ((D + 63) / 64) < 152 * kConvWarps ? 1 : kConvWarps;
+  c.rows = (c.total + c.warps - 1) / c.warps;
+  return c;
 }
 
 bool conv_sizes_ok(int64_t B, int64_t T, int64_t D, int W) {
   if (W < 2 || W > 4 || !extent_ok(B) || !extent_ok(T) || !channels_ok(D)) return false;
-  const int64_t columns = (D + 31) / 32, blocks = conv_cut(T).blocks;
-  return B == 0 || D == 0 || columns <= (kMaxExtent - 1) / blocks / B;   // a block at least for 32 channels and the steps of its warps
+  if (B == 0 || D == 0) return true;
+  const int64_t columns = (D + 31) / 32, segments = T < 1 ? 1 : (T + kSegment - 1) / kSegment;
+  return segments < kMaxExtent / B && columns <= (kMaxExtent - 1) / conv_cut(B, T, D).rows;   // a block at least for 32 channels and its warps
 }
 
 // Whether pieces of K channels of every step lie at multiples of their size.
@@ -539,13 +554,14 @@ bool in_pieces(const gem_seq_t& s, int dtype, int64_t B, int64_t T, int64_t D, i
 
 template <typename E, int W, int K>
 cudaError_t launch_forward_as(ConvArgs p, int form, int64_t B, cudaStream_t stream) {
-  const ConvCut cut = conv_cut(p.T);
+  const ConvCut cut = conv_cut(B, p.T, p.D);
   const bool whole = p.T <= kSegment;   // a warp has the whole sequence
   float* const state_last = p.state_last;
   if (!whole) p.state_last = nullptr;
   p.columns = (p.D + 32 * K - 1) / (32 * K);
-  p.blocks = int(cut.blocks);
-  const dim3 grid(unsigned(B * p.blocks * p.columns)), block(unsigned(cut.warps * 32));
+  p.segments = unsigned(cut.segments);
+  p.total = unsigned(cut.total);
+  const dim3 grid(unsigned(cut.rows * p.columns)), block(unsigned(cut.warps * 32));
   const cudaError_t e = form == GEM_CONV_SILU ? launch_pdl(conv_forward_kernel<E, W, K, true>, grid, block, 0, stream, p)
                                               : launch_pdl(conv_forward_kernel<E, W, K, false>, grid, block, 0, stream, p);
   if (e != cudaSuccess || whole || !state_last) return e;
@@ -554,10 +570,11 @@ cudaError_t launch_forward_as(ConvArgs p, int form, int64_t B, cudaStream_t stre
 }
 template <typename E, int W, int K>
 cudaError_t launch_backward_as(ConvArgs p, int form, int64_t B, cudaStream_t stream) {
-  const ConvCut cut = conv_cut(p.T);
+  const ConvCut cut = conv_cut(B, p.T, p.D);
   p.columns = (p.D + 32 * K - 1) / (32 * K);
-  p.blocks = int(cut.blocks);
-  const dim3 grid(unsigned(B * p.blocks * p.columns)), block(unsigned(cut.warps * 32));
+  p.segments = unsigned(cut.segments);
+  p.total = unsigned(cut.total);
+  const dim3 grid(unsigned(cut.rows * p.columns)), block(unsigned(cut.warps * 32));
   return form == GEM_CONV_SILU ? launch_pdl(conv_backward_kernel<E, W, K, true>, grid, block, 0, stream, p)
                                : launch_pdl(conv_backward_kernel<E, W, K, false>, grid, block, 0, stream, p);
 }
@@ -615,7 +632,7 @@ int gem_conv_forward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W
 
 int64_t gem_conv_workspace(int64_t B, int64_t T, int64_t D, int W) {
   if (!conv_sizes_ok(B, T, D, W)) return -1;
-  return B * conv_cut(T).blocks * (W + 1) * D;
+  return conv_cut(B, T, D).rows * (W + 1) * D;
 }
 
 int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int W,
@@ -652,9 +669,13 @@ int gem_conv_backward(int dtype, int form, int64_t B, int64_t T, int64_t D, int 
     const bool pairs = in_pieces(p.x, dtype, B, T, D, 2) && in_pieces(p.dy, dtype, B, T, D, 2) && in_pieces(p.y, dtype, B, T, D, 2);
     e = BY_TYPE(launch_conv, p, form, B, W, pairs ? 2 : 1, true, on);
   }
-  if (e == cudaSuccess && sums)
-    e = launch_pdl(conv_join_kernel, dim3(unsigned((D + 31) / 32), unsigned(W + 1)), dim3(kJoinWarps * 32), 0, on,
-                   static_cast<const float*>(workspace), B * conv_cut(T).blocks, int(D), W, dweight, dbias);
+  if (e == cudaSuccess && sums) {
+    const int64_t rows = conv_cut(B, T, D).rows;
+    const dim3 joins(unsigned((D + 31) / 32), unsigned(W + 1));
+    const float* const partial = workspace;
+    e = rows > kManyRows ? launch_pdl(conv_join_kernel<32>, joins, dim3(32 * 32), 0, on, partial, rows, int(D), W, dweight, dbias)
+                         : launch_pdl(conv_join_kernel<8>, joins, dim3(8 * 32), 0, on, partial, rows, int(D), W, dweight, dbias);
+  }
   return launch_status(e);
 }
 

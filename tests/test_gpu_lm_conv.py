@@ -88,6 +88,14 @@ def test_shapes(B, T, D):
     Case(T, B, T, D, 4, "bf16", resets=0.01).check()
 
 
+@pytest.mark.parametrize("B,T,D", [(701, 9, 40), (650, 1, 65), (90, 500, 70), (3, 5000, 260), (1, 70001, 8), (333, 65, 128), (1201, 64, 5)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_blocks_of_several_segments(B, T, D, dtype):
+    """Blocks whose warps have segments of one sequence, of several, and none."""
+    lengths = np.random.default_rng(B).integers(-1, T + 2, B).tolist()
+    Case(B, B, T, D, 4 if T > 1 else 3, dtype, resets=0.05, lengths=lengths).check()
+
+
 def test_without_state_bias_and_last_gradient():
     Case(6, 2, 100, 40, 4, "f32", state=False, bias=False).check()
 
