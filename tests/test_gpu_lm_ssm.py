@@ -134,6 +134,12 @@ def test_cuts_of_time(B, T, D, N, G, dtype):
     Case(T + 1, B, T, D, N, G, dtype, lengths=[(b * 53 + 700) % (T + 1) for b in range(B)], resets=0.004).check()
 
 
+@pytest.mark.parametrize("B,T,D,N,G", [(600, 5, 20, 7, 1), (300, 18, 66, 64, 2), (17, 40, 33, 16, 1)])
+def test_many_sequences(B, T, D, N, G):
+    """The parameters' gradients are sums over more sequences than a thread reads at a time."""
+    Case(B, B, T, D, N, G, "bf16", resets=0.05).check()
+
+
 def test_slow_decays_over_a_long_sequence():
     """States that remember thousands of steps, through every split."""
     Case(3, 1, 6000, 16, 16, 1, "f32", slow=True).check()
