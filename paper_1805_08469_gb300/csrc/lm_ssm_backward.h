@@ -174,10 +174,11 @@ __global__ void __launch_bounds__(kSsmThreads, STATES ? 4 : kBackwardResident<LS
         const Quad b = quad(bc[t * LS + a.g]);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-          if (check.value && (resets >> t & 1)) now[k] = zeros();
           const float2 v = steps[t][a.pos + k * S::lanes];
           now[k].a = fma<2>(decay(v.x, A2[k].a, more[k].a), now[k].a, splat<2>(v.y) * b.a);
           now[k].b = fma<2>(decay(v.x, A2[k].b, more[k].b), now[k].b, splat<2>(v.y) * b.b);
+          // (not 0 times a decay, which may be infinite)
+          if (check.value && (resets >> t & 1)) now[k] = {splat<2>(v.y) * b.a, splat<2>(v.y) * b.b};
         }
       };
       // half: steps from t1 on, whose states are computed again into h from the one before them

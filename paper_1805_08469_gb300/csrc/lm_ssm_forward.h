@@ -133,9 +133,10 @@ __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmAr
             const int t = t1 + i;
             if (!STATES) y[k][t] = 0.0f;
             if (check.value && t >= count) continue;
-            if (check.value && (resets >> t & 1)) h[k] = zeros();
             h[k].a = fma<2>(dec[i].a, h[k].a, splat<2>(v[i][k].y) * b[i].a);
             h[k].b = fma<2>(dec[i].b, h[k].b, splat<2>(v[i][k].y) * b[i].b);
+            // (not 0 times a decay, which may be infinite)
+            if (check.value && (resets >> t & 1)) h[k] = {splat<2>(v[i][k].y) * b[i].a, splat<2>(v[i][k].y) * b[i].b};
             if (STATES) {
               sum[k] += v[i][k].x;
             } else {
@@ -231,12 +232,13 @@ __global__ void __launch_bounds__(kSsmThreads) ssm_step_kernel(const SsmArgs p) 
   if (p.in.softplus) step = softplus<1>({step}).v[0];
   float y = 0.0f;
   if (live) {
-    if (p.in.reset && p.in.reset[b]) h = zeros();
+    const bool drop = p.in.reset && p.in.reset[b];
     A2 = {A2.a * splat<2>(kLog2e), A2.b * splat<2>(kLog2e)};
     const Vec<2> in = splat<2>(step * x);
     const Quad more = nudges(step, A2);
-    h.a = fma<2>(decay(step, A2.a, more.a), h.a, in * bs.template at<2>(0));
-    h.b = fma<2>(decay(step, A2.b, more.b), h.b, in * bs.template at<2>(2));
+    const Quad input = {in * bs.template at<2>(0), in * bs.template at<2>(2)};
+    h = {fma<2>(decay(step, A2.a, more.a), h.a, input.a), fma<2>(decay(step, A2.b, more.b), h.b, input.b)};
+    if (drop) h = input;   // (not 0 times a decay, which may be infinite)
     const Vec<2> m = fma<2>(cs.template at<2>(2), h.b, cs.template at<2>(0) * h.a);
     y = m.v[0] + m.v[1];
   }
