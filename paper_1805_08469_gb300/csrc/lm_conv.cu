@@ -78,7 +78,6 @@ template <>
 struct Raw<float, 4> {
   float4 x;
   __device__ __forceinline__ void read(const float* p) { x = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void clear() { x = make_float4(0, 0, 0, 0); }
   __device__ __forceinline__ Channels<4> floats() const { return {{{x.x, x.y}, {x.z, x.w}}}; }
 };
 template <typename E>
@@ -94,21 +93,18 @@ template <typename E>
 struct Raw<E, 4> {
   uint2 x;
   __device__ __forceinline__ void read(const E* p) { x = *reinterpret_cast<const uint2*>(p); }
-  __device__ __forceinline__ void clear() { x = make_uint2(0, 0); }
   __device__ __forceinline__ Channels<4> floats() const { return {{two<E>(x.x), two<E>(x.y)}}; }
 };
 template <>
 struct Raw<float, 2> {
   float2 x;
   __device__ __forceinline__ void read(const float* p) { x = *reinterpret_cast<const float2*>(p); }
-  __device__ __forceinline__ void clear() { x = make_float2(0, 0); }
   __device__ __forceinline__ Channels<2> floats() const { return {{{x.x, x.y}}}; }
 };
 template <typename E>
 struct Raw<E, 2> {
   uint32_t x;
   __device__ __forceinline__ void read(const E* p) { x = *reinterpret_cast<const uint32_t*>(p); }
-  __device__ __forceinline__ void clear() { x = 0; }
   __device__ __forceinline__ Channels<2> floats() const { return {{two<E>(x)}}; }
 };
 template <typename E, int K>
@@ -230,11 +226,11 @@ struct Window {
 // Feeds a thread the elements of N sequences, a group of steps at a time, loaded ahead.  Four or two channels: by
 // asynchronous copies into places of the thread's own in shared memory (its registers are taken by sums and taps); one:
 // into registers.  What lies past the last step, or a thread without channels gets, is not defined.
-template <typename E, int N>
+template <typename E>
 constexpr int kStages = sizeof(E) == 2 ? 4 : 2;
 template <typename E, int K, int N>
 struct Feed {
-  using Shared = Raw<E, K>[kStages<E, N>][N][kGroup][kConvWarps * 32];
+  using Shared = Raw<E, K>[kStages<E>][N][kGroup][kConvWarps * 32];
   Shared& ring;
   const E* at[N];      // the next step to load
   int64_t stride[N];
@@ -255,16 +251,16 @@ struct Feed {
   }
   __device__ __forceinline__ void start() {
 #pragma unroll
-    for (int i = 0; i + 1 < kStages<E, N>; ++i) issue(i);
+    for (int i = 0; i + 1 < kStages<E>; ++i) issue(i);
   }
   __device__ __forceinline__ void take(Raw<E, K> (&to)[N][kGroup]) {
-    asm volatile("cp.async.wait_group %0;" ::"n"(kStages<E, N> - 2) : "memory");
-    issue(stage == 0 ? kStages<E, N> - 1 : stage - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages<E> - 2) : "memory");
+    issue(stage == 0 ? kStages<E> - 1 : stage - 1);
 #pragma unroll
     for (int i = 0; i < N; ++i)
 #pragma unroll
       for (int u = 0; u < kGroup; ++u) to[i][u] = ring[stage][i][u][threadIdx.x];
-    stage = stage + 1 == kStages<E, N> ? 0 : stage + 1;
+    stage = stage + 1 == kStages<E> ? 0 : stage + 1;
   }
 };
 template <typename E, int N>

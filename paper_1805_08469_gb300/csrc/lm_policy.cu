@@ -143,7 +143,7 @@ __device__ __forceinline__ Stats policy_stats(const uint4* data, int pieces, int
 }
 
 template <typename E, bool LOG>
-__global__ void __launch_bounds__(kRowThreads, 3) policy_kernel(const PolicyArgs p, int64_t N, int C, int slots) {
+__global__ void __launch_bounds__(kRowThreads, 3) policy_kernel(const PolicyArgs p, int64_t N, int C) {
   extern __shared__ uint4 data[];
   __shared__ Stats all[2][kRowCluster * kRowParts];
   pdl_entry();
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) policy_kernel(const PolicyArgs
 
 // Short rows: a warp for each.
 template <typename E, bool LOG>
-__global__ void __launch_bounds__(kShortWarps * 32, 8) policy_short_kernel(const PolicyArgs p, int64_t N, unsigned warp_bytes, int slots) {
+__global__ void __launch_bounds__(kShortWarps * 32, 8) policy_short_kernel(const PolicyArgs p, int64_t N, unsigned warp_bytes) {
   extern __shared__ uint4 shared[];
   pdl_entry();
   const int64_t n = int64_t(blockIdx.x) * kShortWarps + threadIdx.x / 32;
@@ -314,7 +314,7 @@ cudaError_t launch_policy_as(const PolicyArgs& p, int dtype, int64_t N, cudaStre
   if (row_is_short(dtype, p.V)) return launch_short<policy_short_kernel<E, LOG>>(p, dtype, N, 0, stream);
   const RowCut c = row_cut(dtype, N, p.V, 0);
   if (c.cluster == 0) return launch_pdl(policy_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p, N);
-  return launch_rows<policy_kernel<E, LOG>>(c, N, stream, p, N, c.cluster, c.slots);
+  return launch_rows<policy_kernel<E, LOG>>(c, N, stream, p, N, c.cluster);
 }
 // (the entropy's sum is taken where either the bonus or the entropy itself is asked for)
 template <typename E>

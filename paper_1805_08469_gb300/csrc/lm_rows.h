@@ -373,15 +373,15 @@ cudaError_t launch_rows(const RowCut& c, int64_t N, cudaStream_t stream, const A
 }
 
 // Rows of up to 8 KB take a warp each (8192 x 1000 bf16, 8 entries: 16 us against 48 in blocks that stay).
-template <auto KERNEL, typename Args>
-cudaError_t launch_short(const Args& p, int dtype, int64_t N, size_t more_bytes, cudaStream_t stream) {
-  const int slots = int(int64_t(p.V) * dtype_size(dtype) / 16);
-  const unsigned warp_bytes = unsigned((size_t(slots) * 16 + more_bytes + 15) / 16 * 16);
+inline int row_slots(int dtype, int64_t V) { return int(V * dtype_size(dtype) / 16); }
+template <auto KERNEL, typename Args, typename... More>
+cudaError_t launch_short(const Args& p, int dtype, int64_t N, size_t more_bytes, cudaStream_t stream, const More&... more) {
+  const unsigned warp_bytes = unsigned((size_t(row_slots(dtype, p.V)) * 16 + more_bytes + 15) / 16 * 16);
   const size_t shared = size_t(warp_bytes) * kShortWarps;
   const cudaError_t e = allow_shared<KERNEL>(shared);
   if (e != cudaSuccess) return e;
   return launch_pdl(KERNEL, dim3(unsigned((N + kShortWarps - 1) / kShortWarps)), dim3(kShortWarps * 32), shared, stream, p, N,
-                    warp_bytes, slots);
+                    warp_bytes, more...);
 }
 inline bool row_is_short(int dtype, int64_t V) { return V * dtype_size(dtype) <= kShortPieces * 16; }
 

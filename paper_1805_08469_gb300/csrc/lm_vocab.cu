@@ -1477,7 +1477,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) token_logp_grad_kernel(const L
 
 template <typename E, Hard HARD>
 cudaError_t launch_distill_as(const DistillArgs& p, int dtype, int64_t N, const RowCut& c, cudaStream_t stream) {
-  if (row_is_short(dtype, p.V)) return launch_short<distill_short_kernel<E, HARD>>(p, dtype, N, teacher_bytes(p.K), stream);
+  if (row_is_short(dtype, p.V)) return launch_short<distill_short_kernel<E, HARD>>(p, dtype, N, teacher_bytes(p.K), stream, row_slots(dtype, p.V));
   return launch_rows<distill_kernel<E, HARD>>(c, N, stream, p, N, c.cluster, c.slots);
 }
 
@@ -1495,7 +1495,8 @@ cudaError_t launch_distill(const DistillArgs& p, int dtype, int64_t N, cudaStrea
 template <typename E>
 cudaError_t launch_logp(const LogpArgs& p, int dtype, int64_t N, cudaStream_t stream) {
   if (row_is_short(dtype, p.V))
-    return launch_short<token_logp_short_kernel<E>>(p, dtype, N, p.K > 0 ? kShortList * sizeof(unsigned long long) : 0, stream);
+    return launch_short<token_logp_short_kernel<E>>(p, dtype, N, p.K > 0 ? kShortList * sizeof(unsigned long long) : 0, stream,
+                                                    row_slots(dtype, p.V));
   RowCut c = row_cut(dtype, N, p.V, 2);
   if (c.cluster == 0) return launch_pdl(token_logp_stream_kernel<E>, dim3(unsigned(N)), dim3(kThreads), 0, stream, p);
   // the widest groups of which there are at least 2 K with elements (T C of one lane: at least K)
