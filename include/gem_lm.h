@@ -29,8 +29,9 @@
  *     buffers that other streams use.  Calls can be captured into a CUDA graph.
  *   - Elements are fp32, bf16 or fp16 (gem_dtype), statistics and states fp32.  All arithmetic
  *     is fp32, rounded once when an output of 16 bits is stored; exponentials over rows, those of 16-bit
- *     gates and the gates' quotients are the GPU's approximations (2 units in the last place and what rounding
- *     the argument adds; a quotient 1).  Results do not depend on
+ *     gates, all of the convolution's and the scan's (gates, softplus, decays) and the gates' quotients are the
+ *     GPU's approximations (2 units in the last place and what rounding the argument adds, so that the softplus of v
+ *     below -10 is off by |v| 2^-24 of itself; a quotient 1), 0 below 2^-126.  Results do not depend on
  *     timing: sums are taken in an order that the sizes fix (the embedding gradient's: the tokens).
  *   - Strides and row pitches count elements.  Tensors need the alignment of their element
  *     type, no more (aligned rows are read with wider loads).
@@ -199,7 +200,8 @@ int gem_token_logp_grad(int dtype, int64_t N, int64_t V, const void* logits, int
  *   grad (row n at grad + n * grad_ld, type dtype), may be NULL and may be logits with grad_ld =
  *     ld: row_scale[n] dL/dlogits.
  * A logit of -inf has p = 0, and no gradient unless it is the token's; a logit of NaN or +inf, or a row of -inf
- * alone, makes its row's loss and gradient NaN.  Requires 0 <= clip_low <= 1, 0 <= clip_high, kl and bonus finite and
+ * alone, makes its row's loss and gradient NaN; so may a KL term past fp32 (d above 88, or a token without any
+ * probability).  Requires 0 <= clip_low <= 1, 0 <= clip_high, kl and bonus finite and
  * kl >= 0, 1e-20 <= temperature <= 1e20, 1 <= V <= 2^30, N <= 2^27, ld >= V (or 0), grad_ld >= V. */
 int gem_policy(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
                const int32_t* tokens, const float* old_logp, const float* advantage,
@@ -209,7 +211,8 @@ int gem_policy(int dtype, int64_t N, int64_t V, const void* logits, int64_t ld,
 
 /* Embedding: out[n] = scale table[tokens[n]] for N tokens (int32), rows of D elements: row v of the
  * table at table + v * table_ld (type table_dtype), row n of out at out + n * out_ld (type dtype; rounded
- * once).  A token < 0 has no row: zeros; one >= V gives NaN.  Requires N <= 2^27, 1 <= V <= 2^30, D <= 2^23. */
+ * once).  A token < 0 has no row: zeros; one >= V gives NaN.  Requires N <= 2^27, 1 <= V <= 2^30, D <= 2^23, pitches from
+ * D to 2^30. */
 int gem_embed(int table_dtype, int dtype, int64_t N, int64_t V, int64_t D, const void* table,
               int64_t table_ld, const int32_t* tokens, float scale, void* out, int64_t out_ld,
               void* stream);
@@ -225,8 +228,8 @@ int64_t gem_embed_workspace(int64_t N, int64_t V, int64_t D);
  *   accumulate = 1: the sum is added to what dtable holds (a table that is also the output layer);
  *     rows without a token are not touched.
  *   workspace: gem_embed_workspace bytes, 16-byte aligned, in use until the call's work is done.
- * Sums are fp32, in the order of n and of pieces of it that the tokens alone fix.  What is added to an fp32 dtable
- * counts as 0 below 2^-126. */
+ * Sums are fp32, in the order of n and of pieces of it that the tokens alone fix.  Where an fp32 dtable is added to,
+ * what is added, what it holds there and their sum count as 0 below 2^-126. */
 int gem_embed_grad(int dtype, int grad_dtype, int64_t N, int64_t V, int64_t D, const void* dout,
                    int64_t dout_ld, const int32_t* tokens, float scale, int accumulate,
                    void* dtable, int64_t dtable_ld, void* workspace, void* stream);
@@ -297,7 +300,8 @@ typedef struct {
 int64_t gem_ssm_saved_count(int64_t B, int64_t T, int64_t D, int N);
 
 /* Floats of the workspace of gem_ssm_forward (backward = 0), or of one that serves both calls (backward =
- * 1); may be 0; -1 for a size out of range. */
+ * 1); may be 0; -1 for a size out of range.  Most of the latter, where a group has more than 32 channels (16 for more than
+ * 32 states), are the blocks' parts of db and dc: B T D floats for up to 16 states, 2 B T D for up to 32, 8 B T D for up to 64. */
 int64_t gem_ssm_workspace(int64_t B, int64_t T, int64_t D, int N, int G, int backward);
 
 /* The scan into y [B][T][D], of type dtype as x, dt, b, c and z.
@@ -307,8 +311,8 @@ int64_t gem_ssm_workspace(int64_t B, int64_t T, int64_t D, int N, int G, int bac
  *   saved, may be NULL: gem_ssm_saved_count floats, the state before steps 0, 16, 32, ... for
  *     gem_ssm_backward; those past a sequence's end are not written.
  *   workspace: gem_ssm_workspace floats (NULL where that is 0), in use until the call's work is done.
- * A state or step that is not finite stays so until a reset, but an infinite state becomes NaN where
- * exp(step A) leaves fp32. */
+ * A state or step that is not finite stays so until a reset, but an infinite state may become NaN where
+ * exp(step A) is 0 in fp32, and a state of 0 where it is infinite. */
 int gem_ssm_forward(int dtype, const gem_ssm_t* in, const float* h0, const gem_seq_t* y,
                     float* h_last, float* saved, float* workspace, void* stream);
 
