@@ -1,21 +1,22 @@
 // Embedding of tokens and the gradient of its table (include/gem_lm.h).
 //
 // Lookup: a warp copies a slab of a row, a lane 16 bytes of what it writes (single elements where a row
-// does not lie on such boundaries).  65,536 tokens, rows of 1024 fp32 to bf16: 47 us, HBM bound.
+// does not lie on such boundaries).  65,536 tokens of Zipf frequencies, rows of 1024 fp32 to bf16: 47 us (402 MB read and
+// written, of which repeated rows come from L2; HBM at 48%, its warps wait for their loads).
 //
 // Gradient, in four launches:
 //   zeros  to the table's rows that no token has (where they are not added to); each block looks through the
 //          tokens for those of its rows.
-//   sort   one cluster sorts the tokens with their places (stable, by digits of up to nine bits, the lowest first),
-//          beside the zeros.
+//   sort   one cluster sorts the tokens with their places (stable, by digits of up to nine bits, the lowest first).  A block of it
+//          takes all of an SM's registers, so it starts when the zeros of as many neighbouring SMs are written, beside the last.
 //   sums   the sorted places are cut into chunks of L.  A warp takes a chunk and a slab of columns, adds up each run
 //          of equal tokens in fp32 and writes the row of a run that lies inside the chunk.  What a run has in the
 //          chunk where it began, and in each where it goes on, are partial sums.
 //   join   adds a run's partial sums in the order of the chunks.
 // Every dout row is read once and every row of the table written once, and a heavy token (one word in ten) is
 // spread over as many warps as it has chunks.  The order of every sum is fixed by the tokens.  65,536 tokens of Zipf
-// frequencies, 131,072 rows of 1024 fp32 from bf16: zeros 80 us (400 MB), sort 24 beside them, sums 38 (5 TB/s), join 13 (the
-// heaviest token's 120 partial rows).
+// frequencies, 131,072 rows of 1024 fp32 from bf16: zeros 80 us (450 MB; the first of their blocks end at 55), sort from 66 to 89, sums
+// 38 (5 TB/s), join 13 (the heaviest token's 120 partial rows).
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -314,7 +315,7 @@ __device__ void zero_rows(const EmbedGradArgs& p, unsigned* bitmap, int64_t firs
   __syncthreads();
 }
 
-// A block per SM for an even range of rows each.  It lets the sort start beside it, once what came before has ended.
+// A block per SM for an even range of rows each.  It lets the sort start before the last of them end, once what came before has ended.
 template <typename G>
 __global__ void __launch_bounds__(kSortThreads) embed_zeros_kernel(const EmbedGradArgs p) {
   __shared__ unsigned bitmap[kZeroRows / 32];

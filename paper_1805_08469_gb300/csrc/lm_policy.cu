@@ -3,7 +3,7 @@
 // A row's statistics (maximum, sum and, for entropy and bonus, sum of p log p) give everything that its gradient needs beside
 // the elements, so a row on chip is read from memory once and its gradient written once.  Clusters stay and take row after row:
 // the gradient pass refills each slot with the next row's piece.  One cluster barrier a row.  4096 x 131072 bf16, all
-// terms: 352 us (6.1 TB/s with a tenth of the rows masked), 16 instructions and 2 exponentials an element in 0.67 of the
+// terms: 352 us (5.8 TB/s; a tenth of the rows is masked and not read), 16 instructions and 2 exponentials an element in 0.67 of the
 // issue slots; one block a row that streams it took 3.1 ms.
 #include "lm_rows.h"
 

@@ -10,8 +10,9 @@ namespace ssm {
 // Time is split where a block for every sequence and its channels would leave too few warps on an SM.  A split's first pass
 // costs 60% of the forward one's second, 20% of the backward one's, so the forward pass is split below one and a half
 // blocks an SM, the backward one below two and a half of four; then into whole turns of the blocks that an SM holds, up to three
-// while a block has no more than 40 splits to compose, but not into splits of less than 128 steps.  Both calls, bf16, 16
-// states, in us with 1, 4, 8, 16 and 32 splits: 4 x 2048 x 2048 739, 639, 621, 650, 771; 1 x 16,384 x 2048 4711, 1930, 1433,
+// while a block has no more than 40 splits to compose, but into no more splits than 128 steps go into, rounded up.  (Rounded down, the backward
+// call of 1 x 129 x 512 bf16 takes 33 us instead of 26, of 1 x 200 x 2048 49 instead of 37; the forward ones 10.2, 10.5 and 14.2, 13.8.)  Both calls,
+// bf16, 16 states, in us with 1, 4, 8, 16 and 32 splits: 4 x 2048 x 2048 739, 639, 621, 650, 771; 1 x 16,384 x 2048 4711, 1930, 1433,
 // 1275, 1258; 8 x 2048 x 2048 1125, 1180, 1178, 1259, 1510.  1 x 50,021 x 512 with 38 (one turn) 955, with 64 1012.
 SsmCut ssm_cut(int64_t B, int64_t T, int64_t D, int G, int CH, bool backward, int resident) {
   constexpr int64_t kSms = 152, kMostComposed = 40, kMostSplits = 64, kLeastSteps = 128;

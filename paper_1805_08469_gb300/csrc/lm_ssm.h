@@ -364,7 +364,8 @@ cudaError_t launch_backward(SsmArgs p, cudaStream_t stream);
 inline int state_lanes(int N) { return N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 // Channels of a thread.  Two in the backward pass of more than 16 states: fewer instructions a state, but no more than two
 // blocks an SM (both calls, 3 x 1777 x 1000 x 64: 711 us instead of 770 with one; with 16 states one is as fast or up to
-// 10% faster).
+// 10% faster).  One in the forward pass, bf16 in us with one and with two: 8 x 2048 x 2048 x 16 261, 430; x 32 400, 441; x 64 826, 853; 3
+// x 1777 x 1000 x 64 173, 205.
 constexpr int kForwardK = 1;
 template <int LS>
 constexpr int kBackwardK = LS == 4 ? 1 : 2;

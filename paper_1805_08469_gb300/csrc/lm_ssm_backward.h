@@ -13,8 +13,10 @@
 // second kernel adds up the blocks.  The parameters' gradients are summed over a split in registers, then by that kernel
 // as well.  Splits are composed from the last one back, as in the forward pass.
 //
-// Per state and step 28 warp instructions, two and a half exponentials among them.  8 x 2048 x 2048 x 16 bf16 with a gate: 0.80 ms,
-// 0.53 of the issue slots and 59% of shared memory's cycles with 13 warps an SM, whose latencies bound it (HBM 11%).
+// Per state and step 28 instructions of a thread, two and a half exponentials among them.  8 x 2048 x 2048 x 16 bf16 with a gate: 0.80
+// ms, 0.53 of the issue slots and 59% of shared memory's cycles with 13 warps an SM, whose latencies bound it (HBM 11%).  The registers
+// do not quite suffice: 48 bytes a thread are spilled in that kernel, 170 where single elements are loaded (fp32 148, 212), 56 and 80
+// with 64 states.
 #pragma once
 
 #include "lm_ssm.h"

@@ -8,7 +8,7 @@ namespace lm {
 namespace ssm {
 
 // Goes over a split.  STATES: the first pass of a split time, for the last state and the sum of steps alone.  Per state and step 10
-// warp instructions, an exponential among them (a third of them the staging, whose share falls with N).  8 x 2048 x 2048 x 16 bf16
+// instructions of a thread, an exponential among them (a third of them the staging, whose share falls with N).  8 x 2048 x 2048 x 16 bf16
 // with a gate, states saved: 255 us, 0.60 of the issue slots with 13 warps an SM (HBM 18%).
 template <typename E, int LS, int K, bool WIDE, bool STATES>
 __global__ void __launch_bounds__(kSsmThreads, 4) ssm_forward_kernel(const SsmArgs p) {

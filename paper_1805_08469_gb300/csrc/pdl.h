@@ -13,7 +13,7 @@
 //     running before the commit, or what precedes the commit, has ended.  So no kernel may
 //     touch global memory before its wait, whatever it follows.  The second is the embedding
 //     gradient's embed_zeros_kernel, whose blocks trigger after their own wait: the sort that
-//     follows it in the same call runs beside it and waits at its end;
+//     follows it in the same call starts when enough of them have left and waits for the others at its end;
 //   - dependencies that are not on a kernel of the same stream (event waits, copies) stay
 //     full dependencies.
 // In a kernel launched without the attribute, the wait returns at once.
